@@ -314,6 +314,136 @@ int kv_append(void* kv_pool, int64_t n_pool_blocks, const kv_view* view, const v
               const int32_t* positions, int n_seqs, void* hip_stream);
 
 /*
+ * kv_rope_append -- what lies between the QKV projection and attention: rotary position encoding of
+ * the new tokens' queries and keys, queries to an array, keys and values into the pool.  Several new
+ * tokens per sequence as in paged_prefill_attn: token j of sequence s is row q_offsets[s] + j and
+ * becomes token ctx_lens[s] - q_len[s] + j of its sequence's cache.
+ *   pair i of a head's first rotary_dim elements, (x, y):  (x cos a - y sin a, y cos a + x sin a),
+ *   a = positions[axis_of_pair[i]][row] * inv_freq[i]
+ * Elements from rotary_dim on, and values, are copied.  Positions may have several axes (time,
+ * height, width of a patch of an image or video); the angle is reduced in 64-bit arithmetic, the
+ * rotation is fp32, with one rounding to bf16.
+ *
+ *   q, k, v        device, bf16, the token rows [n_q_local][head_dim], [n_kv_local][head_dim] twice;
+ *                  q_stride, k_stride, v_stride elements between tokens: separate arrays or the parts
+ *                  of a fused QKV row alike
+ *   q_out          device, bf16 [total][n_q_local][head_dim]; may be q itself if q_stride is
+ *                  n_q_local * head_dim, and must not overlap the inputs otherwise
+ *   positions      device, int32 [n_axes][position_stride], 1 <= n_axes <= 4, position_stride >= total
+ *   inv_freq       device, fp32 [rotary_dim / 2]
+ *   axis_of_pair   HOST, int32 [rotary_dim / 2], each in [0, n_axes); null: axis 0 for all pairs
+ *   pairs          KV_ROPE_HALVES: pair i is elements (i, i + rotary_dim / 2); KV_ROPE_ADJACENT: (2 i, 2 i + 1)
+ *   ctx_lens       device, int32 [batch]: cached tokens with the new ones.  A token whose place is
+ *                  negative (ctx_lens < q_len), or whose block lies outside the table's row or the
+ *                  pool, is not written into the pool
+ *   q_offsets      device, int32 [batch + 1], non-decreasing, q_offsets[0] = 0; null: one token per
+ *                  sequence (total = batch).  Rows from q_offsets[batch] on are not touched
+ *   token_pos      device, int32 [batch][n_kv_local][token_pos_stride], or null: the position on axis 0
+ *                  of every token written, at its place in the cache, for kv_evict
+ * Errors: KV_ERR_INVALID_ARG (null pointers, negative sizes, strides too small, an axis out of range,
+ * rotary_dim > head_dim, total != batch without q_offsets), KV_ERR_UNSUPPORTED (head_dim or rotary_dim
+ * not a multiple of 16, rotary_dim > 256, more than 4 axes, strides not multiples of 8 elements,
+ * pointers not 16-byte aligned), KV_ERR_HIP.
+ */
+enum { KV_ROPE_HALVES = 0, KV_ROPE_ADJACENT = 1 };
+int kv_rope_append(void* kv_pool, int64_t n_pool_blocks, const kv_view* view, const void* q, int64_t q_stride,
+                   const void* k, int64_t k_stride, const void* v, int64_t v_stride, void* q_out,
+                   const int32_t* positions, int64_t position_stride, int n_axes, const float* inv_freq,
+                   int rotary_dim, const int32_t* axis_of_pair, int pairs, const int32_t* block_table,
+                   int64_t block_table_stride, const int32_t* ctx_lens, const int32_t* q_offsets, int batch,
+                   int64_t total, int32_t* token_pos, int64_t token_pos_stride, void* hip_stream);
+
+/*
+ * paged_tree_attn -- attention for speculative decoding with a tree of drafted tokens.  The last
+ * q_len[s] = q_offsets[s + 1] - q_offsets[s] of sequence s's ctx_lens[s] cached tokens are drafted (their
+ * K and V are in the pool); drafted token j sees every token before the draft and drafted token i iff
+ * bit i % 64 of tree_mask[q_offsets[s] + j][i / 64] is set (its ancestors and itself; any set of bits is
+ * accepted).  A row that sees no token is zeros.  The softmax and out are those of paged_prefill_attn,
+ * with this mask in place of the causal one.
+ *
+ *   tree_mask      device, uint64 [total_q][mask_words], mask_words >= ceil(max_q_len / 64); bits from
+ *                  q_len[s] on are ignored
+ *   workspace      at least paged_tree_attn_workspace_bytes(...) bytes, 256-byte aligned; contents need
+ *                  not be initialised
+ * Other arguments as paged_prefill_attn, max_q_len <= 256.  Infinities and NaN in the K or V of a drafted
+ * token reach the rows that see it and no others.  Errors: KV_ERR_INVALID_ARG (null pointers, negative sizes,
+ * max_q_len > max_ctx_len, block_table_stride or mask_words too small), KV_ERR_UNSUPPORTED (head_dim not 64 or
+ * 128, group size above 32, block capacity not a multiple of 16, max_q_len > 256), KV_ERR_WORKSPACE, KV_ERR_HIP.
+ */
+size_t paged_tree_attn_workspace_bytes(const kv_view* view, int batch, int64_t total_q, int max_ctx_len,
+                                       int max_q_len);
+int paged_tree_attn(const void* q, void* out, const void* kv_pool, int64_t n_pool_blocks,
+                    const int32_t* block_table, int64_t block_table_stride, const int32_t* ctx_lens,
+                    const int32_t* q_offsets, const uint64_t* tree_mask, int64_t mask_words, int batch,
+                    int64_t total_q, int max_ctx_len, int max_q_len, const kv_view* view, float scale,
+                    void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * kv_accept -- keep the accepted ones of the drafted tokens (after paged_tree_attn and the caller's
+ * verification): the K and V rows of drafted token accepted[s][i], i < n_accepted[s], are moved to
+ * token ctx_lens[s] - q_len[s] + i of the sequence, for all heads of the view, so that the accepted
+ * tokens follow the cache in order.  What lies behind them is left as it is.
+ *   accepted       device, int32 [batch][accepted_stride]: numbers of drafted tokens, each row strictly
+ *                  ascending, in [0, q_len[s]); entries that are not are skipped
+ *   n_accepted     device, int32 [batch], at most accepted_stride and q_len[s] (more counts as that)
+ *   new_lens       device, int32 [batch], written: ctx_lens[s] - q_len[s] + n_accepted[s]; may be null,
+ *                  must not be ctx_lens
+ * Errors: KV_ERR_INVALID_ARG, KV_ERR_HIP.
+ */
+int kv_accept(void* kv_pool, int64_t n_pool_blocks, const kv_view* view, const int32_t* block_table,
+              int64_t block_table_stride, const int32_t* ctx_lens, const int32_t* q_offsets,
+              const int32_t* accepted, int64_t accepted_stride, const int32_t* n_accepted, int batch,
+              int32_t* new_lens, void* hip_stream);
+
+/*
+ * paged_decode_attn_weights -- paged_decode_attn that also adds up, per KV head, how much attention
+ * weight every cached token gets (what kv_evict goes by):
+ *     w[t] = sum over the G query heads of KV head h of softmax_t(scale * q . K[t])
+ *     weights[s][h][t] += w[t] for t < ctx_lens[s] - 1;   weights[s][h][ctx_lens[s] - 1] = w[t]
+ * The newest token's entry is set, not added to, so that a place in the cache may be used again without
+ * clearing anything; entries from ctx_lens[s] on are not touched.
+ *   weights        device, fp32 [batch][n_kv_local][weights_stride], weights_stride >= max_ctx_len
+ *   workspace      at least paged_decode_attn_weights_workspace_bytes(...) bytes (4 bytes per query head
+ *                  and token of the bound, and some MB), 256-byte aligned; contents need not be initialised
+ * Other arguments as paged_decode_attn.  Errors: as paged_tree_attn.
+ */
+size_t paged_decode_attn_weights_workspace_bytes(const kv_view* view, int batch, int max_ctx_len);
+int paged_decode_attn_weights(const void* q, void* out, const void* kv_pool, int64_t n_pool_blocks,
+                              const int32_t* block_table, int64_t block_table_stride,
+                              const int32_t* ctx_lens, int batch, int max_ctx_len, const kv_view* view,
+                              float scale, float* weights, int64_t weights_stride, void* workspace,
+                              size_t workspace_bytes, void* hip_stream);
+
+/*
+ * kv_evict -- bring sequences back to a budget of tokens, each KV head keeping its own.  Of the
+ * n = ctx_lens[s] tokens of (s, head) the first k = min(n, keep_lens[s]) in this order stay: protected tokens
+ * before others, larger weight before smaller (NaN last), lower place before higher.  Protected are tokens with
+ * token_pos < sinks or token_pos >= next_pos[s] - recent.  The cache then holds k tokens: kept tokens from
+ * place k on move into the places below k that were given up, the j-th into the j-th, both in
+ * ascending order; everything else stays where it is (the order of cached tokens does not matter to
+ * attention; token_pos says which is which).  K and V rows, weights and token_pos move alike.
+ *   keep_lens      device, int32 [batch] (negative counts as 0)
+ *   weights        device, fp32 [batch][n_kv_local][stride], stride >= max_ctx_len
+ *   token_pos      device, int32, same shape: positions of the tokens (kv_rope_append writes them)
+ *   next_pos       device, int32 [batch]: the position that the next token takes
+ *   weights_out, token_pos_out  device, [batch][n_kv_local][out_stride]: the arrays as they are afterwards, entries
+ *                  below min(k, out_stride) written; may be weights and token_pos themselves (only what moves is
+ *                  written then, and out_stride must be stride)
+ *   new_lens       device, int32 [batch], written: k; may be null, must not be ctx_lens or keep_lens
+ *   workspace      at least kv_evict_workspace_bytes(...) bytes, 256-byte aligned; contents need not be
+ *                  initialised
+ * Errors: KV_ERR_INVALID_ARG (null pointers, negative sizes, strides too small), KV_ERR_UNSUPPORTED (max_ctx_len
+ * above 2^24), KV_ERR_WORKSPACE, KV_ERR_HIP.
+ */
+size_t kv_evict_workspace_bytes(const kv_view* view, int batch, int max_ctx_len);
+int kv_evict(void* kv_pool, int64_t n_pool_blocks, const kv_view* view, const int32_t* block_table,
+             int64_t block_table_stride, const int32_t* ctx_lens, const int32_t* keep_lens, int batch,
+             int max_ctx_len, const float* weights, const int32_t* token_pos, int64_t stride,
+             const int32_t* next_pos, int sinks, int recent, float* weights_out, int32_t* token_pos_out,
+             int64_t out_stride, int32_t* new_lens, void* workspace, size_t workspace_bytes,
+             void* hip_stream);
+
+/*
  * kv_validate_tables -- debugging aid, NOT for the hot path: copies the tables to the host
  * (synchronises the stream) and checks that every block id a valid token needs lies in
  * [0, n_pool_blocks) (KV_ERR_RANGE) and that no block is used twice within the table

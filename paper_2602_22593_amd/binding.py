@@ -74,6 +74,21 @@ def lib() -> C.CDLL:
     L.kv_linear_view_workspace_bytes.restype = C.c_size_t
     L.kv_repack.argtypes = [vp, i64, vp, vp, vp, i64, vp, i64, vp, C.c_int, C.c_int, vp]
     L.kv_append.argtypes = [vp, i64, vp, vp, vp, vp, i64, vp, C.c_int, vp]
+    L.kv_rope_append.argtypes = [vp, i64, vp, vp, i64, vp, i64, vp, i64, vp, vp, i64, C.c_int, vp, C.c_int, vp, C.c_int, vp,
+                                 i64, vp, vp, C.c_int, i64, vp, i64, vp]
+    L.paged_tree_attn_workspace_bytes.argtypes = [vp, C.c_int, i64, C.c_int, C.c_int]
+    L.paged_tree_attn_workspace_bytes.restype = C.c_size_t
+    L.paged_tree_attn.argtypes = [vp, vp, vp, i64, vp, i64, vp, vp, vp, i64, C.c_int, i64, C.c_int, C.c_int, vp, C.c_float,
+                                  vp, C.c_size_t, vp]
+    L.kv_accept.argtypes = [vp, i64, vp, vp, i64, vp, vp, vp, i64, vp, C.c_int, vp, vp]
+    L.paged_decode_attn_weights_workspace_bytes.argtypes = [vp, C.c_int, C.c_int]
+    L.paged_decode_attn_weights_workspace_bytes.restype = C.c_size_t
+    L.paged_decode_attn_weights.argtypes = [vp, vp, vp, i64, vp, i64, vp, C.c_int, C.c_int, vp, C.c_float, vp, i64, vp,
+                                            C.c_size_t, vp]
+    L.kv_evict_workspace_bytes.argtypes = [vp, C.c_int, C.c_int]
+    L.kv_evict_workspace_bytes.restype = C.c_size_t
+    L.kv_evict.argtypes = [vp, i64, vp, vp, i64, vp, vp, C.c_int, C.c_int, vp, vp, i64, vp, C.c_int, C.c_int, vp, vp, i64, vp,
+                           vp, C.c_size_t, vp]
     L.kv_validate_tables.argtypes = [vp, i64, vp, i64, vp, C.c_int, vp, vp, i64, vp]
     L.kv_set_option.argtypes = [C.c_char_p, i64]
     L.kv_get_option.argtypes = [C.c_char_p]
@@ -430,6 +445,219 @@ def kv_append(kv_pool: torch.Tensor, view: KVView, k_new: torch.Tensor, v_new: t
         block_table.stride(0), _dev(positions, (torch.int32,), "positions"), n_seqs,
         _stream_ptr(stream))
     _check(rc, "kv_append")
+
+
+KV_ROPE_HALVES, KV_ROPE_ADJACENT = 0, 1
+
+
+def _one_device(*tensors) -> torch.device:
+    """The device that all of a call's tensors live on (None: an argument left out)."""
+    device = tensors[0].device
+    for t in tensors[1:]:
+        if t is not None and t.device != device:
+            raise ValueError(f"all tensors must live on one device, got {device} and {t.device}")
+    return device
+
+
+def _launch(device: torch.device, stream, call):
+    """call(stream handle) with ``device`` current, on ``stream`` or by default on that device's current stream."""
+    if device.index == torch._C._cuda_getDevice():
+        return call(_stream_ptr(stream))
+    with torch.cuda.device(device):
+        return call(_stream_ptr(stream))
+
+
+def _blocks_of(kv_pool: torch.Tensor, view: KVView) -> int:
+    n_bytes = kv_pool.numel() * kv_pool.element_size()
+    if n_bytes % view.block_bytes:
+        raise ValueError("kv_pool size is not a whole number of blocks")
+    return n_bytes // view.block_bytes
+
+
+def _table(block_table: torch.Tensor, batch: int) -> int:
+    if block_table.dim() != 2 or block_table.shape[0] != batch:
+        raise ValueError("block_table must be [batch][max_blocks]")
+    return _dev(block_table, (torch.int32,), "block_table")
+
+
+def _ints(t: torch.Tensor, n: int, name: str) -> int:
+    if t.dim() != 1 or t.shape[0] != n:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {(n,)}")
+    return _dev(t, (torch.int32,), name)
+
+
+def _shaped(t: torch.Tensor, shape, dtypes, name: str) -> int:
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    return _dev(t, dtypes, name)
+
+
+def _per_token(t: torch.Tensor, view: KVView, batch: int, dtype, name: str) -> int:
+    """A value per cached token: [batch][n_kv_local][tokens]."""
+    if t.dim() != 3 or tuple(t.shape[:2]) != (batch, view.n_kv_local):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected [{batch}, {view.n_kv_local}, tokens]")
+    return _dev(t, (dtype,), name)
+
+
+def _token_rows(t: torch.Tensor, total: int, heads: int, d: int, name: str):
+    """Rows [total][heads][d] whose tokens may lie apart: address and elements between tokens."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must live in device memory")
+    if t.dtype not in _BF16:
+        raise ValueError(f"{name} has dtype {t.dtype}, expected one of {_BF16}")
+    if tuple(t.shape) != (total, heads, d):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {(total, heads, d)}")
+    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != d):
+        raise ValueError(f"{name} must have contiguous token rows")
+    return t.data_ptr(), t.stride(0) if total > 1 else heads * d
+
+
+def kv_rope_append(kv_pool: torch.Tensor, view: KVView, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                   positions: torch.Tensor, inv_freq: torch.Tensor, block_table: torch.Tensor, ctx_lens: torch.Tensor,
+                   q_offsets: Optional[torch.Tensor] = None, axes=None, pairs: int = KV_ROPE_HALVES,
+                   out: Optional[torch.Tensor] = None, token_pos: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Rotate the new tokens' q and k by their positions; q is returned, k and v go into the pool through ``view``.
+
+    q [total][n_q_local][d], k and v [total][n_kv_local][d] (tokens may lie apart: the parts of a fused QKV row serve);
+    positions int32 [total] or [axes][total]; inv_freq fp32, one per pair; ``axes`` the axis of each pair (a sequence of
+    ints on the host).  ``q_offsets`` int32 [batch + 1], or None for one token per sequence; the new tokens are the last of
+    ctx_lens.  ``token_pos`` int32 [batch][n_kv_local][tokens] gets the positions on axis 0 of what is written.
+    """
+    batch, total, d = int(ctx_lens.shape[0]), int(q.shape[0]), view.head_dim
+    device = _one_device(q, k, v, kv_pool, positions, inv_freq, block_table, ctx_lens, q_offsets, out, token_pos)
+    q_ptr, q_stride = _token_rows(q, total, view.n_q_local, d, "q")
+    k_ptr, k_stride = _token_rows(k, total, view.n_kv_local, d, "k")
+    v_ptr, v_stride = _token_rows(v, total, view.n_kv_local, d, "v")
+    if out is None:
+        out = torch.empty((total, view.n_q_local, d), dtype=q.dtype, device=device)
+    n_axes = 1 if positions.dim() == 1 else int(positions.shape[0])
+    pos_ptr = _shaped(positions, (total,) if positions.dim() == 1 else (n_axes, total), (torch.int32,), "positions")
+    half = int(inv_freq.numel())
+    freq_ptr = _shaped(inv_freq, (half,), (torch.float32,), "inv_freq")
+    if axes is not None:
+        if len(axes) != half:
+            raise ValueError(f"axes has {len(axes)} entries, expected {half}")
+        axes = (C.c_int32 * half)(*axes)
+    elif n_axes != 1:
+        raise ValueError("positions with several axes need axes")
+    args = (_dev(kv_pool, _BF16, "kv_pool"), _blocks_of(kv_pool, view), view.handle, q_ptr, q_stride, k_ptr, k_stride, v_ptr, v_stride,
+            _shaped(out, (total, view.n_q_local, d), _BF16, "out"), pos_ptr, total, n_axes, freq_ptr, 2 * half, axes, pairs,
+            _table(block_table, batch), block_table.stride(0), _ints(ctx_lens, batch, "ctx_lens"),
+            None if q_offsets is None else _ints(q_offsets, batch + 1, "q_offsets"), batch, total,
+            None if token_pos is None else _per_token(token_pos, view, batch, torch.int32, "token_pos"),
+            0 if token_pos is None else int(token_pos.shape[2]))
+    _check(_launch(device, stream, lambda st: lib().kv_rope_append(*args, st)), "kv_rope_append")
+    return out
+
+
+def paged_tree_attn_workspace_bytes(view: KVView, batch: int, total_q: int, max_ctx_len: int, max_q_len: int) -> int:
+    return int(lib().paged_tree_attn_workspace_bytes(view.handle, batch, total_q, max_ctx_len, max_q_len))
+
+
+def paged_tree_attn(q: torch.Tensor, kv_pool: torch.Tensor, block_table: torch.Tensor, ctx_lens: torch.Tensor,
+                    q_offsets: torch.Tensor, tree_mask: torch.Tensor, view: KVView, max_ctx_len: int, max_q_len: int,
+                    out: Optional[torch.Tensor] = None, scale: float = 0.0, workspace: Optional[torch.Tensor] = None,
+                    stream=None) -> torch.Tensor:
+    """Attention of each sequence's last q_len tokens, drafted as a tree: each sees what lies before the draft, and drafted
+    token i where bit i of its row of ``tree_mask`` (int64 [total_q][words of 64]) is set.
+
+    Other arguments as paged_prefill_attn; max_q_len is at most 256.
+    """
+    batch, total = int(ctx_lens.shape[0]), int(q.shape[0])
+    device = _one_device(q, kv_pool, block_table, ctx_lens, q_offsets, tree_mask, out, workspace)
+    shape = (total, view.n_q_local, view.head_dim)
+    q_ptr = _shaped(q, shape, _BF16, "q")
+    if out is None:
+        out = torch.empty_like(q)
+    if tree_mask.dim() != 2 or tree_mask.shape[0] != total:
+        raise ValueError(f"tree_mask has shape {tuple(tree_mask.shape)}, expected [{total}, words]")
+    if workspace is None:
+        workspace = _workspace(device, paged_tree_attn_workspace_bytes(view, batch, total, max_ctx_len, max_q_len), stream)
+    args = (q_ptr, _shaped(out, shape, _BF16, "out"), _dev(kv_pool, _BF16, "kv_pool"), _blocks_of(kv_pool, view),
+            _table(block_table, batch), block_table.stride(0), _ints(ctx_lens, batch, "ctx_lens"),
+            _ints(q_offsets, batch + 1, "q_offsets"), _dev(tree_mask, (torch.int64, torch.uint64), "tree_mask"),
+            int(tree_mask.shape[1]), batch, total, int(max_ctx_len), int(max_q_len), view.handle, float(scale),
+            _dev(workspace, (torch.uint8,), "workspace"), workspace.numel())
+    _check(_launch(device, stream, lambda st: lib().paged_tree_attn(*args, st)), "paged_tree_attn")
+    return out
+
+
+def kv_accept(kv_pool: torch.Tensor, view: KVView, block_table: torch.Tensor, ctx_lens: torch.Tensor, q_offsets: torch.Tensor,
+              accepted: torch.Tensor, n_accepted: torch.Tensor, new_lens: Optional[torch.Tensor] = None,
+              stream=None) -> torch.Tensor:
+    """Move the K and V rows of the accepted drafted tokens (int32 [batch][n], ascending numbers in the draft) behind the cache,
+    in order; returns the new lengths."""
+    batch = int(ctx_lens.shape[0])
+    device = _one_device(kv_pool, block_table, ctx_lens, q_offsets, accepted, n_accepted, new_lens)
+    if accepted.dim() != 2 or accepted.shape[0] != batch:
+        raise ValueError(f"accepted has shape {tuple(accepted.shape)}, expected [{batch}, n]")
+    if new_lens is None:
+        new_lens = torch.empty_like(ctx_lens)
+    args = (_dev(kv_pool, _BF16, "kv_pool"), _blocks_of(kv_pool, view), view.handle, _table(block_table, batch),
+            block_table.stride(0), _ints(ctx_lens, batch, "ctx_lens"), _ints(q_offsets, batch + 1, "q_offsets"),
+            _dev(accepted, (torch.int32,), "accepted"), int(accepted.shape[1]), _ints(n_accepted, batch, "n_accepted"), batch,
+            _ints(new_lens, batch, "new_lens"))
+    _check(_launch(device, stream, lambda st: lib().kv_accept(*args, st)), "kv_accept")
+    return new_lens
+
+
+def paged_decode_attn_weights_workspace_bytes(view: KVView, batch: int, max_ctx_len: int) -> int:
+    return int(lib().paged_decode_attn_weights_workspace_bytes(view.handle, batch, max_ctx_len))
+
+
+def paged_decode_attn_weights(q: torch.Tensor, kv_pool: torch.Tensor, block_table: torch.Tensor, ctx_lens: torch.Tensor,
+                              view: KVView, max_ctx_len: int, weights: torch.Tensor, out: Optional[torch.Tensor] = None,
+                              scale: float = 0.0, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """paged_decode_attn that also adds the attention weight of every cached token, summed over the query heads of its KV head,
+    to ``weights`` (fp32 [batch][n_kv_local][tokens]; the newest token's entry is set)."""
+    batch = int(ctx_lens.shape[0])
+    device = _one_device(q, kv_pool, block_table, ctx_lens, weights, out, workspace)
+    shape = (batch, view.n_q_local, view.head_dim)
+    q_ptr = _shaped(q, shape, _BF16, "q")
+    if out is None:
+        out = torch.empty_like(q)
+    if workspace is None:
+        workspace = _workspace(device, paged_decode_attn_weights_workspace_bytes(view, batch, max_ctx_len), stream)
+    args = (q_ptr, _shaped(out, shape, _BF16, "out"), _dev(kv_pool, _BF16, "kv_pool"), _blocks_of(kv_pool, view),
+            _table(block_table, batch), block_table.stride(0), _ints(ctx_lens, batch, "ctx_lens"), batch, int(max_ctx_len),
+            view.handle, float(scale), _per_token(weights, view, batch, torch.float32, "weights"), int(weights.shape[2]),
+            _dev(workspace, (torch.uint8,), "workspace"), workspace.numel())
+    _check(_launch(device, stream, lambda st: lib().paged_decode_attn_weights(*args, st)), "paged_decode_attn_weights")
+    return out
+
+
+def kv_evict_workspace_bytes(view: KVView, batch: int, max_ctx_len: int) -> int:
+    return int(lib().kv_evict_workspace_bytes(view.handle, batch, max_ctx_len))
+
+
+def kv_evict(kv_pool: torch.Tensor, view: KVView, block_table: torch.Tensor, ctx_lens: torch.Tensor, keep_lens: torch.Tensor,
+             weights: torch.Tensor, token_pos: torch.Tensor, next_pos: torch.Tensor, max_ctx_len: int, sinks: int = 0,
+             recent: int = 0, weights_out: Optional[torch.Tensor] = None, token_pos_out: Optional[torch.Tensor] = None,
+             new_lens: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Keep the ``keep_lens`` most attended tokens of every KV head (and those before position ``sinks`` and the last
+    ``recent``): the kept ones behind the budget move into the places given up.  ``weights`` and ``token_pos``
+    ([batch][n_kv_local][tokens]) move along, in place unless other arrays are given for the result.  Returns the new lengths."""
+    batch = int(ctx_lens.shape[0])
+    device = _one_device(kv_pool, block_table, ctx_lens, keep_lens, weights, token_pos, next_pos, weights_out, token_pos_out,
+                         new_lens, workspace)
+    weights_out = weights if weights_out is None else weights_out
+    token_pos_out = token_pos if token_pos_out is None else token_pos_out
+    if weights.shape != token_pos.shape or weights_out.shape != token_pos_out.shape:
+        raise ValueError("weights and token_pos must have one shape")
+    if new_lens is None:
+        new_lens = torch.empty_like(ctx_lens)
+    if workspace is None:
+        workspace = _workspace(device, kv_evict_workspace_bytes(view, batch, max_ctx_len), stream)
+    args = (_dev(kv_pool, _BF16, "kv_pool"), _blocks_of(kv_pool, view), view.handle, _table(block_table, batch),
+            block_table.stride(0), _ints(ctx_lens, batch, "ctx_lens"), _ints(keep_lens, batch, "keep_lens"), batch,
+            int(max_ctx_len), _per_token(weights, view, batch, torch.float32, "weights"),
+            _per_token(token_pos, view, batch, torch.int32, "token_pos"), int(weights.shape[2]),
+            _ints(next_pos, batch, "next_pos"), int(sinks), int(recent),
+            _per_token(weights_out, view, batch, torch.float32, "weights_out"),
+            _per_token(token_pos_out, view, batch, torch.int32, "token_pos_out"), int(weights_out.shape[2]),
+            _ints(new_lens, batch, "new_lens"), _dev(workspace, (torch.uint8,), "workspace"), workspace.numel())
+    _check(_launch(device, stream, lambda st: lib().kv_evict(*args, st)), "kv_evict")
+    return new_lens
 
 
 def kv_validate_tables(view: KVView, n_pool_blocks: int, block_table: torch.Tensor,

@@ -1,0 +1,770 @@
+// Attention of few query rows per sequence to a paged KV pool through a layout view, in two entry points that share a kernel:
+//
+//   paged_tree_attn            the last q_len tokens of a sequence are drafted; each sees everything before them and the
+//                              drafted tokens that its mask names (its ancestors in a tree, and itself)
+//   paged_decode_attn_weights  one query token per sequence; besides the output, the attention weight that every cached
+//                              token got is added to a running sum per KV head
+//
+// A pair is (sequence, local KV head, block of 32 RW query rows), its rows being the sequence's new tokens x the G query
+// heads of the KV head; a tile is 32 cached tokens of a pair.  All tiles of a launch lie on one axis that is cut into equal
+// shares, one per workgroup, so that the work is even whatever the lengths.  A pair that lies in one share is finished there,
+// the pieces of a cut one leave (reference, sum of weights, sums of values) in the workspace for a second launch.
+//
+// What bounds it: reading K and V, 4 D bytes a token and KV head, as long as the rows are few: 32 rows x 32 keys take
+// 2 D / 16 + 2 D / 16 products of 32 x 32 x 16, 512 cycles at D = 128, and bring 16 KiB, for which HBM takes 1440 cycles of one
+// compute unit's share.  So up to 32 rows the four wavefronts of a workgroup take different tiles (RW = 1, KW = 4), up to 64
+// two by two, up to 128 all four share a tile, and eight do above: K and V pass through LDS once per workgroup.
+//
+// Per tile, lane l = (c = l % 32, half = l / 32):
+//   S^T[token][c] = K[token][:] . q[c][:]     A operand = K rows from LDS, B operand = q
+//   O^T[e][c]     = sum_t V[t][e] P[c][t]     A operand = V^T by the transposing LDS read
+// Register 4 a + i of S^T holds token 8 a + 4 half + i; contraction index 8 half + 4 a' + i of step c' of the second product
+// stands for token 16 c' + 8 a' + 4 half + i, so weights stay in their lane.
+#include <algorithm>
+
+#include "decode_common.h"
+
+using namespace kvdec;
+
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short bits16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) bits16x4* lds_bits16x4_ptr;
+typedef __attribute__((address_space(3))) void* lds_ptr;
+
+constexpr int kKeys = 32;
+constexpr float kUnset = 1e30f;   // exponent addend of a column that has seen no key yet
+constexpr int kCus = 256;
+constexpr int kMostNodes = 256;   // drafted tokens of a sequence
+constexpr int kChunk = 1024;      // tokens per workgroup of the second launch that adds up weights
+
+struct tree_args {
+    const uint16_t* q;        // [total_q][n_q_local][D]
+    uint16_t* out;
+    const uint16_t* pool;
+    const int32_t* table;
+    int64_t table_stride;
+    const int32_t* ctx_lens;
+    const int32_t* q_off;     // [batch + 1], or null: one query token per sequence
+    const unsigned long long* mask;   // [total_q][mask_words]
+    kv_view_dev v;
+    uint32_t last_block;      // n_pool_blocks - 1
+    float scale_log2e;
+    int32_t group, batch, max_ctx_len, mask_words;
+    int32_t workgroups, least_tiles;   // shares that the axis of tiles is cut into, and the least tiles of a share
+    float* part_o;            // [2 workgroups][32 RW][D]: slot 2 w the first piece of workgroup w, 2 w + 1 its last
+    float* part_ml;           // [2 workgroups][32 RW][2] (reference in exponent units, sum of weights)
+    // weights:
+    float* scores;            // [batch][n_q_local][score_stride] exponents: score * scale * log2(e)
+    float* row_ml;            // [batch][n_q_local][2] of pairs that were not cut
+    float* sums;              // [batch][n_kv_local][sum_stride]
+    int64_t score_stride, sum_stride;
+};
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int64_t uniform64(int64_t x)
+{
+    return (int64_t)((uint64_t)(uint32_t)uniform((int)x) | (uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32);
+}
+
+// Maximum / sum over the two lanes of a column, left in both.
+__device__ __forceinline__ float half_max(float x)
+{
+    const uint32_t c = __builtin_bit_cast(uint32_t, x);
+    const auto h = __builtin_amdgcn_permlane32_swap(c, c, false, false);
+    const uint32_t h0 = h[0], h1 = h[1];
+    return fmaxf(__builtin_bit_cast(float, h0), __builtin_bit_cast(float, h1));
+}
+__device__ __forceinline__ float half_sum(float x)
+{
+    const uint32_t c = __builtin_bit_cast(uint32_t, x);
+    const auto h = __builtin_amdgcn_permlane32_swap(c, c, false, false);
+    const uint32_t h0 = h[0], h1 = h[1];
+    return __builtin_bit_cast(float, h0) + __builtin_bit_cast(float, h1);
+}
+__device__ __forceinline__ float column_max(const f32x16& x)
+{
+    float mx = x[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, x[i]);
+    return half_max(mx);
+}
+// l + the two bf16 values of a packed pair, summed in fp32.
+__device__ __forceinline__ float add_pair(uint32_t packed, float l)
+{
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, packed), __builtin_bit_cast(bf16x2, 0x3f803f80u), l, false);
+}
+// Whether one of the two bf16 values is an infinity or NaN.
+__device__ __forceinline__ bool not_finite(uint32_t x)
+{
+    return (x & 0x7f800000u) == 0x7f800000u || (x & 0x7f80u) == 0x7f80u;
+}
+
+// What a sequence brings: cached tokens, new ones, tiles of a pair, row blocks of a head.
+struct seq_work {
+    int n, q0, q_len, tiles, blocks;
+    __device__ int64_t total(int heads) const { return (int64_t)tiles * blocks * heads; }
+};
+template <int RB>
+__device__ __forceinline__ seq_work work_of(const tree_args& a, int s)
+{
+    seq_work w;
+    w.n = min(a.ctx_lens[s], a.max_ctx_len);
+    w.q0 = a.q_off ? a.q_off[s] : s;
+    w.q_len = a.q_off ? a.q_off[s + 1] - w.q0 : 1;
+    const bool any = w.n > 0 && w.q_len > 0;
+    w.tiles = any ? (w.n + kKeys - 1) / kKeys : 0;
+    w.blocks = any ? (w.q_len * a.group + RB - 1) / RB : 0;
+    return w;
+}
+__device__ __forceinline__ int64_t share_of(const tree_args& a, int64_t total)
+{
+    const int64_t even = (total + a.workgroups - 1) / a.workgroups;
+    return even > a.least_tiles ? even : a.least_tiles;
+}
+
+// Sum of x over the workgroup, in every thread (s_sum: one word per wavefront; free again after the call's barrier pair).
+template <int NT>
+__device__ __forceinline__ int64_t block_sum(int64_t x, int64_t* s_sum)
+{
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) x += __shfl_xor((long long)x, d);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) s_sum[threadIdx.x >> 6] = x;
+    __syncthreads();
+    int64_t t = 0;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) t += s_sum[w];
+    return t;
+}
+
+// The share of this workgroup: [from, to) on the axis, the sequence that holds `from` and its offset in it.
+template <int NT, int RB>
+__device__ __forceinline__ void find_share(const tree_args& a, int64_t* s_sum, int64_t& from, int64_t& to, int& seq, int64_t& offset)
+{
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int each = (a.batch + NT - 1) / NT, s0 = min(tid * each, a.batch), s1 = min(s0 + each, a.batch);
+    int64_t mine = 0;
+    for (int s = s0; s < s1; ++s) mine += work_of<RB>(a, s).total(a.v.n_kv_local);
+    int64_t incl = mine;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int64_t y = __shfl_up((long long)incl, d);
+        incl += lane >= d ? y : 0;
+    }
+    if (lane == 63) s_sum[wave] = incl;
+    __syncthreads();
+    int64_t total = 0, before = incl - mine;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) {
+        total += s_sum[w];
+        before += w < wave ? s_sum[w] : 0;
+    }
+    const int64_t share = share_of(a, total);
+    from = (int64_t)blockIdx.x * share;
+    to = min(from + share, total);
+    __syncthreads();
+    if (from >= before && from < before + mine) {   // one thread at most
+        int s = s0;
+        for (int64_t w; from >= before + (w = work_of<RB>(a, s).total(a.v.n_kv_local)); ++s) before += w;
+        s_sum[0] = s;
+        s_sum[1] = from - before;
+    }
+    __syncthreads();
+    seq = uniform((int)s_sum[0]);
+    offset = uniform64(s_sum[1]);
+    __syncthreads();
+}
+
+// Bytes of the staging buffers of a key group, K or V
+template <int D> constexpr int tile_pieces() { return kKeys * D / 8; }
+
+template <int D, int RW, bool SUMS>
+__global__ __launch_bounds__(RW == 8 ? 512 : 256, RW == 4 ? 3 : RW == 1 ? 1 : 2) void tree_kernel(tree_args a)
+{
+    constexpr int NW = RW < 4 ? 4 : RW, KW = NW / RW, NT = 64 * NW, RB = 32 * RW;
+    constexpr int NJ = D / 32, NK = D / 16, kPieces = tile_pieces<D>(), kRow = 2 * D;
+    // K: piece c of row t at c ^ f(t), V: at c ^ g(t): operand reads without bank conflicts.  An array per buffer: the compiler
+    // then knows that loads landing in one do not touch the operands read from another.
+    __shared__ kv_u32x4 s_k0[KW * kPieces], s_k1[KW * kPieces], s_v0[KW * kPieces], s_v1[KW * kPieces];
+    __shared__ float2 s_ml[KW > 1 ? NW * 32 : 1];
+    __shared__ int64_t s_sum[NW];
+
+    const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
+    const int rw = wave % RW, kg = wave / RW;   // the wavefront's rows and tiles
+    const int col = lane & 31, half = lane >> 5;
+    const kv_view_dev& v = a.v;
+    const int G = a.group, Hl = v.n_kv_local;
+
+    int64_t from, to, offset;
+    int s;
+    find_share<NT, RB>(a, s_sum, from, to, s, offset);
+
+    // ---- what does not change from piece to piece -------------------------------------------------
+    const int64_t stride_bytes = (int64_t)v.token_stride * 2, block_bytes = v.block_elems * 2, plane_bytes = v.plane_elems * 2;
+    const int groups_per_block = v.block_tokens >> 4;
+    // staging: one instruction fills 64 consecutive pieces of 16 bytes, 512 / D rows; a wavefront fills NP of the D / 16
+    // such parts of K and of V (at D = 64 under RW = 8 the lower four wavefronts K, the others V)
+    constexpr bool kSplitPlanes = NK < RW;
+    constexpr int NP = kSplitPlanes ? 1 : NK / RW;
+    constexpr int kRowsEach = 512 / D;
+    const int first_part = kSplitPlanes ? (rw & (NK - 1)) : rw * NP;
+    uint32_t k_lane[NP], v_lane[NP];
+    int row16[NP];
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+        const int row = ((first_part + i) * kRowsEach + lane / (D / 8)) & 15, c = lane & (D / 8 - 1);
+        row16[i] = row;
+        const int kc = D == 128 ? c ^ row : c ^ (row >> 1), vc = D == 128 ? c ^ (4 * (row & 3)) : c ^ (4 * ((row >> 1) & 1));
+        k_lane[i] = (uint32_t)(row * (int)stride_bytes + (kc << 4));
+        v_lane[i] = (uint32_t)(row * (int)stride_bytes + (vc << 4));
+    }
+    uint32_t k_off, v_off[NJ];
+    {
+        const int p = lane & 15, sub = (lane >> 4) & 1;
+        k_off = (uint32_t)(col * kRow + ((half ^ (D == 128 ? (col & 15) : ((col >> 1) & 7))) << 4));
+        const int vrow = 4 * half + (p >> 2), g = D == 128 ? 4 * (vrow & 3) : 4 * ((vrow >> 1) & 1);
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+            v_off[j] = (uint32_t)(vrow * kRow + (((4 * j + 2 * sub + ((p & 3) >> 1)) ^ g) << 4) + (p & 1) * 8);
+    }
+
+    for (int64_t at = from; at < to;) {
+        // ---- the next piece: tiles [t0, t0 + count) of pair (s, h, rb) -----------------------------
+        const seq_work w = work_of<RB>(a, s);
+        if (offset >= w.total(Hl)) {
+            offset -= w.total(Hl);
+            ++s;
+            continue;
+        }
+        const int pair = uniform((int)(offset / w.tiles)), t0 = uniform((int)(offset - (int64_t)pair * w.tiles));
+        const int h = pair / w.blocks, rb = pair - h * w.blocks;
+        const int count = (int)min((int64_t)(w.tiles - t0), to - at);
+        const bool cut = count < w.tiles;
+        const int n = w.n, first = n - w.q_len;          // the first drafted token
+        const int rows = min(w.q_len * G - rb * RB, RB);   // of the pair
+        const bool idle = rw * 32 >= rows;                 // this wavefront has none of them
+        const int mine = kg < count ? (count - kg + KW - 1) / KW : 0, iters = (count + KW - 1) / KW;
+        const int last_group = (n - 1) >> 4;
+
+        // where the groups of 16 tokens lie: lane l knows that of group l % 2 of this wavefront's tile 32 window + l / 2
+        const int32_t* ids = a.table + (int64_t)s * a.table_stride;
+        const char* pool_head = reinterpret_cast<const char*>(a.pool + v.head_off + h * D);
+        auto group_at = [&](int window) { return min(2 * (t0 + kg + (32 * window + (lane >> 1)) * KW) + (lane & 1), last_group); };
+        auto request_ids = [&](int window) { return (uint32_t)ids[group_at(window) / groups_per_block]; };
+        auto places = [&](uint32_t id, int window) {
+            const int g = group_at(window);
+            return (int64_t)min(id, a.last_block) * block_bytes + (int64_t)(g % groups_per_block) * 16 * stride_bytes;
+        };
+        uint32_t next_id = request_ids(0);
+        int64_t place = places(next_id, 0);
+        next_id = request_ids(1);
+        auto stage = [&](int i, kv_u32x4* dk, kv_u32x4* dv) {
+            if ((i & 31) == 0 && i > 0) {
+                place = places(next_id, i >> 5);
+                next_id = request_ids((i >> 5) + 1);
+            }
+            const int tile = t0 + kg + i * KW;
+            const bool end = 2 * tile + 1 >= last_group;
+            auto rows_of = [&](int g) -> const char* {
+                const int l = 2 * (i & 31) + g;
+                const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)place, l);
+                const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(place >> 32), l);
+                return pool_head + (int64_t)((uint64_t)lo | (uint64_t)hi << 32);
+            };
+            auto fill = [&](const uint32_t* at_lane, int64_t plane, kv_u32x4* dst) {
+#pragma unroll
+                for (int p = 0; p < NP; ++p) {
+                    const int part = first_part + p, g = part * kRowsEach >> 4;
+                    // rows past the end of the sequence are its last one again (masked later)
+                    const int limit = n - 1 - 16 * min(2 * tile + g, last_group);
+                    const uint32_t past = end ? (uint32_t)(max(row16[p] - limit, 0) * (int)stride_bytes) : 0u;
+                    const __amdgpu_buffer_rsrc_t r =
+                        __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(rows_of(g) + plane), 0, 0x7ffffff0, 0x00020000);
+                    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr)(dst + kg * kPieces + part * 64), 16, at_lane[p] - past, 0, 0, 0);
+                }
+            };
+            if (!kSplitPlanes || rw < NK) fill(k_lane, 0, dk);
+            if (!kSplitPlanes || rw >= NK) fill(v_lane, plane_bytes, dv);
+        };
+        auto staged = [&]() {
+            __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
+            if constexpr (RW > 1) __syncthreads();
+            else asm volatile("" ::: "memory");
+        };
+        if (mine > 0) stage(0, s_k0, s_v0);
+
+        // ---- this lane's query row ----------------------------------------------------------------
+        const int rho = rb * RB + min(rw * 32 + col, rows - 1);      // (padding columns repeat the last row)
+        const int64_t qrow = (int64_t)(w.q0 + rho / G);
+        const int64_t orow = (qrow * v.n_q_local + h * G + rho % G) * D;
+        const bool real = rw * 32 + col < rows;
+        bf16x8 qb[NK];
+#pragma unroll
+        for (int kk = 0; kk < NK; ++kk)
+            qb[kk] = as_bf16x8(*reinterpret_cast<const kv_u32x4*>(a.q + orow + half * 8 + kk * 16));
+
+        float neg_m = kUnset, l = 0.f;
+        bool unset = true;
+        f32x16 o[NJ];
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[j][i] = 0.f;
+
+        auto k_operand = [&](const kv_u32x4* sk, int kk) {
+            return as_bf16x8(*reinterpret_cast<const kv_u32x4*>(reinterpret_cast<const char*>(sk + kg * kPieces) + (k_off ^ (32 * kk))));
+        };
+        auto v_operand = [&](const kv_u32x4* sv, int c, int j) {
+            const char* const p = reinterpret_cast<const char*>(sv + kg * kPieces) + v_off[j] + c * 16 * kRow;
+            const bits16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_bits16x4_ptr)p);
+            const bits16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_bits16x4_ptr)(p + 8 * kRow));
+            return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        };
+        // Which of the 32 tokens of a tile this lane's row sees
+        auto seen_by_row = [&](int base) -> uint32_t {
+            const int here = n - base;   // tokens of the tile that exist
+            const uint32_t valid = here >= 32 ? ~0u : (1u << here) - 1u;
+            if constexpr (SUMS) return valid;
+            const int o_ = base - first;   // node number of the tile's first token
+            if (o_ <= -32) return valid;
+            const unsigned long long* words = a.mask + qrow * a.mask_words;
+            const int at_word = max(o_, 0) >> 6;
+            const unsigned long long w0 = words[min(at_word, a.mask_words - 1)], w1 = words[min(at_word + 1, a.mask_words - 1)];
+            uint32_t bits;
+            if (o_ < 0) bits = (uint32_t)(w0 << -o_) | ((1u << -o_) - 1u);
+            else bits = (uint32_t)(w0 >> (o_ & 63)) | ((o_ & 63) > 32 ? (uint32_t)(w1 << (64 - (o_ & 63))) : 0u);
+            return bits & valid;
+        };
+        // Sums of values where a masked token may hold an infinity or NaN, which a weight of 0 would turn into NaN: token by token,
+        // without those of no weight.
+        auto add_values_one_by_one = [&](const kv_u32x4* sv, const uint32_t* pw) {
+#pragma unroll 1
+            for (int t = 0; t < 32; ++t) {
+                const int u = 2 * (t >> 3) + ((t & 3) >> 1);
+                uint32_t two = pw[0];
+#pragma unroll
+                for (int x = 1; x < 8; ++x) two = u == x ? pw[x] : two;
+                two = (uint32_t)__shfl((int)two, col + 32 * ((t >> 2) & 1));
+                const float wt = (t & 1) ? bf16_hi(two) : bf16_lo(two);
+                const char* row = reinterpret_cast<const char*>(sv + kg * kPieces) + t * kRow;
+                const int g = D == 128 ? 4 * (t & 3) : 4 * ((t >> 1) & 1);
+#pragma unroll
+                for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                    for (int u4 = 0; u4 < 4; ++u4) {   // elements 32 j + 8 u4 + 4 half ..
+                        const kv_u32x2 x = *reinterpret_cast<const kv_u32x2*>(row + (((4 * j + u4) ^ g) << 4) + 8 * half);
+                        if (wt != 0.f) {
+                            o[j][4 * u4 + 0] += wt * bf16_lo(x[0]);
+                            o[j][4 * u4 + 1] += wt * bf16_hi(x[0]);
+                            o[j][4 * u4 + 2] += wt * bf16_lo(x[1]);
+                            o[j][4 * u4 + 3] += wt * bf16_hi(x[1]);
+                        }
+                    }
+            }
+        };
+        auto tile_step = [&](int i, const kv_u32x4* sk, const kv_u32x4* sv) {
+            const int base = kKeys * (t0 + kg + i * KW);
+            f32x16 sc;
+#pragma unroll
+            for (int x = 0; x < 16; ++x) sc[x] = 0.f;
+#pragma unroll
+            for (int kk = 0; kk < NK; ++kk) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_operand(sk, kk), qb[kk], sc, 0, 0, 0);
+            // tiles that hold drafted tokens or the end of the sequence
+            const bool edge = base + kKeys > (SUMS ? n : first);
+            if (edge) {
+                const uint32_t seen = seen_by_row(base) >> (4 * half);
+#pragma unroll
+                for (int x = 0; x < 16; ++x) sc[x] = (seen >> (8 * (x >> 2) + (x & 3))) & 1 ? sc[x] : kNegInf;
+            }
+            if constexpr (SUMS) {
+                if (real) {
+                    float* dst = a.scores + ((int64_t)s * v.n_q_local + h * G + rho % G) * a.score_stride + base + 4 * half;
+#pragma unroll
+                    for (int u = 0; u < 4; ++u)
+                        *reinterpret_cast<f32x4*>(dst + 8 * u) =
+                            f32x4{sc[4 * u] * a.scale_log2e, sc[4 * u + 1] * a.scale_log2e, sc[4 * u + 2] * a.scale_log2e, sc[4 * u + 3] * a.scale_log2e};
+                }
+            }
+            // Exponents against a reference that may lag behind the running maximum by 2^8 (weights up to 2^8 are as exact), so that the
+            // accumulators are rescaled rarely.  A column without a key yet has none; its first key sets it.
+            if (unset) {
+                const float mx = column_max(sc);
+                if (neg_m == kUnset && mx != kNegInf) neg_m = -mx * a.scale_log2e;
+                unset = __builtin_amdgcn_ballot_w64(neg_m == kUnset) != 0;
+            }
+            constexpr float kLag = 8.0f;
+            f32x16 ex;
+            float top = kNegInf;
+#pragma unroll
+            for (int x = 0; x < 16; ++x) {
+                ex[x] = __builtin_fmaf(sc[x], a.scale_log2e, neg_m);
+                top = fmaxf(top, ex[x]);
+            }
+            if (__builtin_amdgcn_ballot_w64(top > kLag) != 0) {
+                // (from the scores again: exponents far above the old reference have lost the digits that the new one needs)
+                const float next = fminf(neg_m, -column_max(sc) * a.scale_log2e), alpha = fast_exp2(next - neg_m);
+                l *= alpha;
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) o[j] *= alpha;
+                neg_m = next;
+#pragma unroll
+                for (int x = 0; x < 16; ++x) ex[x] = __builtin_fmaf(sc[x], a.scale_log2e, neg_m);
+            }
+            uint32_t pw[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const float e0 = fast_exp2(ex[2 * u]), e1 = fast_exp2(ex[2 * u + 1]);
+                pw[u] = pack_bf16x2(e0, e1);
+                if constexpr (SUMS) l += e0 + e1;   // the weights handed out are not rounded
+                else l = add_pair(pw[u], l);        // the same rounding above and below the fraction
+            }
+            if (edge) {
+                bool odd = false;
+#pragma unroll
+                for (int x = 0; x < kPieces / 64; ++x) {
+                    const kv_u32x4 y = sv[kg * kPieces + x * 64 + lane];
+                    odd = odd || not_finite(y[0]) || not_finite(y[1]) || not_finite(y[2]) || not_finite(y[3]);
+                }
+                if (__builtin_amdgcn_ballot_w64(odd) != 0) {
+                    add_values_one_by_one(sv, pw);
+                    return;
+                }
+            }
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const bf16x8 pb = as_bf16x8(kv_u32x4{pw[4 * c], pw[4 * c + 1], pw[4 * c + 2], pw[4 * c + 3]});
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand(sv, c, j), pb, o[j], 0, 0, 0);
+            }
+        };
+        // Tile i + 1 lands while tile i is worked on.  The barrier (of wavefronts that share tiles) says both that every
+        // part of tile i is there and that nobody reads tile i - 1 any more.
+        for (int i = 0; i < iters; i += 2) {
+            staged();
+            if (i + 1 < mine) stage(i + 1, s_k1, s_v1);
+            if (i < mine && !idle) tile_step(i, s_k0, s_v0);
+            if (i + 1 >= iters) break;
+            staged();
+            if (i + 2 < mine) stage(i + 2, s_k0, s_v0);
+            if (i + 1 < mine && !idle) tile_step(i + 1, s_k1, s_v1);
+        }
+
+        // ---- the piece's rows ----------------------------------------------------------------------
+        l = half_sum(l);
+        const int slot = 2 * (int)blockIdx.x + (at > from ? 1 : 0), srow = rw * 32 + col;
+        // groups of four accumulator registers: x = 4 j + u4 holds elements 8 x + 4 half ..
+        constexpr int NX = 4 * NJ, XW = NX / KW;   // each of the KW wavefronts of a row finishes XW of them
+        f32x4 acc[XW];
+        float m_all, l_all;
+        if constexpr (KW > 1) {
+            // wavefronts that took different tiles of the same rows add up: all leave their sums in LDS
+            if (half == 0) s_ml[wave * 32 + col] = make_float2(l != 0.f ? -neg_m : kNegInf, l);
+            __syncthreads();   // (nobody reads a tile any more)
+            auto area = [&](int x) { return x == 0 ? s_k0 : x == 1 ? s_k1 : x == 2 ? s_v0 : s_v1; };
+            kv_u32x4* mine_at = area(wave) + lane;
+#pragma unroll
+            for (int x = 0; x < NX; ++x)
+                mine_at[x * 64] = __builtin_bit_cast(kv_u32x4, f32x4{o[x >> 2][4 * (x & 3)], o[x >> 2][4 * (x & 3) + 1],
+                                                                     o[x >> 2][4 * (x & 3) + 2], o[x >> 2][4 * (x & 3) + 3]});
+            __syncthreads();
+            m_all = kNegInf;
+            l_all = 0.f;
+#pragma unroll
+            for (int k = 0; k < KW; ++k) m_all = fmaxf(m_all, s_ml[(k * RW + rw) * 32 + col].x);
+#pragma unroll
+            for (int x = 0; x < XW; ++x) acc[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < KW; ++k) {
+                const float2 ml = s_ml[(k * RW + rw) * 32 + col];
+                const float f = ml.y != 0.f ? fast_exp2(ml.x - m_all) : 0.f;
+                l_all += f * ml.y;
+                const kv_u32x4* from_k = area(k * RW + rw) + lane;
+#pragma unroll
+                for (int x = 0; x < XW; ++x) {
+                    const f32x4 y = __builtin_bit_cast(f32x4, from_k[(kg * XW + x) * 64]);
+                    if (f != 0.f) acc[x] += y * f;
+                }
+            }
+            __syncthreads();   // (before the next piece's tiles land)
+        } else {
+            m_all = l != 0.f ? -neg_m : kNegInf;
+            l_all = l;
+#pragma unroll
+            for (int x = 0; x < XW; ++x) acc[x] = f32x4{o[x >> 2][4 * (x & 3)], o[x >> 2][4 * (x & 3) + 1],
+                                                        o[x >> 2][4 * (x & 3) + 2], o[x >> 2][4 * (x & 3) + 3]};
+            if constexpr (RW > 1) __syncthreads();
+        }
+        if (real) {
+            const int x0 = KW > 1 ? kg * XW : 0;
+            if (cut) {
+                float* dst = a.part_o + ((int64_t)slot * RB + srow) * D + 4 * half;
+#pragma unroll
+                for (int x = 0; x < XW; ++x) *reinterpret_cast<f32x4*>(dst + 8 * (x0 + x)) = acc[x];
+                if (kg == 0 && half == 0) *reinterpret_cast<float2*>(a.part_ml + ((int64_t)slot * RB + srow) * 2) = make_float2(m_all, l_all);
+            } else {
+                const float inv = 1.0f / l_all;   // (0 where the row sees nothing: zeros then; NaN stays NaN)
+#pragma unroll
+                for (int x = 0; x < XW; ++x) {
+                    uint2 pk = make_uint2(pack_bf16x2(acc[x][0] * inv, acc[x][1] * inv), pack_bf16x2(acc[x][2] * inv, acc[x][3] * inv));
+                    if (l_all == 0.f) pk = make_uint2(0u, 0u);
+                    *reinterpret_cast<uint2*>(a.out + orow + 8 * (x0 + x) + 4 * half) = pk;
+                }
+                if (SUMS && kg == 0 && half == 0)
+                    *reinterpret_cast<float2*>(a.row_ml + ((int64_t)s * v.n_q_local + h * G + rho % G) * 2) = make_float2(m_all, l_all);
+            }
+        }
+        at += count;
+        offset += count;
+    }
+}
+
+// The second launch.  Block (s, pair of s, part): the pieces of a cut pair's rows are added up in the order of the workgroups,
+//   out[row] = sum_z o_z 2^(m_z - M) / sum_z l_z 2^(m_z - M),  M = max_z m_z,
+// D / 4 lanes a row.  Rows of sequences without tokens are zeros.  SUMS: the parts are chunks of tokens; each works out (M, L) of the pair's
+// G rows and adds sum_g 2^(score_g - M_g) / L_g to the tokens of its chunk; part 0 adds up the rows too.
+template <int D, int RW, bool SUMS>
+__global__ __launch_bounds__(256) void tree_merge_kernel(tree_args a)
+{
+    constexpr int NT = 256, RB = 32 * RW, kLanes = D / 4, kRows = NT / kLanes;
+    __shared__ int64_t s_sum[NT / 64];
+    __shared__ float2 s_ml[SUMS ? 32 : 1];
+    const int s = blockIdx.x, Hl = a.v.n_kv_local, G = a.group, tid = threadIdx.x;
+    const seq_work w = work_of<RB>(a, s);
+    const int pair = blockIdx.y;
+    const int cg = tid % kLanes, r = tid / kLanes;
+    if (w.n <= 0 && w.q_len > 0) {   // nothing cached: zeros (block y writes head y's rows)
+        if (pair < Hl)
+            for (int x = blockIdx.z * kRows + r; x < w.q_len * G; x += gridDim.z * kRows)
+                *reinterpret_cast<uint2*>(a.out + ((int64_t)(w.q0 + x / G) * a.v.n_q_local + pair * G + x % G) * D + 4 * cg) = make_uint2(0u, 0u);
+        return;
+    }
+    if (pair >= w.blocks * Hl) return;
+    const int h = pair / w.blocks, rb = pair - h * w.blocks;
+    if (!SUMS && (int)blockIdx.z * kRows >= w.q_len * G - rb * RB) return;
+    int64_t before = 0, all = 0;
+    for (int x = tid; x < a.batch; x += NT) {
+        const int64_t y = work_of<RB>(a, x).total(Hl);
+        all += y;
+        before += x < s ? y : 0;
+    }
+    all = block_sum<NT>(all, s_sum);
+    before = block_sum<NT>(before, s_sum);
+    const int64_t share = share_of(a, all), from = before + (int64_t)pair * w.tiles, to = from + w.tiles;
+    const int w0 = uniform((int)(from / share)), w1 = uniform((int)((to - 1) / share));
+    const int rows = min(w.q_len * G - rb * RB, RB);
+    auto slot_of = [&](int x) { return 2 * (int64_t)x + (x == w0 && from > (int64_t)x * share ? 1 : 0); };
+    if constexpr (SUMS) {
+        if (tid < G) {
+            float m = kNegInf, l = 0.f;
+            if (w0 == w1) {
+                const float2 ml = *reinterpret_cast<const float2*>(a.row_ml + ((int64_t)s * a.v.n_q_local + h * G + tid) * 2);
+                m = ml.x;
+                l = ml.y;
+            } else {
+                for (int x = w0; x <= w1; ++x) {
+                    const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + (slot_of(x) * RB + tid) * 2);
+                    if (ml.y == 0.f) continue;
+                    const float mn = fmaxf(m, ml.x);
+                    l = l * fast_exp2(m - mn) + ml.y * fast_exp2(ml.x - mn);
+                    m = mn;
+                }
+            }
+            s_ml[tid] = make_float2(m, l != 0.f ? 1.0f / l : 0.f);
+        }
+        __syncthreads();
+        float* sums = a.sums + ((int64_t)s * Hl + h) * a.sum_stride;
+        const float* scores = a.scores + ((int64_t)s * a.v.n_q_local + h * G) * a.score_stride;
+        const int end = min(((int)blockIdx.z + 1) * kChunk, w.n);
+        for (int t = (int)blockIdx.z * kChunk + tid; t < end; t += NT) {
+            float x = 0.f;
+            for (int g = 0; g < G; ++g) {
+                const float2 ml = s_ml[g];
+                const float e = scores[g * a.score_stride + t];
+                x += e == kNegInf ? 0.f : fast_exp2(e - ml.x) * ml.y;
+            }
+            sums[t] = t == w.n - 1 ? x : sums[t] + x;   // (the newest token has no sum yet)
+        }
+        if (blockIdx.z > 0) return;
+    }
+    if (w0 == w1) return;   // written by the main kernel
+    for (int row = SUMS ? r : (int)blockIdx.z * kRows + r; row < rows; row += SUMS ? kRows : rows) {
+        float m = kNegInf, l = 0.f;
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+        for (int x = w0; x <= w1; ++x) {
+            const int64_t at = slot_of(x) * RB + row;
+            const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + at * 2);
+            const f32x4 y = *reinterpret_cast<const f32x4*>(a.part_o + at * D + 4 * cg);
+            if (ml.y == 0.f) continue;
+            const float mn = fmaxf(m, ml.x), keep = fast_exp2(m - mn), f = fast_exp2(ml.x - mn);
+            l = l * keep + ml.y * f;
+            acc = acc * keep + y * f;
+            m = mn;
+        }
+        const float inv = 1.0f / l;
+        const int rho = rb * RB + row;
+        *reinterpret_cast<uint2*>(a.out + ((int64_t)(w.q0 + rho / G) * a.v.n_q_local + h * G + rho % G) * D + 4 * cg) =
+            l != 0.f ? make_uint2(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)) : make_uint2(0u, 0u);
+    }
+}
+
+// ---- host ------------------------------------------------------------------------------------------
+
+// Wavefronts that share a tile, by the bound on a pair's rows
+int row_waves(int64_t rows) { return rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 ? 4 : 8; }
+
+struct tree_plan {
+    int rw;
+    int32_t workgroups, least;
+    size_t part_o, part_ml, bytes;
+};
+tree_plan plan_tree(const kv_view* view, int batch, int max_ctx_len, int max_q_len)
+{
+    tree_plan p;
+    const int64_t rows = (int64_t)max_q_len * view->group;
+    p.rw = row_waves(rows);
+    const int rb = 32 * p.rw;
+    const int64_t blocks = (rows + rb - 1) / rb, tiles = ((int64_t)max_ctx_len + kKeys - 1) / kKeys;
+    p.least = p.rw == 1 ? 4 : p.rw == 2 ? 2 : 1;
+    const int64_t most = (blocks * view->n_kv_local * batch * tiles + p.least - 1) / p.least;
+    const int fill = kCus * (p.rw == 2 ? 2 : p.rw == 4 ? 3 : 1);
+    p.workgroups = (int32_t)std::min<int64_t>(most, fill);
+    const size_t records = (size_t)2 * p.workgroups * rb;
+    p.part_o = records * view->geom.head_dim * 4;
+    p.part_ml = records * 8;
+    p.bytes = p.part_o + p.part_ml;
+    return p;
+}
+
+template <int D, int RW, bool SUMS>
+void launch(const tree_args& a, int64_t most_blocks, int parts, hipStream_t st)
+{
+    hipLaunchKernelGGL((tree_kernel<D, RW, SUMS>), dim3((unsigned)a.workgroups), dim3(RW == 8 ? 512 : 256), 0, st, a);
+    hipLaunchKernelGGL((tree_merge_kernel<D, RW, SUMS>), dim3((unsigned)a.batch, (unsigned)(a.v.n_kv_local * most_blocks), (unsigned)parts),
+                       dim3(256), 0, st, a);
+}
+template <int D>
+void launch_tree(int rw, const tree_args& a, int64_t most_rows, hipStream_t st)
+{
+    const int rb = 32 * rw, rows_each = 256 / (D / 4);
+    const int64_t blocks = (most_rows + rb - 1) / rb;
+    const int parts = (int)((std::min<int64_t>(most_rows, rb) + rows_each - 1) / rows_each);
+    switch (rw) {
+        case 1: launch<D, 1, false>(a, blocks, parts, st); break;
+        case 2: launch<D, 2, false>(a, blocks, parts, st); break;
+        case 4: launch<D, 4, false>(a, blocks, parts, st); break;
+        default: launch<D, 8, false>(a, blocks, parts, st); break;
+    }
+}
+
+// The checks that both entry points make, and the arguments that they share.
+int common_args(tree_args& a, const void* q, void* out, const void* kv_pool, int64_t n_pool_blocks, const int32_t* block_table,
+                int64_t block_table_stride, const int32_t* ctx_lens, int batch, int max_ctx_len, const kv_view* view, float scale)
+{
+    if (!q || !out || !ctx_lens || !kv_pool || !block_table || n_pool_blocks < 1) return KV_ERR_INVALID_ARG;
+    if (block_table_stride < ((int64_t)max_ctx_len + view->block_tokens - 1) / view->block_tokens) return KV_ERR_INVALID_ARG;
+    const int d = view->geom.head_dim;
+    if ((d != 64 && d != 128) || view->block_tokens % 16 != 0 || view->group > 32) return KV_ERR_UNSUPPORTED;
+    if ((int64_t)view->row_heads * d * 2 * 16 > 0x7fffffff || n_pool_blocks > 0x7fffffff) return KV_ERR_UNSUPPORTED;
+    a = tree_args{};
+    a.q = (const uint16_t*)q;
+    a.out = (uint16_t*)out;
+    a.pool = (const uint16_t*)kv_pool;
+    a.table = block_table;
+    a.table_stride = block_table_stride;
+    a.ctx_lens = ctx_lens;
+    a.v = kv_view_to_dev(view);
+    a.last_block = (uint32_t)(n_pool_blocks - 1);
+    a.scale_log2e = (scale > 0.f ? scale : 1.0f / sqrtf((float)d)) * 1.4426950408889634f;
+    a.group = view->group;
+    a.batch = batch;
+    a.max_ctx_len = max_ctx_len;
+    return KV_OK;
+}
+
+int64_t score_stride(int max_ctx_len) { return ((int64_t)max_ctx_len + kKeys - 1) / kKeys * kKeys; }
+
+}  // namespace
+
+extern "C" size_t paged_tree_attn_workspace_bytes(const kv_view* view, int batch, int64_t total_q, int max_ctx_len, int max_q_len)
+{
+    if (!kv_view_ok(view) || batch <= 0 || total_q <= 0 || max_ctx_len <= 0 || max_q_len <= 0) return 0;
+    return plan_tree(view, batch, max_ctx_len, max_q_len).bytes;
+}
+
+extern "C" int paged_tree_attn(const void* q, void* out, const void* kv_pool, int64_t n_pool_blocks, const int32_t* block_table,
+                               int64_t block_table_stride, const int32_t* ctx_lens, const int32_t* q_offsets,
+                               const uint64_t* tree_mask, int64_t mask_words, int batch, int64_t total_q, int max_ctx_len,
+                               int max_q_len, const kv_view* view, float scale, void* workspace, size_t workspace_bytes,
+                               void* hip_stream)
+{
+    if (!kv_view_ok(view) || batch < 0 || total_q < 0 || max_ctx_len < 0 || max_q_len < 0 || n_pool_blocks < 0 ||
+        block_table_stride < 0 || max_q_len > max_ctx_len || mask_words < 0)
+        return KV_ERR_INVALID_ARG;
+    if (batch == 0 || max_q_len == 0 || total_q == 0) return KV_OK;
+    if (!q_offsets || !tree_mask || mask_words < (max_q_len + 63) / 64) return KV_ERR_INVALID_ARG;
+    if (max_q_len > kMostNodes || mask_words > 0x7fffffff) return KV_ERR_UNSUPPORTED;
+    tree_args a;
+    if (const int rc = common_args(a, q, out, kv_pool, n_pool_blocks, block_table, block_table_stride, ctx_lens, batch, max_ctx_len,
+                                   view, scale))
+        return rc;
+    const tree_plan p = plan_tree(view, batch, max_ctx_len, max_q_len);
+    if (!workspace || ((uintptr_t)workspace & 255u)) return KV_ERR_INVALID_ARG;
+    if (workspace_bytes < p.bytes) return KV_ERR_WORKSPACE;
+    a.q_off = q_offsets;
+    a.mask = (const unsigned long long*)tree_mask;
+    a.mask_words = (int32_t)mask_words;
+    a.workgroups = p.workgroups;
+    a.least_tiles = p.least;
+    a.part_o = (float*)workspace;
+    a.part_ml = (float*)((char*)workspace + p.part_o);
+    const int64_t rows = (int64_t)max_q_len * view->group;
+    if ((rows + 31) / 32 * view->n_kv_local > 65535) return KV_ERR_UNSUPPORTED;
+    hipStream_t st = (hipStream_t)hip_stream;
+    if (view->geom.head_dim == 128) launch_tree<128>(p.rw, a, rows, st);
+    else launch_tree<64>(p.rw, a, rows, st);
+    return kv_record_hip_error(hipGetLastError(), "paged_tree_attn launch");
+}
+
+extern "C" size_t paged_decode_attn_weights_workspace_bytes(const kv_view* view, int batch, int max_ctx_len)
+{
+    if (!kv_view_ok(view) || batch <= 0 || max_ctx_len <= 0) return 0;
+    const size_t rows = (size_t)batch * view->n_q_local;
+    return plan_tree(view, batch, max_ctx_len, 1).bytes + rows * (8 + 4 * (size_t)score_stride(max_ctx_len));
+}
+
+extern "C" int paged_decode_attn_weights(const void* q, void* out, const void* kv_pool, int64_t n_pool_blocks,
+                                         const int32_t* block_table, int64_t block_table_stride, const int32_t* ctx_lens, int batch,
+                                         int max_ctx_len, const kv_view* view, float scale, float* weights, int64_t weights_stride,
+                                         void* workspace, size_t workspace_bytes, void* hip_stream)
+{
+    if (!kv_view_ok(view) || batch < 0 || max_ctx_len < 0 || n_pool_blocks < 0 || block_table_stride < 0) return KV_ERR_INVALID_ARG;
+    if (batch == 0) return KV_OK;
+    if (!weights || weights_stride < max_ctx_len) return KV_ERR_INVALID_ARG;
+    tree_args a;
+    if (const int rc = common_args(a, q, out, kv_pool, n_pool_blocks, block_table, block_table_stride, ctx_lens, batch, max_ctx_len,
+                                   view, scale))
+        return rc;
+    const tree_plan p = plan_tree(view, batch, std::max(max_ctx_len, 1), 1);
+    const size_t rows = (size_t)batch * view->n_q_local;
+    if (max_ctx_len > 0) {
+        if (!workspace || ((uintptr_t)workspace & 255u)) return KV_ERR_INVALID_ARG;
+        if (workspace_bytes < paged_decode_attn_weights_workspace_bytes(view, batch, max_ctx_len)) return KV_ERR_WORKSPACE;
+    }
+    a.workgroups = p.workgroups;
+    a.least_tiles = p.least;
+    a.score_stride = score_stride(max_ctx_len);
+    a.scores = (float*)workspace;   // (its rows are read and written 16 bytes at a time)
+    a.part_o = a.scores + rows * a.score_stride;
+    a.part_ml = a.part_o + p.part_o / 4;
+    a.row_ml = a.part_ml + p.part_ml / 4;
+    a.sums = weights;
+    a.sum_stride = weights_stride;
+    const int64_t chunks = std::max<int64_t>(((int64_t)max_ctx_len + kChunk - 1) / kChunk, 1);
+    if (chunks > 65535 || view->n_kv_local > 65535) return KV_ERR_UNSUPPORTED;
+    hipStream_t st = (hipStream_t)hip_stream;
+    if (view->geom.head_dim == 128) launch<128, 1, true>(a, 1, (int)chunks, st);
+    else launch<64, 1, true>(a, 1, (int)chunks, st);
+    return kv_record_hip_error(hipGetLastError(), "paged_decode_attn_weights launch");
+}
