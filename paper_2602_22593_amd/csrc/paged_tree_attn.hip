@@ -6,9 +6,11 @@
 //                              token got is added to a running sum per KV head
 //
 // A pair is (sequence, local KV head, block of 32 RW query rows), its rows being the sequence's new tokens x the G query
-// heads of the KV head; a tile is 32 cached tokens of a pair.  All tiles of a launch lie on one axis that is cut into equal
-// shares, one per workgroup, so that the work is even whatever the lengths.  A pair that lies in one share is finished there,
-// the pieces of a cut one leave (reference, sum of weights, sums of values) in the workspace for a second launch.
+// heads of the KV head; a tile is 32 cached tokens of a pair.  The tiles of one head lie on one axis that is cut into equal
+// shares, so that the work is even whatever the lengths.  A team of workgroups, one per head, takes a share: where the heads of
+// a token lie side by side, the whole row is asked for at about one time (64 sequences of 512 to 4096, 8 heads: MEASURED).  A pair
+// that lies in one share is finished there, the pieces of a cut one leave (reference, sum of weights, sums of values) in the
+// workspace for a second launch.
 //
 // What bounds it: reading K and V, 4 D bytes a token and KV head, as long as the rows are few: 32 rows x 32 keys take
 // 2 D / 16 + 2 D / 16 products of 32 x 32 x 16, 512 cycles at D = 128, and bring 16 KiB, for which HBM takes 1440 cycles of one
@@ -21,6 +23,7 @@
 // Register 4 a + i of S^T holds token 8 a + 4 half + i; contraction index 8 half + 4 a' + i of step c' of the second product
 // stands for token 16 c' + 8 a' + 4 half + i, so weights stay in their lane.
 #include <algorithm>
+#include <type_traits>
 
 #include "decode_common.h"
 
@@ -37,7 +40,7 @@ constexpr int kKeys = 32;
 constexpr float kUnset = 1e30f;   // exponent addend of a column that has seen no key yet
 constexpr int kCus = 256;
 constexpr int kMostNodes = 256;   // drafted tokens of a sequence
-constexpr int kChunk = 1024;      // tokens per workgroup of the second launch that adds up weights
+constexpr int kEdgeTiles = kMostNodes / kKeys + 1;   // tiles that they lie in
 
 struct tree_args {
     const uint16_t* q;        // [total_q][n_q_local][D]
@@ -52,14 +55,15 @@ struct tree_args {
     uint32_t last_block;      // n_pool_blocks - 1
     float scale_log2e;
     int32_t group, batch, max_ctx_len, mask_words;
-    int32_t workgroups, least_tiles;   // shares that the axis of tiles is cut into, and the least tiles of a share
-    float* part_o;            // [2 workgroups][32 RW][D]: slot 2 w the first piece of workgroup w, 2 w + 1 its last
-    float* part_ml;           // [2 workgroups][32 RW][2] (reference in exponent units, sum of weights)
+    int32_t teams, least_tiles;   // shares that the axis of tiles is cut into, and the least tiles of a share
+    float* part_o;            // [2 teams n_kv_local][32 RW][D]: slot 2 w the first piece of workgroup w, 2 w + 1 its last
+    float* part_ml;           // [2 teams n_kv_local][32 RW][2] (reference in exponent units, sum of weights)
     // weights:
     float* scores;            // [batch][n_q_local][score_stride] exponents: score * scale * log2(e)
     float* row_ml;            // [batch][n_q_local][2] of pairs that were not cut
     float* sums;              // [batch][n_kv_local][sum_stride]
     int64_t score_stride, sum_stride;
+    int32_t chunk;            // tokens per workgroup of the launch that adds up weights
 };
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
@@ -104,7 +108,7 @@ __device__ __forceinline__ bool not_finite(uint32_t x)
 // What a sequence brings: cached tokens, new ones, tiles of a pair, row blocks of a head.
 struct seq_work {
     int n, q0, q_len, tiles, blocks;
-    __device__ int64_t total(int heads) const { return (int64_t)tiles * blocks * heads; }
+    __device__ int64_t total() const { return (int64_t)tiles * blocks; }   // of a head
 };
 template <int RB>
 __device__ __forceinline__ seq_work work_of(const tree_args& a, int s)
@@ -120,7 +124,7 @@ __device__ __forceinline__ seq_work work_of(const tree_args& a, int s)
 }
 __device__ __forceinline__ int64_t share_of(const tree_args& a, int64_t total)
 {
-    const int64_t even = (total + a.workgroups - 1) / a.workgroups;
+    const int64_t even = (total + a.teams - 1) / a.teams;
     return even > a.least_tiles ? even : a.least_tiles;
 }
 
@@ -139,14 +143,14 @@ __device__ __forceinline__ int64_t block_sum(int64_t x, int64_t* s_sum)
     return t;
 }
 
-// The share of this workgroup: [from, to) on the axis, the sequence that holds `from` and its offset in it.
+// The share of this team: [from, to) on the axis, the sequence that holds `from` and its offset in it.
 template <int NT, int RB>
-__device__ __forceinline__ void find_share(const tree_args& a, int64_t* s_sum, int64_t& from, int64_t& to, int& seq, int64_t& offset)
+__device__ __forceinline__ void find_share(const tree_args& a, int team, int64_t* s_sum, int64_t& from, int64_t& to, int& seq, int64_t& offset)
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int each = (a.batch + NT - 1) / NT, s0 = min(tid * each, a.batch), s1 = min(s0 + each, a.batch);
     int64_t mine = 0;
-    for (int s = s0; s < s1; ++s) mine += work_of<RB>(a, s).total(a.v.n_kv_local);
+    for (int s = s0; s < s1; ++s) mine += work_of<RB>(a, s).total();
     int64_t incl = mine;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
@@ -162,12 +166,12 @@ __device__ __forceinline__ void find_share(const tree_args& a, int64_t* s_sum, i
         before += w < wave ? s_sum[w] : 0;
     }
     const int64_t share = share_of(a, total);
-    from = (int64_t)blockIdx.x * share;
+    from = (int64_t)team * share;
     to = min(from + share, total);
     __syncthreads();
     if (from >= before && from < before + mine) {   // one thread at most
         int s = s0;
-        for (int64_t w; from >= before + (w = work_of<RB>(a, s).total(a.v.n_kv_local)); ++s) before += w;
+        for (int64_t w; from >= before + (w = work_of<RB>(a, s).total()); ++s) before += w;
         s_sum[0] = s;
         s_sum[1] = from - before;
     }
@@ -181,14 +185,19 @@ __device__ __forceinline__ void find_share(const tree_args& a, int64_t* s_sum, i
 template <int D> constexpr int tile_pieces() { return kKeys * D / 8; }
 
 template <int D, int RW, bool SUMS>
-__global__ __launch_bounds__(RW == 8 ? 512 : 256, RW == 4 ? 3 : RW == 1 ? 1 : 2) void tree_kernel(tree_args a)
+__global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args a)
 {
     constexpr int NW = RW < 4 ? 4 : RW, KW = NW / RW, NT = 64 * NW, RB = 32 * RW;
     constexpr int NJ = D / 32, NK = D / 16, kPieces = tile_pieces<D>(), kRow = 2 * D;
     // K: piece c of row t at c ^ f(t), V: at c ^ g(t): operand reads without bank conflicts.  An array per buffer: the compiler
     // then knows that loads landing in one do not touch the operands read from another.
+    constexpr int NB = RW >= 4 ? 4 : 2, kMore = NB > 2 ? KW * kPieces : 1;
     __shared__ kv_u32x4 s_k0[KW * kPieces], s_k1[KW * kPieces], s_v0[KW * kPieces], s_v1[KW * kPieces];
+    __shared__ kv_u32x4 s_k2[kMore], s_k3[kMore], s_v2[kMore], s_v3[kMore];
+    auto k_buf = [&](int x) { return NB == 2 ? ((x & 1) ? s_k1 : s_k0) : (x & 2) ? ((x & 1) ? s_k3 : s_k2) : ((x & 1) ? s_k1 : s_k0); };
+    auto v_buf = [&](int x) { return NB == 2 ? ((x & 1) ? s_v1 : s_v0) : (x & 2) ? ((x & 1) ? s_v3 : s_v2) : ((x & 1) ? s_v1 : s_v0); };
     __shared__ float2 s_ml[KW > 1 ? NW * 32 : 1];
+    __shared__ uint32_t s_seen[SUMS ? 1 : kEdgeTiles][SUMS ? 1 : RB];   // which tokens of the tiles that hold drafted ones a row sees
     __shared__ int64_t s_sum[NW];
 
     const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
@@ -199,7 +208,8 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, RW == 4 ? 3 : RW == 1 ? 1 : 2)
 
     int64_t from, to, offset;
     int s;
-    find_share<NT, RB>(a, s_sum, from, to, s, offset);
+    const int team = (int)blockIdx.x / Hl, h = (int)blockIdx.x - team * Hl;
+    find_share<NT, RB>(a, team, s_sum, from, to, s, offset);
 
     // ---- what does not change from piece to piece -------------------------------------------------
     const int64_t stride_bytes = (int64_t)v.token_stride * 2, block_bytes = v.block_elems * 2, plane_bytes = v.plane_elems * 2;
@@ -211,11 +221,10 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, RW == 4 ? 3 : RW == 1 ? 1 : 2)
     constexpr int kRowsEach = 512 / D;
     const int first_part = kSplitPlanes ? (rw & (NK - 1)) : rw * NP;
     uint32_t k_lane[NP], v_lane[NP];
-    int row16[NP];
+    const int row_first = (first_part * kRowsEach & 15) + lane / (D / 8);   // within a group, of the first part
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
         const int row = ((first_part + i) * kRowsEach + lane / (D / 8)) & 15, c = lane & (D / 8 - 1);
-        row16[i] = row;
         const int kc = D == 128 ? c ^ row : c ^ (row >> 1), vc = D == 128 ? c ^ (4 * (row & 3)) : c ^ (4 * ((row >> 1) & 1));
         k_lane[i] = (uint32_t)(row * (int)stride_bytes + (kc << 4));
         v_lane[i] = (uint32_t)(row * (int)stride_bytes + (vc << 4));
@@ -223,23 +232,22 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, RW == 4 ? 3 : RW == 1 ? 1 : 2)
     uint32_t k_off, v_off[NJ];
     {
         const int p = lane & 15, sub = (lane >> 4) & 1;
-        k_off = (uint32_t)(col * kRow + ((half ^ (D == 128 ? (col & 15) : ((col >> 1) & 7))) << 4));
+        k_off = (uint32_t)(kg * kPieces * 16 + col * kRow + ((half ^ (D == 128 ? (col & 15) : ((col >> 1) & 7))) << 4));
         const int vrow = 4 * half + (p >> 2), g = D == 128 ? 4 * (vrow & 3) : 4 * ((vrow >> 1) & 1);
 #pragma unroll
         for (int j = 0; j < NJ; ++j)
-            v_off[j] = (uint32_t)(vrow * kRow + (((4 * j + 2 * sub + ((p & 3) >> 1)) ^ g) << 4) + (p & 1) * 8);
+            v_off[j] = (uint32_t)(kg * kPieces * 16 + vrow * kRow + (((4 * j + 2 * sub + ((p & 3) >> 1)) ^ g) << 4) + (p & 1) * 8);
     }
 
     for (int64_t at = from; at < to;) {
-        // ---- the next piece: tiles [t0, t0 + count) of pair (s, h, rb) -----------------------------
+        // ---- the next piece: tiles [t0, t0 + count) of block rb of sequence s -----------------------------
         const seq_work w = work_of<RB>(a, s);
-        if (offset >= w.total(Hl)) {
-            offset -= w.total(Hl);
+        if (offset >= w.total()) {
+            offset -= w.total();
             ++s;
             continue;
         }
-        const int pair = uniform((int)(offset / w.tiles)), t0 = uniform((int)(offset - (int64_t)pair * w.tiles));
-        const int h = pair / w.blocks, rb = pair - h * w.blocks;
+        const int rb = uniform((int)(offset / w.tiles)), t0 = uniform((int)(offset - (int64_t)rb * w.tiles));
         const int count = (int)min((int64_t)(w.tiles - t0), to - at);
         const bool cut = count < w.tiles;
         const int n = w.n, first = n - w.q_len;          // the first drafted token
@@ -257,88 +265,207 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, RW == 4 ? 3 : RW == 1 ? 1 : 2)
             const int g = group_at(window);
             return (int64_t)min(id, a.last_block) * block_bytes + (int64_t)(g % groups_per_block) * 16 * stride_bytes;
         };
-        uint32_t next_id = request_ids(0);
-        int64_t place = places(next_id, 0);
-        next_id = request_ids(1);
-        auto stage = [&](int i, kv_u32x4* dk, kv_u32x4* dv) {
+        // Tiles are staged in order, K of a tile before its V: the places of the next tile's groups for each
+        struct cursor {
+            int i;          // tile that is fetched next
+            int64_t place;  // of this window
+            uint32_t id;    // of the next
+        };
+        cursor at_k{0, places(request_ids(0), 0), 0}, at_v;
+        at_k.id = request_ids(1);
+        const cursor at_start = at_k;
+        at_v = at_k;
+        auto stage = [&](cursor& x, const uint32_t (&at_lane)[NP], int64_t plane, kv_u32x4* dst) {
+            const int i = x.i++;
+            if (i >= mine) return;
             if ((i & 31) == 0 && i > 0) {
-                place = places(next_id, i >> 5);
-                next_id = request_ids((i >> 5) + 1);
+                x.place = places(x.id, i >> 5);
+                x.id = request_ids((i >> 5) + 1);
             }
             const int tile = t0 + kg + i * KW;
-            const bool end = 2 * tile + 1 >= last_group;
-            auto rows_of = [&](int g) -> const char* {
+            auto rows_of = [&](int g) {
                 const int l = 2 * (i & 31) + g;
-                const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)place, l);
-                const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(place >> 32), l);
-                return pool_head + (int64_t)((uint64_t)lo | (uint64_t)hi << 32);
+                const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)x.place, l);
+                const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(x.place >> 32), l);
+                return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(pool_head + plane + (int64_t)((uint64_t)lo | (uint64_t)hi << 32)), 0,
+                                                         0x7ffffff0, 0x00020000);
             };
-            auto fill = [&](const uint32_t* at_lane, int64_t plane, kv_u32x4* dst) {
+            // (a wavefront that fills parts of both groups looks two places up, the others one)
+            constexpr bool kBoth = NP * kRowsEach > 16;
+            const __amdgpu_buffer_rsrc_t r0 = rows_of(first_part * kRowsEach >> 4), r1 = kBoth ? rows_of(1) : r0;
+            auto fill = [&](auto end) {
 #pragma unroll
                 for (int p = 0; p < NP; ++p) {
-                    const int part = first_part + p, g = part * kRowsEach >> 4;
-                    // rows past the end of the sequence are its last one again (masked later)
-                    const int limit = n - 1 - 16 * min(2 * tile + g, last_group);
-                    const uint32_t past = end ? (uint32_t)(max(row16[p] - limit, 0) * (int)stride_bytes) : 0u;
-                    const __amdgpu_buffer_rsrc_t r =
-                        __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(rows_of(g) + plane), 0, 0x7ffffff0, 0x00020000);
-                    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr)(dst + kg * kPieces + part * 64), 16, at_lane[p] - past, 0, 0, 0);
+                    const int g = kBoth ? p * kRowsEach >> 4 : first_part * kRowsEach >> 4;
+                    uint32_t off = at_lane[p];
+                    if constexpr (decltype(end)::value) {   // rows past the end of the sequence are its last one again (masked later)
+                        const int limit = n - 1 - 16 * min(2 * tile + g, last_group), row = (p * kRowsEach & 15) + row_first;
+                        off -= (uint32_t)(max((row & 15) - limit, 0) * (int)stride_bytes);
+                    }
+                    __builtin_amdgcn_raw_ptr_buffer_load_lds(kBoth && g ? r1 : r0, (lds_ptr)(dst + kg * kPieces + (first_part + p) * 64), 16, off,
+                                                             0, 0, 0);
                 }
             };
-            if (!kSplitPlanes || rw < NK) fill(k_lane, 0, dk);
-            if (!kSplitPlanes || rw >= NK) fill(v_lane, plane_bytes, dv);
+            if (2 * tile + 1 < last_group) fill(std::false_type());
+            else fill(std::true_type());
         };
-        auto staged = [&]() {
-            __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
+        auto stage_k = [&](kv_u32x4* dst) {
+            if (!kSplitPlanes || rw < NK) stage(at_k, k_lane, 0, dst);
+        };
+        auto stage_v = [&](kv_u32x4* dst) {
+            if (!kSplitPlanes || rw >= NK) stage(at_v, v_lane, plane_bytes, dst);
+        };
+        // this wavefront's loads have landed, and then those of the wavefronts that share its tiles
+        auto staged = [&](auto under_way) {   // but for the last so many
+            constexpr int kLeft = decltype(under_way)::value;
+            __builtin_amdgcn_s_waitcnt(0x0f70 | (kLeft & 15) | (kLeft >> 4) << 14);   // vmcnt
             if constexpr (RW > 1) __syncthreads();
             else asm volatile("" ::: "memory");
         };
-        if (mine > 0) stage(0, s_k0, s_v0);
+#pragma unroll
+        for (int x = 0; x < NB - 1; ++x) {
+            stage_k(k_buf(x));
+            stage_v(v_buf(x));
+        }
+        stage_k(k_buf(NB - 1));
 
         // ---- this lane's query row ----------------------------------------------------------------
         const int rho = rb * RB + min(rw * 32 + col, rows - 1);      // (padding columns repeat the last row)
         const int64_t qrow = (int64_t)(w.q0 + rho / G);
         const int64_t orow = (qrow * v.n_q_local + h * G + rho % G) * D;
-        const bool real = rw * 32 + col < rows;
+        const int srow = rw * 32 + col;
+        const bool real = srow < rows;
         bf16x8 qb[NK];
 #pragma unroll
         for (int kk = 0; kk < NK; ++kk)
             qb[kk] = as_bf16x8(*reinterpret_cast<const kv_u32x4*>(a.q + orow + half * 8 + kk * 16));
 
-        float neg_m = kUnset, l = 0.f;
-        bool unset = true;
+        const int first_edge = (SUMS ? n : first) >> 5;   // tiles from there on hold drafted tokens or the end of the sequence
+        if constexpr (!SUMS) {
+            if (t0 + count > first_edge) {
+                // The windows of 32 tokens that the tiles are, cut out of the rows' mask words; what lies before the draft is seen
+                if ((int)threadIdx.x < rows) {
+                    const uint32_t* words = reinterpret_cast<const uint32_t*>(a.mask) +
+                                            ((int64_t)w.q0 + (rb * RB + (int)threadIdx.x) / G) * 2 * a.mask_words;
+                    const int shift = first & 31;
+                    uint32_t before = ~0u;
+#pragma unroll
+                    for (int e = 0; e < kEdgeTiles; ++e) {
+                        const int here = n - kKeys * (first_edge + e);   // tokens of the tile that exist
+                        if (here <= 0) break;
+                        const uint32_t word = e < 2 * a.mask_words ? words[e] : 0u;
+                        const uint32_t window = (uint32_t)((((uint64_t)word << 32 | before) << shift) >> 32);
+                        s_seen[e][threadIdx.x] = here >= 32 ? window : window & ((1u << here) - 1u);
+                        before = word;
+                    }
+                }
+                __syncthreads();
+            }
+        }
+
+        float neg_m, l;
+        bool unset;
         f32x16 o[NJ];
+        auto clear = [&]() {
+            neg_m = kUnset;
+            l = 0.f;
+            unset = true;
 #pragma unroll
-        for (int j = 0; j < NJ; ++j)
+            for (int j = 0; j < NJ; ++j)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) o[j][i] = 0.f;
+                for (int i = 0; i < 16; ++i) o[j][i] = 0.f;
+        };
+        clear();
 
         auto k_operand = [&](const kv_u32x4* sk, int kk) {
-            return as_bf16x8(*reinterpret_cast<const kv_u32x4*>(reinterpret_cast<const char*>(sk + kg * kPieces) + (k_off ^ (32 * kk))));
+            uint32_t off = k_off;   // (opaque: the compiler would keep an offset per step in registers)
+            if (kk > 0) asm volatile("v_xor_b32 %0, %1, %2" : "=v"(off) : "i"(32 * kk), "v"(k_off));
+            return as_bf16x8(*reinterpret_cast<const kv_u32x4*>(reinterpret_cast<const char*>(sk) + off));
         };
-        auto v_operand = [&](const kv_u32x4* sv, int c, int j) {
-            const char* const p = reinterpret_cast<const char*>(sv + kg * kPieces) + v_off[j] + c * 16 * kRow;
+        auto v_operand = [&](const kv_u32x4* sv, int u) {   // u = NJ c + j
+            const char* const p = reinterpret_cast<const char*>(sv) + v_off[u % NJ] + (u / NJ) * 16 * kRow;
             const bits16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_bits16x4_ptr)p);
             const bits16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_bits16x4_ptr)(p + 8 * kRow));
             return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
         };
-        // Which of the 32 tokens of a tile this lane's row sees
-        auto seen_by_row = [&](int base) -> uint32_t {
-            const int here = n - base;   // tokens of the tile that exist
-            const uint32_t valid = here >= 32 ? ~0u : (1u << here) - 1u;
-            if constexpr (SUMS) return valid;
-            const int o_ = base - first;   // node number of the tile's first token
-            if (o_ <= -32) return valid;
-            const unsigned long long* words = a.mask + qrow * a.mask_words;
-            const int at_word = max(o_, 0) >> 6;
-            const unsigned long long w0 = words[min(at_word, a.mask_words - 1)], w1 = words[min(at_word + 1, a.mask_words - 1)];
-            uint32_t bits;
-            if (o_ < 0) bits = (uint32_t)(w0 << -o_) | ((1u << -o_) - 1u);
-            else bits = (uint32_t)(w0 >> (o_ & 63)) | ((o_ & 63) > 32 ? (uint32_t)(w1 << (64 - (o_ & 63))) : 0u);
-            return bits & valid;
+        f32x16 sc, ex;    // scores of a tile, then exponents: score scale log2(e) - reference
+        uint32_t pw[8];   // weights
+        auto zero = [&]() {
+            f32x16 x;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[e] = 0.f;
+            return x;
         };
-        // Sums of values where a masked token may hold an infinity or NaN, which a weight of 0 would turn into NaN: token by token,
-        // without those of no weight.
+        auto weights = [&](int u) {   // two of the sixteen
+            const float e0 = fast_exp2(ex[2 * u]), e1 = fast_exp2(ex[2 * u + 1]);
+            pw[u] = pack_bf16x2(e0, e1);
+            if constexpr (SUMS) l += e0 + e1;   // the weights handed out are not rounded
+            else l = add_pair(pw[u], l);        // the same rounding above and below the fraction
+        };
+        auto weight_operand = [&](int c) { return as_bf16x8(kv_u32x4{pw[4 * c], pw[4 * c + 1], pw[4 * c + 2], pw[4 * c + 3]}); };
+        auto keep_scores = [&](int base) {
+            if constexpr (SUMS) {
+                if (real) {
+                    float* dst = a.scores + ((int64_t)s * v.n_q_local + h * G + rho % G) * a.score_stride + base + 4 * half;
+#pragma unroll
+                    for (int u = 0; u < 4; ++u)
+                        *reinterpret_cast<f32x4*>(dst + 8 * u) =
+                            f32x4{sc[4 * u] * a.scale_log2e, sc[4 * u + 1] * a.scale_log2e, sc[4 * u + 2] * a.scale_log2e, sc[4 * u + 3] * a.scale_log2e};
+                }
+            }
+        };
+        // A column without a key yet has no reference; its first key sets it.
+        auto first_reference = [&]() {
+            if (unset) {
+                const float mx = column_max(sc);
+                if (neg_m == kUnset && mx != kNegInf) neg_m = -mx * a.scale_log2e;
+                unset = __builtin_amdgcn_ballot_w64(neg_m == kUnset) != 0;
+            }
+        };
+        // The reference may lag behind the running maximum by 2^8 (weights up to 2^8 are as exact), so that the accumulators are
+        // rescaled rarely.
+        constexpr float kLag = 8.0f;
+        auto move_reference = [&](float top) {
+            if (__builtin_amdgcn_ballot_w64(top > kLag) != 0) {
+                // (from the scores again: exponents far above the old reference have lost the digits that the new one needs)
+                const float next = fminf(neg_m, -column_max(sc) * a.scale_log2e), alpha = fast_exp2(next - neg_m);
+                l *= alpha;
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) o[j] *= alpha;
+                neg_m = next;
+#pragma unroll
+                for (int x = 0; x < 16; ++x) ex[x] = __builtin_fmaf(sc[x], a.scale_log2e, neg_m);
+            }
+        };
+        auto exponents = [&]() {
+            float top = kNegInf;
+#pragma unroll
+            for (int x = 0; x < 16; ++x) {
+                ex[x] = __builtin_fmaf(sc[x], a.scale_log2e, neg_m);
+                top = fmaxf(top, ex[x]);
+            }
+            move_reference(top);
+        };
+        auto scores = [&](const kv_u32x4* sk) {
+            bf16x8 ka[NK];
+#pragma unroll
+            for (int kk = 0; kk < NK; ++kk) ka[kk] = k_operand(sk, kk);
+            __builtin_amdgcn_sched_barrier(0);
+            sc = zero();
+#pragma unroll
+            for (int kk = 0; kk < NK; ++kk) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[kk], qb[kk], sc, 0, 0, 0);
+        };
+        auto values = [&](const kv_u32x4* sv) {
+            bf16x8 va[2 * NJ];
+#pragma unroll
+            for (int u = 0; u < 2 * NJ; ++u) va[u] = v_operand(sv, u);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int u = 0; u < 2 * NJ; ++u)
+                o[u % NJ] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[u], weight_operand(u / NJ), o[u % NJ], 0, 0, 0);
+        };
+        // Sums of values where a token that a row does not see may hold an infinity or NaN, which its weight of 0 would turn into NaN:
+        // token by token, without those of no weight.
         auto add_values_one_by_one = [&](const kv_u32x4* sv, const uint32_t* pw) {
 #pragma unroll 1
             for (int t = 0; t < 32; ++t) {
@@ -364,96 +491,149 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, RW == 4 ? 3 : RW == 1 ? 1 : 2)
                     }
             }
         };
-        auto tile_step = [&](int i, const kv_u32x4* sk, const kv_u32x4* sv) {
-            const int base = kKeys * (t0 + kg + i * KW);
-            f32x16 sc;
+        auto hide = [&](int tile) {   // scores of tokens that the row does not see
+            if (tile < first_edge) return;
+            uint32_t seen;
+            if constexpr (SUMS) seen = n - kKeys * tile >= 32 ? ~0u : (1u << (n - kKeys * tile)) - 1u;
+            else seen = s_seen[tile - first_edge][srow];
+            seen >>= 4 * half;
 #pragma unroll
-            for (int x = 0; x < 16; ++x) sc[x] = 0.f;
-#pragma unroll
-            for (int kk = 0; kk < NK; ++kk) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_operand(sk, kk), qb[kk], sc, 0, 0, 0);
-            // tiles that hold drafted tokens or the end of the sequence
-            const bool edge = base + kKeys > (SUMS ? n : first);
-            if (edge) {
-                const uint32_t seen = seen_by_row(base) >> (4 * half);
-#pragma unroll
-                for (int x = 0; x < 16; ++x) sc[x] = (seen >> (8 * (x >> 2) + (x & 3))) & 1 ? sc[x] : kNegInf;
-            }
-            if constexpr (SUMS) {
-                if (real) {
-                    float* dst = a.scores + ((int64_t)s * v.n_q_local + h * G + rho % G) * a.score_stride + base + 4 * half;
-#pragma unroll
-                    for (int u = 0; u < 4; ++u)
-                        *reinterpret_cast<f32x4*>(dst + 8 * u) =
-                            f32x4{sc[4 * u] * a.scale_log2e, sc[4 * u + 1] * a.scale_log2e, sc[4 * u + 2] * a.scale_log2e, sc[4 * u + 3] * a.scale_log2e};
-                }
-            }
-            // Exponents against a reference that may lag behind the running maximum by 2^8 (weights up to 2^8 are as exact), so that the
-            // accumulators are rescaled rarely.  A column without a key yet has none; its first key sets it.
-            if (unset) {
-                const float mx = column_max(sc);
-                if (neg_m == kUnset && mx != kNegInf) neg_m = -mx * a.scale_log2e;
-                unset = __builtin_amdgcn_ballot_w64(neg_m == kUnset) != 0;
-            }
-            constexpr float kLag = 8.0f;
-            f32x16 ex;
-            float top = kNegInf;
-#pragma unroll
-            for (int x = 0; x < 16; ++x) {
-                ex[x] = __builtin_fmaf(sc[x], a.scale_log2e, neg_m);
-                top = fmaxf(top, ex[x]);
-            }
-            if (__builtin_amdgcn_ballot_w64(top > kLag) != 0) {
-                // (from the scores again: exponents far above the old reference have lost the digits that the new one needs)
-                const float next = fminf(neg_m, -column_max(sc) * a.scale_log2e), alpha = fast_exp2(next - neg_m);
-                l *= alpha;
-#pragma unroll
-                for (int j = 0; j < NJ; ++j) o[j] *= alpha;
-                neg_m = next;
-#pragma unroll
-                for (int x = 0; x < 16; ++x) ex[x] = __builtin_fmaf(sc[x], a.scale_log2e, neg_m);
-            }
-            uint32_t pw[8];
-#pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const float e0 = fast_exp2(ex[2 * u]), e1 = fast_exp2(ex[2 * u + 1]);
-                pw[u] = pack_bf16x2(e0, e1);
-                if constexpr (SUMS) l += e0 + e1;   // the weights handed out are not rounded
-                else l = add_pair(pw[u], l);        // the same rounding above and below the fraction
-            }
-            if (edge) {
-                bool odd = false;
-#pragma unroll
-                for (int x = 0; x < kPieces / 64; ++x) {
-                    const kv_u32x4 y = sv[kg * kPieces + x * 64 + lane];
-                    odd = odd || not_finite(y[0]) || not_finite(y[1]) || not_finite(y[2]) || not_finite(y[3]);
-                }
-                if (__builtin_amdgcn_ballot_w64(odd) != 0) {
-                    add_values_one_by_one(sv, pw);
-                    return;
-                }
-            }
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                const bf16x8 pb = as_bf16x8(kv_u32x4{pw[4 * c], pw[4 * c + 1], pw[4 * c + 2], pw[4 * c + 3]});
-#pragma unroll
-                for (int j = 0; j < NJ; ++j) o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand(sv, c, j), pb, o[j], 0, 0, 0);
-            }
+            for (int x = 0; x < 16; ++x) sc[x] = (seen >> (8 * (x >> 2) + (x & 3))) & 1 ? sc[x] : kNegInf;
         };
-        // Tile i + 1 lands while tile i is worked on.  The barrier (of wavefronts that share tiles) says both that every
-        // part of tile i is there and that nobody reads tile i - 1 any more.
-        for (int i = 0; i < iters; i += 2) {
-            staged();
-            if (i + 1 < mine) stage(i + 1, s_k1, s_v1);
-            if (i < mine && !idle) tile_step(i, s_k0, s_v0);
-            if (i + 1 >= iters) break;
-            staged();
-            if (i + 2 < mine) stage(i + 2, s_k0, s_v0);
-            if (i + 1 < mine && !idle) tile_step(i + 1, s_k1, s_v1);
+        auto whole_step = [&](auto careful, int i, const kv_u32x4* sk, const kv_u32x4* sv) {
+            const int tile = t0 + kg + i * KW;
+            scores(sk);
+            hide(tile);
+            keep_scores(kKeys * tile);
+            first_reference();
+            exponents();
+#pragma unroll
+            for (int u = 0; u < 8; ++u) weights(u);
+            if (decltype(careful)::value && tile >= first_edge) add_values_one_by_one(sv, pw);
+            else values(sv);
+        };
+        // The chain of a tile is cut across tiles: the weights of tile i are made beside the score products of tile i + 1, its
+        // output products run beside the exponents of tile i + 1.  The order is pinned: a product, the vector
+        // instructions that fit under it, the operand read of the second product after it.  The loads of the
+        // NB - 1 tiles after it are under way meanwhile.
+        constexpr int kAhead = 2;
+        auto step = [&](auto phase, int i) {
+            constexpr int B = decltype(phase)::value;   // i % NB
+            kv_u32x4* const k_next = k_buf(B + 1);
+            kv_u32x4* const v_now = v_buf(B);
+            stage_v(v_buf(B + NB - 1));
+            stage_k(k_buf(B));
+            if (!idle) {
+                bf16x8 ka[NK], va[2 * NJ];
+#pragma unroll
+                for (int kk = 0; kk < kAhead; ++kk) ka[kk] = k_operand(k_next, kk);
+                __builtin_amdgcn_sched_barrier(0);
+                sc = zero();
+#pragma unroll
+                for (int kk = 0; kk < NK; ++kk) {
+                    sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[kk], qb[kk], sc, 0, 0, 0);
+                    if (kk + kAhead < NK) ka[kk + kAhead] = k_operand(k_next, kk + kAhead);
+                    else va[kk + kAhead - NK] = v_operand(v_now, kk + kAhead - NK);
+#pragma unroll
+                    for (int u = kk * 8 / NK; u < (kk + 1) * 8 / NK; ++u) {
+                        weights(u);
+                        asm volatile("" : "+v"(pw[u]), "+v"(l));   // (else moved to where they are used)
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                const bf16x8 pb[2] = {weight_operand(0), weight_operand(1)};
+                const int tile = t0 + kg + (i + 1) * KW;
+                hide(tile);
+                keep_scores(kKeys * tile);
+                first_reference();
+                float top = kNegInf;
+#pragma unroll
+                for (int u = 0; u < 2 * NJ; ++u) {
+                    o[u % NJ] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[u], pb[u / NJ], o[u % NJ], 0, 0, 0);
+                    if (u + kAhead < 2 * NJ) va[u + kAhead] = v_operand(v_now, u + kAhead);
+                    // (the first two give the last score product time to finish)
+#pragma unroll
+                    for (int x = u < 2 ? 16 : 16 * (u - 2) / (2 * NJ - 2); x < (u < 2 ? 0 : 16 * (u - 1) / (2 * NJ - 2)); ++x) {
+                        ex[x] = __builtin_fmaf(sc[x], a.scale_log2e, neg_m);
+                        top = fmaxf(top, ex[x]);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                move_reference(top);
+            }
+            // K of tile i + 2 and V of tile i + 1 are needed next: what the last NB - 2 steps asked for may still be under way
+            if (NB > 2 && i + NB < mine) staged(std::integral_constant<int, (NB - 2) * (kSplitPlanes ? 1 : 2) * NP>());
+            else staged(std::integral_constant<int, 0>());
+        };
+        staged(std::integral_constant<int, 0>());
+        const int common = count / KW;   // tiles that every key group has
+        int i = 0;
+        if (common > 0) {
+            if (!idle) {
+                scores(s_k0);
+                hide(t0 + kg);
+                keep_scores(kKeys * (t0 + kg));
+                first_reference();
+                exponents();
+            }
+            if constexpr (RW > 1) __syncthreads();   // (K of tile 0 is read, its buffer may be filled again)
+            for (; i + NB < common; i += NB) {
+                step(std::integral_constant<int, 0>(), i);
+                step(std::integral_constant<int, 1>(), i + 1);
+                if constexpr (NB > 2) {
+                    step(std::integral_constant<int, 2>(), i + 2);
+                    step(std::integral_constant<int, 3>(), i + 3);
+                }
+            }
+            if (i + 1 < common) {
+                step(std::integral_constant<int, 0>(), i);
+                ++i;
+                if (NB > 2 && i + 1 < common) {
+                    step(std::integral_constant<int, 1>(), i);
+                    ++i;
+                    if (NB > 2 && i + 1 < common) {
+                        step(std::integral_constant<int, 2>(), i);
+                        ++i;
+                    }
+                }
+            }
+            // the last one
+            if constexpr (KW > 1) stage_v(v_buf(i + 1));
+            if (!idle) {
+#pragma unroll
+                for (int u = 0; u < 8; ++u) weights(u);
+                values(v_buf(i));
+            }
+            ++i;
+            if constexpr (KW > 1) staged(std::integral_constant<int, 0>());
+        }
+        if (KW > 1 && i < mine && !idle) whole_step(std::false_type(), i, k_buf(i), v_buf(i));   // one that only some key groups have
+        // A value that is no number in a tile where rows do not see every token may have reached rows that do not see it: once more then,
+        // tile by tile, with care.
+        if (t0 + count > first_edge) {
+            float probe = 0.f;
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int x = 0; x < 16; ++x) probe = __builtin_fmaf(o[j][x], 0.f, probe);   // 0, or NaN
+            if (__syncthreads_or(!(probe == 0.f))) {
+                clear();
+                at_k = at_start;
+                at_v = at_start;
+#pragma unroll 1
+                for (i = 0; i < iters; ++i) {
+                    stage_k(s_k0);
+                    stage_v(s_v0);
+                    staged(std::integral_constant<int, 0>());
+                    if (i < mine && !idle) whole_step(std::true_type(), i, s_k0, s_v0);
+                    __syncthreads();
+                }
+            }
         }
 
         // ---- the piece's rows ----------------------------------------------------------------------
         l = half_sum(l);
-        const int slot = 2 * (int)blockIdx.x + (at > from ? 1 : 0), srow = rw * 32 + col;
+        const int slot = 2 * (int)blockIdx.x + (at > from ? 1 : 0);
         // groups of four accumulator registers: x = 4 j + u4 holds elements 8 x + 4 half ..
         constexpr int NX = 4 * NJ, XW = NX / KW;   // each of the KW wavefronts of a row finishes XW of them
         f32x4 acc[XW];
@@ -475,16 +655,18 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, RW == 4 ? 3 : RW == 1 ? 1 : 2)
             for (int k = 0; k < KW; ++k) m_all = fmaxf(m_all, s_ml[(k * RW + rw) * 32 + col].x);
 #pragma unroll
             for (int x = 0; x < XW; ++x) acc[x] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
+            // (a wavefront that saw no key has weight 0, whatever its sums are)
+#pragma unroll 1
             for (int k = 0; k < KW; ++k) {
                 const float2 ml = s_ml[(k * RW + rw) * 32 + col];
                 const float f = ml.y != 0.f ? fast_exp2(ml.x - m_all) : 0.f;
                 l_all += f * ml.y;
-                const kv_u32x4* from_k = area(k * RW + rw) + lane;
+                const kv_u32x4* from_k = area(k * RW + rw) + kg * XW * 64 + lane;
 #pragma unroll
                 for (int x = 0; x < XW; ++x) {
-                    const f32x4 y = __builtin_bit_cast(f32x4, from_k[(kg * XW + x) * 64]);
-                    if (f != 0.f) acc[x] += y * f;
+                    const f32x4 y = __builtin_bit_cast(f32x4, from_k[x * 64]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[x][e] = f != 0.f ? __builtin_fmaf(y[e], f, acc[x][e]) : acc[x][e];
                 }
             }
             __syncthreads();   // (before the next piece's tiles land)
@@ -520,93 +702,210 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, RW == 4 ? 3 : RW == 1 ? 1 : 2)
     }
 }
 
-// The second launch.  Block (s, pair of s, part): the pieces of a cut pair's rows are added up in the order of the workgroups,
+// The second launch adds up the pieces of cut pairs, whose slots follow from the shares,
 //   out[row] = sum_z o_z 2^(m_z - M) / sum_z l_z 2^(m_z - M),  M = max_z m_z,
-// D / 4 lanes a row.  Rows of sequences without tokens are zeros.  SUMS: the parts are chunks of tokens; each works out (M, L) of the pair's
-// G rows and adds sum_g 2^(score_g - M_g) / L_g to the tokens of its chunk; part 0 adds up the rows too.
-template <int D, int RW, bool SUMS>
-__global__ __launch_bounds__(256) void tree_merge_kernel(tree_args a)
+// D / 4 lanes a row.  What bounds it is the latency of the partials' loads, so several are requested at once.  Rows of
+// sequences without tokens are zeros.
+struct piece_list {
+    int rows, h, rb;          // rows of the pair
+    int w0, w1;               // teams that hold its first and last piece
+    int skew;                 // the first piece is the last of its workgroup
+    int64_t heads;
+    __device__ int64_t slot(int z) const { return 2 * ((int64_t)(w0 + z) * heads + h) + (z == 0 ? skew : 0); }
+    __device__ int count() const { return w1 - w0 + 1; }
+};
+template <int RB>
+__device__ __forceinline__ piece_list pieces_of(const tree_args& a, const seq_work& w, int s, int h, int rb, int64_t* s_sum)
 {
-    constexpr int NT = 256, RB = 32 * RW, kLanes = D / 4, kRows = NT / kLanes;
-    __shared__ int64_t s_sum[NT / 64];
-    __shared__ float2 s_ml[SUMS ? 32 : 1];
-    const int s = blockIdx.x, Hl = a.v.n_kv_local, G = a.group, tid = threadIdx.x;
-    const seq_work w = work_of<RB>(a, s);
-    const int pair = blockIdx.y;
-    const int cg = tid % kLanes, r = tid / kLanes;
-    if (w.n <= 0 && w.q_len > 0) {   // nothing cached: zeros (block y writes head y's rows)
-        if (pair < Hl)
-            for (int x = blockIdx.z * kRows + r; x < w.q_len * G; x += gridDim.z * kRows)
-                *reinterpret_cast<uint2*>(a.out + ((int64_t)(w.q0 + x / G) * a.v.n_q_local + pair * G + x % G) * D + 4 * cg) = make_uint2(0u, 0u);
-        return;
-    }
-    if (pair >= w.blocks * Hl) return;
-    const int h = pair / w.blocks, rb = pair - h * w.blocks;
-    if (!SUMS && (int)blockIdx.z * kRows >= w.q_len * G - rb * RB) return;
     int64_t before = 0, all = 0;
-    for (int x = tid; x < a.batch; x += NT) {
-        const int64_t y = work_of<RB>(a, x).total(Hl);
+    for (int x = threadIdx.x; x < a.batch; x += 256) {
+        const int64_t y = work_of<RB>(a, x).total();
         all += y;
         before += x < s ? y : 0;
     }
-    all = block_sum<NT>(all, s_sum);
-    before = block_sum<NT>(before, s_sum);
-    const int64_t share = share_of(a, all), from = before + (int64_t)pair * w.tiles, to = from + w.tiles;
-    const int w0 = uniform((int)(from / share)), w1 = uniform((int)((to - 1) / share));
-    const int rows = min(w.q_len * G - rb * RB, RB);
-    auto slot_of = [&](int x) { return 2 * (int64_t)x + (x == w0 && from > (int64_t)x * share ? 1 : 0); };
-    if constexpr (SUMS) {
-        if (tid < G) {
-            float m = kNegInf, l = 0.f;
-            if (w0 == w1) {
-                const float2 ml = *reinterpret_cast<const float2*>(a.row_ml + ((int64_t)s * a.v.n_q_local + h * G + tid) * 2);
-                m = ml.x;
-                l = ml.y;
-            } else {
-                for (int x = w0; x <= w1; ++x) {
-                    const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + (slot_of(x) * RB + tid) * 2);
-                    if (ml.y == 0.f) continue;
-                    const float mn = fmaxf(m, ml.x);
-                    l = l * fast_exp2(m - mn) + ml.y * fast_exp2(ml.x - mn);
-                    m = mn;
-                }
-            }
-            s_ml[tid] = make_float2(m, l != 0.f ? 1.0f / l : 0.f);
+    all = block_sum<256>(all, s_sum);
+    before = block_sum<256>(before, s_sum);
+    const int64_t share = share_of(a, all), from = before + (int64_t)rb * w.tiles, to = from + w.tiles;
+    piece_list p;
+    p.rows = min(w.q_len * a.group - rb * RB, RB);
+    p.h = h;
+    p.rb = rb;
+    p.w0 = uniform((int)(from / share));
+    p.w1 = uniform((int)((to - 1) / share));
+    p.skew = from > (int64_t)p.w0 * share;
+    p.heads = a.v.n_kv_local;
+    return p;
+}
+// (m, l, acc) and the pieces z, z + step, .. below count added up: kBatch are requested at a time, the last one again past the end.
+template <int D, int RB>
+__device__ __forceinline__ void add_pieces(const tree_args& a, const piece_list& p, int row, int cg, int z, int step, float& m, float& l, f32x4& acc)
+{
+    constexpr int kBatch = 8;
+    const int count = p.count();
+    for (; z < count; z += kBatch * step) {
+        float2 ml[kBatch];
+        f32x4 x[kBatch];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            const int64_t at = p.slot(min(z + u * step, count - 1)) * RB + row;
+            ml[u] = *reinterpret_cast<const float2*>(a.part_ml + at * 2);
+            x[u] = *reinterpret_cast<const f32x4*>(a.part_o + at * D + 4 * cg);
         }
-        __syncthreads();
-        float* sums = a.sums + ((int64_t)s * Hl + h) * a.sum_stride;
-        const float* scores = a.scores + ((int64_t)s * a.v.n_q_local + h * G) * a.score_stride;
-        const int end = min(((int)blockIdx.z + 1) * kChunk, w.n);
-        for (int t = (int)blockIdx.z * kChunk + tid; t < end; t += NT) {
-            float x = 0.f;
-            for (int g = 0; g < G; ++g) {
-                const float2 ml = s_ml[g];
-                const float e = scores[g * a.score_stride + t];
-                x += e == kNegInf ? 0.f : fast_exp2(e - ml.x) * ml.y;
-            }
-            sums[t] = t == w.n - 1 ? x : sums[t] + x;   // (the newest token has no sum yet)
+        float mn = m;
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            if (z + u * step >= count) ml[u].y = 0.f;
+            mn = fmaxf(mn, ml[u].y != 0.f ? ml[u].x : kNegInf);
         }
-        if (blockIdx.z > 0) return;
+        const float keep = l != 0.f ? fast_exp2(m - mn) : 0.f;
+        l *= keep;
+        acc *= keep;
+        m = mn;
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            if (ml[u].y == 0.f) continue;
+            const float f = fast_exp2(ml[u].x - mn);
+            l += ml[u].y * f;
+            acc += x[u] * f;
+        }
     }
-    if (w0 == w1) return;   // written by the main kernel
-    for (int row = SUMS ? r : (int)blockIdx.z * kRows + r; row < rows; row += SUMS ? kRows : rows) {
-        float m = kNegInf, l = 0.f;
-        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-        for (int x = w0; x <= w1; ++x) {
-            const int64_t at = slot_of(x) * RB + row;
-            const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + at * 2);
-            const f32x4 y = *reinterpret_cast<const f32x4*>(a.part_o + at * D + 4 * cg);
+}
+template <int D>
+__device__ __forceinline__ void store_row(const tree_args& a, const seq_work& w, int h, int rho, int cg, float l, const f32x4& acc)
+{
+    const float inv = 1.0f / l;
+    *reinterpret_cast<uint2*>(a.out + ((int64_t)(w.q0 + rho / a.group) * a.v.n_q_local + h * a.group + rho % a.group) * D + 4 * cg) =
+        l != 0.f ? make_uint2(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)) : make_uint2(0u, 0u);
+}
+// A row's pieces shared among the groups of D / 4 lanes of a workgroup
+template <int D, int RB>
+__device__ __forceinline__ void add_row_together(const tree_args& a, const seq_work& w, const piece_list& p, int row, f32x4* s_acc, float2* s_ml)
+{
+    constexpr int kLanes = D / 4, kGroups = 256 / kLanes;
+    const int cg = threadIdx.x % kLanes, r = threadIdx.x / kLanes;
+    float m = kNegInf, l = 0.f;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    add_pieces<D, RB>(a, p, row, cg, r, kGroups, m, l, acc);
+    __syncthreads();
+    s_acc[threadIdx.x] = acc;
+    if (cg == 0) s_ml[r] = make_float2(m, l);
+    __syncthreads();
+    if (r == 0) {
+        for (int z = 1; z < kGroups; ++z) {
+            const float2 ml = s_ml[z];
             if (ml.y == 0.f) continue;
-            const float mn = fmaxf(m, ml.x), keep = fast_exp2(m - mn), f = fast_exp2(ml.x - mn);
+            const float mn = fmaxf(m, ml.x), keep = l != 0.f ? fast_exp2(m - mn) : 0.f, f = fast_exp2(ml.x - mn);
             l = l * keep + ml.y * f;
-            acc = acc * keep + y * f;
+            acc = acc * keep + s_acc[z * kLanes + cg] * f;
             m = mn;
         }
-        const float inv = 1.0f / l;
-        const int rho = rb * RB + row;
-        *reinterpret_cast<uint2*>(a.out + ((int64_t)(w.q0 + rho / G) * a.v.n_q_local + h * G + rho % G) * D + 4 * cg) =
-            l != 0.f ? make_uint2(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)) : make_uint2(0u, 0u);
+        store_row<D>(a, w, p.h, p.rb * RB + row, cg, l, acc);
     }
+}
+template <int D>
+__device__ __forceinline__ void zero_rows(const tree_args& a, const seq_work& w, int h)
+{
+    constexpr int kLanes = D / 4, kRows = 256 / kLanes;
+    for (int x = blockIdx.z * kRows + (int)threadIdx.x / kLanes; x < w.q_len * a.group; x += gridDim.z * kRows)
+        store_row<D>(a, w, h, x, (int)threadIdx.x % kLanes, 0.f, f32x4{0.f, 0.f, 0.f, 0.f});
+}
+
+// Block (s, pair of s, part): TOGETHER: row `part` by the whole workgroup (few rows with long lists); otherwise 1024 / D rows.
+template <int D, int RW, bool TOGETHER>
+__global__ __launch_bounds__(256) void tree_merge_kernel(tree_args a)
+{
+    constexpr int RB = 32 * RW, kLanes = D / 4, kRows = 256 / kLanes;
+    __shared__ int64_t s_sum[4];
+    __shared__ f32x4 s_acc[TOGETHER ? 256 : 1];
+    __shared__ float2 s_ml[kRows];
+    const int s = blockIdx.x, pair = blockIdx.y;
+    const seq_work w = work_of<RB>(a, s);
+    if (w.n <= 0 && w.q_len > 0 && pair < a.v.n_kv_local) zero_rows<D>(a, w, pair);
+    if (pair >= w.blocks * a.v.n_kv_local) return;
+    const int h = pair / w.blocks, rb = pair - h * w.blocks, row0 = (int)blockIdx.z * (TOGETHER ? 1 : kRows);
+    if (row0 >= w.q_len * a.group - rb * RB) return;
+    const piece_list p = pieces_of<RB>(a, w, s, h, rb, s_sum);
+    if (p.count() == 1 || row0 >= p.rows) return;   // written by the main kernel
+    if constexpr (TOGETHER) {
+        add_row_together<D, RB>(a, w, p, row0, s_acc, s_ml);
+    } else {
+        const int cg = threadIdx.x % kLanes, row = row0 + (int)threadIdx.x / kLanes;
+        if (row >= p.rows) return;
+        float m = kNegInf, l = 0.f;
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+        add_pieces<D, RB>(a, p, row, cg, 0, 1, m, l, acc);
+        store_row<D>(a, w, h, rb * RB + row, cg, l, acc);
+    }
+}
+
+// Block (s, h, chunk of tokens): (M, L) of the pair's G rows, then sum_g 2^(score_g - M_g) / L_g to the chunk's tokens; the rows of a cut
+// pair are shared out over the chunks' workgroups.
+template <int D>
+__global__ __launch_bounds__(256) void weights_kernel(tree_args a)
+{
+    constexpr int RB = 32, kRows = 256 / (D / 4);
+    __shared__ int64_t s_sum[4];
+    __shared__ f32x4 s_acc[256];
+    __shared__ float2 s_ml[kRows], s_row[4][32];
+    const int s = blockIdx.x, h = blockIdx.y, G = a.group, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const seq_work w = work_of<RB>(a, s);
+    if (w.n <= 0) {
+        zero_rows<D>(a, w, h);
+        return;
+    }
+    if ((int)blockIdx.z * a.chunk >= w.n && (int)blockIdx.z >= G) return;
+    const piece_list p = pieces_of<RB>(a, w, s, h, 0, s_sum);
+    const bool cut = p.count() > 1;
+    // lane l of a wavefront takes row l % Gp, Gp = G rounded up to a power of two, and every (256 / Gp)-th piece
+    int gp = 1;
+    while (gp < G) gp <<= 1;
+    const int g = lane & (gp - 1);
+    float m = kNegInf, l = 0.f;
+    auto add = [&](float m2, float l2) {
+        const float mn = fmaxf(m, m2);
+        l = (l != 0.f ? l * fast_exp2(m - mn) : 0.f) + (l2 != 0.f ? l2 * fast_exp2(m2 - mn) : 0.f);
+        m = mn;
+    };
+    if (g < G) {
+        if (!cut) {
+            const float2 ml = *reinterpret_cast<const float2*>(a.row_ml + ((int64_t)s * a.v.n_q_local + h * G + g) * 2);
+            m = ml.x;
+            l = ml.y;
+        } else {
+            for (int z = tid / gp; z < p.count(); z += 256 / gp) {
+                const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + (p.slot(z) * RB + g) * 2);
+                add(ml.x, ml.y);
+            }
+        }
+    }
+    if (cut) {
+        for (int d = gp; d < 64; d <<= 1) {
+            const float m2 = __shfl_xor(m, d), l2 = __shfl_xor(l, d);
+            add(m2, l2);
+        }
+        if (lane < gp) s_row[wave][g] = make_float2(m, l);
+        __syncthreads();
+        m = kNegInf;
+        l = 0.f;
+        for (int x = 0; x < 4; ++x) add(s_row[x][g].x, s_row[x][g].y);
+        __syncthreads();
+    }
+    if (wave == 0 && lane < gp) s_row[0][g] = make_float2(m, l != 0.f ? 1.0f / l : 0.f);
+    __syncthreads();
+    float* sums = a.sums + ((int64_t)s * a.v.n_kv_local + h) * a.sum_stride;
+    const float* scores = a.scores + ((int64_t)s * a.v.n_q_local + h * G) * a.score_stride;
+    const int end = min(((int)blockIdx.z + 1) * a.chunk, w.n);
+    for (int t = (int)blockIdx.z * a.chunk + tid; t < end; t += 256) {
+        float x = 0.f;
+        for (int y = 0; y < G; ++y) {
+            const float e = scores[y * a.score_stride + t];
+            const float2 ml = s_row[0][y];
+            x += e == kNegInf ? 0.f : fast_exp2(e - ml.x) * ml.y;
+        }
+        sums[t] = t == w.n - 1 ? x : sums[t] + x;   // (the newest token has no sum yet)
+    }
+    if (cut)
+        for (int row = blockIdx.z; row < G; row += gridDim.z) add_row_together<D, RB>(a, w, p, row, s_acc, s_ml);
 }
 
 // ---- host ------------------------------------------------------------------------------------------
@@ -616,7 +915,7 @@ int row_waves(int64_t rows) { return rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 1
 
 struct tree_plan {
     int rw;
-    int32_t workgroups, least;
+    int32_t teams, least;
     size_t part_o, part_ml, bytes;
 };
 tree_plan plan_tree(const kv_view* view, int batch, int max_ctx_len, int max_q_len)
@@ -626,36 +925,45 @@ tree_plan plan_tree(const kv_view* view, int batch, int max_ctx_len, int max_q_l
     p.rw = row_waves(rows);
     const int rb = 32 * p.rw;
     const int64_t blocks = (rows + rb - 1) / rb, tiles = ((int64_t)max_ctx_len + kKeys - 1) / kKeys;
-    p.least = p.rw == 1 ? 4 : p.rw == 2 ? 2 : 1;
-    const int64_t most = (blocks * view->n_kv_local * batch * tiles + p.least - 1) / p.least;
-    const int fill = kCus * (p.rw == 2 ? 2 : p.rw == 4 ? 3 : 1);
-    p.workgroups = (int32_t)std::min<int64_t>(most, fill);
-    const size_t records = (size_t)2 * p.workgroups * rb;
+    p.least = p.rw == 1 ? 16 : p.rw == 2 ? 8 : 4;
+    const int64_t most = (blocks * batch * tiles + p.least - 1) / p.least;
+    const int fill = kCus * (p.rw == 2 || p.rw == 4 ? 2 : 1);   // workgroups that the chip holds
+    p.teams = (int32_t)std::max<int64_t>(std::min<int64_t>(most, fill / view->n_kv_local), 1);
+    const size_t records = (size_t)2 * p.teams * view->n_kv_local * rb;
     p.part_o = records * view->geom.head_dim * 4;
     p.part_ml = records * 8;
     p.bytes = p.part_o + p.part_ml;
     return p;
 }
 
-template <int D, int RW, bool SUMS>
-void launch(const tree_args& a, int64_t most_blocks, int parts, hipStream_t st)
+template <int D, int RW>
+void launch(const tree_args& a, int64_t most_rows, hipStream_t st)
 {
-    hipLaunchKernelGGL((tree_kernel<D, RW, SUMS>), dim3((unsigned)a.workgroups), dim3(RW == 8 ? 512 : 256), 0, st, a);
-    hipLaunchKernelGGL((tree_merge_kernel<D, RW, SUMS>), dim3((unsigned)a.batch, (unsigned)(a.v.n_kv_local * most_blocks), (unsigned)parts),
-                       dim3(256), 0, st, a);
+    constexpr int RB = 32 * RW, kRows = 1024 / D;
+    const unsigned pairs = (unsigned)(a.v.n_kv_local * ((most_rows + RB - 1) / RB)), rows = (unsigned)std::min<int64_t>(most_rows, RB);
+    hipLaunchKernelGGL((tree_kernel<D, RW, false>), dim3((unsigned)(a.teams * a.v.n_kv_local)), dim3(RW == 8 ? 512 : 256), 0, st, a);
+    // Few pairs have long lists of pieces: a workgroup a row
+    if ((int64_t)a.batch * pairs <= 64)
+        hipLaunchKernelGGL((tree_merge_kernel<D, RW, true>), dim3((unsigned)a.batch, pairs, rows), dim3(256), 0, st, a);
+    else
+        hipLaunchKernelGGL((tree_merge_kernel<D, RW, false>), dim3((unsigned)a.batch, pairs, (rows + kRows - 1) / kRows), dim3(256), 0, st, a);
 }
 template <int D>
 void launch_tree(int rw, const tree_args& a, int64_t most_rows, hipStream_t st)
 {
-    const int rb = 32 * rw, rows_each = 256 / (D / 4);
-    const int64_t blocks = (most_rows + rb - 1) / rb;
-    const int parts = (int)((std::min<int64_t>(most_rows, rb) + rows_each - 1) / rows_each);
     switch (rw) {
-        case 1: launch<D, 1, false>(a, blocks, parts, st); break;
-        case 2: launch<D, 2, false>(a, blocks, parts, st); break;
-        case 4: launch<D, 4, false>(a, blocks, parts, st); break;
-        default: launch<D, 8, false>(a, blocks, parts, st); break;
+        case 1: launch<D, 1>(a, most_rows, st); break;
+        case 2: launch<D, 2>(a, most_rows, st); break;
+        case 4: launch<D, 4>(a, most_rows, st); break;
+        default: launch<D, 8>(a, most_rows, st); break;
     }
+}
+template <int D>
+void launch_weights(const tree_args& a, int64_t chunks, hipStream_t st)
+{
+    const unsigned heads = (unsigned)a.v.n_kv_local;
+    hipLaunchKernelGGL((tree_kernel<D, 1, true>), dim3((unsigned)a.teams * heads), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((weights_kernel<D>), dim3((unsigned)a.batch, heads, (unsigned)chunks), dim3(256), 0, st, a);
 }
 
 // The checks that both entry points make, and the arguments that they share.
@@ -715,7 +1023,7 @@ extern "C" int paged_tree_attn(const void* q, void* out, const void* kv_pool, in
     a.q_off = q_offsets;
     a.mask = (const unsigned long long*)tree_mask;
     a.mask_words = (int32_t)mask_words;
-    a.workgroups = p.workgroups;
+    a.teams = p.teams;
     a.least_tiles = p.least;
     a.part_o = (float*)workspace;
     a.part_ml = (float*)((char*)workspace + p.part_o);
@@ -752,7 +1060,7 @@ extern "C" int paged_decode_attn_weights(const void* q, void* out, const void* k
         if (!workspace || ((uintptr_t)workspace & 255u)) return KV_ERR_INVALID_ARG;
         if (workspace_bytes < paged_decode_attn_weights_workspace_bytes(view, batch, max_ctx_len)) return KV_ERR_WORKSPACE;
     }
-    a.workgroups = p.workgroups;
+    a.teams = p.teams;
     a.least_tiles = p.least;
     a.score_stride = score_stride(max_ctx_len);
     a.scores = (float*)workspace;   // (its rows are read and written 16 bytes at a time)
@@ -761,10 +1069,13 @@ extern "C" int paged_decode_attn_weights(const void* q, void* out, const void* k
     a.row_ml = a.part_ml + p.part_ml / 4;
     a.sums = weights;
     a.sum_stride = weights_stride;
-    const int64_t chunks = std::max<int64_t>(((int64_t)max_ctx_len + kChunk - 1) / kChunk, 1);
+    // 1024 tokens a workgroup, 256 where that leaves most of the chip idle
+    auto chunks_of = [&](int chunk) { return std::max<int64_t>(((int64_t)max_ctx_len + chunk - 1) / chunk, 1); };
+    a.chunk = batch * (int64_t)view->n_kv_local * chunks_of(1024) < 4 * kCus ? 256 : 1024;
+    const int64_t chunks = chunks_of(a.chunk);
     if (chunks > 65535 || view->n_kv_local > 65535) return KV_ERR_UNSUPPORTED;
     hipStream_t st = (hipStream_t)hip_stream;
-    if (view->geom.head_dim == 128) launch<128, 1, true>(a, 1, (int)chunks, st);
-    else launch<64, 1, true>(a, 1, (int)chunks, st);
+    if (view->geom.head_dim == 128) launch_weights<128>(a, chunks, st);
+    else launch_weights<64>(a, chunks, st);
     return kv_record_hip_error(hipGetLastError(), "paged_decode_attn_weights launch");
 }
