@@ -58,6 +58,8 @@ struct tree_args {
     int32_t teams, least_tiles;   // shares that the axis of tiles is cut into, and the least tiles of a share
     float* part_o;            // [2 teams n_kv_local][32 RW][D]: slot 2 w the first piece of workgroup w, 2 w + 1 its last
     float* part_ml;           // [2 teams n_kv_local][32 RW][2] (reference in exponent units, sum of weights)
+    int2* ends;               // [batch][blocks][n_kv_local] of every pair: team of its first piece x 2 + whether that is the team's last, of its last
+    int32_t most_blocks;      // row blocks of a sequence by the host's bound
     // weights:
     float* scores;            // [batch][n_q_local][score_stride] exponents: score * scale * log2(e)
     float* row_ml;            // [batch][n_q_local][2] of pairs that were not cut
@@ -128,21 +130,6 @@ __device__ __forceinline__ int64_t share_of(const tree_args& a, int64_t total)
     return even > a.least_tiles ? even : a.least_tiles;
 }
 
-// Sum of x over the workgroup, in every thread (s_sum: one word per wavefront; free again after the call's barrier pair).
-template <int NT>
-__device__ __forceinline__ int64_t block_sum(int64_t x, int64_t* s_sum)
-{
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) x += __shfl_xor((long long)x, d);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) s_sum[threadIdx.x >> 6] = x;
-    __syncthreads();
-    int64_t t = 0;
-#pragma unroll
-    for (int w = 0; w < NT / 64; ++w) t += s_sum[w];
-    return t;
-}
-
 // The share of this team: [from, to) on the axis, the sequence that holds `from` and its offset in it.
 template <int NT, int RB>
 __device__ __forceinline__ void find_share(const tree_args& a, int team, int64_t* s_sum, int64_t& from, int64_t& to, int& seq, int64_t& offset)
@@ -198,6 +185,7 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
     auto v_buf = [&](int x) { return NB == 2 ? ((x & 1) ? s_v1 : s_v0) : (x & 2) ? ((x & 1) ? s_v3 : s_v2) : ((x & 1) ? s_v1 : s_v0); };
     __shared__ float2 s_ml[KW > 1 ? NW * 32 : 1];
     __shared__ uint32_t s_seen[SUMS ? 1 : kEdgeTiles][SUMS ? 1 : RB];   // which tokens of the tiles that hold drafted ones a row sees
+    __shared__ f32x4 s_out[SUMS ? KW : 1][SUMS ? 32 : 1][8];   // scores on their way out
     __shared__ int64_t s_sum[NW];
 
     const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
@@ -302,8 +290,9 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
                         const int limit = n - 1 - 16 * min(2 * tile + g, last_group), row = (p * kRowsEach & 15) + row_first;
                         off -= (uint32_t)(max((row & 15) - limit, 0) * (int)stride_bytes);
                     }
+                    // (non-temporal where one block of rows is all there is; several blocks read the tile again)
                     __builtin_amdgcn_raw_ptr_buffer_load_lds(kBoth && g ? r1 : r0, (lds_ptr)(dst + kg * kPieces + (first_part + p) * 64), 16, off,
-                                                             0, 0, 0);
+                                                             0, 0, RW < 8 ? 2 : 0);
                 }
             };
             if (2 * tile + 1 < last_group) fill(std::false_type());
@@ -403,15 +392,18 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
             else l = add_pair(pw[u], l);        // the same rounding above and below the fraction
         };
         auto weight_operand = [&](int c) { return as_bf16x8(kv_u32x4{pw[4 * c], pw[4 * c + 1], pw[4 * c + 2], pw[4 * c + 3]}); };
+        // Scores leave through LDS, so that a store writes whole lines: 8 lanes a row of 32 tokens, 8 rows at a time
         auto keep_scores = [&](int base) {
             if constexpr (SUMS) {
                 if (real) {
-                    float* dst = a.scores + ((int64_t)s * v.n_q_local + h * G + rho % G) * a.score_stride + base + 4 * half;
 #pragma unroll
                     for (int u = 0; u < 4; ++u)
-                        *reinterpret_cast<f32x4*>(dst + 8 * u) =
+                        s_out[kg][col][2 * u + half] =
                             f32x4{sc[4 * u] * a.scale_log2e, sc[4 * u + 1] * a.scale_log2e, sc[4 * u + 2] * a.scale_log2e, sc[4 * u + 3] * a.scale_log2e};
                 }
+                float* dst = a.scores + ((int64_t)s * v.n_q_local + h * G) * a.score_stride + base;
+                for (int r = lane >> 3; r < G; r += 8)
+                    *reinterpret_cast<f32x4*>(dst + r * a.score_stride + 4 * (lane & 7)) = s_out[kg][r][lane & 7];
             }
         };
         // A column without a key yet has no reference; its first key sets it.
@@ -562,8 +554,9 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
                 move_reference(top);
             }
             // K of tile i + 2 and V of tile i + 1 are needed next: what the last NB - 2 steps asked for may still be under way
+            // (the last one is scores on their way out)
             if (NB > 2 && i + NB < mine) staged(std::integral_constant<int, (NB - 2) * (kSplitPlanes ? 1 : 2) * NP>());
-            else staged(std::integral_constant<int, 0>());
+            else staged(std::integral_constant<int, SUMS ? 1 : 0>());
         };
         staged(std::integral_constant<int, 0>());
         const int common = count / KW;   // tiles that every key group has
@@ -697,6 +690,11 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
                     *reinterpret_cast<float2*>(a.row_ml + ((int64_t)s * v.n_q_local + h * G + rho % G) * 2) = make_float2(m_all, l_all);
             }
         }
+        if (threadIdx.x == 0 && rb < a.most_blocks) {
+            int2* ends = a.ends + ((int64_t)s * a.most_blocks + rb) * Hl + h;
+            if (t0 == 0) ends->x = 2 * team + (at > from ? 1 : 0);
+            if (t0 + count == w.tiles) ends->y = team;
+        }
         at += count;
         offset += count;
     }
@@ -710,29 +708,21 @@ struct piece_list {
     int rows, h, rb;          // rows of the pair
     int w0, w1;               // teams that hold its first and last piece
     int skew;                 // the first piece is the last of its workgroup
-    int64_t heads;
+    int heads;
     __device__ int64_t slot(int z) const { return 2 * ((int64_t)(w0 + z) * heads + h) + (z == 0 ? skew : 0); }
     __device__ int count() const { return w1 - w0 + 1; }
 };
 template <int RB>
-__device__ __forceinline__ piece_list pieces_of(const tree_args& a, const seq_work& w, int s, int h, int rb, int64_t* s_sum)
+__device__ __forceinline__ piece_list pieces_of(const tree_args& a, const seq_work& w, int s, int h, int rb)
 {
-    int64_t before = 0, all = 0;
-    for (int x = threadIdx.x; x < a.batch; x += 256) {
-        const int64_t y = work_of<RB>(a, x).total();
-        all += y;
-        before += x < s ? y : 0;
-    }
-    all = block_sum<256>(all, s_sum);
-    before = block_sum<256>(before, s_sum);
-    const int64_t share = share_of(a, all), from = before + (int64_t)rb * w.tiles, to = from + w.tiles;
+    const int2 ends = a.ends[((int64_t)s * a.most_blocks + rb) * a.v.n_kv_local + h];
     piece_list p;
     p.rows = min(w.q_len * a.group - rb * RB, RB);
     p.h = h;
     p.rb = rb;
-    p.w0 = uniform((int)(from / share));
-    p.w1 = uniform((int)((to - 1) / share));
-    p.skew = from > (int64_t)p.w0 * share;
+    p.w0 = uniform(ends.x >> 1);
+    p.w1 = uniform(ends.y);
+    p.skew = uniform(ends.x & 1);
     p.heads = a.v.n_kv_local;
     return p;
 }
@@ -740,9 +730,9 @@ __device__ __forceinline__ piece_list pieces_of(const tree_args& a, const seq_wo
 template <int D, int RB>
 __device__ __forceinline__ void add_pieces(const tree_args& a, const piece_list& p, int row, int cg, int z, int step, float& m, float& l, f32x4& acc)
 {
-    constexpr int kBatch = 8;
     const int count = p.count();
-    for (; z < count; z += kBatch * step) {
+    auto add = [&](auto batch) {
+        constexpr int kBatch = decltype(batch)::value;
         float2 ml[kBatch];
         f32x4 x[kBatch];
 #pragma unroll
@@ -768,6 +758,13 @@ __device__ __forceinline__ void add_pieces(const tree_args& a, const piece_list&
             l += ml[u].y * f;
             acc += x[u] * f;
         }
+        z += kBatch * step;
+    };
+    while (z < count) {
+        const int left = (count - z + step - 1) / step;
+        if (left <= 2) add(std::integral_constant<int, 2>());
+        else if (left <= 4) add(std::integral_constant<int, 4>());
+        else add(std::integral_constant<int, 8>());
     }
 }
 template <int D>
@@ -815,16 +812,15 @@ template <int D, int RW, bool TOGETHER>
 __global__ __launch_bounds__(256) void tree_merge_kernel(tree_args a)
 {
     constexpr int RB = 32 * RW, kLanes = D / 4, kRows = 256 / kLanes;
-    __shared__ int64_t s_sum[4];
     __shared__ f32x4 s_acc[TOGETHER ? 256 : 1];
     __shared__ float2 s_ml[kRows];
     const int s = blockIdx.x, pair = blockIdx.y;
     const seq_work w = work_of<RB>(a, s);
     if (w.n <= 0 && w.q_len > 0 && pair < a.v.n_kv_local) zero_rows<D>(a, w, pair);
-    if (pair >= w.blocks * a.v.n_kv_local) return;
+    if (pair >= min(w.blocks, a.most_blocks) * a.v.n_kv_local) return;
     const int h = pair / w.blocks, rb = pair - h * w.blocks, row0 = (int)blockIdx.z * (TOGETHER ? 1 : kRows);
     if (row0 >= w.q_len * a.group - rb * RB) return;
-    const piece_list p = pieces_of<RB>(a, w, s, h, rb, s_sum);
+    const piece_list p = pieces_of<RB>(a, w, s, h, rb);
     if (p.count() == 1 || row0 >= p.rows) return;   // written by the main kernel
     if constexpr (TOGETHER) {
         add_row_together<D, RB>(a, w, p, row0, s_acc, s_ml);
@@ -844,7 +840,6 @@ template <int D>
 __global__ __launch_bounds__(256) void weights_kernel(tree_args a)
 {
     constexpr int RB = 32, kRows = 256 / (D / 4);
-    __shared__ int64_t s_sum[4];
     __shared__ f32x4 s_acc[256];
     __shared__ float2 s_ml[kRows], s_row[4][32];
     const int s = blockIdx.x, h = blockIdx.y, G = a.group, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -854,7 +849,7 @@ __global__ __launch_bounds__(256) void weights_kernel(tree_args a)
         return;
     }
     if ((int)blockIdx.z * a.chunk >= w.n && (int)blockIdx.z >= G) return;
-    const piece_list p = pieces_of<RB>(a, w, s, h, 0, s_sum);
+    const piece_list p = pieces_of<RB>(a, w, s, h, 0);
     const bool cut = p.count() > 1;
     // lane l of a wavefront takes row l % Gp, Gp = G rounded up to a power of two, and every (256 / Gp)-th piece
     int gp = 1;
@@ -895,14 +890,23 @@ __global__ __launch_bounds__(256) void weights_kernel(tree_args a)
     float* sums = a.sums + ((int64_t)s * a.v.n_kv_local + h) * a.sum_stride;
     const float* scores = a.scores + ((int64_t)s * a.v.n_q_local + h * G) * a.score_stride;
     const int end = min(((int)blockIdx.z + 1) * a.chunk, w.n);
-    for (int t = (int)blockIdx.z * a.chunk + tid; t < end; t += 256) {
-        float x = 0.f;
-        for (int y = 0; y < G; ++y) {
-            const float e = scores[y * a.score_stride + t];
-            const float2 ml = s_row[0][y];
-            x += e == kNegInf ? 0.f : fast_exp2(e - ml.x) * ml.y;
+    for (int t = (int)blockIdx.z * a.chunk + 4 * tid; t < end; t += 4 * 256) {   // (rows of scores are padded to whole tiles)
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+        for (int y0 = 0; y0 < G; y0 += 4) {
+            f32x4 e[4];
+#pragma unroll
+            for (int y = 0; y < 4; ++y) e[y] = *reinterpret_cast<const f32x4*>(scores + min(y0 + y, G - 1) * a.score_stride + t);
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                if (y0 + y >= G) break;
+                const float2 ml = s_row[0][y0 + y];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) x[c] += e[y][c] == kNegInf ? 0.f : fast_exp2(e[y][c] - ml.x) * ml.y;
+            }
         }
-        sums[t] = t == w.n - 1 ? x : sums[t] + x;   // (the newest token has no sum yet)
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            if (t + c < end) sums[t + c] = t + c == w.n - 1 ? x[c] : sums[t + c] + x[c];   // (the newest token has no sum yet)
     }
     if (cut)
         for (int row = blockIdx.z; row < G; row += gridDim.z) add_row_together<D, RB>(a, w, p, row, s_acc, s_ml);
@@ -916,7 +920,8 @@ int row_waves(int64_t rows) { return rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 1
 struct tree_plan {
     int rw;
     int32_t teams, least;
-    size_t part_o, part_ml, bytes;
+    int32_t blocks;
+    size_t part_o, part_ml, ends, bytes;
 };
 tree_plan plan_tree(const kv_view* view, int batch, int max_ctx_len, int max_q_len)
 {
@@ -925,14 +930,18 @@ tree_plan plan_tree(const kv_view* view, int batch, int max_ctx_len, int max_q_l
     p.rw = row_waves(rows);
     const int rb = 32 * p.rw;
     const int64_t blocks = (rows + rb - 1) / rb, tiles = ((int64_t)max_ctx_len + kKeys - 1) / kKeys;
-    p.least = p.rw == 1 ? 16 : p.rw == 2 ? 8 : 4;
+    // Shorter shares cost more in pieces than they save (us per call with least tiles 4, 2, 1 / 8, 4, 4 / 16, 8, 4: 2 sequences of 512 to
+    // 4096, up to 64 rows, 23.2 / 19.8 / 23.9; weights of 2 such sequences 23.4 / 19.3 / 26.2; 2 of 1000 to 2000, 256 rows, 33.8 / 27.5 / 27.4)
+    p.least = p.rw == 1 ? 8 : 4;
     const int64_t most = (blocks * batch * tiles + p.least - 1) / p.least;
     const int fill = kCus * (p.rw == 2 || p.rw == 4 ? 2 : 1);   // workgroups that the chip holds
     p.teams = (int32_t)std::max<int64_t>(std::min<int64_t>(most, fill / view->n_kv_local), 1);
     const size_t records = (size_t)2 * p.teams * view->n_kv_local * rb;
     p.part_o = records * view->geom.head_dim * 4;
     p.part_ml = records * 8;
-    p.bytes = p.part_o + p.part_ml;
+    p.blocks = (int32_t)blocks;
+    p.ends = (size_t)batch * blocks * view->n_kv_local * 8;
+    p.bytes = p.part_o + p.part_ml + p.ends;
     return p;
 }
 
@@ -942,8 +951,8 @@ void launch(const tree_args& a, int64_t most_rows, hipStream_t st)
     constexpr int RB = 32 * RW, kRows = 1024 / D;
     const unsigned pairs = (unsigned)(a.v.n_kv_local * ((most_rows + RB - 1) / RB)), rows = (unsigned)std::min<int64_t>(most_rows, RB);
     hipLaunchKernelGGL((tree_kernel<D, RW, false>), dim3((unsigned)(a.teams * a.v.n_kv_local)), dim3(RW == 8 ? 512 : 256), 0, st, a);
-    // Few pairs have long lists of pieces: a workgroup a row
-    if ((int64_t)a.batch * pairs <= 64)
+    // Few rows have long lists of pieces: a workgroup a row
+    if ((int64_t)a.batch * pairs * rows <= 4096)
         hipLaunchKernelGGL((tree_merge_kernel<D, RW, true>), dim3((unsigned)a.batch, pairs, rows), dim3(256), 0, st, a);
     else
         hipLaunchKernelGGL((tree_merge_kernel<D, RW, false>), dim3((unsigned)a.batch, pairs, (rows + kRows - 1) / kRows), dim3(256), 0, st, a);
@@ -1026,7 +1035,9 @@ extern "C" int paged_tree_attn(const void* q, void* out, const void* kv_pool, in
     a.teams = p.teams;
     a.least_tiles = p.least;
     a.part_o = (float*)workspace;
-    a.part_ml = (float*)((char*)workspace + p.part_o);
+    a.part_ml = a.part_o + p.part_o / 4;
+    a.ends = (int2*)(a.part_ml + p.part_ml / 4);
+    a.most_blocks = p.blocks;
     const int64_t rows = (int64_t)max_q_len * view->group;
     if ((rows + 31) / 32 * view->n_kv_local > 65535) return KV_ERR_UNSUPPORTED;
     hipStream_t st = (hipStream_t)hip_stream;
@@ -1067,6 +1078,8 @@ extern "C" int paged_decode_attn_weights(const void* q, void* out, const void* k
     a.part_o = a.scores + rows * a.score_stride;
     a.part_ml = a.part_o + p.part_o / 4;
     a.row_ml = a.part_ml + p.part_ml / 4;
+    a.ends = (int2*)(a.row_ml + 2 * rows);
+    a.most_blocks = 1;
     a.sums = weights;
     a.sum_stride = weights_stride;
     // 1024 tokens a workgroup, 256 where that leaves most of the chip idle
