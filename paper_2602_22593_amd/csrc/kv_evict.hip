@@ -81,9 +81,12 @@ __global__ __launch_bounds__(kThreads) void kv_accept_kernel(accept_args a)
 // Slots below k that are not kept are holes; kept tokens from slot k on fill them, the j-th the j-th.  There are as many of
 // one as of the other, no row is both source and destination, and nothing else moves.
 //
-// kv_evict_select_kernel, a workgroup per (sequence, head): the k-th weight by counting digits of the weights' order-preserving
-// integers, most significant first, among the protected tokens if there are k of them and among the others if not; then
-// wavefronts that each own a range of slots number holes and sources by ballots.  kv_evict_move_kernel copies the rows.
+// The k-th weight is found by counting digits (11, 11 and 10 bits) of the weights' order-preserving integers, most
+// significant first, among the protected tokens if there are k of them and among the others if not.  Then holes and sources
+// are numbered in the order of their slots, by ballots of 64 and sums over those.  Up to 8192 tokens by one workgroup per
+// (sequence, head) that holds them in registers (evict_select_kernel); more by parts of 4096, a launch per step, with the digits
+// counted in the workspace (one workgroup for 131072 tokens took 260 us, bound by its own loads).  evict_move_kernel copies the
+// rows, all independent of each other.
 
 struct evict_args {
     uint16_t* pool;
@@ -102,10 +105,18 @@ struct evict_args {
     int32_t* counts;             // [batch][n_kv_local] moves
     int32_t* lists;              // [batch][n_kv_local][2][most]: holes, sources
     int64_t most;
+    // sequences of more than kAlone tokens:
+    int32_t parts;               // of kPart tokens, by the host's bound
+    int32_t* bins;               // [batch][n_kv_local][kAllBins], cleared first
+    int4* part_counts;           // [batch][n_kv_local][parts] (over, on) below k, (over, on) from there on
 };
 
-constexpr int kSelectThreads = 1024, kWaves = kSelectThreads / 64;
-constexpr int kDigit = 11, kBins = 1 << kDigit;
+constexpr int kDigits[3] = {11, 11, 10};
+constexpr int kBins = 2048;
+constexpr int kHeld = 8;                        // tokens a lane holds
+constexpr int kAlone = 1024 * kHeld, kPart = 512 * kHeld;
+constexpr int kAllBins = 2 * kBins + 2 * kBins + 2;   // first digit of both classes, second, third, number of protected tokens
+constexpr int kSecond = 2 * kBins, kThird = 3 * kBins, kProtected = 4 * kBins;
 
 // Integers in the order of the weights; NaN below all, the two zeros alike.
 __device__ __forceinline__ uint32_t order_of(float w)
@@ -115,164 +126,354 @@ __device__ __forceinline__ uint32_t order_of(float w)
     return (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
 
-__device__ __forceinline__ int evict_keep(const evict_args& a, int s, int n) { return min(n, max(a.keep_lens[s], 0)); }
-
-__global__ __launch_bounds__(kSelectThreads) void kv_evict_select_kernel(evict_args a)
-{
-    __shared__ int s_bins[kBins];
-    __shared__ int s_wave[kWaves][4];
-    __shared__ int s_pick[2];
-    const int s = blockIdx.x, h = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int Hl = a.v.n_kv_local;
-    const int64_t sh = (int64_t)s * Hl + h;
-    const int n = min(max(a.ctx_lens[s], 0), a.max_ctx_len), k = evict_keep(a, s, n);
-    const float* weights = a.weights + sh * a.stride;
-    const int32_t* pos = a.token_pos + sh * a.stride;
-    float* weights_out = a.weights_out + sh * a.out_stride;
-    int32_t* pos_out = a.token_pos_out + sh * a.out_stride;
-    const bool elsewhere = a.weights_out != a.weights, pos_elsewhere = a.token_pos_out != a.token_pos;
-    if (h == 0 && tid == 0 && a.new_lens) a.new_lens[s] = k;
-    if (k == n) {   // nothing leaves
-        if (tid == 0 && a.counts) a.counts[sh] = 0;
-        for (int t = tid; t < min((int64_t)n, a.out_stride); t += kSelectThreads) {
-            if (elsewhere) weights_out[t] = weights[t];
-            if (pos_elsewhere) pos_out[t] = pos[t];
-        }
-        return;
+// What a workgroup knows of its (sequence, head).
+struct evict_pair {
+    int n, k, s;
+    int64_t sh, youngest;
+    __device__ evict_pair(const evict_args& a, int s_, int h) : s(s_)
+    {
+        sh = (int64_t)s * a.v.n_kv_local + h;
+        n = min(max(a.ctx_lens[s], 0), a.max_ctx_len);
+        k = min(n, max(a.keep_lens[s], 0));
+        youngest = (int64_t)a.next_pos[s] - a.recent;
     }
-    const int64_t youngest = (int64_t)a.next_pos[s] - a.recent;
-    auto is_protected = [&](int p) { return p < a.sinks || (int64_t)p >= youngest; };
+};
 
-    // how many are protected, and which class is divided
-    int here = 0;
-    for (int t = tid; t < n; t += kSelectThreads) here += is_protected(pos[t]);
+// The tokens base + NT i + thread of a workgroup: order numbers and classes (0 none, 1 ordinary, 2 protected).
+template <int NT>
+struct held_tokens {
+    uint32_t key[kHeld];
+    int cls[kHeld];
+    __device__ void load(const evict_args& a, const evict_pair& p, int base)
+    {
+        float w[kHeld];
+        int pos[kHeld];
 #pragma unroll
-    for (int d = 32; d > 0; d >>= 1) here += __shfl_xor(here, d);
-    if (lane == 0) s_wave[wave][0] = here;
-    __syncthreads();
-    int shielded = 0;
-    for (int w = 0; w < kWaves; ++w) shielded += s_wave[w][0];
-    const bool among = shielded >= k;            // the line lies among the protected ones
-    int rest = among ? k : k - shielded;         // of the divided class these many stay
-    __syncthreads();
-
-    // the order number of the last one that stays: its digits from the top
-    uint32_t prefix = 0;
-    int shift = 32;
-    for (int pass = 0; pass < 3 && rest > 0; ++pass) {
-        const int width = pass < 2 ? kDigit : 32 - 2 * kDigit;
-        for (int b = tid; b < kBins; b += kSelectThreads) s_bins[b] = 0;
-        __syncthreads();
-        for (int t = tid; t < n; t += kSelectThreads) {
-            if (is_protected(pos[t]) != among) continue;
-            const uint32_t u = order_of(weights[t]);
-            if (shift < 32 && (u >> shift) != prefix) continue;
-            atomicAdd(&s_bins[(u >> (shift - width)) & ((1 << width) - 1)], 1);
+        for (int i = 0; i < kHeld; ++i) {
+            const int t = base + NT * i + (int)threadIdx.x;
+            const int64_t at = p.sh * a.stride + min(t, p.n - 1);
+            w[i] = a.weights[at];
+            pos[i] = a.token_pos[at];
         }
-        __syncthreads();
-        // the bin that holds the rest-th from the top: lane l of the first wavefront looks at bins of 1 / 64 of the range
-        if (wave == 0) {
-            const int bins = 1 << width, each = bins / 64, top = bins - 1 - lane * each;
-            int sum = 0;
-            for (int b = 0; b < each; ++b) sum += s_bins[top - b];
-            int incl = sum;
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) {
+            key[i] = order_of(w[i]);
+            cls[i] = base + NT * i + (int)threadIdx.x >= p.n ? 0 : pos[i] < a.sinks || (int64_t)pos[i] >= p.youngest ? 2 : 1;
+        }
+    }
+    // Counts the digit of `width` bits below bit `shift` of those of the class whose upper bits are `prefix`.
+    __device__ void count(int* bins, int of_class, int shift, int width, uint32_t prefix) const
+    {
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) {
+            const bool in = cls[i] == of_class && (shift == 32 || (key[i] >> (shift & 31)) == prefix);
+            unsigned long long left = __builtin_amdgcn_ballot_w64(in);
+            if (left == 0) continue;
+            const int bin = (int)(key[i] >> (shift - width)) & ((1 << width) - 1);
+            // tokens alike (many weigh nothing) are counted by one lane; the rest adds by itself
+            const int leader = __builtin_ctzll(left), its = __builtin_amdgcn_readlane(bin, leader);
+            const unsigned long long same = __builtin_amdgcn_ballot_w64(in && bin == its);
+            if ((int)(threadIdx.x & 63) == leader) atomicAdd(&bins[its], __builtin_popcountll(same));
+            if (in && bin != its) atomicAdd(&bins[bin], 1);
+        }
+    }
+};
+
+// Sum over the workgroup, in every thread; s_part: a word per wavefront.
+template <int NT>
+__device__ __forceinline__ int block_total(int x, int* s_part)
+{
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) s_part[threadIdx.x >> 6] = x;
+    __syncthreads();
+    int t = 0;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) t += s_part[w];
+    return t;
+}
+
+// The bin that holds the rest-th of those counted, from the top, and how many of it are wanted.  Bins in LDS or in device memory.
+template <int NT>
+__device__ __forceinline__ void pick_bin(const int* bins, int n_bins, int& rest, int& bin, int* s_part, int* s_pick)
+{
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, each = n_bins / NT;   // consecutive bins a thread, the top first
+    int mine[kBins / NT], sum = 0;
+#pragma unroll
+    for (int b = 0; b < kBins / NT; ++b) {
+        mine[b] = b < each ? bins[n_bins - 1 - (tid * each + b)] : 0;
+        sum += mine[b];
+    }
+    int incl = sum;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int y = __shfl_up(incl, d);
+        incl += lane >= d ? y : 0;
+    }
+    if (lane == 63) s_part[wave] = incl;
+    __syncthreads();
+    for (int w = 0; w < NT / 64; ++w) incl += w < wave ? s_part[w] : 0;
+    int before = incl - sum;
+    if (before < rest && rest <= incl) {
+#pragma unroll
+        for (int b = 0; b < kBins / NT; ++b) {
+            if (before < rest && rest <= before + mine[b]) {
+                s_pick[0] = n_bins - 1 - (tid * each + b);
+                s_pick[1] = rest - before;
+            }
+            before += mine[b];
+        }
+    }
+    __syncthreads();
+    bin = s_pick[0];
+    rest = s_pick[1];
+    __syncthreads();
+}
+
+// Where the line lies: `over` it stay all, `on` it the first `equals` by slot.
+struct evict_line {
+    int divided;       // the class that is divided; all of a higher one stay, none of a lower one
+    uint32_t key;
+    int equals;        // 0: nothing of the divided class stays
+    __device__ bool over(uint32_t key_, int cls) const { return cls > divided || (cls == divided && equals > 0 && key_ > key); }
+    __device__ bool on(uint32_t key_, int cls) const { return cls == divided && equals > 0 && key_ == key; }
+};
+
+// Kept tokens before a place, from sums over what lies before it: x, y over and on the line below slot k, z, w from there on.
+__device__ __forceinline__ int kept_low(const evict_line& l, int over_low, int on_low) { return over_low + min(l.equals, on_low); }
+__device__ __forceinline__ int kept_high(const evict_line& l, int on_low, int over_high, int on_high, int all_on_low)
+{
+    return over_high + max(min(l.equals, on_low + on_high) - min(l.equals, all_on_low), 0);
+}
+
+// Lists holes and sources among a workgroup's tokens and copies what stays, given the counts before them and of the whole pair;
+// s_counts [4][NT / 64 * kHeld].  alone: the workgroup holds all of the pair's tokens, the counts before are 0 and those of the whole are its own.
+template <int NT>
+__device__ __forceinline__ void list_moves(const evict_args& a, const evict_pair& p, const evict_line& line, const held_tokens<NT>& x, int base, int4 before,
+                                           int all_on_low, bool alone, int (*s_counts)[NT / 64 * kHeld], int* s_total)
+{
+    constexpr int NW = NT / 64, kSub = NW * kHeld;   // groups of 64 slots, in their order
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    unsigned long long over_b[kHeld], on_b[kHeld];
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+        const int t = base + NT * i + tid;
+        over_b[i] = __builtin_amdgcn_ballot_w64(line.over(x.key[i], x.cls[i]));
+        on_b[i] = __builtin_amdgcn_ballot_w64(line.on(x.key[i], x.cls[i]));
+        const unsigned long long low = __builtin_amdgcn_ballot_w64(t < p.k);
+        if (lane < 4) {
+            const unsigned long long which = (lane & 1 ? on_b[i] : over_b[i]) & (lane & 2 ? ~low : low);
+            s_counts[lane][NW * i + wave] = __builtin_popcountll(which);
+        }
+    }
+    __syncthreads();
+    if (wave < 4) {   // wavefront c: exclusive sums of counts c
+        int run = 0;
+#pragma unroll
+        for (int b = 0; b < kSub; b += 64) {
+            const int y = s_counts[wave][b + lane];
+            int incl = y;
 #pragma unroll
             for (int d = 1; d < 64; d <<= 1) {
-                const int y = __shfl_up(incl, d);
-                incl += lane >= d ? y : 0;
+                const int z = __shfl_up(incl, d);
+                incl += lane >= d ? z : 0;
             }
-            const int before = incl - sum;
-            if (before < rest && rest <= incl) {
-                int left = rest - before, b = top;
-                while (s_bins[b] < left) left -= s_bins[b--];
-                s_pick[0] = b;
-                s_pick[1] = left;
-            }
+            s_counts[wave][b + lane] = run + incl - y;
+            run += __shfl(incl, 63);
         }
-        __syncthreads();
-        prefix = prefix << width | (uint32_t)s_pick[0];
-        rest = s_pick[1];
-        shift -= width;
-        __syncthreads();
-    }
-    // stays: above the line in the divided class, or on it among the first `rest` by slot; and all of the upper class
-    const int equals = rest;
-    const bool none = (among ? k : k - shielded) == 0;
-    auto state = [&](int t, bool& over, bool& on) {
-        over = on = false;
-        if (t >= n) return;
-        const bool p = is_protected(pos[t]);
-        if (p != among) {
-            over = p;
-            return;
-        }
-        if (none) return;
-        const uint32_t u = order_of(weights[t]);
-        over = u > prefix;
-        on = u == prefix;
-    };
-    const int each = ((n + kWaves - 1) / kWaves + 63) & ~63, t0 = min(wave * each, n), t1 = min(t0 + each, n);
-    int over_low = 0, on_low = 0, over_high = 0, on_high = 0;   // in slots below k, and from there on
-    for (int t = t0; t < t1; t += 64) {
-        bool over, on;
-        state(t + lane < t1 ? t + lane : n, over, on);
-        const bool low = t + lane < k;
-        over_low += __builtin_popcountll(__builtin_amdgcn_ballot_w64(over && low));
-        on_low += __builtin_popcountll(__builtin_amdgcn_ballot_w64(on && low));
-        over_high += __builtin_popcountll(__builtin_amdgcn_ballot_w64(over && !low));
-        on_high += __builtin_popcountll(__builtin_amdgcn_ballot_w64(on && !low));
-    }
-    if (lane == 0) {
-        s_wave[wave][0] = over_low;
-        s_wave[wave][1] = on_low;
-        s_wave[wave][2] = over_high;
-        s_wave[wave][3] = on_high;
+        if (lane == 0) s_total[wave] = run;
     }
     __syncthreads();
-    int on_before = 0, holes = 0, sources = 0, all_sources = 0;   // before this wavefront's range
-    {
-        int seen = 0, kept_low = 0, kept_high = 0;
-        for (int w = 0; w < kWaves; ++w) {
-            if (w == wave) {
-                on_before = seen;
-                holes = min(t0, k) - kept_low;
-                sources = kept_high;
-            }
-            const int low = min(max(equals - seen, 0), s_wave[w][1]);
-            kept_low += s_wave[w][0] + low;
-            seen += s_wave[w][1];
-            const int high = min(max(equals - seen, 0), s_wave[w][3]);
-            kept_high += s_wave[w][2] + high;
-            seen += s_wave[w][3];
-        }
-        all_sources = kept_high;
-    }
-    if (tid == 0) a.counts[sh] = all_sources;
-    int32_t* hole_list = a.lists + sh * 2 * a.most;
+    if (alone) all_on_low = s_total[1];
+    int32_t* hole_list = a.lists + p.sh * 2 * a.most;
     int32_t* source_list = hole_list + a.most;
+    const bool elsewhere = a.weights_out != a.weights, pos_elsewhere = a.token_pos_out != a.token_pos;
     const unsigned long long below = (1ull << lane) - 1;
-    for (int t = t0; t < t1; t += 64) {
-        bool over, on;
-        const int at = t + lane;
-        state(at < t1 ? at : n, over, on);
-        const unsigned long long ons = __builtin_amdgcn_ballot_w64(on);
-        const bool kept = over || (on && on_before + __builtin_popcountll(ons & below) < equals);
-        on_before += __builtin_popcountll(ons);
-        const bool inside = at < t1, hole = inside && at < k && !kept, source = inside && at >= k && kept;
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+        const int t = base + NT * i + tid, at = NW * i + wave;
+        if (base + NT * i >= p.n) break;
+        const int over_low = before.x + s_counts[0][at], on_low = before.y + s_counts[1][at];
+        const int over_high = before.z + s_counts[2][at], on_high = before.w + s_counts[3][at];
+        const int on_before = on_low + on_high;
+        const bool is_on = on_b[i] >> lane & 1;
+        const bool kept = (over_b[i] >> lane & 1) || (is_on && on_before + __builtin_popcountll(on_b[i] & below) < line.equals);
+        const bool hole = t < p.k && !kept, source = t >= p.k && kept;   // (p.k <= n, and nothing past n is kept)
         const unsigned long long hole_b = __builtin_amdgcn_ballot_w64(hole), source_b = __builtin_amdgcn_ballot_w64(source);
-        if (hole) hole_list[holes + __builtin_popcountll(hole_b & below)] = at;
-        if (source) source_list[sources + __builtin_popcountll(source_b & below)] = at;
-        holes += __builtin_popcountll(hole_b);
-        sources += __builtin_popcountll(source_b);
-        if (inside && at < k && kept && at < a.out_stride) {
-            if (elsewhere) weights_out[at] = weights[at];
-            if (pos_elsewhere) pos_out[at] = pos[at];
+        const int holes = min(t - lane, p.k) - kept_low(line, over_low, on_low);
+        const int sources = kept_high(line, on_low, over_high, on_high, all_on_low);
+        if (hole) hole_list[holes + __builtin_popcountll(hole_b & below)] = t;
+        if (source) source_list[sources + __builtin_popcountll(source_b & below)] = t;
+        if (t < p.k && kept && t < a.out_stride) {
+            const int64_t from = p.sh * a.stride + t, to = p.sh * a.out_stride + t;
+            if (elsewhere) a.weights_out[to] = a.weights[from];
+            if (pos_elsewhere) a.token_pos_out[to] = a.token_pos[from];
+        }
+    }
+    if (alone && tid == 0) a.counts[p.sh] = p.k - kept_low(line, s_total[0], s_total[1]);
+}
+
+// Nothing leaves: only copies, by `parts` workgroups.
+__device__ __forceinline__ void copy_all(const evict_args& a, const evict_pair& p, int part, int parts)
+{
+    const bool elsewhere = a.weights_out != a.weights, pos_elsewhere = a.token_pos_out != a.token_pos;
+    for (int64_t t = (int64_t)part * blockDim.x + threadIdx.x; t < min((int64_t)p.n, a.out_stride); t += (int64_t)parts * blockDim.x) {
+        if (elsewhere) a.weights_out[p.sh * a.out_stride + t] = a.weights[p.sh * a.stride + t];
+        if (pos_elsewhere) a.token_pos_out[p.sh * a.out_stride + t] = a.token_pos[p.sh * a.stride + t];
+    }
+}
+
+__global__ __launch_bounds__(1024) void evict_select_kernel(evict_args a)
+{
+    constexpr int NT = 1024;
+    __shared__ int s_bins[kBins], s_part[NT / 64], s_pick[2], s_total[4];
+    __shared__ int s_counts[4][NT / 64 * kHeld];
+    const int tid = threadIdx.x;
+    const evict_pair p(a, blockIdx.x, blockIdx.y);
+    if (blockIdx.y == 0 && tid == 0 && a.new_lens) a.new_lens[p.s] = p.k;
+    if (p.k == p.n) {
+        if (tid == 0 && a.counts) a.counts[p.sh] = 0;
+        copy_all(a, p, 0, 1);
+        return;
+    }
+    held_tokens<NT> x;
+    x.load(a, p, 0);
+    int here = 0;
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) here += x.cls[i] == 2;
+    const int shielded = block_total<NT>(here, s_part);
+    evict_line line;
+    line.divided = shielded >= p.k ? 2 : 1;
+    line.key = 0;
+    line.equals = line.divided == 2 ? p.k : p.k - shielded;
+    int shift = 32;
+    if (line.equals > 0) {
+#pragma unroll
+        for (int d = 0; d < 3; ++d) {
+            for (int b = tid; b < kBins; b += NT) s_bins[b] = 0;
+            __syncthreads();
+            x.count(s_bins, line.divided, shift, kDigits[d], line.key);
+            __syncthreads();
+            int bin;
+            pick_bin<NT>(s_bins, 1 << kDigits[d], line.equals, bin, s_part, s_pick);
+            line.key = line.key << kDigits[d] | (uint32_t)bin;
+            shift -= kDigits[d];
+        }
+    }
+    list_moves<NT>(a, p, line, x, 0, make_int4(0, 0, 0, 0), 0, true, s_counts, s_total);
+}
+
+// ---- more than kAlone tokens: a launch per step, block (part, head, sequence)
+__global__ __launch_bounds__(256) void evict_clear_kernel(int32_t* bins, int64_t n)
+{
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) bins[i] = 0;
+}
+
+// The line as far as the digits counted so far tell.
+template <int NT>
+__device__ __forceinline__ evict_line line_after(const evict_args& a, const evict_pair& p, int digits, int* s_part, int* s_pick)
+{
+    const int* bins = a.bins + p.sh * kAllBins;
+    const int shielded = bins[kProtected];
+    evict_line line;
+    line.divided = shielded >= p.k ? 2 : 1;
+    line.key = 0;
+    line.equals = line.divided == 2 ? p.k : p.k - shielded;
+    if (line.equals == 0) return line;
+    for (int d = 0; d < digits; ++d) {
+        const int at = d == 0 ? (line.divided - 1) * kBins : d == 1 ? kSecond : kThird;
+        int bin;
+        pick_bin<NT>(bins + at, 1 << kDigits[d], line.equals, bin, s_part, s_pick);
+        line.key = line.key << kDigits[d] | (uint32_t)bin;
+    }
+    return line;
+}
+
+template <int STEP>   // 0, 1, 2: counts that digit; 3: counts tokens over and on the line; 4: lists the moves
+__global__ __launch_bounds__(512) void evict_part_kernel(evict_args a)
+{
+    constexpr int NT = 512;
+    __shared__ int s_bins[STEP == 0 ? 2 * kBins : STEP < 3 ? kBins : 1], s_part[NT / 64], s_pick[2], s_total[4];
+    __shared__ int s_counts[4][STEP == 4 ? NT / 64 * kHeld : 64];
+    const int tid = threadIdx.x, part = blockIdx.x, base = part * kPart;
+    const evict_pair p(a, blockIdx.z, blockIdx.y);
+    if (STEP == 0 && part == 0 && blockIdx.y == 0 && tid == 0 && a.new_lens) a.new_lens[p.s] = p.k;
+    if (p.k == p.n) {
+        if (STEP == 4) copy_all(a, p, part, gridDim.x);
+        if (STEP == 4 && part == 0 && tid == 0) a.counts[p.sh] = 0;
+        return;
+    }
+    if (base >= p.n) return;
+    int32_t* bins = a.bins + p.sh * kAllBins;
+    held_tokens<NT> x;
+    x.load(a, p, base);
+    if constexpr (STEP < 3) {
+        evict_line line{1, 0, 1};
+        if constexpr (STEP > 0) {
+            line = line_after<NT>(a, p, STEP, s_part, s_pick);
+            if (line.equals == 0) return;
+        }
+        constexpr int kCounted = STEP == 0 ? 2 * kBins : 1 << kDigits[STEP];
+        for (int b = tid; b < kCounted; b += NT) s_bins[b] = 0;
+        __syncthreads();
+        if constexpr (STEP == 0) {
+            int here = 0;
+#pragma unroll
+            for (int i = 0; i < kHeld; ++i) here += x.cls[i] == 2;
+            const int shielded = block_total<NT>(here, s_part);
+            if (tid == 0 && shielded) atomicAdd(&bins[kProtected], shielded);
+            x.count(s_bins, 1, 32, kDigits[0], 0);
+            x.count(s_bins + kBins, 2, 32, kDigits[0], 0);
+        } else {
+            x.count(s_bins, line.divided, STEP == 1 ? 32 - kDigits[0] : kDigits[2], kDigits[STEP], line.key);
+        }
+        __syncthreads();
+        int32_t* to = bins + (STEP == 0 ? 0 : STEP == 1 ? kSecond : kThird);
+        for (int b = tid; b < kCounted; b += NT)
+            if (s_bins[b]) atomicAdd(&to[b], s_bins[b]);
+    } else {
+        const evict_line line = line_after<NT>(a, p, 3, s_part, s_pick);
+        int4* counts = a.part_counts + p.sh * a.parts;
+        if constexpr (STEP == 3) {
+            int c[4] = {0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < kHeld; ++i) {
+                const int high = base + NT * i + tid >= p.k ? 2 : 0;
+                c[high] += line.over(x.key[i], x.cls[i]);
+                c[high + 1] += line.on(x.key[i], x.cls[i]);
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) c[q] = block_total<NT>(c[q], s_part);
+            if (tid == 0) counts[part] = make_int4(c[0], c[1], c[2], c[3]);
+        } else {
+            int4 before = make_int4(0, 0, 0, 0), all = make_int4(0, 0, 0, 0);
+            const int parts = (p.n + kPart - 1) / kPart;
+            for (int q = tid; q < parts; q += NT) {
+                const int4 c = counts[q];
+                all.x += c.x;
+                all.y += c.y;
+                if (q < part) {
+                    before.x += c.x;
+                    before.y += c.y;
+                    before.z += c.z;
+                    before.w += c.w;
+                }
+            }
+            before.x = block_total<NT>(before.x, s_part);
+            before.y = block_total<NT>(before.y, s_part);
+            before.z = block_total<NT>(before.z, s_part);
+            before.w = block_total<NT>(before.w, s_part);
+            all.x = block_total<NT>(all.x, s_part);
+            all.y = block_total<NT>(all.y, s_part);
+            if (part == 0 && tid == 0) a.counts[p.sh] = p.k - kept_low(line, all.x, all.y);
+            list_moves<NT>(a, p, line, x, base, before, all.y, false, s_counts, s_total);
         }
     }
 }
 
 // Block (x, head, sequence): moves x, x + gridDim.x, .. by groups that fill the workgroup.
-__global__ __launch_bounds__(kThreads) void kv_evict_move_kernel(evict_args a)
+__global__ __launch_bounds__(kThreads) void evict_move_kernel(evict_args a)
 {
     const kv_view_dev& v = a.v;
     const int h = blockIdx.y, s = blockIdx.z, tid = threadIdx.x;
@@ -314,7 +515,24 @@ __global__ __launch_bounds__(kThreads) void kv_evict_move_kernel(evict_args a)
     }
 }
 
-int64_t most_moves(int max_ctx_len) { return max_ctx_len / 2 + 1; }
+// Where things lie in the workspace
+struct evict_room {
+    int64_t heads, most, parts;
+    size_t lists, bins, counts, bytes;
+};
+evict_room room_for(const kv_view* view, int batch, int max_ctx_len)
+{
+    auto whole = [](size_t x) { return (x + 255) / 256 * 256; };
+    evict_room r;
+    r.heads = (int64_t)batch * view->n_kv_local;
+    r.most = max_ctx_len / 2 + 1;   // a hole and a source are two tokens
+    r.parts = max_ctx_len > kAlone ? (max_ctx_len + kPart - 1) / kPart : 0;
+    r.lists = whole(r.heads * 4);
+    r.bins = r.lists + whole(r.heads * 8 * r.most);
+    r.counts = r.bins + (r.parts ? whole(r.heads * 4 * kAllBins) : 0);
+    r.bytes = r.counts + whole(r.heads * 16 * r.parts);
+    return r;
+}
 
 }  // namespace
 
@@ -346,7 +564,7 @@ extern "C" int kv_accept(void* kv_pool, int64_t n_pool_blocks, const kv_view* vi
 extern "C" size_t kv_evict_workspace_bytes(const kv_view* view, int batch, int max_ctx_len)
 {
     if (!kv_view_ok(view) || batch <= 0 || max_ctx_len <= 0) return 0;
-    return (size_t)batch * view->n_kv_local * 4 * (1 + 2 * (size_t)most_moves(max_ctx_len));
+    return room_for(view, batch, max_ctx_len).bytes;
 }
 
 extern "C" int kv_evict(void* kv_pool, int64_t n_pool_blocks, const kv_view* view, const int32_t* block_table,
@@ -388,18 +606,34 @@ extern "C" int kv_evict(void* kv_pool, int64_t n_pool_blocks, const kv_view* vie
     a.recent = recent;
     a.max_ctx_len = max_ctx_len;
     a.v = kv_view_to_dev(view);
-    const int64_t heads = (int64_t)batch * view->n_kv_local;
-    a.counts = (int32_t*)workspace;
-    a.lists = a.counts + heads;
-    a.most = most_moves(max_ctx_len);
     hipStream_t st = (hipStream_t)hip_stream;
-    hipLaunchKernelGGL(kv_evict_select_kernel, dim3((unsigned)batch, (unsigned)view->n_kv_local), dim3(kSelectThreads), 0, st, a);
-    if (max_ctx_len > 0) {
-        // workgroups for eight rounds of the chip, each moving 8 tokens or more at a time
-        int64_t each = (2048 + heads - 1) / heads;
-        const int64_t useful = (a.most * view->geom.head_dim / 4 + kThreads * 4 - 1) / (kThreads * 4);
-        if (each > useful) each = useful;
-        hipLaunchKernelGGL(kv_evict_move_kernel, dim3((unsigned)each, (unsigned)view->n_kv_local, (unsigned)batch), dim3(kThreads), 0, st, a);
+    if (max_ctx_len == 0) {   // (no workspace: only new_lens is written)
+        hipLaunchKernelGGL(evict_select_kernel, dim3((unsigned)batch, (unsigned)view->n_kv_local), dim3(1024), 0, st, a);
+        return kv_record_hip_error(hipGetLastError(), "kv_evict launch");
     }
+    const evict_room r = room_for(view, batch, max_ctx_len);
+    a.counts = (int32_t*)workspace;
+    a.lists = (int32_t*)((char*)workspace + r.lists);
+    a.most = r.most;
+    if (r.parts == 0) {
+        hipLaunchKernelGGL(evict_select_kernel, dim3((unsigned)batch, (unsigned)view->n_kv_local), dim3(1024), 0, st, a);
+    } else {
+        a.parts = (int32_t)r.parts;
+        a.bins = (int32_t*)((char*)workspace + r.bins);
+        a.part_counts = (int4*)((char*)workspace + r.counts);
+        const int64_t words = r.heads * kAllBins;
+        hipLaunchKernelGGL(evict_clear_kernel, dim3((unsigned)((words + 2047) / 2048 < 1024 ? (words + 2047) / 2048 : 1024)), dim3(256), 0, st, a.bins, words);
+        const dim3 grid((unsigned)r.parts, (unsigned)view->n_kv_local, (unsigned)batch);
+        hipLaunchKernelGGL(evict_part_kernel<0>, grid, dim3(512), 0, st, a);
+        hipLaunchKernelGGL(evict_part_kernel<1>, grid, dim3(512), 0, st, a);
+        hipLaunchKernelGGL(evict_part_kernel<2>, grid, dim3(512), 0, st, a);
+        hipLaunchKernelGGL(evict_part_kernel<3>, grid, dim3(512), 0, st, a);
+        hipLaunchKernelGGL(evict_part_kernel<4>, grid, dim3(512), 0, st, a);
+    }
+    // workgroups for eight rounds of the chip, each moving 8 tokens or more at a time
+    int64_t each = (2048 + r.heads - 1) / r.heads;
+    const int64_t useful = (r.most * view->geom.head_dim / 4 + kThreads * 4 - 1) / (kThreads * 4);
+    if (each > useful) each = useful;
+    hipLaunchKernelGGL(evict_move_kernel, dim3((unsigned)each, (unsigned)view->n_kv_local, (unsigned)batch), dim3(kThreads), 0, st, a);
     return kv_record_hip_error(hipGetLastError(), "kv_evict launch");
 }

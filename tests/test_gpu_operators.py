@@ -304,6 +304,9 @@ def evict_inputs(c, rng, ties=True):
     (G8B, (DP, 8, 6), [1500], [20], 16, 1000),                # more protected than the budget holds
     ((6, 2, 96, 5), (TP, 2, 1), [23, 77], [11, 33], 1, 3),
     (TINY, (DP, 1, 0), [20000], [9000], 4, 500),
+    (TINY, (DP, 1, 0), [8192, 8191, 4097], [4096, 8190, 1], 0, 0),   # the most that one workgroup takes
+    (TINY, (TP, 2, 0), [8193, 12288, 100, 0, 9000], [8192, 4096, 100, 5, 0], 4, 64),
+    (TINY, (DP, 2, 1), [13000, 10000], [300, 4200], 16, 6000),      # long, and more protected than the budget holds in one
 ])
 def test_evict(geom, triple, ctx, keep, sinks, recent, in_place):
     c = ref.case(geom, triple, ctx, [0] * len(ctx))
