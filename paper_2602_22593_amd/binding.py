@@ -177,6 +177,7 @@ def _dev_rows(t: torch.Tensor, dtypes, name: str) -> int:
 
 
 _BF16 = (torch.bfloat16, torch.int16, torch.uint16)
+_WORDS = (torch.int64, torch.uint64)
 _workspaces = {}
 _calls_module = None
 
@@ -187,7 +188,7 @@ class _InPython:
     def _none(*_):
         return None
 
-    decode = prefill = linear = append = repack = _none
+    decode = prefill = linear = append = repack = rope = accept = tree = weights = _none
 
 
 def _calls():
@@ -209,6 +210,8 @@ def _calls():
         m.setup(tuple(C.cast(f, C.c_void_p).value for f in functions),
                 (torch.Tensor, torch.nn.Parameter, kv_weight_view), (_BF16, torch.int32, torch.uint8),
                 (torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream), _workspaces)
+        operators = (L.kv_rope_append, L.kv_accept, L.paged_tree_attn, L.paged_decode_attn_weights)
+        m.setup_operators(tuple(C.cast(f, C.c_void_p).value for f in operators), (torch.float32, _WORDS))
         _calls_module = m
     return _calls_module
 
@@ -523,6 +526,12 @@ def kv_rope_append(kv_pool: torch.Tensor, view: KVView, q: torch.Tensor, k: torc
     ints on the host).  ``q_offsets`` int32 [batch + 1], or None for one token per sequence; the new tokens are the last of
     ctx_lens.  ``token_pos`` int32 [batch][n_kv_local][tokens] gets the positions on axis 0 of what is written.
     """
+    if out is not None:
+        rc = (_calls_module or _calls()).rope(kv_pool, view, q, k, v, positions, inv_freq, block_table, ctx_lens, q_offsets, axes,
+                                              pairs, out, token_pos, stream)
+        if rc is not None:
+            _check(rc, "kv_rope_append")
+            return out
     batch, total, d = int(ctx_lens.shape[0]), int(q.shape[0]), view.head_dim
     device = _one_device(q, k, v, kv_pool, positions, inv_freq, block_table, ctx_lens, q_offsets, out, token_pos)
     q_ptr, q_stride = _token_rows(q, total, view.n_q_local, d, "q")
@@ -563,6 +572,12 @@ def paged_tree_attn(q: torch.Tensor, kv_pool: torch.Tensor, block_table: torch.T
 
     Other arguments as paged_prefill_attn; max_q_len is at most 256.
     """
+    if out is not None and workspace is not None:
+        rc = (_calls_module or _calls()).tree(q, kv_pool, block_table, ctx_lens, q_offsets, tree_mask, view, max_ctx_len, max_q_len,
+                                              out, scale, workspace, stream)
+        if rc is not None:
+            _check(rc, "paged_tree_attn")
+            return out
     batch, total = int(ctx_lens.shape[0]), int(q.shape[0])
     device = _one_device(q, kv_pool, block_table, ctx_lens, q_offsets, tree_mask, out, workspace)
     shape = (total, view.n_q_local, view.head_dim)
@@ -575,7 +590,7 @@ def paged_tree_attn(q: torch.Tensor, kv_pool: torch.Tensor, block_table: torch.T
         workspace = _workspace(device, paged_tree_attn_workspace_bytes(view, batch, total, max_ctx_len, max_q_len), stream)
     args = (q_ptr, _shaped(out, shape, _BF16, "out"), _dev(kv_pool, _BF16, "kv_pool"), _blocks_of(kv_pool, view),
             _table(block_table, batch), block_table.stride(0), _ints(ctx_lens, batch, "ctx_lens"),
-            _ints(q_offsets, batch + 1, "q_offsets"), _dev(tree_mask, (torch.int64, torch.uint64), "tree_mask"),
+            _ints(q_offsets, batch + 1, "q_offsets"), _dev(tree_mask, _WORDS, "tree_mask"),
             int(tree_mask.shape[1]), batch, total, int(max_ctx_len), int(max_q_len), view.handle, float(scale),
             _dev(workspace, (torch.uint8,), "workspace"), workspace.numel())
     _check(_launch(device, stream, lambda st: lib().paged_tree_attn(*args, st)), "paged_tree_attn")
@@ -587,6 +602,12 @@ def kv_accept(kv_pool: torch.Tensor, view: KVView, block_table: torch.Tensor, ct
               stream=None) -> torch.Tensor:
     """Move the K and V rows of the accepted drafted tokens (int32 [batch][n], ascending numbers in the draft) behind the cache,
     in order; returns the new lengths."""
+    if new_lens is not None:
+        rc = (_calls_module or _calls()).accept(kv_pool, view, block_table, ctx_lens, q_offsets, accepted, n_accepted, new_lens,
+                                                stream)
+        if rc is not None:
+            _check(rc, "kv_accept")
+            return new_lens
     batch = int(ctx_lens.shape[0])
     device = _one_device(kv_pool, block_table, ctx_lens, q_offsets, accepted, n_accepted, new_lens)
     if accepted.dim() != 2 or accepted.shape[0] != batch:
@@ -610,6 +631,12 @@ def paged_decode_attn_weights(q: torch.Tensor, kv_pool: torch.Tensor, block_tabl
                               scale: float = 0.0, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """paged_decode_attn that also adds the attention weight of every cached token, summed over the query heads of its KV head,
     to ``weights`` (fp32 [batch][n_kv_local][tokens]; the newest token's entry is set)."""
+    if out is not None and workspace is not None:
+        rc = (_calls_module or _calls()).weights(q, kv_pool, block_table, ctx_lens, view, max_ctx_len, weights, out, scale, workspace,
+                                                 stream)
+        if rc is not None:
+            _check(rc, "paged_decode_attn_weights")
+            return out
     batch = int(ctx_lens.shape[0])
     device = _one_device(q, kv_pool, block_table, ctx_lens, weights, out, workspace)
     shape = (batch, view.n_q_local, view.head_dim)

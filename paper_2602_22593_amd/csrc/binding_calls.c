@@ -27,6 +27,16 @@ typedef int (*append_fn)(void*, int64_t, const kv_view*, const void*, const void
 typedef int (*repack_fn)(void*, int64_t, const kv_view*, const kv_view*, const int32_t*, int64_t, const int32_t*, int64_t,
                          const int32_t*, int, int, void*);
 
+typedef int (*rope_fn)(void*, int64_t, const kv_view*, const void*, int64_t, const void*, int64_t, const void*, int64_t, void*,
+                       const int32_t*, int64_t, int, const float*, int, const int32_t*, int, const int32_t*, int64_t,
+                       const int32_t*, const int32_t*, int, int64_t, int32_t*, int64_t, void*);
+typedef int (*accept_fn)(void*, int64_t, const kv_view*, const int32_t*, int64_t, const int32_t*, const int32_t*, const int32_t*,
+                         int64_t, const int32_t*, int, int32_t*, void*);
+typedef int (*tree_fn)(const void*, void*, const void*, int64_t, const int32_t*, int64_t, const int32_t*, const int32_t*,
+                       const uint64_t*, int64_t, int, int64_t, int, int, const kv_view*, float, void*, size_t, void*);
+typedef int (*weights_fn)(const void*, void*, const void*, int64_t, const int32_t*, int64_t, const int32_t*, int, int,
+                          const kv_view*, float, float*, int64_t, void*, size_t, void*);
+
 static decode_fn f_decode;
 static prefill_fn f_prefill;
 static prefill_bytes_fn f_prefill_bytes;
@@ -35,12 +45,18 @@ static linear_bytes_fn f_linear_bytes;
 static append_fn f_append;
 static repack_fn f_repack;
 
+static rope_fn f_rope;
+static accept_fn f_accept;
+static tree_fn f_tree;
+static weights_fn f_weights;
+
 static PyObject *tensor_type, *parameter_type, *weight_view_type;   /* exact types only */
 static PyObject *bf16_types, *int32_type, *uint8_type;              /* dtypes: a tuple, and two */
+static PyObject *float_type, *word_types;                           /* float32; the two of 64-bit masks */
 static PyObject *get_device, *raw_stream, *workspaces;              /* of torch._C; the binding's dict */
 static PyObject *n_is_cuda, *n_dtype, *n_is_contiguous, *n_data_ptr, *n_shape, *n_stride, *n_numel, *n_element_size,
     *n_get_device, *n_cuda_stream, *n_handle, *n_value, *n_block_bytes, *n_n_q_local, *n_n_kv_local, *n_head_dim, *n_scratch,
-    *n_zero, *n_one;
+    *n_zero, *n_one, *n_two;
 
 /* All helpers return 1, or 0 where the Python code is to answer (an exception may be set then: `answer` clears it). */
 
@@ -335,6 +351,215 @@ static PyObject* call_repack(PyObject* self, PyObject* const* a, Py_ssize_t narg
     return answer(ok, rc);
 }
 
+/* The device that is current, which the calls below want all their tensors on (the Python code sorts the others out). */
+static int current(int64_t* out) { return to_int64(PyObject_CallNoArgs(get_device), out); }
+
+/* dev(), on that device (of the GPU: the others have no number), with its sizes as given (sizes of -1 are found out) */
+static int shaped(PyObject* t, PyObject* dtype, int64_t device, int n, int64_t* size, void** out)
+{
+    int64_t found[3], on;
+    if (!sizes(t, n, found)) return 0;
+    for (int i = 0; i < n; ++i) {
+        if (size[i] >= 0 && size[i] != found[i]) return 0;
+        size[i] = found[i];
+    }
+    if (!dtype_is(t, dtype) || !ask_int(t, n_get_device, NULL, &on) || on != device || on < 0) return 0;
+    PyObject* c = ask(t, n_is_contiguous, NULL);
+    const int yes = c == Py_True;
+    Py_XDECREF(c);
+    return yes && address(t, out);
+}
+
+/* binding._token_rows: [tokens][heads][d], tokens may lie apart */
+static int token_rows(PyObject* t, int64_t device, int64_t tokens, int64_t heads, int64_t d, void** out, int64_t* row)
+{
+    int64_t found[3], s, on;
+    if (!sizes(t, 3, found) || found[0] != tokens || found[1] != heads || found[2] != d ||
+        !dtype_is(t, bf16_types) || !ask_int(t, n_get_device, NULL, &on) || on != device || on < 0)
+        return 0;
+    if (!ask_int(t, n_stride, n_two, &s) || s != 1 || (heads > 1 && !(ask_int(t, n_stride, n_one, &s) && s == d))) return 0;
+    if (tokens > 1) {
+        if (!ask_int(t, n_stride, n_zero, row)) return 0;
+    } else {
+        *row = heads * d;
+    }
+    return address(t, out);
+}
+
+/* What all of the calls below ask of the pool, its view and its table. */
+typedef struct {
+    int64_t device, batch, blocks, row, hq, hkv, d, bb;
+    void *pool, *table, *ctx;
+    const kv_view* view;
+} cache_args;
+static int cache_of(PyObject* pool, PyObject* view, PyObject* table, PyObject* ctx, cache_args* c)
+{
+    int64_t on, tab[2];
+    c->batch = -1;
+    if (!current(&c->device) || !shaped(ctx, int32_type, c->device, 1, &c->batch, &c->ctx) || c->batch > INT32_MAX) return 0;
+    tab[0] = c->batch;
+    tab[1] = -1;
+    return shaped(table, int32_type, c->device, 2, tab, &c->table) && ask_int(table, n_stride, n_zero, &c->row) &&
+           int_attr(view, n_n_q_local, &c->hq) && int_attr(view, n_n_kv_local, &c->hkv) && int_attr(view, n_head_dim, &c->d) &&
+           int_attr(view, n_block_bytes, &c->bb) && view_handle(view, &c->view) && dev(pool, bf16_types, &c->pool) &&
+           ask_int(pool, n_get_device, NULL, &on) && on == c->device && pool_blocks(pool, c->bb, 1, &c->blocks);
+}
+
+/* rope(kv_pool, view, q, k, v, positions, inv_freq, block_table, ctx_lens, q_offsets, axes, pairs, out, token_pos, stream) */
+static PyObject* call_rope(PyObject* self, PyObject* const* a, Py_ssize_t nargs)
+{
+    ARGS(15)
+    enum { kMost = 128 };
+    int64_t q[3], q_row, k_row, v_row, pos[2] = {-1, -1}, half = -1, off, out[3], per[3] = {0, 0, 0}, pairs, stream;
+    void *pq, *pk, *pv, *pout, *ppos, *pfreq, *poff = NULL, *pper = NULL;
+    int32_t axes[kMost];
+    cache_args c;
+    int rc = 0, n_axes = 1;
+    int ok = cache_of(a[0], a[1], a[7], a[8], &c) && sizes(a[2], 3, q) && token_rows(a[2], c.device, q[0], c.hq, c.d, &pq, &q_row) &&
+             token_rows(a[3], c.device, q[0], c.hkv, c.d, &pk, &k_row) && token_rows(a[4], c.device, q[0], c.hkv, c.d, &pv, &v_row);
+    if (ok) {
+        out[0] = pos[0] = q[0];
+        out[1] = c.hq;
+        out[2] = c.d;
+        if (!shaped(a[5], int32_type, c.device, 1, pos, &ppos)) {
+            PyErr_Clear();
+            pos[0] = -1;
+            pos[1] = q[0];
+            ok = shaped(a[5], int32_type, c.device, 2, pos, &ppos) && pos[0] >= 1 && pos[0] <= 4;
+            n_axes = (int)pos[0];
+        }
+        ok = ok && shaped(a[6], float_type, c.device, 1, &half, &pfreq) && half <= kMost && shaped(a[12], bf16_types, c.device, 3, out, &pout) &&
+             int_arg(a[11], &pairs) && stream_handle(a[14], NULL, &stream);
+    }
+    if (ok && a[10] != Py_None) {
+        ok = (PyList_CheckExact(a[10]) || PyTuple_CheckExact(a[10])) && PySequence_Fast_GET_SIZE(a[10]) == half;
+        for (int64_t i = 0; ok && i < half; ++i) {
+            int64_t x;
+            ok = int_arg(PySequence_Fast_GET_ITEM(a[10], i), &x);
+            axes[i] = (int32_t)x;
+        }
+    } else if (n_axes != 1) {
+        ok = 0;
+    }
+    if (ok && a[9] != Py_None) {
+        off = c.batch + 1;
+        ok = shaped(a[9], int32_type, c.device, 1, &off, &poff);
+    }
+    if (ok && a[13] != Py_None) {
+        per[0] = c.batch;
+        per[1] = c.hkv;
+        per[2] = -1;
+        ok = shaped(a[13], int32_type, c.device, 3, per, &pper);
+    }
+    if (ok) {
+        Py_BEGIN_ALLOW_THREADS
+        rc = f_rope(c.pool, c.blocks, c.view, pq, q_row, pk, k_row, pv, v_row, pout, ppos, q[0], n_axes, pfreq, (int)(2 * half),
+                    a[10] == Py_None ? NULL : axes, (int)pairs, c.table, c.row, c.ctx, poff, (int)c.batch, q[0], pper, per[2],
+                    (void*)(uintptr_t)stream);
+        Py_END_ALLOW_THREADS
+    }
+    return answer(ok, rc);
+}
+
+/* accept(kv_pool, view, block_table, ctx_lens, q_offsets, accepted, n_accepted, new_lens, stream) */
+static PyObject* call_accept(PyObject* self, PyObject* const* a, Py_ssize_t nargs)
+{
+    ARGS(9)
+    int64_t off, acc[2], n, stream;
+    void *poff, *pacc, *pn, *pnew;
+    cache_args c;
+    int rc = 0, ok = cache_of(a[0], a[1], a[2], a[3], &c);
+    if (ok) {
+        off = c.batch + 1;
+        acc[0] = n = c.batch;
+        acc[1] = -1;
+        ok = shaped(a[4], int32_type, c.device, 1, &off, &poff) && shaped(a[5], int32_type, c.device, 2, acc, &pacc) &&
+             shaped(a[6], int32_type, c.device, 1, &n, &pn) && shaped(a[7], int32_type, c.device, 1, &n, &pnew) &&
+             stream_handle(a[8], NULL, &stream);
+    }
+    if (ok) {
+        Py_BEGIN_ALLOW_THREADS
+        rc = f_accept(c.pool, c.blocks, c.view, c.table, c.row, c.ctx, poff, pacc, acc[1], pn, (int)c.batch, pnew,
+                      (void*)(uintptr_t)stream);
+        Py_END_ALLOW_THREADS
+    }
+    return answer(ok, rc);
+}
+
+/* tree(q, kv_pool, block_table, ctx_lens, q_offsets, tree_mask, view, max_ctx_len, max_q_len, out, scale, workspace, stream) */
+static PyObject* call_tree(PyObject* self, PyObject* const* a, Py_ssize_t nargs)
+{
+    ARGS(13)
+    int64_t q[3], off, mask[2], max_ctx, max_q, ws = -1, stream;
+    void *pq, *pout, *poff, *pmask, *pws;
+    cache_args c;
+    float scale;
+    int rc = 0, ok = cache_of(a[1], a[6], a[2], a[3], &c);
+    if (ok) {
+        q[0] = mask[1] = -1;
+        q[1] = c.hq;
+        q[2] = c.d;
+        off = c.batch + 1;
+        ok = shaped(a[0], bf16_types, c.device, 3, q, &pq) && shaped(a[9], bf16_types, c.device, 3, q, &pout) &&
+             shaped(a[4], int32_type, c.device, 1, &off, &poff);
+        mask[0] = q[0];
+        ok = ok && shaped(a[5], word_types, c.device, 2, mask, &pmask) && int_arg(a[7], &max_ctx) && int_arg(a[8], &max_q) &&
+             float_arg(a[10], &scale) && shaped(a[11], uint8_type, c.device, 1, &ws, &pws) && stream_handle(a[12], NULL, &stream);
+    }
+    if (ok) {
+        Py_BEGIN_ALLOW_THREADS
+        rc = f_tree(pq, pout, c.pool, c.blocks, c.table, c.row, c.ctx, poff, pmask, mask[1], (int)c.batch, q[0], (int)max_ctx,
+                    (int)max_q, c.view, scale, pws, (size_t)ws, (void*)(uintptr_t)stream);
+        Py_END_ALLOW_THREADS
+    }
+    return answer(ok, rc);
+}
+
+/* weights(q, kv_pool, block_table, ctx_lens, view, max_ctx_len, weights, out, scale, workspace, stream) */
+static PyObject* call_weights(PyObject* self, PyObject* const* a, Py_ssize_t nargs)
+{
+    ARGS(11)
+    int64_t q[3], per[3], max_ctx, ws = -1, stream;
+    void *pq, *pout, *pper, *pws;
+    cache_args c;
+    float scale;
+    int rc = 0, ok = cache_of(a[1], a[4], a[2], a[3], &c);
+    if (ok) {
+        q[0] = per[0] = c.batch;
+        q[1] = c.hq;
+        per[1] = c.hkv;
+        q[2] = c.d;
+        per[2] = -1;
+        ok = shaped(a[0], bf16_types, c.device, 3, q, &pq) && shaped(a[7], bf16_types, c.device, 3, q, &pout) &&
+             shaped(a[6], float_type, c.device, 3, per, &pper) && int_arg(a[5], &max_ctx) && float_arg(a[8], &scale) &&
+             shaped(a[9], uint8_type, c.device, 1, &ws, &pws) && stream_handle(a[10], NULL, &stream);
+    }
+    if (ok) {
+        Py_BEGIN_ALLOW_THREADS
+        rc = f_weights(pq, pout, c.pool, c.blocks, c.table, c.row, c.ctx, (int)c.batch, (int)max_ctx, c.view, scale, pper, per[2],
+                       pws, (size_t)ws, (void*)(uintptr_t)stream);
+        Py_END_ALLOW_THREADS
+    }
+    return answer(ok, rc);
+}
+
+/* setup_operators((addresses of rope, accept, tree, weights), (float32, dtypes of mask words)); after setup() */
+static PyObject* setup_operators(PyObject* self, PyObject* args)
+{
+    unsigned long long f[4];
+    PyObject *f32, *words;
+    if (!PyArg_ParseTuple(args, "(KKKK)(OO)", f, f + 1, f + 2, f + 3, &f32, &words)) return NULL;
+    f_rope = (rope_fn)(uintptr_t)f[0];
+    f_accept = (accept_fn)(uintptr_t)f[1];
+    f_tree = (tree_fn)(uintptr_t)f[2];
+    f_weights = (weights_fn)(uintptr_t)f[3];
+    Py_INCREF(f32);
+    Py_XSETREF(float_type, f32);
+    Py_INCREF(words);
+    Py_XSETREF(word_types, words);
+    Py_RETURN_NONE;
+}
+
 /* setup((addresses of the seven functions), (types), (dtypes), (torch._C functions), dict) */
 static PyObject* setup(PyObject* self, PyObject* args)
 {
@@ -366,6 +591,11 @@ static PyMethodDef methods[] = {
     {"prefill", (PyCFunction)(void (*)(void))call_prefill, METH_FASTCALL, NULL},
     {"linear", (PyCFunction)(void (*)(void))call_linear, METH_FASTCALL, NULL},
     {"append", (PyCFunction)(void (*)(void))call_append, METH_FASTCALL, NULL},
+    {"setup_operators", setup_operators, METH_VARARGS, NULL},
+    {"rope", (PyCFunction)(void (*)(void))call_rope, METH_FASTCALL, NULL},
+    {"accept", (PyCFunction)(void (*)(void))call_accept, METH_FASTCALL, NULL},
+    {"tree", (PyCFunction)(void (*)(void))call_tree, METH_FASTCALL, NULL},
+    {"weights", (PyCFunction)(void (*)(void))call_weights, METH_FASTCALL, NULL},
     {"repack", (PyCFunction)(void (*)(void))call_repack, METH_FASTCALL, NULL},
     {NULL, NULL, 0, NULL},
 };
@@ -386,6 +616,6 @@ PyMODINIT_FUNC PyInit__calls(void)
     };
     for (size_t i = 0; i < sizeof(names) / sizeof(names[0]); ++i)
         if (!*names[i].to && !(*names[i].to = PyUnicode_InternFromString(names[i].text))) return NULL;
-    if (!(n_zero = PyLong_FromLong(0)) || !(n_one = PyLong_FromLong(1))) return NULL;
+    if (!(n_zero = PyLong_FromLong(0)) || !(n_one = PyLong_FromLong(1)) || !(n_two = PyLong_FromLong(2))) return NULL;
     return PyModule_Create(&module);
 }

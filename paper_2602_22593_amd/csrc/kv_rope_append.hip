@@ -4,9 +4,11 @@
 // With frequencies f_0 .. f_{R/2 - 1} and an axis for each, the pair (x, y) of number i becomes (x cos a - y sin a, y cos a + x sin a),
 // a = position on axis(i) * f_i.  Elements from R on pass as they are, and so do the values.
 //
-// Bound by reading and writing every row once.  A workgroup takes a few tokens: their cosines and sines go into LDS once and
-// serve all heads; then every lane moves items of two 16-byte pieces, the two halves of eight pairs, so that a
-// rotation needs nothing of another lane.  D / 16 items a head, consecutive lanes on consecutive pieces.
+// Bound by reading and writing every row once: 17000 tokens of 32 query and 8 KV heads of 128, 420 MB, take 87 us, the rate of a
+// large copy (4.8 TB/s).  A workgroup takes one or two tokens: their cosines and sines go into LDS once and serve all heads; then every
+// lane moves items of two 16-byte pieces, the two halves of eight pairs, so that a rotation needs nothing of another
+// lane.  D / 16 items a head, consecutive lanes on consecutive pieces.  Small workgroups with one item a lane at a time hide the
+// chain before the rows (lengths, positions, cosines) behind each other: eight tokens and four items 105 us, four and two 91.
 #include "kv_internal.h"
 
 #include "decode_common.h"
@@ -16,9 +18,8 @@ using namespace kvdec;
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMostTokens = 8;    // per workgroup
+constexpr int kMostTokens = 2;    // per workgroup
 constexpr int kMostPairs = 128;   // of a head
-constexpr int kUnroll = 4;
 
 struct rope_args {
     const uint16_t *q, *k, *v_new;
@@ -106,68 +107,39 @@ __global__ __launch_bounds__(kThreads) void kv_rope_append_kernel(rope_args a)
     const int per_head = v.head_dim >> 4, heads = v.n_q_local + 2 * v.n_kv_local, per_token = heads * per_head;
     const int rotated = a.pairs >> 3;   // items of a head that turn
     const int items = n * per_token;
-    for (int x0 = tid; x0 < items; x0 += kThreads * kUnroll) {
-        kv_u32x4 lo[kUnroll], hi[kUnroll];
-        uint16_t* to[kUnroll];
-        int where[kUnroll], apart[kUnroll];   // (token, first pair) of a rotation, or -1; elements between the two pieces
+    for (int x = tid; x < items; x += kThreads) {
+        const int j = x / per_token, y = x - j * per_token, h = y / per_head, c = y - h * per_head;
+        const int64_t place = s_place[j], i = i0 + j;
+        const bool query = h < v.n_q_local, value = h >= v.n_q_local + v.n_kv_local;
+        if (place == -2 || (!query && place < 0)) continue;
+        const bool turns = !value && c < rotated, halves = turns && !a.adjacent;
+        const int at = halves ? 8 * c : 16 * c, apart = halves ? a.pairs : 8;   // of the item's two pieces
+        const int hk = value ? h - v.n_q_local - v.n_kv_local : h - v.n_q_local;
+        const uint16_t* src = (query ? a.q + i * a.q_stride + h * v.head_dim : (value ? a.v_new + i * a.v_stride : a.k + i * a.k_stride) + hk * v.head_dim) + at;
+        uint16_t* to = (query ? a.out + (i * v.n_q_local + h) * v.head_dim : a.pool + place + (value ? v.plane_elems : 0) + hk * v.head_dim) + at;
+        kv_u32x4 lo = *reinterpret_cast<const kv_u32x4*>(src), hi = *reinterpret_cast<const kv_u32x4*>(src + apart);
+        if (turns) {
+            const float2* turn = &s_turn[j][8 * c];
+            if (a.adjacent) {
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            const int x = x0 + u * kThreads;
-            to[u] = nullptr;
-            where[u] = -1;
-            apart[u] = 8;
-            if (x >= items) continue;
-            const int j = x / per_token, y = x - j * per_token, h = y / per_head, c = y - h * per_head;
-            const int64_t place = s_place[j], i = i0 + j;
-            if (place == -2) continue;
-            const uint16_t* src;
-            int at = 16 * c;
-            const bool value = h >= v.n_q_local + v.n_kv_local;
-            if (!value && c < rotated) {
-                where[u] = j * kMostPairs + 8 * c;
-                if (!a.adjacent) {
-                    at = 8 * c;
-                    apart[u] = a.pairs;
+                for (int e = 0; e < 4; ++e) {
+                    const float2 t = turn[e], t2 = turn[4 + e];
+                    const float xa = bf16_lo(lo[e]), ya = bf16_hi(lo[e]), xb = bf16_lo(hi[e]), yb = bf16_hi(hi[e]);
+                    lo[e] = pack_bf16x2(xa * t.x - ya * t.y, ya * t.x + xa * t.y);
+                    hi[e] = pack_bf16x2(xb * t2.x - yb * t2.y, yb * t2.x + xb * t2.y);
                 }
-            }
-            if (h < v.n_q_local) {
-                src = a.q + i * a.q_stride + h * v.head_dim;
-                to[u] = a.out + (i * v.n_q_local + h) * v.head_dim + at;
             } else {
-                if (place < 0) continue;
-                const int hk = value ? h - v.n_q_local - v.n_kv_local : h - v.n_q_local;
-                src = (value ? a.v_new + i * a.v_stride : a.k + i * a.k_stride) + hk * v.head_dim;
-                to[u] = a.pool + place + (value ? v.plane_elems : 0) + hk * v.head_dim + at;
-            }
-            lo[u] = *reinterpret_cast<const kv_u32x4*>(src + at);
-            hi[u] = *reinterpret_cast<const kv_u32x4*>(src + at + apart[u]);
-        }
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            if (!to[u]) continue;
-            if (where[u] >= 0) {
-                const float2* turn = &s_turn[0][0] + where[u];
-                if (a.adjacent) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float2 t = turn[e], t2 = turn[4 + e];
-                        const float x = bf16_lo(lo[u][e]), y = bf16_hi(lo[u][e]), x2 = bf16_lo(hi[u][e]), y2 = bf16_hi(hi[u][e]);
-                        lo[u][e] = pack_bf16x2(x * t.x - y * t.y, y * t.x + x * t.y);
-                        hi[u][e] = pack_bf16x2(x2 * t2.x - y2 * t2.y, y2 * t2.x + x2 * t2.y);
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float2 t = turn[2 * e], t2 = turn[2 * e + 1];
-                        const float x = bf16_lo(lo[u][e]), x2 = bf16_hi(lo[u][e]), y = bf16_lo(hi[u][e]), y2 = bf16_hi(hi[u][e]);
-                        lo[u][e] = pack_bf16x2(x * t.x - y * t.y, x2 * t2.x - y2 * t2.y);
-                        hi[u][e] = pack_bf16x2(y * t.x + x * t.y, y2 * t2.x + x2 * t2.y);
-                    }
+                for (int e = 0; e < 4; ++e) {
+                    const float2 t = turn[2 * e], t2 = turn[2 * e + 1];
+                    const float xa = bf16_lo(lo[e]), xb = bf16_hi(lo[e]), ya = bf16_lo(hi[e]), yb = bf16_hi(hi[e]);
+                    lo[e] = pack_bf16x2(xa * t.x - ya * t.y, xb * t2.x - yb * t2.y);
+                    hi[e] = pack_bf16x2(ya * t.x + xa * t.y, yb * t2.x + xb * t2.y);
                 }
             }
-            *reinterpret_cast<kv_u32x4*>(to[u]) = lo[u];
-            *reinterpret_cast<kv_u32x4*>(to[u] + apart[u]) = hi[u];
         }
+        *reinterpret_cast<kv_u32x4*>(to) = lo;
+        *reinterpret_cast<kv_u32x4*>(to + apart) = hi;
     }
 }
 
