@@ -54,7 +54,9 @@ struct tree_args {
     kv_view_dev v;
     uint32_t last_block;      // n_pool_blocks - 1
     float scale_log2e;
-    int32_t group, batch, max_ctx_len, mask_words;
+    int32_t group, batch, max_ctx_len, max_q_len, mask_words;
+    int32_t few;              // up to 64 sequences, and their tiles are counted in 32 bits
+    int32_t group_shift;      // log2 of the group rounded up to a power of two
     int32_t teams, least_tiles;   // shares that the axis of tiles is cut into, and the least tiles of a share
     float* part_o;            // [2 teams n_kv_local][32 RW][D]: slot 2 w the first piece of workgroup w, 2 w + 1 its last
     float* part_ml;           // [2 teams n_kv_local][32 RW][2] (reference in exponent units, sum of weights)
@@ -118,7 +120,8 @@ __device__ __forceinline__ seq_work work_of(const tree_args& a, int s)
     seq_work w;
     w.n = min(a.ctx_lens[s], a.max_ctx_len);
     w.q0 = a.q_off ? a.q_off[s] : s;
-    w.q_len = a.q_off ? a.q_off[s + 1] - w.q0 : 1;
+    w.q_len = a.q_off ? min(a.q_off[s + 1] - w.q0, a.max_q_len) : 1;
+    if (a.q_off && w.n > 0) w.q_len = min(w.q_len, w.n);   // (both bounds are the caller's to keep; no address depends on it)
     const bool any = w.n > 0 && w.q_len > 0;
     w.tiles = any ? (w.n + kKeys - 1) / kKeys : 0;
     w.blocks = any ? (w.q_len * a.group + RB - 1) / RB : 0;
@@ -194,10 +197,36 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
     const kv_view_dev& v = a.v;
     const int G = a.group, Hl = v.n_kv_local;
 
+    const int team = (int)blockIdx.x / Hl, h = (int)blockIdx.x - team * Hl;
     int64_t from, to, offset;
     int s;
-    const int team = (int)blockIdx.x / Hl, h = (int)blockIdx.x - team * Hl;
-    find_share<NT, RB>(a, team, s_sum, from, to, s, offset);
+    // Up to 64 sequences a wavefront holds in its lanes and finds its share by itself: one trip to memory, no barriers
+    const bool few = a.few != 0;
+    seq_work lane_work = {0, 0, 0, 0, 0};
+    if (few) {
+        if (lane < a.batch) lane_work = work_of<RB>(a, lane);
+        const int here = lane_work.tiles * lane_work.blocks;
+        int incl = here;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int y = __shfl_up(incl, d);
+            incl += lane >= d ? y : 0;
+        }
+        const int total = __builtin_amdgcn_readlane(incl, 63);
+        const int64_t share = share_of(a, total);
+        from = team * share;
+        to = min(from + share, (int64_t)total);
+        s = min(__builtin_popcountll(__builtin_amdgcn_ballot_w64(incl <= from)), 63);
+        offset = from - __builtin_amdgcn_readlane(incl - here, s);
+    } else {
+        find_share<NT, RB>(a, team, s_sum, from, to, s, offset);
+    }
+    auto sequence = [&](int x) {
+        if (!few) return work_of<RB>(a, x);
+        return seq_work{__builtin_amdgcn_readlane(lane_work.n, x), __builtin_amdgcn_readlane(lane_work.q0, x),
+                        __builtin_amdgcn_readlane(lane_work.q_len, x), __builtin_amdgcn_readlane(lane_work.tiles, x),
+                        __builtin_amdgcn_readlane(lane_work.blocks, x)};
+    };
 
     // ---- what does not change from piece to piece -------------------------------------------------
     const int64_t stride_bytes = (int64_t)v.token_stride * 2, block_bytes = v.block_elems * 2, plane_bytes = v.plane_elems * 2;
@@ -229,7 +258,7 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
 
     for (int64_t at = from; at < to;) {
         // ---- the next piece: tiles [t0, t0 + count) of block rb of sequence s -----------------------------
-        const seq_work w = work_of<RB>(a, s);
+        const seq_work w = sequence(s);
         if (offset >= w.total()) {
             offset -= w.total();
             ++s;
@@ -241,13 +270,15 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
         const int n = w.n, first = n - w.q_len;          // the first drafted token
         const int rows = min(w.q_len * G - rb * RB, RB);   // of the pair
         const bool idle = rw * 32 >= rows;                 // this wavefront has none of them
-        const int mine = kg < count ? (count - kg + KW - 1) / KW : 0, iters = (count + KW - 1) / KW;
+        // each key group takes tiles that follow each other: [kt0, kt0 + mine)
+        const int mine = count / KW + (kg < count % KW ? 1 : 0), iters = (count + KW - 1) / KW;
+        const int kt0 = t0 + kg * (count / KW) + min(kg, count % KW);
         const int last_group = (n - 1) >> 4;
 
         // where the groups of 16 tokens lie: lane l knows that of group l % 2 of this wavefront's tile 32 window + l / 2
         const int32_t* ids = a.table + (int64_t)s * a.table_stride;
         const char* pool_head = reinterpret_cast<const char*>(a.pool + v.head_off + h * D);
-        auto group_at = [&](int window) { return min(2 * (t0 + kg + (32 * window + (lane >> 1)) * KW) + (lane & 1), last_group); };
+        auto group_at = [&](int window) { return min(2 * (kt0 + 32 * window + (lane >> 1)) + (lane & 1), last_group); };
         auto request_ids = [&](int window) { return (uint32_t)ids[group_at(window) / groups_per_block]; };
         auto places = [&](uint32_t id, int window) {
             const int g = group_at(window);
@@ -270,7 +301,7 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
                 x.place = places(x.id, i >> 5);
                 x.id = request_ids((i >> 5) + 1);
             }
-            const int tile = t0 + kg + i * KW;
+            const int tile = kt0 + i;
             auto rows_of = [&](int g) {
                 const int l = 2 * (i & 31) + g;
                 const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)x.place, l);
@@ -392,19 +423,29 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
             else l = add_pair(pw[u], l);        // the same rounding above and below the fraction
         };
         auto weight_operand = [&](int c) { return as_bf16x8(kv_u32x4{pw[4 * c], pw[4 * c + 1], pw[4 * c + 2], pw[4 * c + 3]}); };
-        // Scores leave through LDS, so that a store writes whole lines: 8 lanes a row of 32 tokens, 8 rows at a time
-        auto keep_scores = [&](int base) {
+        // Scores of as many tiles as make 32 rows leave together, through LDS, whole lines at a time.  (The loads of later tiles are
+        // counted in order with the stores, whose way out is long: storing every tile's takes 64 sequences of 512 to 4096
+        // 131 us in place of 114.)  Returns whether it stored four times.
+        auto keep_scores = [&](int i) -> bool {
             if constexpr (SUMS) {
+                const int slots = 32 >> a.group_shift, slot = i & (slots - 1);
                 if (real) {
 #pragma unroll
                     for (int u = 0; u < 4; ++u)
-                        s_out[kg][col][2 * u + half] =
+                        s_out[kg][(slot << a.group_shift) + col][2 * u + half] =
                             f32x4{sc[4 * u] * a.scale_log2e, sc[4 * u + 1] * a.scale_log2e, sc[4 * u + 2] * a.scale_log2e, sc[4 * u + 3] * a.scale_log2e};
                 }
-                float* dst = a.scores + ((int64_t)s * v.n_q_local + h * G) * a.score_stride + base;
-                for (int r = lane >> 3; r < G; r += 8)
-                    *reinterpret_cast<f32x4*>(dst + r * a.score_stride + 4 * (lane & 7)) = s_out[kg][r][lane & 7];
+                if (slot < slots - 1 && i < mine - 1) return false;
+                float* dst = a.scores + ((int64_t)s * v.n_q_local + h * G) * a.score_stride;
+#pragma unroll
+                for (int r0 = 0; r0 < 32; r0 += 8) {
+                    const int r = r0 + (lane >> 3), x = r >> a.group_shift, g = r & ((1 << a.group_shift) - 1);
+                    if (x <= slot && g < G)
+                        *reinterpret_cast<f32x4*>(dst + g * a.score_stride + kKeys * (kt0 + i - slot + x) + 4 * (lane & 7)) = s_out[kg][r][lane & 7];
+                }
+                return slot == slots - 1;
             }
+            return false;
         };
         // A column without a key yet has no reference; its first key sets it.
         auto first_reference = [&]() {
@@ -493,10 +534,10 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
             for (int x = 0; x < 16; ++x) sc[x] = (seen >> (8 * (x >> 2) + (x & 3))) & 1 ? sc[x] : kNegInf;
         };
         auto whole_step = [&](auto careful, int i, const kv_u32x4* sk, const kv_u32x4* sv) {
-            const int tile = t0 + kg + i * KW;
+            const int tile = kt0 + i;
             scores(sk);
             hide(tile);
-            keep_scores(kKeys * tile);
+            keep_scores(i);
             first_reference();
             exponents();
 #pragma unroll
@@ -509,12 +550,14 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
         // instructions that fit under it, the operand read of the second product after it.  The loads of the
         // NB - 1 tiles after it are under way meanwhile.
         constexpr int kAhead = 2;
+        constexpr bool kStoresLast = SUMS;
         auto step = [&](auto phase, int i) {
             constexpr int B = decltype(phase)::value;   // i % NB
             kv_u32x4* const k_next = k_buf(B + 1);
             kv_u32x4* const v_now = v_buf(B);
             stage_v(v_buf(B + NB - 1));
             stage_k(k_buf(B));
+            bool stored = false;
             if (!idle) {
                 bf16x8 ka[NK], va[2 * NJ];
 #pragma unroll
@@ -534,9 +577,9 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
                     __builtin_amdgcn_sched_barrier(0);
                 }
                 const bf16x8 pb[2] = {weight_operand(0), weight_operand(1)};
-                const int tile = t0 + kg + (i + 1) * KW;
+                const int tile = kt0 + i + 1;
                 hide(tile);
-                keep_scores(kKeys * tile);
+                stored = keep_scores(i + 1);
                 first_reference();
                 float top = kNegInf;
 #pragma unroll
@@ -554,9 +597,9 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
                 move_reference(top);
             }
             // K of tile i + 2 and V of tile i + 1 are needed next: what the last NB - 2 steps asked for may still be under way
-            // (the last one is scores on their way out)
             if (NB > 2 && i + NB < mine) staged(std::integral_constant<int, (NB - 2) * (kSplitPlanes ? 1 : 2) * NP>());
-            else staged(std::integral_constant<int, SUMS ? 1 : 0>());
+            else if (stored && kStoresLast) staged(std::integral_constant<int, 4>());   // (scores on their way out)
+            else staged(std::integral_constant<int, 0>());
         };
         staged(std::integral_constant<int, 0>());
         const int common = count / KW;   // tiles that every key group has
@@ -564,8 +607,8 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
         if (common > 0) {
             if (!idle) {
                 scores(s_k0);
-                hide(t0 + kg);
-                keep_scores(kKeys * (t0 + kg));
+                hide(kt0);
+                keep_scores(0);
                 first_reference();
                 exponents();
             }
@@ -843,6 +886,20 @@ __global__ __launch_bounds__(256) void weights_kernel(tree_args a)
     __shared__ f32x4 s_acc[256];
     __shared__ float2 s_ml[kRows], s_row[4][32];
     const int s = blockIdx.x, h = blockIdx.y, G = a.group, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    float* sums = a.sums + ((int64_t)s * a.v.n_kv_local + h) * a.sum_stride;
+    const float* scores = a.scores + ((int64_t)s * a.v.n_q_local + h * G) * a.score_stride;
+    // Four tokens a thread.  Their sums and the scores of four query heads are asked for before anything is known of the sequence: what
+    // bounds this launch is one trip to memory after another.  (Rows of scores are padded to whole tiles.)
+    const int t = (int)blockIdx.z * a.chunk + 4 * tid;
+    const bool here = 4 * tid < a.chunk && t < a.max_ctx_len;
+    f32x4 e[4] = {};
+    float prior[4] = {0.f, 0.f, 0.f, 0.f};
+    if (here) {
+#pragma unroll
+        for (int y = 0; y < 4; ++y) e[y] = *reinterpret_cast<const f32x4*>(scores + min(y, G - 1) * a.score_stride + t);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) prior[c] = sums[min(t + c, a.max_ctx_len - 1)];
+    }
     const seq_work w = work_of<RB>(a, s);
     if (w.n <= 0) {
         zero_rows<D>(a, w, h);
@@ -887,15 +944,14 @@ __global__ __launch_bounds__(256) void weights_kernel(tree_args a)
     }
     if (wave == 0 && lane < gp) s_row[0][g] = make_float2(m, l != 0.f ? 1.0f / l : 0.f);
     __syncthreads();
-    float* sums = a.sums + ((int64_t)s * a.v.n_kv_local + h) * a.sum_stride;
-    const float* scores = a.scores + ((int64_t)s * a.v.n_q_local + h * G) * a.score_stride;
     const int end = min(((int)blockIdx.z + 1) * a.chunk, w.n);
-    for (int t = (int)blockIdx.z * a.chunk + 4 * tid; t < end; t += 4 * 256) {   // (rows of scores are padded to whole tiles)
+    if (here && t < end) {
         f32x4 x = {0.f, 0.f, 0.f, 0.f};
         for (int y0 = 0; y0 < G; y0 += 4) {
-            f32x4 e[4];
+            if (y0 > 0) {
 #pragma unroll
-            for (int y = 0; y < 4; ++y) e[y] = *reinterpret_cast<const f32x4*>(scores + min(y0 + y, G - 1) * a.score_stride + t);
+                for (int y = 0; y < 4; ++y) e[y] = *reinterpret_cast<const f32x4*>(scores + min(y0 + y, G - 1) * a.score_stride + t);
+            }
 #pragma unroll
             for (int y = 0; y < 4; ++y) {
                 if (y0 + y >= G) break;
@@ -906,7 +962,7 @@ __global__ __launch_bounds__(256) void weights_kernel(tree_args a)
         }
 #pragma unroll
         for (int c = 0; c < 4; ++c)
-            if (t + c < end) sums[t + c] = t + c == w.n - 1 ? x[c] : sums[t + c] + x[c];   // (the newest token has no sum yet)
+            if (t + c < end) sums[t + c] = t + c == w.n - 1 ? x[c] : prior[c] + x[c];   // (the newest token has no sum yet)
     }
     if (cut)
         for (int row = blockIdx.z; row < G; row += gridDim.z) add_row_together<D, RB>(a, w, p, row, s_acc, s_ml);
@@ -919,7 +975,7 @@ int row_waves(int64_t rows) { return rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 1
 
 struct tree_plan {
     int rw;
-    int32_t teams, least;
+    int32_t teams, least, few;
     int32_t blocks;
     size_t part_o, part_ml, ends, bytes;
 };
@@ -940,6 +996,7 @@ tree_plan plan_tree(const kv_view* view, int batch, int max_ctx_len, int max_q_l
     p.part_o = records * view->geom.head_dim * 4;
     p.part_ml = records * 8;
     p.blocks = (int32_t)blocks;
+    p.few = batch <= 64 && blocks * batch * tiles < 0x7fffffff;
     p.ends = (size_t)batch * blocks * view->n_kv_local * 8;
     p.bytes = p.part_o + p.part_ml + p.ends;
     return p;
@@ -995,6 +1052,7 @@ int common_args(tree_args& a, const void* q, void* out, const void* kv_pool, int
     a.last_block = (uint32_t)(n_pool_blocks - 1);
     a.scale_log2e = (scale > 0.f ? scale : 1.0f / sqrtf((float)d)) * 1.4426950408889634f;
     a.group = view->group;
+    while ((1 << a.group_shift) < a.group) ++a.group_shift;
     a.batch = batch;
     a.max_ctx_len = max_ctx_len;
     return KV_OK;
@@ -1032,8 +1090,10 @@ extern "C" int paged_tree_attn(const void* q, void* out, const void* kv_pool, in
     a.q_off = q_offsets;
     a.mask = (const unsigned long long*)tree_mask;
     a.mask_words = (int32_t)mask_words;
+    a.max_q_len = max_q_len;
     a.teams = p.teams;
     a.least_tiles = p.least;
+    a.few = p.few;
     a.part_o = (float*)workspace;
     a.part_ml = a.part_o + p.part_o / 4;
     a.ends = (int2*)(a.part_ml + p.part_ml / 4);
@@ -1073,6 +1133,7 @@ extern "C" int paged_decode_attn_weights(const void* q, void* out, const void* k
     }
     a.teams = p.teams;
     a.least_tiles = p.least;
+    a.few = p.few;
     a.score_stride = score_stride(max_ctx_len);
     a.scores = (float*)workspace;   // (its rows are read and written 16 bytes at a time)
     a.part_o = a.scores + rows * a.score_stride;
