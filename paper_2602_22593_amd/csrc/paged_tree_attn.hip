@@ -205,19 +205,36 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
     seq_work lane_work = {0, 0, 0, 0, 0};
     if (few) {
         if (lane < a.batch) lane_work = work_of<RB>(a, lane);
-        const int here = lane_work.tiles * lane_work.blocks;
-        int incl = here;
+        auto inclusive = [&](int x) {
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int y = __shfl_up(incl, d);
-            incl += lane >= d ? y : 0;
+            for (int d = 1; d < 64; d <<= 1) {
+                const int y = __shfl_up(x, d);
+                x += lane >= d ? y : 0;
+            }
+            return x;
+        };
+        // Where there are teams enough for shares of the least length that each end with their pair, a team has one piece: what a
+        // workgroup does before its first tile and after its last counts for more there than even shares
+        const int each = (lane_work.tiles + a.least_tiles - 1) / a.least_tiles, units = each * lane_work.blocks;
+        int incl = inclusive(units);
+        if (__builtin_amdgcn_readlane(incl, 63) <= a.teams) {
+            if (team >= __builtin_amdgcn_readlane(incl, 63)) return;
+            s = __builtin_popcountll(__builtin_amdgcn_ballot_w64(incl <= team));
+            const int unit = team - __builtin_amdgcn_readlane(incl - units, s), e = __builtin_amdgcn_readlane(each, s);
+            const int tiles = __builtin_amdgcn_readlane(lane_work.tiles, s), at = (unit % e) * a.least_tiles;
+            offset = (int64_t)(unit / e) * tiles + at;
+            from = 0;
+            to = min(a.least_tiles, tiles - at);
+        } else {
+            const int here = lane_work.tiles * lane_work.blocks;
+            incl = inclusive(here);
+            const int total = __builtin_amdgcn_readlane(incl, 63);
+            const int64_t share = share_of(a, total);
+            from = team * share;
+            to = min(from + share, (int64_t)total);
+            s = min(__builtin_popcountll(__builtin_amdgcn_ballot_w64(incl <= from)), 63);
+            offset = from - __builtin_amdgcn_readlane(incl - here, s);
         }
-        const int total = __builtin_amdgcn_readlane(incl, 63);
-        const int64_t share = share_of(a, total);
-        from = team * share;
-        to = min(from + share, (int64_t)total);
-        s = min(__builtin_popcountll(__builtin_amdgcn_ballot_w64(incl <= from)), 63);
-        offset = from - __builtin_amdgcn_readlane(incl - here, s);
     } else {
         find_share<NT, RB>(a, team, s_sum, from, to, s, offset);
     }
@@ -989,7 +1006,7 @@ tree_plan plan_tree(const kv_view* view, int batch, int max_ctx_len, int max_q_l
     // Shorter shares cost more in pieces than they save (us per call with least tiles 4, 2, 1 / 8, 4, 4 / 16, 8, 4: 2 sequences of 512 to
     // 4096, up to 64 rows, 23.2 / 19.8 / 23.9; weights of 2 such sequences 23.4 / 19.3 / 26.2; 2 of 1000 to 2000, 256 rows, 33.8 / 27.5 / 27.4)
     p.least = p.rw == 1 ? 8 : 4;
-    const int64_t most = (blocks * batch * tiles + p.least - 1) / p.least;
+    const int64_t most = blocks * batch * ((tiles + p.least - 1) / p.least);
     const int fill = kCus * (p.rw == 2 || p.rw == 4 ? 2 : 1);   // workgroups that the chip holds
     p.teams = (int32_t)std::max<int64_t>(std::min<int64_t>(most, fill / view->n_kv_local), 1);
     const size_t records = (size_t)2 * p.teams * view->n_kv_local * rb;
