@@ -58,7 +58,7 @@ struct tree_args {
     int32_t few;              // up to 64 sequences, and their tiles are counted in 32 bits
     int32_t group_shift;      // log2 of the group rounded up to a power of two
     int32_t teams, least_tiles;   // shares that the axis of tiles is cut into, and the least tiles of a share
-    float* part_o;            // [2 teams n_kv_local][32 RW][D]: slot 2 w the first piece of workgroup w, 2 w + 1 its last
+    f32x4* part_o;            // [2 teams n_kv_local][RW][D / 8][64]: slot 2 w the first piece of workgroup w, 2 w + 1 its last
     float* part_ml;           // [2 teams n_kv_local][32 RW][2] (reference in exponent units, sum of weights)
     int2* ends;               // [batch][blocks][n_kv_local] of every pair: team of its first piece x 2 + whether that is the team's last, of its last
     int32_t most_blocks;      // row blocks of a sequence by the host's bound
@@ -734,9 +734,10 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
         if (real) {
             const int x0 = KW > 1 ? kg * XW : 0;
             if (cut) {
-                float* dst = a.part_o + ((int64_t)slot * RB + srow) * D + 4 * half;
+                // (as they lie in the registers: a store is 1 KiB in one place)
+                f32x4* dst = a.part_o + (((int64_t)slot * RW + rw) * NX + x0) * 64 + lane;
 #pragma unroll
-                for (int x = 0; x < XW; ++x) *reinterpret_cast<f32x4*>(dst + 8 * (x0 + x)) = acc[x];
+                for (int x = 0; x < XW; ++x) dst[x * 64] = acc[x];
                 if (kg == 0 && half == 0) *reinterpret_cast<float2*>(a.part_ml + ((int64_t)slot * RB + srow) * 2) = make_float2(m_all, l_all);
             } else {
                 const float inv = 1.0f / l_all;   // (0 where the row sees nothing: zeros then; NaN stays NaN)
@@ -761,9 +762,10 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
 }
 
 // The second launch adds up the pieces of cut pairs, whose slots follow from the shares,
-//   out[row] = sum_z o_z 2^(m_z - M) / sum_z l_z 2^(m_z - M),  M = max_z m_z,
-// D / 4 lanes a row.  What bounds it is the latency of the partials' loads, so several are requested at once.  Rows of
-// sequences without tokens are zeros.
+//   out[row] = sum_z o_z 2^(m_z - M) / sum_z l_z 2^(m_z - M),  M = max_z m_z.
+// A wavefront takes 32 rows and a quarter of the workgroup's columns as the main kernel's lanes held them.  What bounds it is one
+// trip to memory after another, so a lane's loads of several pieces are under way at once.  Rows of sequences without tokens are
+// zeros.
 struct piece_list {
     int rows, h, rb;          // rows of the pair
     int w0, w1;               // teams that hold its first and last piece
@@ -786,20 +788,27 @@ __device__ __forceinline__ piece_list pieces_of(const tree_args& a, const seq_wo
     p.heads = a.v.n_kv_local;
     return p;
 }
-// (m, l, acc) and the pieces z, z + step, .. below count added up: kBatch are requested at a time, the last one again past the end.
-template <int D, int RB>
-__device__ __forceinline__ void add_pieces(const tree_args& a, const piece_list& p, int row, int cg, int z, int step, float& m, float& l, f32x4& acc)
+constexpr int kGroups = 4;   // of four accumulator registers that a wavefront adds up
+
+// (m, l, acc) and the pieces z, z + step, .. added up: up to MOST are requested at a time, the last one again past the end.
+// Lane (col, half) has row 32 block + col, elements 8 (x0 + x) + 4 half ..
+template <int D, int RB, int MOST>
+__device__ __forceinline__ void add_pieces(const tree_args& a, const piece_list& p, int block, int x0, int z, int step, float& m, float& l,
+                                           f32x4 (&acc)[kGroups])
 {
-    const int count = p.count();
+    const int count = p.count(), lane = threadIdx.x & 63, row = min(32 * block + (lane & 31), p.rows - 1);
+    const int from = row - 32 * block + (lane & 32);   // (lanes past the last row repeat it)
     auto add = [&](auto batch) {
         constexpr int kBatch = decltype(batch)::value;
         float2 ml[kBatch];
-        f32x4 x[kBatch];
+        f32x4 y[kBatch][kGroups];
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
-            const int64_t at = p.slot(min(z + u * step, count - 1)) * RB + row;
-            ml[u] = *reinterpret_cast<const float2*>(a.part_ml + at * 2);
-            x[u] = *reinterpret_cast<const f32x4*>(a.part_o + at * D + 4 * cg);
+            const int64_t slot = p.slot(min(z + u * step, count - 1));
+            ml[u] = *reinterpret_cast<const float2*>(a.part_ml + (slot * RB + row) * 2);
+            const f32x4* src = a.part_o + ((slot * (RB / 32) + block) * (D / 8) + x0) * 64 + from;
+#pragma unroll
+            for (int x = 0; x < kGroups; ++x) y[u][x] = src[x * 64];
         }
         float mn = m;
 #pragma unroll
@@ -809,99 +818,113 @@ __device__ __forceinline__ void add_pieces(const tree_args& a, const piece_list&
         }
         const float keep = l != 0.f ? fast_exp2(m - mn) : 0.f;
         l *= keep;
-        acc *= keep;
+#pragma unroll
+        for (int x = 0; x < kGroups; ++x) acc[x] *= keep;
         m = mn;
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
             if (ml[u].y == 0.f) continue;
             const float f = fast_exp2(ml[u].x - mn);
             l += ml[u].y * f;
-            acc += x[u] * f;
+#pragma unroll
+            for (int x = 0; x < kGroups; ++x) acc[x] += y[u][x] * f;
         }
         z += kBatch * step;
     };
     while (z < count) {
-        const int left = (count - z + step - 1) / step;
-        if (left <= 2) add(std::integral_constant<int, 2>());
-        else if (left <= 4) add(std::integral_constant<int, 4>());
-        else add(std::integral_constant<int, 8>());
+        if (MOST == 2 || (count - z + step - 1) / step <= 2) add(std::integral_constant<int, 2>());
+        else add(std::integral_constant<int, MOST>());
     }
 }
-template <int D>
-__device__ __forceinline__ void store_row(const tree_args& a, const seq_work& w, int h, int rho, int cg, float l, const f32x4& acc)
+// N groups of a lane's row: zeros where it has seen nothing
+template <int D, int N>
+__device__ __forceinline__ void store_row(const tree_args& a, const seq_work& w, int h, int rho, int element, float l, const f32x4 (&acc)[N])
 {
     const float inv = 1.0f / l;
-    *reinterpret_cast<uint2*>(a.out + ((int64_t)(w.q0 + rho / a.group) * a.v.n_q_local + h * a.group + rho % a.group) * D + 4 * cg) =
-        l != 0.f ? make_uint2(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)) : make_uint2(0u, 0u);
+    uint16_t* dst = a.out + ((int64_t)(w.q0 + rho / a.group) * a.v.n_q_local + h * a.group + rho % a.group) * D + element;
+#pragma unroll
+    for (int x = 0; x < N; ++x)
+        *reinterpret_cast<uint2*>(dst + 8 * x) =
+            l != 0.f ? make_uint2(pack_bf16x2(acc[x][0] * inv, acc[x][1] * inv), pack_bf16x2(acc[x][2] * inv, acc[x][3] * inv)) : make_uint2(0u, 0u);
 }
-// A row's pieces shared among the groups of D / 4 lanes of a workgroup
-template <int D, int RB>
-__device__ __forceinline__ void add_row_together(const tree_args& a, const seq_work& w, const piece_list& p, int row, f32x4* s_acc, float2* s_ml)
+// One set of columns of 32 rows by the whole workgroup, whose wavefronts share the pieces out and add up in LDS
+struct merge_room {
+    f32x4 acc[4][kGroups][64];
+    float2 ml[4][64];
+};
+template <int D, int RB, int MOST>
+__device__ __forceinline__ void add_together(const tree_args& a, const seq_work& w, const piece_list& p, int block, int x0, merge_room& room)
 {
-    constexpr int kLanes = D / 4, kGroups = 256 / kLanes;
-    const int cg = threadIdx.x % kLanes, r = threadIdx.x / kLanes;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = 32 * block + (lane & 31);
     float m = kNegInf, l = 0.f;
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    add_pieces<D, RB>(a, p, row, cg, r, kGroups, m, l, acc);
+    f32x4 acc[kGroups] = {};
+    add_pieces<D, RB, MOST>(a, p, block, x0, wave, 4, m, l, acc);
     __syncthreads();
-    s_acc[threadIdx.x] = acc;
-    if (cg == 0) s_ml[r] = make_float2(m, l);
+#pragma unroll
+    for (int x = 0; x < kGroups; ++x) room.acc[wave][x][lane] = acc[x];
+    room.ml[wave][lane] = make_float2(m, l);
     __syncthreads();
-    if (r == 0) {
-        for (int z = 1; z < kGroups; ++z) {
-            const float2 ml = s_ml[z];
-            if (ml.y == 0.f) continue;
-            const float mn = fmaxf(m, ml.x), keep = l != 0.f ? fast_exp2(m - mn) : 0.f, f = fast_exp2(ml.x - mn);
-            l = l * keep + ml.y * f;
-            acc = acc * keep + s_acc[z * kLanes + cg] * f;
-            m = mn;
-        }
-        store_row<D>(a, w, p.h, p.rb * RB + row, cg, l, acc);
+    // wavefront x finishes group x
+    m = kNegInf;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) m = fmaxf(m, room.ml[k][lane].x);
+    l = 0.f;
+    f32x4 all[1] = {};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const float2 ml = room.ml[k][lane];
+        if (ml.y == 0.f) continue;
+        const float f = fast_exp2(ml.x - m);
+        l += ml.y * f;
+        all[0] += room.acc[k][wave][lane] * f;
     }
+    if (row < p.rows) store_row<D>(a, w, p.h, p.rb * RB + row, 8 * (x0 + wave) + 4 * (lane >> 5), l, all);
 }
 template <int D>
 __device__ __forceinline__ void zero_rows(const tree_args& a, const seq_work& w, int h)
 {
     constexpr int kLanes = D / 4, kRows = 256 / kLanes;
+    const f32x4 none[1] = {};
     for (int x = blockIdx.z * kRows + (int)threadIdx.x / kLanes; x < w.q_len * a.group; x += gridDim.z * kRows)
-        store_row<D>(a, w, h, x, (int)threadIdx.x % kLanes, 0.f, f32x4{0.f, 0.f, 0.f, 0.f});
+        store_row<D>(a, w, h, x, 4 * ((int)threadIdx.x % kLanes), 0.f, none);
 }
 
-// Block (s, pair of s, part): TOGETHER: row `part` by the whole workgroup (few rows with long lists); otherwise 1024 / D rows.
-template <int D, int RW, bool TOGETHER>
+// Block (s, pair of s, part): 32 rows (at D = 64: 64), or TOGETHER 32 rows and 32 of their columns, where lists are long and few.
+template <int D, int RB, bool TOGETHER>
 __global__ __launch_bounds__(256) void tree_merge_kernel(tree_args a)
 {
-    constexpr int RB = 32 * RW, kLanes = D / 4, kRows = 256 / kLanes;
-    __shared__ f32x4 s_acc[TOGETHER ? 256 : 1];
-    __shared__ float2 s_ml[kRows];
-    const int s = blockIdx.x, pair = blockIdx.y;
+    constexpr int kParts = D / 8 / kGroups, kBlocks = TOGETHER ? 1 : 4 / kParts;   // column sets of a row; blocks of rows of a workgroup
+    __shared__ merge_room room;   // (TOGETHER)
+    const int s = blockIdx.x, pair = blockIdx.y, lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
     const seq_work w = work_of<RB>(a, s);
     if (w.n <= 0 && w.q_len > 0 && pair < a.v.n_kv_local) zero_rows<D>(a, w, pair);
     if (pair >= min(w.blocks, a.most_blocks) * a.v.n_kv_local) return;
-    const int h = pair / w.blocks, rb = pair - h * w.blocks, row0 = (int)blockIdx.z * (TOGETHER ? 1 : kRows);
-    if (row0 >= w.q_len * a.group - rb * RB) return;
+    const int h = pair / w.blocks, rb = pair - h * w.blocks, part = blockIdx.z;
+    const int first_block = TOGETHER ? part / kParts : part * kBlocks;
+    if (32 * first_block >= w.q_len * a.group - rb * RB) return;
     const piece_list p = pieces_of<RB>(a, w, s, h, rb);
-    if (p.count() == 1 || row0 >= p.rows) return;   // written by the main kernel
+    if (p.count() == 1) return;   // written by the main kernel
     if constexpr (TOGETHER) {
-        add_row_together<D, RB>(a, w, p, row0, s_acc, s_ml);
+        add_together<D, RB, 4>(a, w, p, first_block, part % kParts * kGroups, room);
     } else {
-        const int cg = threadIdx.x % kLanes, row = row0 + (int)threadIdx.x / kLanes;
-        if (row >= p.rows) return;
+        const int block = first_block + wave / kParts, x0 = wave % kParts * kGroups, row = 32 * block + (lane & 31);
+        if (32 * block >= p.rows) return;
         float m = kNegInf, l = 0.f;
-        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-        add_pieces<D, RB>(a, p, row, cg, 0, 1, m, l, acc);
-        store_row<D>(a, w, h, rb * RB + row, cg, l, acc);
+        f32x4 acc[kGroups] = {};
+        add_pieces<D, RB, 4>(a, p, block, x0, 0, 1, m, l, acc);
+        if (row < p.rows) store_row<D>(a, w, h, rb * RB + row, 8 * x0 + 4 * (lane >> 5), l, acc);
     }
 }
 
 // Block (s, h, chunk of tokens): (M, L) of the pair's G rows, then sum_g 2^(score_g - M_g) / L_g to the chunk's tokens; the rows of a cut
 // pair are shared out over the chunks' workgroups.
-template <int D>
+// LONG: lists of more than eight pieces, which cost registers that hide more of the rest's latency where they are short.
+template <int D, bool LONG>
 __global__ __launch_bounds__(256) void weights_kernel(tree_args a)
 {
-    constexpr int RB = 32, kRows = 256 / (D / 4);
-    __shared__ f32x4 s_acc[256];
-    __shared__ float2 s_ml[kRows], s_row[4][32];
+    constexpr int RB = 32;
+    __shared__ merge_room room;
+    __shared__ float2 s_row[4][32];
     const int s = blockIdx.x, h = blockIdx.y, G = a.group, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     float* sums = a.sums + ((int64_t)s * a.v.n_kv_local + h) * a.sum_stride;
     const float* scores = a.scores + ((int64_t)s * a.v.n_q_local + h * G) * a.score_stride;
@@ -922,7 +945,7 @@ __global__ __launch_bounds__(256) void weights_kernel(tree_args a)
         zero_rows<D>(a, w, h);
         return;
     }
-    if ((int)blockIdx.z * a.chunk >= w.n && (int)blockIdx.z >= G) return;
+    if ((int)blockIdx.z * a.chunk >= w.n && (int)blockIdx.z >= D / 8 / kGroups) return;
     const piece_list p = pieces_of<RB>(a, w, s, h, 0);
     const bool cut = p.count() > 1;
     // lane l of a wavefront takes row l % Gp, Gp = G rounded up to a power of two, and every (256 / Gp)-th piece
@@ -982,7 +1005,7 @@ __global__ __launch_bounds__(256) void weights_kernel(tree_args a)
             if (t + c < end) sums[t + c] = t + c == w.n - 1 ? x[c] : prior[c] + x[c];   // (the newest token has no sum yet)
     }
     if (cut)
-        for (int row = blockIdx.z; row < G; row += gridDim.z) add_row_together<D, RB>(a, w, p, row, s_acc, s_ml);
+        for (int x = blockIdx.z; x < D / 8 / kGroups; x += gridDim.z) add_together<D, RB, LONG ? 4 : 2>(a, w, p, 0, x * kGroups, room);
 }
 
 // ---- host ------------------------------------------------------------------------------------------
@@ -1022,14 +1045,15 @@ tree_plan plan_tree(const kv_view* view, int batch, int max_ctx_len, int max_q_l
 template <int D, int RW>
 void launch(const tree_args& a, int64_t most_rows, hipStream_t st)
 {
-    constexpr int RB = 32 * RW, kRows = 1024 / D;
-    const unsigned pairs = (unsigned)(a.v.n_kv_local * ((most_rows + RB - 1) / RB)), rows = (unsigned)std::min<int64_t>(most_rows, RB);
+    constexpr int RB = 32 * RW, kParts = D / 8 / kGroups, kBlocks = 4 / kParts;
+    const unsigned pairs = (unsigned)(a.v.n_kv_local * ((most_rows + RB - 1) / RB));
+    const unsigned blocks = (unsigned)((std::min<int64_t>(most_rows, RB) + 31) / 32);
     hipLaunchKernelGGL((tree_kernel<D, RW, false>), dim3((unsigned)(a.teams * a.v.n_kv_local)), dim3(RW == 8 ? 512 : 256), 0, st, a);
-    // Few rows have long lists of pieces: a workgroup a row
-    if ((int64_t)a.batch * pairs * rows <= 4096)
-        hipLaunchKernelGGL((tree_merge_kernel<D, RW, true>), dim3((unsigned)a.batch, pairs, rows), dim3(256), 0, st, a);
+    // Few pairs have long lists of pieces
+    if ((int64_t)a.batch * pairs * blocks <= 256)
+        hipLaunchKernelGGL((tree_merge_kernel<D, RB, true>), dim3((unsigned)a.batch, pairs, blocks * kParts), dim3(256), 0, st, a);
     else
-        hipLaunchKernelGGL((tree_merge_kernel<D, RW, false>), dim3((unsigned)a.batch, pairs, (rows + kRows - 1) / kRows), dim3(256), 0, st, a);
+        hipLaunchKernelGGL((tree_merge_kernel<D, RB, false>), dim3((unsigned)a.batch, pairs, (blocks + kBlocks - 1) / kBlocks), dim3(256), 0, st, a);
 }
 template <int D>
 void launch_tree(int rw, const tree_args& a, int64_t most_rows, hipStream_t st)
@@ -1046,7 +1070,8 @@ void launch_weights(const tree_args& a, int64_t chunks, hipStream_t st)
 {
     const unsigned heads = (unsigned)a.v.n_kv_local;
     hipLaunchKernelGGL((tree_kernel<D, 1, true>), dim3((unsigned)a.teams * heads), dim3(256), 0, st, a);
-    hipLaunchKernelGGL((weights_kernel<D>), dim3((unsigned)a.batch, heads, (unsigned)chunks), dim3(256), 0, st, a);
+    if (a.teams > 8 * a.batch) hipLaunchKernelGGL((weights_kernel<D, true>), dim3((unsigned)a.batch, heads, (unsigned)chunks), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((weights_kernel<D, false>), dim3((unsigned)a.batch, heads, (unsigned)chunks), dim3(256), 0, st, a);
 }
 
 // The checks that both entry points make, and the arguments that they share.
@@ -1111,8 +1136,8 @@ extern "C" int paged_tree_attn(const void* q, void* out, const void* kv_pool, in
     a.teams = p.teams;
     a.least_tiles = p.least;
     a.few = p.few;
-    a.part_o = (float*)workspace;
-    a.part_ml = a.part_o + p.part_o / 4;
+    a.part_o = (f32x4*)workspace;
+    a.part_ml = (float*)workspace + p.part_o / 4;
     a.ends = (int2*)(a.part_ml + p.part_ml / 4);
     a.most_blocks = p.blocks;
     const int64_t rows = (int64_t)max_q_len * view->group;
@@ -1153,8 +1178,9 @@ extern "C" int paged_decode_attn_weights(const void* q, void* out, const void* k
     a.few = p.few;
     a.score_stride = score_stride(max_ctx_len);
     a.scores = (float*)workspace;   // (its rows are read and written 16 bytes at a time)
-    a.part_o = a.scores + rows * a.score_stride;
-    a.part_ml = a.part_o + p.part_o / 4;
+    float* const parts = a.scores + rows * a.score_stride;
+    a.part_o = (f32x4*)parts;
+    a.part_ml = parts + p.part_o / 4;
     a.row_ml = a.part_ml + p.part_ml / 4;
     a.ends = (int2*)(a.row_ml + 2 * rows);
     a.most_blocks = 1;
