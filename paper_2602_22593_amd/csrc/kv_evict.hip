@@ -115,8 +115,8 @@ constexpr int kDigits[3] = {11, 11, 10};
 constexpr int kBins = 2048;
 constexpr int kHeld = 8;                        // tokens a lane holds
 constexpr int kAlone = 1024 * kHeld, kPart = 512 * kHeld;
-constexpr int kAllBins = 2 * kBins + 2 * kBins + 2;   // first digit of both classes, second, third, number of protected tokens
-constexpr int kSecond = 2 * kBins, kThird = 3 * kBins, kProtected = 4 * kBins;
+constexpr int kAllBins = 4 * kBins + 16;   // first digit of both classes, second, third, number of protected tokens, lines
+constexpr int kSecond = 2 * kBins, kThird = 3 * kBins, kProtected = 4 * kBins, kLines = kProtected + 1;
 
 // Integers in the order of the weights; NaN below all, the two zeros alike.
 __device__ __forceinline__ uint32_t order_of(float w)
@@ -370,24 +370,59 @@ __global__ __launch_bounds__(256) void evict_clear_kernel(int32_t* bins, int64_t
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) bins[i] = 0;
 }
 
-// The line as far as the digits counted so far tell.
+// The line as far as the digits counted so far tell: what the launch before found, and one digit more, left for the next launch.
 template <int NT>
-__device__ __forceinline__ evict_line line_after(const evict_args& a, const evict_pair& p, int digits, int* s_part, int* s_pick)
+__device__ __forceinline__ evict_line next_line(const evict_args& a, const evict_pair& p, int digit, bool writes, int* s_part, int* s_pick)
 {
-    const int* bins = a.bins + p.sh * kAllBins;
-    const int shielded = bins[kProtected];
+    int* const bins = a.bins + p.sh * kAllBins;
+    int* const kept = bins + kLines;   // (divided, key, equals) after each digit
     evict_line line;
-    line.divided = shielded >= p.k ? 2 : 1;
-    line.key = 0;
-    line.equals = line.divided == 2 ? p.k : p.k - shielded;
-    if (line.equals == 0) return line;
-    for (int d = 0; d < digits; ++d) {
-        const int at = d == 0 ? (line.divided - 1) * kBins : d == 1 ? kSecond : kThird;
-        int bin;
-        pick_bin<NT>(bins + at, 1 << kDigits[d], line.equals, bin, s_part, s_pick);
-        line.key = line.key << kDigits[d] | (uint32_t)bin;
+    if (digit == 0) {
+        const int shielded = bins[kProtected];
+        line.divided = shielded >= p.k ? 2 : 1;
+        line.key = 0;
+        line.equals = line.divided == 2 ? p.k : p.k - shielded;
+    } else {
+        line.divided = kept[3 * (digit - 1)];
+        line.key = (uint32_t)kept[3 * (digit - 1) + 1];
+        line.equals = kept[3 * (digit - 1) + 2];
+    }
+    if (digit < 3) {
+        if (line.equals > 0) {
+            const int at = digit == 0 ? (line.divided - 1) * kBins : digit == 1 ? kSecond : kThird;
+            int bin;
+            pick_bin<NT>(bins + at, 1 << kDigits[digit], line.equals, bin, s_part, s_pick);
+            line.key = line.key << kDigits[digit] | (uint32_t)bin;
+        }
+        if (writes && threadIdx.x == 0) {
+            kept[3 * digit] = line.divided;
+            kept[3 * digit + 1] = (int)line.key;
+            kept[3 * digit + 2] = line.equals;
+        }
     }
     return line;
+}
+
+// Sums of six counts over the workgroup, in every thread.
+template <int NT>
+__device__ __forceinline__ void block_totals(int (&x)[6], int (*s_six)[6])
+{
+#pragma unroll
+    for (int q = 0; q < 6; ++q)
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) x[q] += __shfl_xor(x[q], d);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+        for (int q = 0; q < 6; ++q) s_six[threadIdx.x >> 6][q] = x[q];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < 6; ++q) {
+        x[q] = 0;
+#pragma unroll
+        for (int w = 0; w < NT / 64; ++w) x[q] += s_six[w][q];
+    }
 }
 
 template <int STEP>   // 0, 1, 2: counts that digit; 3: counts tokens over and on the line; 4: lists the moves
@@ -395,7 +430,7 @@ __global__ __launch_bounds__(512) void evict_part_kernel(evict_args a)
 {
     constexpr int NT = 512;
     __shared__ int s_bins[STEP == 0 ? 2 * kBins : STEP < 3 ? kBins : 1], s_part[NT / 64], s_pick[2], s_total[4];
-    __shared__ int s_counts[4][STEP == 4 ? NT / 64 * kHeld : 64];
+    __shared__ int s_counts[4][STEP == 4 ? NT / 64 * kHeld : 64], s_six[NT / 64][6];
     const int tid = threadIdx.x, part = blockIdx.x, base = part * kPart;
     const evict_pair p(a, blockIdx.z, blockIdx.y);
     if (STEP == 0 && part == 0 && blockIdx.y == 0 && tid == 0 && a.new_lens) a.new_lens[p.s] = p.k;
@@ -411,7 +446,7 @@ __global__ __launch_bounds__(512) void evict_part_kernel(evict_args a)
     if constexpr (STEP < 3) {
         evict_line line{1, 0, 1};
         if constexpr (STEP > 0) {
-            line = line_after<NT>(a, p, STEP, s_part, s_pick);
+            line = next_line<NT>(a, p, STEP - 1, part == 0, s_part, s_pick);
             if (line.equals == 0) return;
         }
         constexpr int kCounted = STEP == 0 ? 2 * kBins : 1 << kDigits[STEP];
@@ -433,41 +468,38 @@ __global__ __launch_bounds__(512) void evict_part_kernel(evict_args a)
         for (int b = tid; b < kCounted; b += NT)
             if (s_bins[b]) atomicAdd(&to[b], s_bins[b]);
     } else {
-        const evict_line line = line_after<NT>(a, p, 3, s_part, s_pick);
+        const evict_line line = next_line<NT>(a, p, STEP - 1, part == 0, s_part, s_pick);
         int4* counts = a.part_counts + p.sh * a.parts;
         if constexpr (STEP == 3) {
-            int c[4] = {0, 0, 0, 0};
+            int c[6] = {0, 0, 0, 0, 0, 0};
 #pragma unroll
             for (int i = 0; i < kHeld; ++i) {
-                const int high = base + NT * i + tid >= p.k ? 2 : 0;
-                c[high] += line.over(x.key[i], x.cls[i]);
-                c[high + 1] += line.on(x.key[i], x.cls[i]);
+                const int high = base + NT * i + tid >= p.k;
+                const int over = line.over(x.key[i], x.cls[i]), on = line.on(x.key[i], x.cls[i]);
+                c[0] += high ? 0 : over;
+                c[1] += high ? 0 : on;
+                c[2] += high ? over : 0;
+                c[3] += high ? on : 0;
             }
-#pragma unroll
-            for (int q = 0; q < 4; ++q) c[q] = block_total<NT>(c[q], s_part);
+            block_totals<NT>(c, s_six);
             if (tid == 0) counts[part] = make_int4(c[0], c[1], c[2], c[3]);
         } else {
-            int4 before = make_int4(0, 0, 0, 0), all = make_int4(0, 0, 0, 0);
+            int c[6] = {0, 0, 0, 0, 0, 0};   // before this part; over and on the line below slot k in all
             const int parts = (p.n + kPart - 1) / kPart;
             for (int q = tid; q < parts; q += NT) {
-                const int4 c = counts[q];
-                all.x += c.x;
-                all.y += c.y;
+                const int4 y = counts[q];
+                c[4] += y.x;
+                c[5] += y.y;
                 if (q < part) {
-                    before.x += c.x;
-                    before.y += c.y;
-                    before.z += c.z;
-                    before.w += c.w;
+                    c[0] += y.x;
+                    c[1] += y.y;
+                    c[2] += y.z;
+                    c[3] += y.w;
                 }
             }
-            before.x = block_total<NT>(before.x, s_part);
-            before.y = block_total<NT>(before.y, s_part);
-            before.z = block_total<NT>(before.z, s_part);
-            before.w = block_total<NT>(before.w, s_part);
-            all.x = block_total<NT>(all.x, s_part);
-            all.y = block_total<NT>(all.y, s_part);
-            if (part == 0 && tid == 0) a.counts[p.sh] = p.k - kept_low(line, all.x, all.y);
-            list_moves<NT>(a, p, line, x, base, before, all.y, false, s_counts, s_total);
+            block_totals<NT>(c, s_six);
+            if (part == 0 && tid == 0) a.counts[p.sh] = p.k - kept_low(line, c[4], c[5]);
+            list_moves<NT>(a, p, line, x, base, make_int4(c[0], c[1], c[2], c[3]), c[5], false, s_counts, s_total);
         }
     }
 }
