@@ -171,14 +171,14 @@ __device__ __forceinline__ void find_share(const tree_args& a, int team, int64_t
     __syncthreads();
 }
 
-// Bytes of the staging buffers of a key group, K or V
-template <int D> constexpr int tile_pieces() { return kKeys * D / 8; }
 
-template <int D, int RW, bool SUMS>
+template <int D, int RW, int HW, bool SUMS>
 __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args a)
 {
-    constexpr int NW = RW < 4 ? 4 : RW, KW = NW / RW, NT = 64 * NW, RB = 32 * RW;
-    constexpr int NJ = D / 32, NK = D / 16, kPieces = tile_pieces<D>(), kRow = 2 * D;
+    constexpr int NW = RW < 4 ? 4 : RW, KW = NW / (RW * HW), NT = 64 * NW, RB = 32 * RW;
+    constexpr int NJ = D / 32, NK = D / 16, kRow = 2 * D, kStride = HW * kRow;   // bytes of a token's row, and of the heads' rows in LDS
+    constexpr int kPieces = kKeys * kStride / 16;                                 // of a staged tile, K or V
+    constexpr bool kShared = RW * HW > 1;                                         // wavefronts share what is staged
     // K: piece c of row t at c ^ f(t), V: at c ^ g(t): operand reads without bank conflicts.  An array per buffer: the compiler
     // then knows that loads landing in one do not touch the operands read from another.
     constexpr int NB = RW >= 4 ? 4 : 2, kMore = NB > 2 ? KW * kPieces : 1;
@@ -188,16 +188,16 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
     auto v_buf = [&](int x) { return NB == 2 ? ((x & 1) ? s_v1 : s_v0) : (x & 2) ? ((x & 1) ? s_v3 : s_v2) : ((x & 1) ? s_v1 : s_v0); };
     __shared__ float2 s_ml[KW > 1 ? NW * 32 : 1];
     __shared__ uint32_t s_seen[SUMS ? 1 : kEdgeTiles][SUMS ? 1 : RB];   // which tokens of the tiles that hold drafted ones a row sees
-    __shared__ f32x4 s_out[SUMS ? KW : 1][SUMS ? 32 : 1][8];   // scores on their way out
+    __shared__ f32x4 s_out[SUMS ? NW : 1][SUMS ? 32 : 1][8];   // scores on their way out
     __shared__ int64_t s_sum[NW];
 
     const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
-    const int rw = wave % RW, kg = wave / RW;   // the wavefront's rows and tiles
+    const int rw = wave % RW, kg = wave / RW % KW, hw = wave / (RW * KW);   // the wavefront's rows, tiles and head
     const int col = lane & 31, half = lane >> 5;
     const kv_view_dev& v = a.v;
     const int G = a.group, Hl = v.n_kv_local;
 
-    const int team = (int)blockIdx.x / Hl, h = (int)blockIdx.x - team * Hl;
+    const int sets = Hl / HW, team = (int)blockIdx.x / sets, h0 = ((int)blockIdx.x - team * sets) * HW, h = h0 + hw;
     int64_t from, to, offset;
     int s;
     // Up to 64 sequences a wavefront holds in its lanes and finds its share by itself: one trip to memory, no barriers
@@ -252,25 +252,28 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
     // such parts of K and of V (at D = 64 under RW = 8 the lower four wavefronts K, the others V)
     constexpr bool kSplitPlanes = NK < RW;
     constexpr int NP = kSplitPlanes ? 1 : NK / RW;
-    constexpr int kRowsEach = 512 / D;
-    const int first_part = kSplitPlanes ? (rw & (NK - 1)) : rw * NP;
+    constexpr int kTokenPieces = kStride / 16, kRowsEach = 64 / kTokenPieces;
+    const int first_part = kSplitPlanes ? (rw & (NK - 1)) : (hw * RW + rw) * NP;
+    // (rows of 128 bytes fill half the banks: with four heads side by side odd tokens have the heads of a pair exchanged)
+    auto head_place = [](int head, int token) { return D == 64 && HW > 1 ? head ^ (token & 1) : head; };
     uint32_t k_lane[NP], v_lane[NP];
-    const int row_first = (first_part * kRowsEach & 15) + lane / (D / 8);   // within a group, of the first part
+    const int row_first = (first_part * kRowsEach & 15) + lane / kTokenPieces;   // within a group, of the first part
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-        const int row = ((first_part + i) * kRowsEach + lane / (D / 8)) & 15, c = lane & (D / 8 - 1);
+        const int row = ((first_part + i) * kRowsEach + lane / kTokenPieces) & 15, c = lane & (D / 8 - 1);
+        const int head = head_place(lane % kTokenPieces / (D / 8), row) * (D / 8);
         const int kc = D == 128 ? c ^ row : c ^ (row >> 1), vc = D == 128 ? c ^ (4 * (row & 3)) : c ^ (4 * ((row >> 1) & 1));
-        k_lane[i] = (uint32_t)(row * (int)stride_bytes + (kc << 4));
-        v_lane[i] = (uint32_t)(row * (int)stride_bytes + (vc << 4));
+        k_lane[i] = (uint32_t)(row * (int)stride_bytes + ((head + kc) << 4));
+        v_lane[i] = (uint32_t)(row * (int)stride_bytes + ((head + vc) << 4));
     }
     uint32_t k_off, v_off[NJ];
     {
         const int p = lane & 15, sub = (lane >> 4) & 1;
-        k_off = (uint32_t)(kg * kPieces * 16 + col * kRow + ((half ^ (D == 128 ? (col & 15) : ((col >> 1) & 7))) << 4));
+        k_off = (uint32_t)(kg * kPieces * 16 + col * kStride + head_place(hw, col) * kRow + ((half ^ (D == 128 ? (col & 15) : ((col >> 1) & 7))) << 4));
         const int vrow = 4 * half + (p >> 2), g = D == 128 ? 4 * (vrow & 3) : 4 * ((vrow >> 1) & 1);
 #pragma unroll
         for (int j = 0; j < NJ; ++j)
-            v_off[j] = (uint32_t)(kg * kPieces * 16 + vrow * kRow + (((4 * j + 2 * sub + ((p & 3) >> 1)) ^ g) << 4) + (p & 1) * 8);
+            v_off[j] = (uint32_t)(kg * kPieces * 16 + vrow * kStride + head_place(hw, vrow) * kRow + (((4 * j + 2 * sub + ((p & 3) >> 1)) ^ g) << 4) + (p & 1) * 8);
     }
 
     for (int64_t at = from; at < to;) {
@@ -294,7 +297,7 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
 
         // where the groups of 16 tokens lie: lane l knows that of group l % 2 of this wavefront's tile 32 window + l / 2
         const int32_t* ids = a.table + (int64_t)s * a.table_stride;
-        const char* pool_head = reinterpret_cast<const char*>(a.pool + v.head_off + h * D);
+        const char* pool_head = reinterpret_cast<const char*>(a.pool + v.head_off + h0 * D);
         auto group_at = [&](int window) { return min(2 * (kt0 + 32 * window + (lane >> 1)) + (lane & 1), last_group); };
         auto request_ids = [&](int window) { return (uint32_t)ids[group_at(window) / groups_per_block]; };
         auto places = [&](uint32_t id, int window) {
@@ -356,7 +359,7 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
         auto staged = [&](auto under_way) {   // but for the last so many
             constexpr int kLeft = decltype(under_way)::value;
             __builtin_amdgcn_s_waitcnt(0x0f70 | (kLeft & 15) | (kLeft >> 4) << 14);   // vmcnt
-            if constexpr (RW > 1) __syncthreads();
+            if constexpr (kShared) __syncthreads();
             else asm volatile("" ::: "memory");
         };
 #pragma unroll
@@ -420,9 +423,9 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
             return as_bf16x8(*reinterpret_cast<const kv_u32x4*>(reinterpret_cast<const char*>(sk) + off));
         };
         auto v_operand = [&](const kv_u32x4* sv, int u) {   // u = NJ c + j
-            const char* const p = reinterpret_cast<const char*>(sv) + v_off[u % NJ] + (u / NJ) * 16 * kRow;
+            const char* const p = reinterpret_cast<const char*>(sv) + v_off[u % NJ] + (u / NJ) * 16 * kStride;
             const bits16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_bits16x4_ptr)p);
-            const bits16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_bits16x4_ptr)(p + 8 * kRow));
+            const bits16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_bits16x4_ptr)(p + 8 * kStride));
             return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
         };
         f32x16 sc, ex;    // scores of a tile, then exponents: score scale log2(e) - reference
@@ -449,7 +452,7 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
                 if (real) {
 #pragma unroll
                     for (int u = 0; u < 4; ++u)
-                        s_out[kg][(slot << a.group_shift) + col][2 * u + half] =
+                        s_out[wave][(slot << a.group_shift) + col][2 * u + half] =
                             f32x4{sc[4 * u] * a.scale_log2e, sc[4 * u + 1] * a.scale_log2e, sc[4 * u + 2] * a.scale_log2e, sc[4 * u + 3] * a.scale_log2e};
                 }
                 if (slot < slots - 1 && i < mine - 1) return false;
@@ -458,7 +461,7 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
                 for (int r0 = 0; r0 < 32; r0 += 8) {
                     const int r = r0 + (lane >> 3), x = r >> a.group_shift, g = r & ((1 << a.group_shift) - 1);
                     if (x <= slot && g < G)
-                        *reinterpret_cast<f32x4*>(dst + g * a.score_stride + kKeys * (kt0 + i - slot + x) + 4 * (lane & 7)) = s_out[kg][r][lane & 7];
+                        *reinterpret_cast<f32x4*>(dst + g * a.score_stride + kKeys * (kt0 + i - slot + x) + 4 * (lane & 7)) = s_out[wave][r][lane & 7];
                 }
                 return slot == slots - 1;
             }
@@ -525,7 +528,7 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
                 for (int x = 1; x < 8; ++x) two = u == x ? pw[x] : two;
                 two = (uint32_t)__shfl((int)two, col + 32 * ((t >> 2) & 1));
                 const float wt = (t & 1) ? bf16_hi(two) : bf16_lo(two);
-                const char* row = reinterpret_cast<const char*>(sv + kg * kPieces) + t * kRow;
+                const char* row = reinterpret_cast<const char*>(sv + kg * kPieces) + t * kStride + head_place(hw, t) * kRow;
                 const int g = D == 128 ? 4 * (t & 3) : 4 * ((t >> 1) & 1);
 #pragma unroll
                 for (int j = 0; j < NJ; ++j)
@@ -629,7 +632,7 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
                 first_reference();
                 exponents();
             }
-            if constexpr (RW > 1) __syncthreads();   // (K of tile 0 is read, its buffer may be filled again)
+            if constexpr (kShared) __syncthreads();   // (K of tile 0 is read, its buffer may be filled again)
             for (; i + NB < common; i += NB) {
                 step(std::integral_constant<int, 0>(), i);
                 step(std::integral_constant<int, 1>(), i + 1);
@@ -686,7 +689,7 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
 
         // ---- the piece's rows ----------------------------------------------------------------------
         l = half_sum(l);
-        const int slot = 2 * (int)blockIdx.x + (at > from ? 1 : 0);
+        const int slot = 2 * (team * Hl + h) + (at > from ? 1 : 0);
         // groups of four accumulator registers: x = 4 j + u4 holds elements 8 x + 4 half ..
         constexpr int NX = 4 * NJ, XW = NX / KW;   // each of the KW wavefronts of a row finishes XW of them
         f32x4 acc[XW];
@@ -729,7 +732,7 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
 #pragma unroll
             for (int x = 0; x < XW; ++x) acc[x] = f32x4{o[x >> 2][4 * (x & 3)], o[x >> 2][4 * (x & 3) + 1],
                                                         o[x >> 2][4 * (x & 3) + 2], o[x >> 2][4 * (x & 3) + 3]};
-            if constexpr (RW > 1) __syncthreads();
+            if constexpr (kShared) __syncthreads();
         }
         if (real) {
             const int x0 = KW > 1 ? kg * XW : 0;
@@ -751,7 +754,7 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
                     *reinterpret_cast<float2*>(a.row_ml + ((int64_t)s * v.n_q_local + h * G + rho % G) * 2) = make_float2(m_all, l_all);
             }
         }
-        if (threadIdx.x == 0 && rb < a.most_blocks) {
+        if (lane == 0 && rw == 0 && kg == 0 && rb < a.most_blocks) {
             int2* ends = a.ends + ((int64_t)s * a.most_blocks + rb) * Hl + h;
             if (t0 == 0) ends->x = 2 * team + (at > from ? 1 : 0);
             if (t0 + count == w.tiles) ends->y = team;
@@ -1010,11 +1013,13 @@ __global__ __launch_bounds__(256) void weights_kernel(tree_args a)
 
 // ---- host ------------------------------------------------------------------------------------------
 
+constexpr int64_t kWideBytes = 100000000;   // of K and V by the bound
+
 // Wavefronts that share a tile, by the bound on a pair's rows
 int row_waves(int64_t rows) { return rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 ? 4 : 8; }
 
 struct tree_plan {
-    int rw;
+    int rw, hw;   // wavefronts that share a tile's rows; heads of a workgroup
     int32_t teams, least, few;
     int32_t blocks;
     size_t part_o, part_ml, ends, bytes;
@@ -1025,12 +1030,13 @@ tree_plan plan_tree(const kv_view* view, int batch, int max_ctx_len, int max_q_l
     const int64_t rows = (int64_t)max_q_len * view->group;
     p.rw = row_waves(rows);
     const int rb = 32 * p.rw;
+    p.hw = p.rw == 1 && view->n_kv_local % 4 == 0 && (int64_t)batch * max_ctx_len * view->n_kv_local * view->geom.head_dim * 4 >= kWideBytes ? 4 : 1;
     const int64_t blocks = (rows + rb - 1) / rb, tiles = ((int64_t)max_ctx_len + kKeys - 1) / kKeys;
     // Shorter shares cost more in pieces than they save (us per call with least tiles 4, 2, 1 / 8, 4, 4 / 16, 8, 4: 2 sequences of 512 to
     // 4096, up to 64 rows, 23.2 / 19.8 / 23.9; weights of 2 such sequences 23.4 / 19.3 / 26.2; 2 of 1000 to 2000, 256 rows, 33.8 / 27.5 / 27.4)
     p.least = p.rw == 1 ? 8 : 4;
     const int64_t most = blocks * batch * ((tiles + p.least - 1) / p.least);
-    const int fill = kCus * (p.rw == 2 || p.rw == 4 ? 2 : 1);   // workgroups that the chip holds
+    const int fill = kCus * (p.rw == 2 || p.rw == 4 ? 2 : 1) * p.hw;   // heads that the chip holds workgroups for
     p.teams = (int32_t)std::max<int64_t>(std::min<int64_t>(most, fill / view->n_kv_local), 1);
     const size_t records = (size_t)2 * p.teams * view->n_kv_local * rb;
     p.part_o = records * view->geom.head_dim * 4;
@@ -1042,13 +1048,13 @@ tree_plan plan_tree(const kv_view* view, int batch, int max_ctx_len, int max_q_l
     return p;
 }
 
-template <int D, int RW>
+template <int D, int RW, int HW>
 void launch(const tree_args& a, int64_t most_rows, hipStream_t st)
 {
     constexpr int RB = 32 * RW, kParts = D / 8 / kGroups, kBlocks = 4 / kParts;
     const unsigned pairs = (unsigned)(a.v.n_kv_local * ((most_rows + RB - 1) / RB));
     const unsigned blocks = (unsigned)((std::min<int64_t>(most_rows, RB) + 31) / 32);
-    hipLaunchKernelGGL((tree_kernel<D, RW, false>), dim3((unsigned)(a.teams * a.v.n_kv_local)), dim3(RW == 8 ? 512 : 256), 0, st, a);
+    hipLaunchKernelGGL((tree_kernel<D, RW, HW, false>), dim3((unsigned)(a.teams * (a.v.n_kv_local / HW))), dim3(RW == 8 ? 512 : 256), 0, st, a);
     // Few pairs have long lists of pieces
     if ((int64_t)a.batch * pairs * blocks <= 256)
         hipLaunchKernelGGL((tree_merge_kernel<D, RB, true>), dim3((unsigned)a.batch, pairs, blocks * kParts), dim3(256), 0, st, a);
@@ -1056,20 +1062,21 @@ void launch(const tree_args& a, int64_t most_rows, hipStream_t st)
         hipLaunchKernelGGL((tree_merge_kernel<D, RB, false>), dim3((unsigned)a.batch, pairs, (blocks + kBlocks - 1) / kBlocks), dim3(256), 0, st, a);
 }
 template <int D>
-void launch_tree(int rw, const tree_args& a, int64_t most_rows, hipStream_t st)
+void launch_tree(const tree_plan& p, const tree_args& a, int64_t most_rows, hipStream_t st)
 {
-    switch (rw) {
-        case 1: launch<D, 1>(a, most_rows, st); break;
-        case 2: launch<D, 2>(a, most_rows, st); break;
-        case 4: launch<D, 4>(a, most_rows, st); break;
-        default: launch<D, 8>(a, most_rows, st); break;
+    switch (p.rw) {
+        case 1: p.hw == 4 ? launch<D, 1, 4>(a, most_rows, st) : launch<D, 1, 1>(a, most_rows, st); break;
+        case 2: launch<D, 2, 1>(a, most_rows, st); break;
+        case 4: launch<D, 4, 1>(a, most_rows, st); break;
+        default: launch<D, 8, 1>(a, most_rows, st); break;
     }
 }
 template <int D>
-void launch_weights(const tree_args& a, int64_t chunks, hipStream_t st)
+void launch_weights(const tree_plan& p, const tree_args& a, int64_t chunks, hipStream_t st)
 {
     const unsigned heads = (unsigned)a.v.n_kv_local;
-    hipLaunchKernelGGL((tree_kernel<D, 1, true>), dim3((unsigned)a.teams * heads), dim3(256), 0, st, a);
+    if (p.hw == 4) hipLaunchKernelGGL((tree_kernel<D, 1, 4, true>), dim3((unsigned)a.teams * heads / 4), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((tree_kernel<D, 1, 1, true>), dim3((unsigned)a.teams * heads), dim3(256), 0, st, a);
     if (a.teams > 8 * a.batch) hipLaunchKernelGGL((weights_kernel<D, true>), dim3((unsigned)a.batch, heads, (unsigned)chunks), dim3(256), 0, st, a);
     else hipLaunchKernelGGL((weights_kernel<D, false>), dim3((unsigned)a.batch, heads, (unsigned)chunks), dim3(256), 0, st, a);
 }
@@ -1143,8 +1150,8 @@ extern "C" int paged_tree_attn(const void* q, void* out, const void* kv_pool, in
     const int64_t rows = (int64_t)max_q_len * view->group;
     if ((rows + 31) / 32 * view->n_kv_local > 65535) return KV_ERR_UNSUPPORTED;
     hipStream_t st = (hipStream_t)hip_stream;
-    if (view->geom.head_dim == 128) launch_tree<128>(p.rw, a, rows, st);
-    else launch_tree<64>(p.rw, a, rows, st);
+    if (view->geom.head_dim == 128) launch_tree<128>(p, a, rows, st);
+    else launch_tree<64>(p, a, rows, st);
     return kv_record_hip_error(hipGetLastError(), "paged_tree_attn launch");
 }
 
@@ -1192,7 +1199,7 @@ extern "C" int paged_decode_attn_weights(const void* q, void* out, const void* k
     const int64_t chunks = chunks_of(a.chunk);
     if (chunks > 65535 || view->n_kv_local > 65535) return KV_ERR_UNSUPPORTED;
     hipStream_t st = (hipStream_t)hip_stream;
-    if (view->geom.head_dim == 128) launch_weights<128>(a, chunks, st);
-    else launch_weights<64>(a, chunks, st);
+    if (view->geom.head_dim == 128) launch_weights<128>(p, a, chunks, st);
+    else launch_weights<64>(p, a, chunks, st);
     return kv_record_hip_error(hipGetLastError(), "paged_decode_attn_weights launch");
 }

@@ -216,6 +216,32 @@ def test_tree_bounds_larger_than_needed_and_rows_behind():
     assert (out[14:] == 7.0).all()
 
 
+@pytest.mark.parametrize("geom,triple,ctx,q_lens", [
+    (G8B, (DP, 1, 0), [40, 31, 32, 33, 700, 1, 64], [8, 1, 2, 3, 4, 1, 8]),    # four heads a workgroup, 1 KiB a token
+    (G8B, (TP, 2, 1), [900, 64, 15, 5], [8, 1, 7, 5]),
+    (G8B, (DP, 2, 1), [300, 77], [3, 8]),                                     # the rank's half of a row
+    ((16, 4, 64, 16), (DP, 1, 0), [500, 33, 8, 1000], [8, 1, 8, 2]),            # rows of 128 bytes
+    ((24, 12, 64, 32), (TP, 3, 2), [130, 31], [16, 15]),
+    (G8B, (DP, 1, 0), [5000], [8]),
+])
+def test_tree_and_weights_of_heads_side_by_side(geom, triple, ctx, q_lens):
+    """Bounds of a large batch, for which several heads of a token are read together."""
+    c = ref.case(geom, triple, ctx, q_lens)
+    bound = 150000
+    table = np.pad(c.table, ((0, 0), (0, -(-bound // c.info["block_tokens"]) - c.table.shape[1])), constant_values=-1)
+    seen, words = ref.tree_masks(c.q_lens, np.random.default_rng(16))
+    want, tol = ref.tree_attention(c, seen)
+    off, view = c.q_off.astype(np.int32), view_of(c)
+    got = kv.paged_tree_attn(dev(c.q), dev(c.pool), dev(table), dev(c.ctx), dev(off), dev(words), view, bound, max(q_lens))
+    within(host(got), want, tol)
+    c.q = wl.randn_bf16((len(ctx), c.info["n_q_local"], geom[2]), wl.generator(61, wl.SUB_QUERY))
+    prior = np.random.default_rng(17).exponential(1e-3, (len(ctx), c.info["n_kv_local"], bound)).astype(np.float32)
+    want, tol, sums, sums_tol = ref.decode_weights(c, prior)
+    weights = dev(prior)
+    within(host(kv.paged_decode_attn_weights(dev(c.q), dev(c.pool), dev(table), dev(c.ctx), view, bound, weights)), want, tol)
+    assert (np.abs(host(weights).astype(np.float64) - sums) <= sums_tol).all()
+
+
 # ---- kv_accept ---------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("geom,triple,ctx,q_lens,counts", [
