@@ -1013,7 +1013,11 @@ __global__ __launch_bounds__(256) void weights_kernel(tree_args a)
 
 // ---- host ------------------------------------------------------------------------------------------
 
-constexpr int64_t kWideBytes = 100000000;   // of K and V by the bound
+// Several heads to a workgroup, by the bytes of K and V by the bound: below, more and shorter pieces cost more than rows of 512 and 1024
+// bytes bring.  us per call, one head / several: 8 heads, drafts of up to 8, 4 sequences of 512 to 4096 21.3 / 23.1, 8 of them
+// 28.7 / 26.0, 32 71.6 / 64.8, 128 239 / 228; 4 heads, 128 sequences 128 / 120; 64 of 100 to 1000 36.4 / 27.5; drafts of up to 16
+// (two heads) 128 sequences 269 / 251.  Two heads of 128 rows are slower (290 / 302).
+constexpr int64_t kWideBytes = 100000000;
 
 // Wavefronts that share a tile, by the bound on a pair's rows
 int row_waves(int64_t rows) { return rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 ? 4 : 8; }
@@ -1030,7 +1034,8 @@ tree_plan plan_tree(const kv_view* view, int batch, int max_ctx_len, int max_q_l
     const int64_t rows = (int64_t)max_q_len * view->group;
     p.rw = row_waves(rows);
     const int rb = 32 * p.rw;
-    p.hw = p.rw == 1 && view->n_kv_local % 4 == 0 && (int64_t)batch * max_ctx_len * view->n_kv_local * view->geom.head_dim * 4 >= kWideBytes ? 4 : 1;
+    const bool wide = (int64_t)batch * max_ctx_len * view->n_kv_local * view->geom.head_dim * 4 >= kWideBytes;
+    p.hw = !wide ? 1 : p.rw == 1 && view->n_kv_local % 4 == 0 ? 4 : p.rw == 2 && view->n_kv_local % 2 == 0 ? 2 : 1;
     const int64_t blocks = (rows + rb - 1) / rb, tiles = ((int64_t)max_ctx_len + kKeys - 1) / kKeys;
     // Shorter shares cost more in pieces than they save (us per call with least tiles 4, 2, 1 / 8, 4, 4 / 16, 8, 4: 2 sequences of 512 to
     // 4096, up to 64 rows, 23.2 / 19.8 / 23.9; weights of 2 such sequences 23.4 / 19.3 / 26.2; 2 of 1000 to 2000, 256 rows, 33.8 / 27.5 / 27.4)
@@ -1066,7 +1071,7 @@ void launch_tree(const tree_plan& p, const tree_args& a, int64_t most_rows, hipS
 {
     switch (p.rw) {
         case 1: p.hw == 4 ? launch<D, 1, 4>(a, most_rows, st) : launch<D, 1, 1>(a, most_rows, st); break;
-        case 2: launch<D, 2, 1>(a, most_rows, st); break;
+        case 2: p.hw == 2 ? launch<D, 2, 2>(a, most_rows, st) : launch<D, 2, 1>(a, most_rows, st); break;
         case 4: launch<D, 4, 1>(a, most_rows, st); break;
         default: launch<D, 8, 1>(a, most_rows, st); break;
     }
