@@ -384,10 +384,12 @@ int paged_tree_attn(const void* q, void* out, const void* kv_pool, int64_t n_poo
  * token ctx_lens[s] - q_len[s] + i of the sequence, for all heads of the view, so that the accepted
  * tokens follow the cache in order.  What lies behind them is left as it is.
  *   accepted       device, int32 [batch][accepted_stride]: numbers of drafted tokens, each row strictly
- *                  ascending, in [0, q_len[s]); entries that are not are skipped
+ *                  ascending, in [0, q_len[s]).  An entry below its own index (in an ascending row there is
+ *                  none) or not below q_len[s] moves nothing
  *   n_accepted     device, int32 [batch], at most accepted_stride and q_len[s] (more counts as that)
  *   new_lens       device, int32 [batch], written: ctx_lens[s] - q_len[s] + n_accepted[s]; may be null,
  *                  must not be ctx_lens
+ * No block may belong to two sequences of the call, unless nothing in it moves.
  * Errors: KV_ERR_INVALID_ARG, KV_ERR_HIP.
  */
 int kv_accept(void* kv_pool, int64_t n_pool_blocks, const kv_view* view, const int32_t* block_table,
@@ -432,6 +434,8 @@ int paged_decode_attn_weights(const void* q, void* out, const void* kv_pool, int
  *   new_lens       device, int32 [batch], written: k; may be null, must not be ctx_lens or keep_lens
  *   workspace      at least kv_evict_workspace_bytes(...) bytes, 256-byte aligned; contents need not be
  *                  initialised
+ * No block may belong to two sequences of the call, unless nothing in it moves (a prompt that several share is
+ * copied first).  A row whose block lies outside the pool is not moved.
  * Errors: KV_ERR_INVALID_ARG (null pointers, negative sizes, strides too small), KV_ERR_UNSUPPORTED (max_ctx_len
  * above 2^24), KV_ERR_WORKSPACE, KV_ERR_HIP.
  */

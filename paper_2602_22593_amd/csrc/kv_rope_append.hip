@@ -84,7 +84,7 @@ __global__ __launch_bounds__(kThreads) void kv_rope_append_kernel(rope_args a)
             if (t >= 0 && b < a.table_stride) {
                 const int32_t id = a.table[(int64_t)s * a.table_stride + b];
                 if (id >= 0 && id < a.n_pool_blocks) place = (int64_t)id * v.block_elems + (int64_t)slot * v.token_stride + v.head_off;
-                if (a.token_pos && t < a.token_pos_stride)
+                if (place >= 0 && a.token_pos && t < a.token_pos_stride)
                     for (int h = lane; h < v.n_kv_local; h += 64)
                         a.token_pos[((int64_t)s * v.n_kv_local + h) * a.token_pos_stride + t] = a.positions[i];
             }
