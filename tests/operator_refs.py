@@ -33,7 +33,8 @@ def place(c, s, t):
 def heads_of(c, s):
     """K and V of the exposed heads of sequence s in float64, [tokens][heads][d]."""
     h0, hl = c.info["kv_head0"], c.info["n_kv_local"]
-    a, b = int(c.seq_off[s]), int(c.seq_off[s + 1])
+    a = int(c.seq_off[s])
+    b = a + int(c.ctx[s])
     return bf16_bits_to_f64(c.K[a:b, h0:h0 + hl]), bf16_bits_to_f64(c.V[a:b, h0:h0 + hl])
 
 
