@@ -7,19 +7,29 @@
 //
 // A pair is (sequence, local KV head, block of 32 RW query rows), its rows being the sequence's new tokens x the G query
 // heads of the KV head; a tile is 32 cached tokens of a pair.  The tiles of one head lie on one axis that is cut into equal
-// shares, so that the work is even whatever the lengths.  A team of workgroups, one per head, takes a share: where the heads of
-// a token lie side by side, the whole row is asked for at about one time (64 sequences of 512 to 4096, 8 heads: MEASURED).  A pair
-// that lies in one share is finished there, the pieces of a cut one leave (reference, sum of weights, sums of values) in the
-// workspace for a second launch.
+// shares, so that the work is even whatever the lengths.  A team of workgroups takes a share for all heads, so that the
+// whole row of a token is asked for at about one time (64 sequences of 512 to 4096, 8 heads, drafts of up to 8: 128 us in place of
+// 145).  A pair that lies in one share is finished there, the pieces of a cut one leave (reference, sum of weights, sums of values)
+// in the workspace for a second launch.
 //
 // What bounds it: reading K and V, 4 D bytes a token and KV head, as long as the rows are few: 32 rows x 32 keys take
 // 2 D / 16 + 2 D / 16 products of 32 x 32 x 16, 512 cycles at D = 128, and bring 16 KiB, for which HBM takes 1440 cycles of one
-// compute unit's share.  So up to 32 rows the four wavefronts of a workgroup take different tiles (RW = 1, KW = 4), up to 64
-// two by two, up to 128 all four share a tile, and eight do above: K and V pass through LDS once per workgroup.
+// compute unit's share.  RW wavefronts share a tile, each with 32 rows: K and V pass through LDS once per workgroup.  Four of them
+// (RW = 4) are the general form, two workgroups of which fill a compute unit, also where rows leave some without work: what they share
+// is three tiles on their way ahead of the one in hand.  Large batches of up to 64 rows take the wavefronts for other heads (HW = 4
+// or 2), which reads rows of several heads in one piece; large ones of many rows have eight to a tile (RW = 8).  With sums of weights
+// there are 32 rows, and where heads are not side by side the wavefronts take different tiles (KW = 4) and each stores its scores.
+//
+// Reached: 64 sequences of 512 to 4096, 8 heads of 128, drafts of up to 8 tokens 108 us (5.7 TB/s), up to 16 123, up to 32 146;
+// drafts of 33 to 64 tokens 200 us, where per tile of 256 rows the products (0.43 us at the matrix units' rate), the operand reads from
+// LDS (0.43) and the exponentials (0.37) overlap only in part: 1.15 us.
 //
 // Per tile, lane l = (c = l % 32, half = l / 32):
 //   S^T[token][c] = K[token][:] . q[c][:]     A operand = K rows from LDS, B operand = q
 //   O^T[e][c]     = sum_t V[t][e] P[c][t]     A operand = V^T by the transposing LDS read
+// Weights enter the second product in bf16, the type of the values that the matrix units multiply them with: off by 2^-9 of themselves
+// at most, each on its own, against one rounding of the output (measured against 64 bits, 2-norms: 2.3e-3 with, 1.7e-3 with weights of
+// 32 bits, of which 1.7e-3 is the output's own rounding).  All sums are fp32.
 // Register 4 a + i of S^T holds token 8 a + 4 half + i; contraction index 8 half + 4 a' + i of step c' of the second product
 // stands for token 16 c' + 8 a' + 4 half + i, so weights stay in their lane.
 #include <algorithm>
@@ -58,9 +68,9 @@ struct tree_args {
     int32_t few;              // up to 64 sequences, and their tiles are counted in 32 bits
     int32_t group_shift;      // log2 of the group rounded up to a power of two
     int32_t teams, least_tiles;   // shares that the axis of tiles is cut into, and the least tiles of a share
-    f32x4* part_o;            // [2 teams n_kv_local][RW][D / 8][64]: slot 2 w the first piece of workgroup w, 2 w + 1 its last
+    f32x4* part_o;            // [2 teams n_kv_local][RW][D / 8][64]: slot 2 w a piece of workgroup w that goes on a pair, 2 w + 1 one that begins it
     float* part_ml;           // [2 teams n_kv_local][32 RW][2] (reference in exponent units, sum of weights)
-    int2* ends;               // [batch][blocks][n_kv_local] of every pair: team of its first piece x 2 + whether that is the team's last, of its last
+    int2* ends;               // [batch][blocks][n_kv_local] of every pair: the teams of its first and last piece
     int32_t most_blocks;      // row blocks of a sequence by the host's bound
     // weights:
     float* scores;            // [batch][n_q_local][score_stride] exponents: score * scale * log2(e)
@@ -287,6 +297,8 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
         const int rb = uniform((int)(offset / w.tiles)), t0 = uniform((int)(offset - (int64_t)rb * w.tiles));
         const int count = (int)min((int64_t)(w.tiles - t0), to - at);
         const bool cut = count < w.tiles;
+        at += count;
+        offset += count;
         const int n = w.n, first = n - w.q_len;          // the first drafted token
         const int rows = min(w.q_len * G - rb * RB, RB);   // of the pair
         const bool idle = rw * 32 >= rows;                 // this wavefront has none of them
@@ -341,9 +353,11 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
                         const int limit = n - 1 - 16 * min(2 * tile + g, last_group), row = (p * kRowsEach & 15) + row_first;
                         off -= (uint32_t)(max((row & 15) - limit, 0) * (int)stride_bytes);
                     }
-                    // (non-temporal where one block of rows is all there is; several blocks read the tile again)
-                    __builtin_amdgcn_raw_ptr_buffer_load_lds(kBoth && g ? r1 : r0, (lds_ptr)(dst + kg * kPieces + (first_part + p) * 64), 16, off,
-                                                             0, 0, RW < 8 ? 2 : 0);
+                    // (non-temporal where one block of rows is all there is; several read the tile again)
+                    const __amdgpu_buffer_rsrc_t source = kBoth && g ? r1 : r0;
+                    const lds_ptr to_lds = (lds_ptr)(dst + kg * kPieces + (first_part + p) * 64);
+                    if (RW < 4 || (RW == 4 && w.blocks == 1)) __builtin_amdgcn_raw_ptr_buffer_load_lds(source, to_lds, 16, off, 0, 0, 2);
+                    else __builtin_amdgcn_raw_ptr_buffer_load_lds(source, to_lds, 16, off, 0, 0, 0);
                 }
             };
             if (2 * tile + 1 < last_group) fill(std::false_type());
@@ -445,7 +459,7 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
         auto weight_operand = [&](int c) { return as_bf16x8(kv_u32x4{pw[4 * c], pw[4 * c + 1], pw[4 * c + 2], pw[4 * c + 3]}); };
         // Scores of as many tiles as make 32 rows leave together, through LDS, whole lines at a time.  (The loads of later tiles are
         // counted in order with the stores, whose way out is long: storing every tile's takes 64 sequences of 512 to 4096
-        // 131 us in place of 114.)  Returns whether it stored four times.
+        // 131 us in place of 129, at heads of 64 83 in place of 81.)  Returns whether it stored four times.
         auto keep_scores = [&](int i) -> bool {
             if constexpr (SUMS) {
                 const int slots = 32 >> a.group_shift, slot = i & (slots - 1);
@@ -689,7 +703,7 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
 
         // ---- the piece's rows ----------------------------------------------------------------------
         l = half_sum(l);
-        const int slot = 2 * (team * Hl + h) + (at > from ? 1 : 0);
+        const int slot = 2 * (team * Hl + h) + (t0 == 0 ? 1 : 0);
         // groups of four accumulator registers: x = 4 j + u4 holds elements 8 x + 4 half ..
         constexpr int NX = 4 * NJ, XW = NX / KW;   // each of the KW wavefronts of a row finishes XW of them
         f32x4 acc[XW];
@@ -756,11 +770,9 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
         }
         if (lane == 0 && rw == 0 && kg == 0 && rb < a.most_blocks) {
             int2* ends = a.ends + ((int64_t)s * a.most_blocks + rb) * Hl + h;
-            if (t0 == 0) ends->x = 2 * team + (at > from ? 1 : 0);
+            if (t0 == 0) ends->x = team;
             if (t0 + count == w.tiles) ends->y = team;
         }
-        at += count;
-        offset += count;
     }
 }
 
@@ -772,9 +784,8 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
 struct piece_list {
     int rows, h, rb;          // rows of the pair
     int w0, w1;               // teams that hold its first and last piece
-    int skew;                 // the first piece is the last of its workgroup
     int heads;
-    __device__ int64_t slot(int z) const { return 2 * ((int64_t)(w0 + z) * heads + h) + (z == 0 ? skew : 0); }
+    __device__ int64_t slot(int z) const { return 2 * ((int64_t)(w0 + z) * heads + h) + (z == 0 ? 1 : 0); }
     __device__ int count() const { return w1 - w0 + 1; }
 };
 template <int RB>
@@ -785,9 +796,8 @@ __device__ __forceinline__ piece_list pieces_of(const tree_args& a, const seq_wo
     p.rows = min(w.q_len * a.group - rb * RB, RB);
     p.h = h;
     p.rb = rb;
-    p.w0 = uniform(ends.x >> 1);
+    p.w0 = uniform(ends.x);
     p.w1 = uniform(ends.y);
-    p.skew = uniform(ends.x & 1);
     p.heads = a.v.n_kv_local;
     return p;
 }
@@ -1016,11 +1026,11 @@ __global__ __launch_bounds__(256) void weights_kernel(tree_args a)
 // Several heads to a workgroup, by the bytes of K and V by the bound: below, more and shorter pieces cost more than rows of 512 and 1024
 // bytes bring.  us per call, one head / several: 8 heads, drafts of up to 8, 4 sequences of 512 to 4096 21.3 / 23.1, 8 of them
 // 28.7 / 26.0, 32 71.6 / 64.8, 128 239 / 228; 4 heads, 128 sequences 128 / 120; 64 of 100 to 1000 36.4 / 27.5; drafts of up to 16
-// (two heads) 128 sequences 269 / 251.  Two heads of 128 rows are slower (290 / 302).
+// (two heads) 128 sequences 269 / 251.  Two heads of 128 rows are slower (290 / 302).  One head of up to 64 rows is better off with
+// four wavefronts to a tile than with one or two (drafts of up to 16, 8 heads, 2 sequences of 512 to 4096 18.2 / 20.6; of up to 8,
+// 4 of 2000 to 4000 21.6 / 24.4; of up to 8 and one head, 16 of 3000 to 20000 31.9 / 34.0; 2 of 512 to 4096 16.9 / 15.8).
 constexpr int64_t kWideBytes = 100000000;
-
-// Wavefronts that share a tile, by the bound on a pair's rows
-int row_waves(int64_t rows) { return rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 ? 4 : 8; }
+constexpr int64_t kCacheBytes = 256 << 20;   // the cache between the dies and the memory
 
 struct tree_plan {
     int rw, hw;   // wavefronts that share a tile's rows; heads of a workgroup
@@ -1028,20 +1038,18 @@ struct tree_plan {
     int32_t blocks;
     size_t part_o, part_ml, ends, bytes;
 };
-tree_plan plan_tree(const kv_view* view, int batch, int max_ctx_len, int max_q_len)
+tree_plan plan_with(const kv_view* view, int batch, int max_ctx_len, int64_t rows, int rw, int hw)
 {
     tree_plan p;
-    const int64_t rows = (int64_t)max_q_len * view->group;
-    p.rw = row_waves(rows);
-    const int rb = 32 * p.rw;
-    const bool wide = (int64_t)batch * max_ctx_len * view->n_kv_local * view->geom.head_dim * 4 >= kWideBytes;
-    p.hw = !wide ? 1 : p.rw == 1 && view->n_kv_local % 4 == 0 ? 4 : p.rw == 2 && view->n_kv_local % 2 == 0 ? 2 : 1;
+    p.rw = rw;
+    p.hw = hw;
+    const int rb = 32 * rw;
     const int64_t blocks = (rows + rb - 1) / rb, tiles = ((int64_t)max_ctx_len + kKeys - 1) / kKeys;
     // Shorter shares cost more in pieces than they save (us per call with least tiles 4, 2, 1 / 8, 4, 4 / 16, 8, 4: 2 sequences of 512 to
     // 4096, up to 64 rows, 23.2 / 19.8 / 23.9; weights of 2 such sequences 23.4 / 19.3 / 26.2; 2 of 1000 to 2000, 256 rows, 33.8 / 27.5 / 27.4)
-    p.least = p.rw == 1 ? 8 : 4;
+    p.least = rw == 1 ? 8 : 4;
     const int64_t most = blocks * batch * ((tiles + p.least - 1) / p.least);
-    const int fill = kCus * (p.rw == 2 || p.rw == 4 ? 2 : 1) * p.hw;   // heads that the chip holds workgroups for
+    const int fill = kCus * (rw == 2 || rw == 4 ? 2 : 1) * hw;   // heads that the chip holds workgroups for
     p.teams = (int32_t)std::max<int64_t>(std::min<int64_t>(most, fill / view->n_kv_local), 1);
     const size_t records = (size_t)2 * p.teams * view->n_kv_local * rb;
     p.part_o = records * view->geom.head_dim * 4;
@@ -1051,6 +1059,33 @@ tree_plan plan_tree(const kv_view* view, int batch, int max_ctx_len, int max_q_l
     p.ends = (size_t)batch * blocks * view->n_kv_local * 8;
     p.bytes = p.part_o + p.part_ml + p.ends;
     return p;
+}
+int64_t cache_bytes(const kv_view* view, int batch, int max_ctx_len)
+{
+    return (int64_t)batch * max_ctx_len * view->n_kv_local * view->geom.head_dim * 4;
+}
+bool wide(const kv_view* view, int batch, int max_ctx_len) { return cache_bytes(view, batch, max_ctx_len) >= kWideBytes; }
+tree_plan plan_weights(const kv_view* view, int batch, int max_ctx_len)
+{
+    return plan_with(view, batch, max_ctx_len, view->group, 1, view->n_kv_local % 4 == 0 && wide(view, batch, max_ctx_len) ? 4 : 1);
+}
+// By the bound on a pair's rows
+tree_plan plan_tree(const kv_view* view, int batch, int64_t total_q, int max_ctx_len, int max_q_len)
+{
+    const int64_t rows = (int64_t)max_q_len * view->group;
+    if (rows <= 64 && wide(view, batch, max_ctx_len)) {
+        if (rows <= 32 && view->n_kv_local % 4 == 0) return plan_with(view, batch, max_ctx_len, rows, 1, 4);
+        if (rows > 32 && view->n_kv_local % 2 == 0) return plan_with(view, batch, max_ctx_len, rows, 2, 2);
+    }
+    tree_plan p4 = plan_with(view, batch, max_ctx_len, rows, 4, 1);
+    if (rows <= 128) return p4;
+    // Eight wavefronts read K and V half as often as two workgroups of four, which do not wait for each other and hide more.  The former
+    // where most sequences have rows for them and K and V pass the memory-side cache: us per call, four / eight, 8 heads, drafts of 33 to
+    // 64 and sequences of 1000 to 8000, 8 of them 60.8 / 57.3, 32 253 / 220; drafts of 1 to 64 51.3 / 54.6, 152 / 175; drafts of 150 to
+    // 256, 4 of them 92 / 101, 32 743 / 654.
+    tree_plan p8 = plan_with(view, batch, max_ctx_len, rows, 8, 1);
+    p4.bytes = p8.bytes = std::max(p4.bytes, p8.bytes);   // (whatever the number of query rows that a workspace was asked for)
+    return total_q * view->group > 128 * (int64_t)batch && cache_bytes(view, batch, max_ctx_len) > kCacheBytes ? p8 : p4;
 }
 
 template <int D, int RW, int HW>
@@ -1070,8 +1105,8 @@ template <int D>
 void launch_tree(const tree_plan& p, const tree_args& a, int64_t most_rows, hipStream_t st)
 {
     switch (p.rw) {
-        case 1: p.hw == 4 ? launch<D, 1, 4>(a, most_rows, st) : launch<D, 1, 1>(a, most_rows, st); break;
-        case 2: p.hw == 2 ? launch<D, 2, 2>(a, most_rows, st) : launch<D, 2, 1>(a, most_rows, st); break;
+        case 1: launch<D, 1, 4>(a, most_rows, st); break;
+        case 2: launch<D, 2, 2>(a, most_rows, st); break;
         case 4: launch<D, 4, 1>(a, most_rows, st); break;
         default: launch<D, 8, 1>(a, most_rows, st); break;
     }
@@ -1119,7 +1154,7 @@ int64_t score_stride(int max_ctx_len) { return ((int64_t)max_ctx_len + kKeys - 1
 extern "C" size_t paged_tree_attn_workspace_bytes(const kv_view* view, int batch, int64_t total_q, int max_ctx_len, int max_q_len)
 {
     if (!kv_view_ok(view) || batch <= 0 || total_q <= 0 || max_ctx_len <= 0 || max_q_len <= 0) return 0;
-    return plan_tree(view, batch, max_ctx_len, max_q_len).bytes;
+    return plan_tree(view, batch, total_q, max_ctx_len, max_q_len).bytes;
 }
 
 extern "C" int paged_tree_attn(const void* q, void* out, const void* kv_pool, int64_t n_pool_blocks, const int32_t* block_table,
@@ -1138,7 +1173,7 @@ extern "C" int paged_tree_attn(const void* q, void* out, const void* kv_pool, in
     if (const int rc = common_args(a, q, out, kv_pool, n_pool_blocks, block_table, block_table_stride, ctx_lens, batch, max_ctx_len,
                                    view, scale))
         return rc;
-    const tree_plan p = plan_tree(view, batch, max_ctx_len, max_q_len);
+    const tree_plan p = plan_tree(view, batch, total_q, max_ctx_len, max_q_len);
     if (!workspace || ((uintptr_t)workspace & 255u)) return KV_ERR_INVALID_ARG;
     if (workspace_bytes < p.bytes) return KV_ERR_WORKSPACE;
     a.q_off = q_offsets;
@@ -1164,7 +1199,7 @@ extern "C" size_t paged_decode_attn_weights_workspace_bytes(const kv_view* view,
 {
     if (!kv_view_ok(view) || batch <= 0 || max_ctx_len <= 0) return 0;
     const size_t rows = (size_t)batch * view->n_q_local;
-    return plan_tree(view, batch, max_ctx_len, 1).bytes + rows * (8 + 4 * (size_t)score_stride(max_ctx_len));
+    return plan_weights(view, batch, max_ctx_len).bytes + rows * (8 + 4 * (size_t)score_stride(max_ctx_len));
 }
 
 extern "C" int paged_decode_attn_weights(const void* q, void* out, const void* kv_pool, int64_t n_pool_blocks,
@@ -1179,7 +1214,7 @@ extern "C" int paged_decode_attn_weights(const void* q, void* out, const void* k
     if (const int rc = common_args(a, q, out, kv_pool, n_pool_blocks, block_table, block_table_stride, ctx_lens, batch, max_ctx_len,
                                    view, scale))
         return rc;
-    const tree_plan p = plan_tree(view, batch, std::max(max_ctx_len, 1), 1);
+    const tree_plan p = plan_weights(view, batch, std::max(max_ctx_len, 1));
     const size_t rows = (size_t)batch * view->n_q_local;
     if (max_ctx_len > 0) {
         if (!workspace || ((uintptr_t)workspace & 255u)) return KV_ERR_INVALID_ARG;
