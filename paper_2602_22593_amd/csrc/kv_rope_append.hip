@@ -4,11 +4,13 @@
 // With frequencies f_0 .. f_{R/2 - 1} and an axis for each, the pair (x, y) of number i becomes (x cos a - y sin a, y cos a + x sin a),
 // a = position on axis(i) * f_i.  Elements from R on pass as they are, and so do the values.
 //
-// Bound by reading and writing every row once: 17000 tokens of 32 query and 8 KV heads of 128, 420 MB, take 87 us, the rate of a
-// large copy (4.8 TB/s).  A workgroup takes one or two tokens: their cosines and sines go into LDS once and serve all heads; then every
+// Bound by reading and writing every row once: 17000 tokens of 32 query and 8 KV heads of 128, 420 MB, take 81 us (5.2 TB/s; a
+// byte-for-byte copy of as much takes 67).  Stores past the caches: 8 prompts of 500 to 1000 tokens 23 us in place of 28, 2 of 3000 to
+// 4000 29 in place of 38 (whoever reads the rows next does so through another die's L2).  A workgroup takes one or two tokens: their cosines and sines go into LDS once and serve all heads; then every
 // lane moves items of two 16-byte pieces, the two halves of eight pairs, so that a rotation needs nothing of another
 // lane.  D / 16 items a head, consecutive lanes on consecutive pieces.  Small workgroups with one item a lane at a time hide the
-// chain before the rows (lengths, positions, cosines) behind each other: eight tokens and four items 105 us, four and two 91.
+// chain before the rows (lengths, positions, cosines) behind each other: eight tokens and four items 105 us, four and two 91; rows
+// requested before that chain, two or three items a lane, 86 to 94.
 #include "kv_internal.h"
 
 #include "decode_common.h"
@@ -138,8 +140,8 @@ __global__ __launch_bounds__(kThreads) void kv_rope_append_kernel(rope_args a)
                 }
             }
         }
-        *reinterpret_cast<kv_u32x4*>(to) = lo;
-        *reinterpret_cast<kv_u32x4*>(to + apart) = hi;
+        __builtin_nontemporal_store(lo, reinterpret_cast<kv_u32x4*>(to));
+        __builtin_nontemporal_store(hi, reinterpret_cast<kv_u32x4*>(to + apart));
     }
 }
 
