@@ -326,9 +326,42 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
         at_k.id = request_ids(1);
         const cursor at_start = at_k;
         at_v = at_k;
-        auto stage = [&](cursor& x, const uint32_t (&at_lane)[NP], int64_t plane, kv_u32x4* dst) {
+        // ---- this lane's query row, asked for before the tiles: waits count in order ----------------
+        const int rho = rb * RB + min(rw * 32 + col, rows - 1);      // (padding columns repeat the last row)
+        const int64_t qrow = (int64_t)(w.q0 + rho / G);
+        const int64_t orow = (qrow * v.n_q_local + h * G + rho % G) * D;
+        const int srow = rw * 32 + col;
+        const bool real = srow < rows;
+        bf16x8 qb[NK];
+#pragma unroll
+        for (int kk = 0; kk < NK; ++kk)
+            qb[kk] = as_bf16x8(*reinterpret_cast<const kv_u32x4*>(a.q + orow + half * 8 + kk * 16));
+
+        const int first_edge = (SUMS ? n : first) >> 5;   // tiles from there on hold drafted tokens or the end of the sequence
+        if constexpr (!SUMS) {
+            if (t0 + count > first_edge) {
+                // The windows of 32 tokens that the tiles are, cut out of the rows' mask words; what lies before the draft is seen
+                if ((int)threadIdx.x < rows) {
+                    const uint32_t* words = reinterpret_cast<const uint32_t*>(a.mask) +
+                                            ((int64_t)w.q0 + (rb * RB + (int)threadIdx.x) / G) * 2 * a.mask_words;
+                    const int shift = first & 31;
+                    uint32_t before = ~0u;
+#pragma unroll
+                    for (int e = 0; e < kEdgeTiles; ++e) {
+                        const int here = n - kKeys * (first_edge + e);   // tokens of the tile that exist
+                        if (here <= 0) break;
+                        const uint32_t word = e < 2 * a.mask_words ? words[e] : 0u;
+                        const uint32_t window = (uint32_t)((((uint64_t)word << 32 | before) << shift) >> 32);
+                        s_seen[e][threadIdx.x] = here >= 32 ? window : window & ((1u << here) - 1u);
+                        before = word;
+                    }
+                }
+            }
+        }
+
+        auto stage = [&](cursor& x, const uint32_t (&at_lane)[NP], int64_t plane, kv_u32x4* dst, auto sure) {
             const int i = x.i++;
-            if (i >= mine) return;
+            if (!decltype(sure)::value && i >= mine) return;
             if ((i & 31) == 0 && i > 0) {
                 x.place = places(x.id, i >> 5);
                 x.id = request_ids((i >> 5) + 1);
@@ -363,11 +396,11 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
             if (2 * tile + 1 < last_group) fill(std::false_type());
             else fill(std::true_type());
         };
-        auto stage_k = [&](kv_u32x4* dst) {
-            if (!kSplitPlanes || rw < NK) stage(at_k, k_lane, 0, dst);
+        auto stage_k = [&](kv_u32x4* dst, auto sure) {
+            if (!kSplitPlanes || rw < NK) stage(at_k, k_lane, 0, dst, sure);
         };
-        auto stage_v = [&](kv_u32x4* dst) {
-            if (!kSplitPlanes || rw >= NK) stage(at_v, v_lane, plane_bytes, dst);
+        auto stage_v = [&](kv_u32x4* dst, auto sure) {
+            if (!kSplitPlanes || rw >= NK) stage(at_v, v_lane, plane_bytes, dst, sure);
         };
         // this wavefront's loads have landed, and then those of the wavefronts that share its tiles
         auto staged = [&](auto under_way) {   // but for the last so many
@@ -376,46 +409,21 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
             if constexpr (kShared) __syncthreads();
             else asm volatile("" ::: "memory");
         };
+        // Of a ring of several tiles the first steps need K of two and V of one; the others land meanwhile
+        constexpr int kRing = (NB - 2) * (kSplitPlanes ? 1 : 2) * NP;
+        auto start = [&](auto sure) {
 #pragma unroll
-        for (int x = 0; x < NB - 1; ++x) {
-            stage_k(k_buf(x));
-            stage_v(v_buf(x));
-        }
-        stage_k(k_buf(NB - 1));
-
-        // ---- this lane's query row ----------------------------------------------------------------
-        const int rho = rb * RB + min(rw * 32 + col, rows - 1);      // (padding columns repeat the last row)
-        const int64_t qrow = (int64_t)(w.q0 + rho / G);
-        const int64_t orow = (qrow * v.n_q_local + h * G + rho % G) * D;
-        const int srow = rw * 32 + col;
-        const bool real = srow < rows;
-        bf16x8 qb[NK];
-#pragma unroll
-        for (int kk = 0; kk < NK; ++kk)
-            qb[kk] = as_bf16x8(*reinterpret_cast<const kv_u32x4*>(a.q + orow + half * 8 + kk * 16));
-
-        const int first_edge = (SUMS ? n : first) >> 5;   // tiles from there on hold drafted tokens or the end of the sequence
-        if constexpr (!SUMS) {
-            if (t0 + count > first_edge) {
-                // The windows of 32 tokens that the tiles are, cut out of the rows' mask words; what lies before the draft is seen
-                if ((int)threadIdx.x < rows) {
-                    const uint32_t* words = reinterpret_cast<const uint32_t*>(a.mask) +
-                                            ((int64_t)w.q0 + (rb * RB + (int)threadIdx.x) / G) * 2 * a.mask_words;
-                    const int shift = first & 31;
-                    uint32_t before = ~0u;
-#pragma unroll
-                    for (int e = 0; e < kEdgeTiles; ++e) {
-                        const int here = n - kKeys * (first_edge + e);   // tokens of the tile that exist
-                        if (here <= 0) break;
-                        const uint32_t word = e < 2 * a.mask_words ? words[e] : 0u;
-                        const uint32_t window = (uint32_t)((((uint64_t)word << 32 | before) << shift) >> 32);
-                        s_seen[e][threadIdx.x] = here >= 32 ? window : window & ((1u << here) - 1u);
-                        before = word;
-                    }
-                }
-                __syncthreads();
+            for (int x = 0; x < NB - 1; ++x) {
+                stage_k(k_buf(x), sure);
+                stage_v(v_buf(x), sure);
             }
-        }
+            stage_k(k_buf(NB - 1), sure);
+#pragma unroll
+            for (int kk = 0; kk < NK; ++kk) asm volatile("" : "+v"(qb[kk]));   // (q has come before: waited for here, where what is under way is known)
+            staged(std::integral_constant<int, decltype(sure)::value ? kRing : 0>());
+        };
+        if (NB > 2 && mine >= NB) start(std::true_type());
+        else start(std::false_type());
 
         float neg_m, l;
         bool unset;
@@ -589,8 +597,8 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
             constexpr int B = decltype(phase)::value;   // i % NB
             kv_u32x4* const k_next = k_buf(B + 1);
             kv_u32x4* const v_now = v_buf(B);
-            stage_v(v_buf(B + NB - 1));
-            stage_k(k_buf(B));
+            stage_v(v_buf(B + NB - 1), std::false_type());
+            stage_k(k_buf(B), std::false_type());
             bool stored = false;
             if (!idle) {
                 bf16x8 ka[NK], va[2 * NJ];
@@ -631,11 +639,10 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
                 move_reference(top);
             }
             // K of tile i + 2 and V of tile i + 1 are needed next: what the last NB - 2 steps asked for may still be under way
-            if (NB > 2 && i + NB < mine) staged(std::integral_constant<int, (NB - 2) * (kSplitPlanes ? 1 : 2) * NP>());
+            if (NB > 2 && i + NB < mine) staged(std::integral_constant<int, kRing>());
             else if (stored && kStoresLast) staged(std::integral_constant<int, 4>());   // (scores on their way out)
             else staged(std::integral_constant<int, 0>());
         };
-        staged(std::integral_constant<int, 0>());
         const int common = count / KW;   // tiles that every key group has
         int i = 0;
         if (common > 0) {
@@ -668,7 +675,7 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
                 }
             }
             // the last one
-            if constexpr (KW > 1) stage_v(v_buf(i + 1));
+            if constexpr (KW > 1) stage_v(v_buf(i + 1), std::false_type());
             if (!idle) {
 #pragma unroll
                 for (int u = 0; u < 8; ++u) weights(u);
@@ -692,8 +699,8 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
                 at_v = at_start;
 #pragma unroll 1
                 for (i = 0; i < iters; ++i) {
-                    stage_k(s_k0);
-                    stage_v(s_v0);
+                    stage_k(s_k0, std::false_type());
+                    stage_v(s_v0, std::false_type());
                     staged(std::integral_constant<int, 0>());
                     if (i < mine && !idle) whole_step(std::true_type(), i, s_k0, s_v0);
                     __syncthreads();
