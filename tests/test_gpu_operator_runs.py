@@ -356,3 +356,52 @@ def test_scores_of_great_size(geom, q_len):
         within(host(got), want, tol)
         total = host(weights).astype(np.float64).sum(axis=2)
         assert np.abs(total - group).max() <= group * 2.0 ** -18      # n terms and a quotient in fp32
+
+
+@pytest.mark.parametrize("geom,triple,ctx,q_lens", [
+    (G8B, (DP, 1, 0), [600, 256, 1000, 64], [64, 256, 65, 1]),
+    (G8B, (TP, 2, 1), [300, 77, 2000], [256, 77, 1]),
+    (G8B, (DP, 2, 1), [90], [50]),
+    (TINY, (DP, 1, 0), [500, 33, 300, 8], [200, 33, 256, 8]),
+    ((20, 4, 64, 32), (DP, 1, 0), [77, 500, 200], [40, 33, 200]),
+    ((64, 4, 128, 48), (TP, 2, 0), [300, 97, 256, 16], [12, 97, 256, 1]),
+])
+def test_large_batches_of_many_rows(geom, triple, ctx, q_lens):
+    """Bounds and numbers of drafts for which eight wavefronts share a tile; a workspace asked for with other numbers serves."""
+    c = ref.case(geom, triple, ctx, q_lens)
+    bound = 400000
+    table = np.pad(c.table, ((0, 0), (0, -(-bound // c.info["block_tokens"]) - c.table.shape[1])), constant_values=-1)
+    seen, words = ref.tree_masks(c.q_lens, np.random.default_rng(36))
+    want, tol = ref.tree_attention(c, seen)
+    view = view_of(c)
+    sizes = {kv.paged_tree_attn_workspace_bytes(view, len(ctx), total, bound, max(q_lens)) for total in (1, len(c.q), len(ctx) * max(q_lens))}
+    assert len(sizes) == 1
+    workspace = torch.full((sizes.pop(),), 0xff, dtype=torch.uint8, device=DEV)
+    got = kv.paged_tree_attn(dev(c.q), dev(c.pool), dev(table), dev(c.ctx), dev(c.q_off.astype(np.int32)), dev(words), view, bound,
+                             max(q_lens), workspace=workspace)
+    within(host(got), want, tol)
+
+
+@pytest.mark.parametrize("d,bad", [(128, np.nan), (64, np.inf)])
+@pytest.mark.parametrize("q_lens", [[8, 3, 7], [16, 1, 7], [64, 45, 31]])
+def test_large_batches_hide_what_is_not_finite(d, bad, q_lens):
+    """As in small batches: infinities and NaN in drafted tokens' values reach the rows that see them; any bits; rows that see nothing."""
+    ctx = [100, 45, 31]
+    c = ref.case((16, 4, d, 16), (DP, 1, 0), ctx, q_lens)
+    bound = 400000
+    table = np.pad(c.table, ((0, 0), (0, -(-bound // c.info["block_tokens"]) - c.table.shape[1])), constant_values=-1)
+    seen = np.random.default_rng(37).random((len(c.q), 64)) < 0.5
+    rows, h0 = ref.view_rows(c, c.pool)
+    hit = np.zeros(len(seen), bool)
+    for s in range(3):
+        node = int(c.q_lens[s]) // 2
+        b, slot = ref.place(c, s, c.ctx[s] - c.q_lens[s] + node)
+        rows[b, 1, slot, :, ::3] = 0x7FC0 if np.isnan(bad) else 0x7F80
+        hit[c.q_off[s]:c.q_off[s + 1]] = seen[c.q_off[s]:c.q_off[s + 1], node]
+    want, tol = ref.tree_attention(c, seen)
+    got = bf16_bits_to_f64(host(kv.paged_tree_attn(dev(c.q), dev(c.pool), dev(table), dev(c.ctx), dev(c.q_off.astype(np.int32)),
+                                                   dev(ref.pack(seen)), view_of(c), bound, max(q_lens))))
+    assert hit.any() and not hit.all()
+    keep = np.arange(d) % 3 != 0
+    assert (np.abs(got[~hit] - want[~hit]) <= tol[~hit]).all()
+    assert (np.abs(got[hit] - want[hit]) <= tol[hit])[:, :, keep].all() and not np.isfinite(got[hit][:, :, ::3]).any()
