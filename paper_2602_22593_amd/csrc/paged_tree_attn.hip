@@ -20,14 +20,14 @@
 // or 2), which reads rows of several heads in one piece; large ones of many rows have eight to a tile (RW = 8).  With sums of weights
 // there are 32 rows, and where heads are not side by side the wavefronts take different tiles (KW = 4) and each stores its scores.
 //
-// Reached: 64 sequences of 512 to 4096, 8 heads of 128, drafts of up to 8 tokens 108 us (5.7 TB/s), up to 16 123, up to 32 146;
-// drafts of 33 to 64 tokens 200 us, where per tile of 256 rows the products (0.43 us at the matrix units' rate), the operand reads from
-// LDS (0.43) and the exponentials (0.37) overlap only in part: 1.15 us.
+// Reached: 64 sequences of 512 to 4096, 8 heads of 128, drafts of up to 8 tokens 108 us (5.7 TB/s), up to 16 124, up to 32 145, 33 to
+// 64 200.  With 256 rows a tile takes 1.1 us of a compute unit, of which the products are 0.43 at the matrix units' rate and the
+// vector instructions of the softmax 0.45 (75 of 4 cycles and 16 exponentials of 16 for each wavefront): they overlap in part only.
 //
 // Per tile, lane l = (c = l % 32, half = l / 32):
 //   S^T[token][c] = K[token][:] . q[c][:]     A operand = K rows from LDS, B operand = q
 //   O^T[e][c]     = sum_t V[t][e] P[c][t]     A operand = V^T by the transposing LDS read
-// Weights enter the second product in bf16, the type of the values that the matrix units multiply them with: off by 2^-9 of themselves
+// Weights enter the second product in bf16, the type of the values that the matrix units multiply them with: off by 2^-8 of themselves
 // at most, each on its own, against one rounding of the output (measured against 64 bits, 2-norms: 2.3e-3 with, 1.7e-3 with weights of
 // 32 bits, of which 1.7e-3 is the output's own rounding).  All sums are fp32.
 // Register 4 a + i of S^T holds token 8 a + 4 half + i; contraction index 8 half + 4 a' + i of step c' of the second product
