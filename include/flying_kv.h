@@ -364,7 +364,7 @@ int kv_rope_append(void* kv_pool, int64_t n_pool_blocks, const kv_view* view, co
  *   tree_mask      device, uint64 [total_q][mask_words], mask_words >= ceil(max_q_len / 64); bits from
  *                  q_len[s] on are ignored
  *   workspace      at least paged_tree_attn_workspace_bytes(...) bytes, 256-byte aligned; contents need
- *                  not be initialised
+ *                  not be initialised; one for larger bounds serves smaller calls (here and below)
  * Other arguments as paged_prefill_attn, max_q_len <= 256.  Infinities and NaN in the K or V of a drafted
  * token reach the rows that see it and no others.  Errors: KV_ERR_INVALID_ARG (null pointers, negative sizes,
  * max_q_len > max_ctx_len, block_table_stride or mask_words too small), KV_ERR_UNSUPPORTED (head_dim not 64 or

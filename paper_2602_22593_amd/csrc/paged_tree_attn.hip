@@ -1080,19 +1080,20 @@ tree_plan plan_weights(const kv_view* view, int batch, int max_ctx_len)
 tree_plan plan_tree(const kv_view* view, int batch, int64_t total_q, int max_ctx_len, int max_q_len)
 {
     const int64_t rows = (int64_t)max_q_len * view->group;
+    const tree_plan p4 = plan_with(view, batch, max_ctx_len, rows, 4, 1), p8 = plan_with(view, batch, max_ctx_len, rows, 8, 1);
+    tree_plan p = p4;
     if (rows <= 64 && wide(view, batch, max_ctx_len)) {
-        if (rows <= 32 && view->n_kv_local % 4 == 0) return plan_with(view, batch, max_ctx_len, rows, 1, 4);
-        if (rows > 32 && view->n_kv_local % 2 == 0) return plan_with(view, batch, max_ctx_len, rows, 2, 2);
+        if (rows <= 32 && view->n_kv_local % 4 == 0) p = plan_with(view, batch, max_ctx_len, rows, 1, 4);
+        if (rows > 32 && view->n_kv_local % 2 == 0) p = plan_with(view, batch, max_ctx_len, rows, 2, 2);
     }
-    tree_plan p4 = plan_with(view, batch, max_ctx_len, rows, 4, 1);
-    if (rows <= 128) return p4;
     // Eight wavefronts read K and V half as often as two workgroups of four, which do not wait for each other and hide more.  The former
     // where most sequences have rows for them and K and V pass the memory-side cache: us per call, four / eight, 8 heads, drafts of 33 to
     // 64 and sequences of 1000 to 8000, 8 of them 60.8 / 57.3, 32 253 / 220; drafts of 1 to 64 51.3 / 54.6, 152 / 175; drafts of 150 to
     // 256, 4 of them 92 / 101, 32 743 / 654.  (On average 130, 194 and 812 rows; 160 lies between.)
-    tree_plan p8 = plan_with(view, batch, max_ctx_len, rows, 8, 1);
-    p4.bytes = p8.bytes = std::max(p4.bytes, p8.bytes);   // (whatever the number of query rows that a workspace was asked for)
-    return total_q * view->group > 160 * (int64_t)batch && cache_bytes(view, batch, max_ctx_len) > kCacheBytes ? p8 : p4;
+    if (rows > 128 && total_q * view->group > 160 * (int64_t)batch && cache_bytes(view, batch, max_ctx_len) > kCacheBytes) p = p8;
+    // A workspace asked for with larger bounds serves smaller calls, whatever their variant
+    p.bytes = std::max({p.bytes, p4.bytes, p8.bytes});
+    return p;
 }
 
 template <int D, int RW, int HW>

@@ -190,3 +190,15 @@ def test_names_in_the_binding_match_the_header():
     assert "KV_ROPE_HALVES = 0, KV_ROPE_ADJACENT = 1" in text
     assert (kv.KV_ROPE_HALVES, kv.KV_ROPE_ADJACENT) == (0, 1)
     assert np.isfinite(bf16_bits_to_f64(np.array([0x3F80], np.uint16))).all()
+
+
+@pytest.mark.parametrize("geom,p", [((32, 8, 128, 16), 1), ((32, 8, 128, 16), 2), ((64, 8, 128, 16), 8), ((8, 2, 64, 16), 1), ((20, 4, 64, 32), 1)])
+def test_workspaces_for_larger_bounds_serve_smaller_calls(geom, p):
+    view = kv.kv_view_create(*geom, kv.KV_LAYOUT_TP if p > 1 else kv.KV_LAYOUT_DP, p, 0)
+    bounds = [(b, n) for b in (1, 3, 16, 64, 200) for n in (32, 256, 1000, 8192, 8193, 131072)]
+    tree = {(b, n, q): kv.paged_tree_attn_workspace_bytes(view, b, b * q, n, q) for b, n in bounds for q in (1, 8, 9, 16, 17, 32, 33, 64, 256) if q <= n}
+    weights = {x: kv.paged_decode_attn_weights_workspace_bytes(view, *x) for x in bounds}
+    evict = {x: kv.kv_evict_workspace_bytes(view, *x) for x in bounds}
+    for sizes in (tree, weights, evict):
+        for x, need in sizes.items():
+            assert all(given >= need for y, given in sizes.items() if all(j >= i for i, j in zip(x, y))), x
