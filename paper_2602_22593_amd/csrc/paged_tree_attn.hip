@@ -49,6 +49,10 @@ typedef __attribute__((address_space(3))) void* lds_ptr;
 constexpr int kKeys = 32;
 constexpr float kUnset = 1e30f;   // exponent addend of a column that has seen no key yet
 constexpr int kCus = 256;
+// Tiles that take as long as starting and ending a piece.  us per call, shares of even length wherever those of the least do not fit / pieces
+// longer than even ones by up to so many: 8 heads, 4 sequences of 2000 to 4000, drafts of up to 8 20.4 / 18.6, with sums 27.0 / 22.5; 2 of 1000
+// to 8000, drafts of 150 to 256 54.0 / 46.1, 8 of them with drafts of 33 to 64 59.7 / 54.0.  Eight tiles: the same.
+constexpr int kPieceTiles = 4;
 constexpr int kMostNodes = 256;   // drafted tokens of a sequence
 constexpr int kEdgeTiles = kMostNodes / kKeys + 1;   // tiles that they lie in
 
@@ -86,6 +90,17 @@ __device__ __forceinline__ int64_t uniform64(int64_t x)
     return (int64_t)((uint64_t)(uint32_t)uniform((int)x) | (uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32);
 }
 
+// Sums over the lanes up to each one: within rows of 16, then of the row before, then of the 32 lanes before.
+__device__ __forceinline__ int lane_sums(int x)
+{
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);    // row_shr:1, 2, 4, 8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);   // row_bcast:15, 31
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+    return x;
+}
 // Maximum / sum over the two lanes of a column, left in both.
 __device__ __forceinline__ float half_max(float x)
 {
@@ -215,35 +230,31 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
     seq_work lane_work = {0, 0, 0, 0, 0};
     if (few) {
         if (lane < a.batch) lane_work = work_of<RB>(a, lane);
-        auto inclusive = [&](int x) {
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const int y = __shfl_up(x, d);
-                x += lane >= d ? y : 0;
-            }
-            return x;
-        };
-        // Where there are teams enough for shares of the least length that each end with their pair, a team has one piece: what a
-        // workgroup does before its first tile and after its last counts for more there than even shares
-        const int each = (lane_work.tiles + a.least_tiles - 1) / a.least_tiles, units = each * lane_work.blocks;
-        int incl = inclusive(units);
-        if (__builtin_amdgcn_readlane(incl, 63) <= a.teams) {
+        const int here = lane_work.tiles * lane_work.blocks, incl_here = lane_sums(here);
+        const int total = __builtin_amdgcn_readlane(incl_here, 63), share = (int)share_of(a, total);
+        // Where shares that each end with their pair are enough for the teams, a team has one piece, if they are not longer than even
+        // ones by more than what a workgroup does before its first tile and after its last comes to
+        int length = share, incl = 0, each = 0;
+        bool fits = false;
+        for (; length <= share + kPieceTiles; ++length) {
+            each = (lane_work.tiles + length - 1) / length;
+            incl = lane_sums(each * lane_work.blocks);
+            fits = __builtin_amdgcn_readlane(incl, 63) <= a.teams;
+            if (fits) break;
+        }
+        if (fits) {
             if (team >= __builtin_amdgcn_readlane(incl, 63)) return;
             s = __builtin_popcountll(__builtin_amdgcn_ballot_w64(incl <= team));
-            const int unit = team - __builtin_amdgcn_readlane(incl - units, s), e = __builtin_amdgcn_readlane(each, s);
-            const int tiles = __builtin_amdgcn_readlane(lane_work.tiles, s), at = (unit % e) * a.least_tiles;
+            const int unit = team - __builtin_amdgcn_readlane(incl - each * lane_work.blocks, s), e = __builtin_amdgcn_readlane(each, s);
+            const int tiles = __builtin_amdgcn_readlane(lane_work.tiles, s), at = (unit % e) * length;
             offset = (int64_t)(unit / e) * tiles + at;
             from = 0;
-            to = min(a.least_tiles, tiles - at);
+            to = min(length, tiles - at);
         } else {
-            const int here = lane_work.tiles * lane_work.blocks;
-            incl = inclusive(here);
-            const int total = __builtin_amdgcn_readlane(incl, 63);
-            const int64_t share = share_of(a, total);
-            from = team * share;
+            from = (int64_t)team * share;
             to = min(from + share, (int64_t)total);
-            s = min(__builtin_popcountll(__builtin_amdgcn_ballot_w64(incl <= from)), 63);
-            offset = from - __builtin_amdgcn_readlane(incl - here, s);
+            s = min(__builtin_popcountll(__builtin_amdgcn_ballot_w64(incl_here <= from)), 63);
+            offset = from - __builtin_amdgcn_readlane(incl_here - here, s);
         }
     } else {
         find_share<NT, RB>(a, team, s_sum, from, to, s, offset);
@@ -1052,8 +1063,9 @@ tree_plan plan_with(const kv_view* view, int batch, int max_ctx_len, int64_t row
     p.hw = hw;
     const int rb = 32 * rw;
     const int64_t blocks = (rows + rb - 1) / rb, tiles = ((int64_t)max_ctx_len + kKeys - 1) / kKeys;
-    // Shorter shares cost more in pieces than they save (us per call with least tiles 4, 2, 1 / 8, 4, 4 / 16, 8, 4: 2 sequences of 512 to
-    // 4096, up to 64 rows, 23.2 / 19.8 / 23.9; weights of 2 such sequences 23.4 / 19.3 / 26.2; 2 of 1000 to 2000, 256 rows, 33.8 / 27.5 / 27.4)
+    // Shorter shares cost more in pieces than they save (us per call: weights of 2 sequences of 512 to 4096 with least tiles 4 / 8 / 16 23.4 /
+    // 19.3 / 26.2; four wavefronts to a tile, least tiles 2 / 4 / 8: 2 heads, 4 sequences of 512 to 4096 15.5 / 14.2 / 15.1, 8 heads, 16 of
+    // 100 to 500 20.6 / 17.8 / 18.1)
     p.least = rw == 1 ? 8 : 4;
     const int64_t most = blocks * batch * ((tiles + p.least - 1) / p.least);
     const int fill = kCus * (rw == 2 || rw == 4 ? 2 : 1) * hw;   // heads that the chip holds workgroups for

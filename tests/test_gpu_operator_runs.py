@@ -405,3 +405,31 @@ def test_large_batches_hide_what_is_not_finite(d, bad, q_lens):
     keep = np.arange(d) % 3 != 0
     assert (np.abs(got[~hit] - want[~hit]) <= tol[~hit]).all()
     assert (np.abs(got[hit] - want[hit]) <= tol[hit])[:, :, keep].all() and not np.isfinite(got[hit][:, :, ::3]).any()
+
+
+@pytest.mark.parametrize("seed", range(10))
+def test_random_batches(seed):
+    """Ragged batches of 1 to 70 sequences and bounds at random: whatever the shares come to, every tile counts once."""
+    rng = np.random.default_rng(100 + seed)
+    geom = [TINY, (4, 1, 128, 16), (6, 3, 64, 32), G8B][seed % 4]
+    batch = int(rng.integers(1, 9)) if geom is G8B else int(rng.integers(1, 71))
+    most = int(rng.choice([40, 300, 1500]))
+    ctx = rng.integers(0, most + 1, batch)
+    ctx[rng.integers(0, batch)] = most
+    q_lens = np.minimum(rng.integers(0, int(rng.choice([2, 9, 40, 100])), batch), ctx)
+    q_lens[ctx.argmax()] = max(q_lens.max(), 1)
+    c = ref.case(geom, (DP, 1, 0), ctx, q_lens, index=73)
+    seen, words = ref.tree_masks(np.maximum(c.q_lens, 0), rng)
+    want, tol = ref.tree_attention(c, seen)
+    bound, q_bound = most + int(rng.integers(0, 200)), int(min(q_lens.max() + rng.integers(0, 3), most))
+    table = np.pad(c.table, ((0, 0), (0, max(0, -(-bound // c.info["block_tokens"]) - c.table.shape[1]))), constant_values=-1)
+    words = np.pad(words, ((0, 0), (0, max(0, -(-q_bound // 64) - words.shape[1]))))
+    view, tab, n = view_of(c), dev(table), dev(c.ctx)
+    got = kv.paged_tree_attn(dev(c.q), dev(c.pool), tab, n, dev(c.q_off.astype(np.int32)), dev(words), view, bound, q_bound)
+    within(host(got), want, tol)
+    c.q = wl.randn_bf16((batch, geom[0], geom[2]), wl.generator(74, wl.SUB_QUERY))
+    prior = rng.exponential(1e-2, (batch, geom[1], bound)).astype(np.float32)
+    want, tol, sums, sums_tol = ref.decode_weights(c, prior)
+    weights = dev(prior)
+    within(host(kv.paged_decode_attn_weights(dev(c.q), dev(c.pool), tab, n, view, bound, weights)), want, tol)
+    assert (np.abs(host(weights).astype(np.float64) - sums) <= sums_tol).all()
