@@ -1074,7 +1074,7 @@ tree_plan plan_with(const kv_view* view, int batch, int max_ctx_len, int64_t row
     p.part_o = records * view->geom.head_dim * 4;
     p.part_ml = records * 8;
     p.blocks = (int32_t)blocks;
-    p.few = batch <= 64 && blocks * batch * tiles < 0x7fffffff;
+    p.few = batch <= 64 && blocks * batch * tiles < 0x40000000;
     p.ends = (size_t)batch * blocks * view->n_kv_local * 8;
     p.bytes = p.part_o + p.part_ml + p.ends;
     return p;
