@@ -339,7 +339,8 @@ int kv_append(void* kv_pool, int64_t n_pool_blocks, const kv_view* view, const v
  *   q_offsets      device, int32 [batch + 1], non-decreasing, q_offsets[0] = 0; null: one token per
  *                  sequence (total = batch).  Rows from q_offsets[batch] on are not touched
  *   token_pos      device, int32 [batch][n_kv_local][token_pos_stride], or null: the position on axis 0
- *                  of every token written, at its place in the cache, for kv_evict
+ *                  of every token written, at its place in the cache, for kv_evict (places from
+ *                  token_pos_stride on are left out)
  * Errors: KV_ERR_INVALID_ARG (null pointers, negative sizes, strides too small, an axis out of range,
  * rotary_dim > head_dim, total != batch without q_offsets), KV_ERR_UNSUPPORTED (head_dim or rotary_dim
  * not a multiple of 16, rotary_dim > 256, more than 4 axes, strides not multiples of 8 elements,
