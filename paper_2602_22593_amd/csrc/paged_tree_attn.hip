@@ -56,6 +56,29 @@ constexpr int kPieceTiles = 4;
 constexpr int kMostNodes = 256;   // drafted tokens of a sequence
 constexpr int kEdgeTiles = kMostNodes / kKeys + 1;   // tiles that they lie in
 
+// Scores leave in four passes over 8 of 32 rows (tile x in hand, query head g): row r is x = r >> s, g = r & ((1 << s) - 1), s the log2 of the
+// group rounded up.  The compiler branches around a pass in which no lane has a head: how many of the four store.
+constexpr int passes_with_heads(int group)
+{
+    int s = 0, n = 0;
+    while ((1 << s) < group) ++s;
+    for (int r0 = 0; r0 < 32; r0 += 8) {
+        bool any = false;
+        for (int r = r0; r < r0 + 8; ++r) any = any || (r & ((1 << s) - 1)) < group;
+        n += any;
+    }
+    return n;
+}
+constexpr int kMostGroup = 32;
+__host__ __device__ constexpr bool stores_four(int group) { return group <= 16 || group > 24; }
+constexpr bool stores_four_holds()
+{
+    for (int group = 1; group <= kMostGroup; ++group)
+        if (stores_four(group) != (passes_with_heads(group) == 4)) return false;
+    return true;
+}
+static_assert(stores_four_holds(), "a wait that leaves four stores under way needs four stores");
+
 struct tree_args {
     const uint16_t* q;        // [total_q][n_q_local][D]
     uint16_t* out;
@@ -478,7 +501,8 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
         auto weight_operand = [&](int c) { return as_bf16x8(kv_u32x4{pw[4 * c], pw[4 * c + 1], pw[4 * c + 2], pw[4 * c + 3]}); };
         // Scores of as many tiles as make 32 rows leave together, through LDS, whole lines at a time.  (The loads of later tiles are
         // counted in order with the stores, whose way out is long: storing every tile's takes 64 sequences of 512 to 4096
-        // 131 us in place of 129, at heads of 64 83 in place of 81.)  Returns whether it stored four times.
+        // 131 us in place of 129, at heads of 64 83 in place of 81.)  Returns whether it stored four times,
+        // neither fewer nor more: the wait after it leaves as many requests under way.
         auto keep_scores = [&](int i) -> bool {
             if constexpr (SUMS) {
                 const int slots = 32 >> a.group_shift, slot = i & (slots - 1);
@@ -496,7 +520,7 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
                     if (x <= slot && g < G)
                         *reinterpret_cast<f32x4*>(dst + g * a.score_stride + kKeys * (kt0 + i - slot + x) + 4 * (lane & 7)) = s_out[wave][r][lane & 7];
                 }
-                return slot == slots - 1;
+                return slot == slots - 1 && stores_four(G);
             }
             return false;
         };
@@ -1148,7 +1172,7 @@ int common_args(tree_args& a, const void* q, void* out, const void* kv_pool, int
     if (!q || !out || !ctx_lens || !kv_pool || !block_table || n_pool_blocks < 1) return KV_ERR_INVALID_ARG;
     if (block_table_stride < ((int64_t)max_ctx_len + view->block_tokens - 1) / view->block_tokens) return KV_ERR_INVALID_ARG;
     const int d = view->geom.head_dim;
-    if ((d != 64 && d != 128) || view->block_tokens % 16 != 0 || view->group > 32) return KV_ERR_UNSUPPORTED;
+    if ((d != 64 && d != 128) || view->block_tokens % 16 != 0 || view->group > kMostGroup) return KV_ERR_UNSUPPORTED;
     if ((int64_t)view->row_heads * d * 2 * 16 > 0x7fffffff || n_pool_blocks > 0x7fffffff) return KV_ERR_UNSUPPORTED;
     a = tree_args{};
     a.q = (const uint16_t*)q;
