@@ -574,9 +574,14 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
             for (int u = 0; u < 2 * NJ; ++u)
                 o[u % NJ] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[u], weight_operand(u / NJ), o[u % NJ], 0, 0, 0);
         };
+        // The tokens of a tile from first_edge on that this lane's row sees
+        auto seen_of = [&](int tile) -> uint32_t {
+            if constexpr (SUMS) return n - kKeys * tile >= 32 ? ~0u : (1u << (n - kKeys * tile)) - 1u;
+            else return s_seen[tile - first_edge][srow];
+        };
         // Sums of values where a token that a row does not see may hold an infinity or NaN, which its weight of 0 would turn into NaN:
-        // token by token, without those of no weight.
-        auto add_values_one_by_one = [&](const kv_u32x4* sv, const uint32_t* pw) {
+        // token by token, without those.  (One that the row sees counts whatever its weight: 0 times infinity is NaN then.)
+        auto add_values_one_by_one = [&](const kv_u32x4* sv, const uint32_t* pw, uint32_t seen) {
 #pragma unroll 1
             for (int t = 0; t < 32; ++t) {
                 const int u = 2 * (t >> 3) + ((t & 3) >> 1);
@@ -592,7 +597,7 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
 #pragma unroll
                     for (int u4 = 0; u4 < 4; ++u4) {   // elements 32 j + 8 u4 + 4 half ..
                         const kv_u32x2 x = *reinterpret_cast<const kv_u32x2*>(row + (((4 * j + u4) ^ g) << 4) + 8 * half);
-                        if (wt != 0.f) {
+                        if ((seen >> t) & 1) {
                             o[j][4 * u4 + 0] += wt * bf16_lo(x[0]);
                             o[j][4 * u4 + 1] += wt * bf16_hi(x[0]);
                             o[j][4 * u4 + 2] += wt * bf16_lo(x[1]);
@@ -603,10 +608,7 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
         };
         auto hide = [&](int tile) {   // scores of tokens that the row does not see
             if (tile < first_edge) return;
-            uint32_t seen;
-            if constexpr (SUMS) seen = n - kKeys * tile >= 32 ? ~0u : (1u << (n - kKeys * tile)) - 1u;
-            else seen = s_seen[tile - first_edge][srow];
-            seen >>= 4 * half;
+            const uint32_t seen = seen_of(tile) >> (4 * half);
 #pragma unroll
             for (int x = 0; x < 16; ++x) sc[x] = (seen >> (8 * (x >> 2) + (x & 3))) & 1 ? sc[x] : kNegInf;
         };
@@ -619,7 +621,7 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
             exponents();
 #pragma unroll
             for (int u = 0; u < 8; ++u) weights(u);
-            if (decltype(careful)::value && tile >= first_edge) add_values_one_by_one(sv, pw);
+            if (decltype(careful)::value && tile >= first_edge) add_values_one_by_one(sv, pw, seen_of(tile));
             else values(sv);
         };
         // The chain of a tile is cut across tiles: the weights of tile i are made beside the score products of tile i + 1, its
@@ -767,7 +769,8 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
             for (int k = 0; k < KW; ++k) m_all = fmaxf(m_all, s_ml[(k * RW + rw) * 32 + col].x);
 #pragma unroll
             for (int x = 0; x < XW; ++x) acc[x] = f32x4{0.f, 0.f, 0.f, 0.f};
-            // (a wavefront that saw no key has weight 0, whatever its sums are)
+            // (a wavefront that saw no key is left out, whatever its sums are; one that weighs nothing beside the others is not: its sums may
+            // be infinite)
 #pragma unroll 1
             for (int k = 0; k < KW; ++k) {
                 const float2 ml = s_ml[(k * RW + rw) * 32 + col];
@@ -778,7 +781,7 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
                 for (int x = 0; x < XW; ++x) {
                     const f32x4 y = __builtin_bit_cast(f32x4, from_k[x * 64]);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[x][e] = f != 0.f ? __builtin_fmaf(y[e], f, acc[x][e]) : acc[x][e];
+                    for (int e = 0; e < 4; ++e) acc[x][e] = ml.y != 0.f ? __builtin_fmaf(y[e], f, acc[x][e]) : acc[x][e];
                 }
             }
             __syncthreads();   // (before the next piece's tiles land)

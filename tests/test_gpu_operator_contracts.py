@@ -9,6 +9,7 @@ from operator_refs import DP
 from paper_2602_22593_amd import binding as kv
 from paper_2602_22593_amd import workloads as wl
 
+from helpers import bf16_bits_to_f64
 from test_gpu_operators import DEV, dev, host, view_of, within
 
 pytestmark = pytest.mark.gpu
@@ -40,4 +41,67 @@ def test_weights_of_every_group_size(group, heads, ctx, bound, d):
     weights = dev(prior)
     out = kv.paged_decode_attn_weights(dev(c.q), dev(c.pool), dev(wide_table(c, bound)), dev(c.ctx), view_of(c), bound, weights)
     within(host(out), want, tol)
+    assert (np.abs(host(weights).astype(np.float64) - sums) <= sums_tol).all()
+
+
+def set_token(c, s, t, key=None, value=None):
+    """Rows of token t of sequence s: a key of one element that counts, values of every third element; in the pool and in the logical arrays."""
+    rows, _ = ref.view_rows(c, c.pool)
+    b, slot = ref.place(c, s, t)
+    a = int(c.seq_off[s]) + t
+    if key is not None:
+        for k in (rows[b, 0, slot], c.K[a]):
+            k[...] = 0
+            k[..., 0] = key
+    if value is not None:
+        for v in (rows[b, 1, slot], c.V[a]):
+            v[..., ::3] = value
+
+
+EIGHT, FAR, INF, NAN = 0x4100, 0xC40E, 0x7F80, 0x7FC0      # 8, -568: scores of -400 at 128 elements, -568 at 64
+
+
+@pytest.mark.parametrize("bad", [INF, NAN])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("bound,q_lens", [(100, [20, 45, 7]), (400000, [8, 3, 7]), (400000, [16, 1, 7]), (400000, [64, 45, 31])])
+def test_a_tree_row_meets_what_it_sees(bound, q_lens, d, bad):
+    """An infinity or NaN in the values of a drafted token reaches the rows that see it however little it weighs: a weight past the
+    smallest number times infinity is no number.  Rows that do not see it are as without it."""
+    ctx = [100, 45, 31]
+    c = ref.case((16, 4, d, 16), (DP, 1, 0), ctx, q_lens, index=81)
+    c.q[:, :, 0] = EIGHT
+    seen = np.random.default_rng(38).random((len(c.q), 64)) < 0.5
+    for s in range(3):
+        node = int(c.q_lens[s]) // 2
+        set_token(c, s, int(c.ctx[s] - c.q_lens[s]) + node, FAR, bad)
+        if c.q_lens[s] > 1:
+            seen[c.q_off[s]:c.q_off[s + 1], node - 1] = True      # (another one, of ordinary weight)
+    hit = np.array([seen[r, int(c.q_lens[s]) // 2] for s in range(3) for r in range(int(c.q_off[s]), int(c.q_off[s + 1]))])
+    want, tol = ref.tree_attention(c, seen)
+    got = bf16_bits_to_f64(host(kv.paged_tree_attn(dev(c.q), dev(c.pool), dev(wide_table(c, bound)), dev(c.ctx),
+                                                       dev(c.q_off.astype(np.int32)), dev(ref.pack(seen)), view_of(c), bound, max(q_lens))))
+    assert hit.any() and not hit.all()
+    keep = np.arange(d) % 3 != 0
+    assert (np.abs(got[~hit] - want[~hit]) <= tol[~hit]).all()
+    assert (np.abs(got[hit] - want[hit]) <= tol[hit])[:, :, keep].all() and not np.isfinite(got[hit][:, :, ::3]).any()
+
+
+@pytest.mark.parametrize("bad", [INF, NAN])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("heads,bound", [(2, 1000), (4, WIDE)])
+@pytest.mark.parametrize("low", [32, 64, 256])
+def test_a_decode_row_meets_every_value(low, heads, bound, d, bad):
+    """The same with sums of weights: tokens that weigh nothing, a tile, a wavefront's share or a whole piece of them, one with such values."""
+    c = decode_case((4 * heads, heads, d, 16), [1000, 400], index=82)
+    c.q[:, :, 0] = EIGHT
+    for t in range(low):
+        set_token(c, 0, t, FAR)
+    set_token(c, 0, 10, value=bad)
+    prior = np.zeros((2, heads, bound), np.float32)
+    want, tol, sums, sums_tol = ref.decode_weights(c, prior)
+    weights = dev(prior)
+    out = kv.paged_decode_attn_weights(dev(c.q), dev(c.pool), dev(wide_table(c, bound)), dev(c.ctx), view_of(c), bound, weights)
+    got, keep = bf16_bits_to_f64(host(out)), np.arange(d) % 3 != 0
+    assert (np.abs(got - want) <= tol)[:, :, keep].all() and (np.abs(got[1] - want[1]) <= tol[1]).all()
+    assert not np.isfinite(got[0][:, ::3]).any()
     assert (np.abs(host(weights).astype(np.float64) - sums) <= sums_tol).all()
