@@ -389,7 +389,7 @@ int paged_tree_attn(const void* q, void* out, const void* kv_pool, int64_t n_poo
  *                  none) or not below q_len[s] moves nothing
  *   n_accepted     device, int32 [batch], at most accepted_stride and q_len[s] (more counts as that)
  *   new_lens       device, int32 [batch], written: ctx_lens[s] - q_len[s] + n_accepted[s]; may be null,
- *                  must not be ctx_lens
+ *                  must not overlap ctx_lens, q_offsets, accepted or n_accepted
  * No block may belong to two sequences of the call, unless nothing in it moves.
  * Errors: KV_ERR_INVALID_ARG, KV_ERR_HIP.
  */
@@ -432,7 +432,7 @@ int paged_decode_attn_weights(const void* q, void* out, const void* kv_pool, int
  *   weights_out, token_pos_out  device, [batch][n_kv_local][out_stride]: the arrays as they are afterwards, entries
  *                  below min(k, out_stride) written; may be weights and token_pos themselves (only what moves is
  *                  written then, and out_stride must be stride)
- *   new_lens       device, int32 [batch], written: k; may be null, must not be ctx_lens or keep_lens
+ *   new_lens       device, int32 [batch], written: k; may be null, must not overlap ctx_lens, keep_lens or next_pos
  *   workspace      at least kv_evict_workspace_bytes(...) bytes, 256-byte aligned; contents need not be
  *                  initialised
  * No block may belong to two sequences of the call, unless nothing in it moves (a prompt that several share is

@@ -574,7 +574,11 @@ extern "C" int kv_accept(void* kv_pool, int64_t n_pool_blocks, const kv_view* vi
 {
     if (!kv_view_ok(view) || n_pool_blocks < 0 || block_table_stride < 0 || accepted_stride < 0 || batch < 0) return KV_ERR_INVALID_ARG;
     if (batch == 0) return KV_OK;
-    if (!kv_pool || !block_table || !ctx_lens || !q_offsets || !accepted || !n_accepted || new_lens == ctx_lens) return KV_ERR_INVALID_ARG;
+    if (!kv_pool || !block_table || !ctx_lens || !q_offsets || !accepted || !n_accepted) return KV_ERR_INVALID_ARG;
+    // (a sequence's workgroups all read what one of them would overwrite)
+    if (new_lens && (kv_words_meet(new_lens, batch, ctx_lens, batch) || kv_words_meet(new_lens, batch, q_offsets, (int64_t)batch + 1) ||
+                     kv_words_meet(new_lens, batch, n_accepted, batch) || kv_words_meet(new_lens, batch, accepted, batch * accepted_stride)))
+        return KV_ERR_INVALID_ARG;
     accept_args a = {};
     a.pool = (uint16_t*)kv_pool;
     a.n_pool_blocks = n_pool_blocks;
@@ -608,8 +612,10 @@ extern "C" int kv_evict(void* kv_pool, int64_t n_pool_blocks, const kv_view* vie
     if (!kv_view_ok(view) || n_pool_blocks < 0 || block_table_stride < 0 || batch < 0 || max_ctx_len < 0 || sinks < 0 || recent < 0)
         return KV_ERR_INVALID_ARG;
     if (batch == 0) return KV_OK;
-    if (!kv_pool || !block_table || !ctx_lens || !keep_lens || !weights || !token_pos || !next_pos || !weights_out || !token_pos_out ||
-        new_lens == ctx_lens || new_lens == keep_lens)
+    if (!kv_pool || !block_table || !ctx_lens || !keep_lens || !weights || !token_pos || !next_pos || !weights_out || !token_pos_out)
+        return KV_ERR_INVALID_ARG;
+    if (new_lens && (kv_words_meet(new_lens, batch, ctx_lens, batch) || kv_words_meet(new_lens, batch, keep_lens, batch) ||
+                     kv_words_meet(new_lens, batch, next_pos, batch)))
         return KV_ERR_INVALID_ARG;
     if (stride < max_ctx_len || out_stride < 0 || ((weights_out == weights || token_pos_out == token_pos) && out_stride != stride) ||
         block_table_stride < ((int64_t)max_ctx_len + view->block_tokens - 1) / view->block_tokens)

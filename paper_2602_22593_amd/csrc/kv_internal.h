@@ -79,6 +79,13 @@ __device__ __forceinline__ void kv_split_token(const kv_view_dev& v, int t, int&
 
 int kv_record_hip_error(hipError_t e, const char* what);
 
+// Whether two arrays of so many 32-bit words have one in common.
+static inline bool kv_words_meet(const void* a, int64_t n_a, const void* b, int64_t n_b)
+{
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    return x < y + 4 * (uintptr_t)n_b && y < x + 4 * (uintptr_t)n_a;
+}
+
 // Library-wide tunables (kv_set_option).
 int64_t kv_option_chunk_tokens();
 int64_t kv_option_force_kernel();
