@@ -369,7 +369,8 @@ int kv_rope_append(void* kv_pool, int64_t n_pool_blocks, const kv_view* view, co
  * Other arguments as paged_prefill_attn, max_q_len <= 256.  Infinities and NaN in the K or V of a drafted
  * token reach the rows that see it and no others.  Errors: KV_ERR_INVALID_ARG (null pointers, negative sizes,
  * max_q_len > max_ctx_len, block_table_stride or mask_words too small), KV_ERR_UNSUPPORTED (head_dim not 64 or
- * 128, group size above 32, block capacity not a multiple of 16, max_q_len > 256), KV_ERR_WORKSPACE, KV_ERR_HIP.
+ * 128, group size above 32, block capacity not a multiple of 16, max_q_len > 256, kv_pool or q not 16-byte aligned,
+ * out not 8-byte aligned), KV_ERR_WORKSPACE, KV_ERR_HIP.
  */
 size_t paged_tree_attn_workspace_bytes(const kv_view* view, int batch, int64_t total_q, int max_ctx_len,
                                        int max_q_len);
@@ -391,7 +392,7 @@ int paged_tree_attn(const void* q, void* out, const void* kv_pool, int64_t n_poo
  *   new_lens       device, int32 [batch], written: ctx_lens[s] - q_len[s] + n_accepted[s]; may be null,
  *                  must not overlap ctx_lens, q_offsets, accepted or n_accepted
  * No block may belong to two sequences of the call, unless nothing in it moves.
- * Errors: KV_ERR_INVALID_ARG, KV_ERR_HIP.
+ * Errors: KV_ERR_INVALID_ARG, KV_ERR_UNSUPPORTED (kv_pool not 16-byte aligned), KV_ERR_HIP.
  */
 int kv_accept(void* kv_pool, int64_t n_pool_blocks, const kv_view* view, const int32_t* block_table,
               int64_t block_table_stride, const int32_t* ctx_lens, const int32_t* q_offsets,
@@ -438,7 +439,7 @@ int paged_decode_attn_weights(const void* q, void* out, const void* kv_pool, int
  * No block may belong to two sequences of the call, unless nothing in it moves (a prompt that several share is
  * copied first).  A row whose block lies outside the pool is not moved.
  * Errors: KV_ERR_INVALID_ARG (null pointers, negative sizes, strides too small), KV_ERR_UNSUPPORTED (max_ctx_len
- * above 2^24), KV_ERR_WORKSPACE, KV_ERR_HIP.
+ * above 2^24, kv_pool not 16-byte aligned), KV_ERR_WORKSPACE, KV_ERR_HIP.
  */
 size_t kv_evict_workspace_bytes(const kv_view* view, int batch, int max_ctx_len);
 int kv_evict(void* kv_pool, int64_t n_pool_blocks, const kv_view* view, const int32_t* block_table,

@@ -579,6 +579,7 @@ extern "C" int kv_accept(void* kv_pool, int64_t n_pool_blocks, const kv_view* vi
     if (new_lens && (kv_words_meet(new_lens, batch, ctx_lens, batch) || kv_words_meet(new_lens, batch, q_offsets, (int64_t)batch + 1) ||
                      kv_words_meet(new_lens, batch, n_accepted, batch) || kv_words_meet(new_lens, batch, accepted, batch * accepted_stride)))
         return KV_ERR_INVALID_ARG;
+    if (!kv_aligned(kv_pool, 16)) return KV_ERR_UNSUPPORTED;
     accept_args a = {};
     a.pool = (uint16_t*)kv_pool;
     a.n_pool_blocks = n_pool_blocks;
@@ -620,7 +621,7 @@ extern "C" int kv_evict(void* kv_pool, int64_t n_pool_blocks, const kv_view* vie
     if (stride < max_ctx_len || out_stride < 0 || ((weights_out == weights || token_pos_out == token_pos) && out_stride != stride) ||
         block_table_stride < ((int64_t)max_ctx_len + view->block_tokens - 1) / view->block_tokens)
         return KV_ERR_INVALID_ARG;
-    if (max_ctx_len > (1 << 24) || batch > 65535 || view->n_kv_local > 65535) return KV_ERR_UNSUPPORTED;
+    if (!kv_aligned(kv_pool, 16) || max_ctx_len > (1 << 24) || batch > 65535 || view->n_kv_local > 65535) return KV_ERR_UNSUPPORTED;
     if (max_ctx_len > 0) {
         if (!workspace || ((uintptr_t)workspace & 255u)) return KV_ERR_INVALID_ARG;
         if (workspace_bytes < kv_evict_workspace_bytes(view, batch, max_ctx_len)) return KV_ERR_WORKSPACE;

@@ -79,6 +79,8 @@ __device__ __forceinline__ void kv_split_token(const kv_view_dev& v, int t, int&
 
 int kv_record_hip_error(hipError_t e, const char* what);
 
+static inline bool kv_aligned(const void* p, unsigned bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
+
 // Whether two arrays of so many 32-bit words have one in common.
 static inline bool kv_words_meet(const void* a, int64_t n_a, const void* b, int64_t n_b)
 {

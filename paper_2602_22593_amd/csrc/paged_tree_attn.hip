@@ -1176,6 +1176,7 @@ int common_args(tree_args& a, const void* q, void* out, const void* kv_pool, int
     if (block_table_stride < ((int64_t)max_ctx_len + view->block_tokens - 1) / view->block_tokens) return KV_ERR_INVALID_ARG;
     const int d = view->geom.head_dim;
     if ((d != 64 && d != 128) || view->block_tokens % 16 != 0 || view->group > kMostGroup) return KV_ERR_UNSUPPORTED;
+    if (!kv_aligned(kv_pool, 16) || !kv_aligned(q, 16) || !kv_aligned(out, 8)) return KV_ERR_UNSUPPORTED;
     if ((int64_t)view->row_heads * d * 2 * 16 > 0x7fffffff || n_pool_blocks > 0x7fffffff) return KV_ERR_UNSUPPORTED;
     a = tree_args{};
     a.q = (const uint16_t*)q;

@@ -27,3 +27,14 @@ def at(x):
 ])
 def test_new_lengths_meet_no_input(name, changed):
     assert call(name, **changed) == INVALID
+
+
+@pytest.mark.parametrize("name,changed", [
+    *[("paged_tree_attn", {x: at(256 + by)}) for x, by in (("kv_pool", 8), ("q", 8), ("q", 2), ("out", 4))],
+    *[("paged_decode_attn_weights", {x: at(256 + by)}) for x, by in (("kv_pool", 8), ("kv_pool", 2), ("q", 8), ("out", 4))],
+    ("kv_accept", dict(kv_pool=at(264))),
+    ("kv_evict", dict(kv_pool=at(258))),
+])
+def test_addresses_are_those_of_whole_pieces(name, changed):
+    """Rows are moved 16 bytes at a time and output 8."""
+    assert call(name, **changed) == kv.KV_ERR_UNSUPPORTED
