@@ -1130,8 +1130,9 @@ tree_plan plan_tree(const kv_view* view, int batch, int64_t total_q, int max_ctx
     // 64 and sequences of 1000 to 8000, 8 of them 60.8 / 57.3, 32 253 / 220; drafts of 1 to 64 51.3 / 54.6, 152 / 175; drafts of 150 to
     // 256, 4 of them 92 / 101, 32 743 / 654.  (On average 130, 194 and 812 rows; 160 lies between.)
     if (rows > 128 && total_q * view->group > 160 * (int64_t)batch && cache_bytes(view, batch, max_ctx_len) > kCacheBytes) p = p8;
-    // A workspace asked for with larger bounds serves smaller calls, whatever their variant
-    p.bytes = std::max({p.bytes, p4.bytes, p8.bytes});
+    // A workspace asked for with larger bounds serves smaller calls, whatever their variant.  (Teams are rounded down to whole ones: of 12
+    // heads two side by side leave 85 x 64 rows each, one 42 x 128.)
+    p.bytes = std::max({p.bytes, p4.bytes, p8.bytes, view->n_kv_local % 2 == 0 ? plan_with(view, batch, max_ctx_len, rows, 2, 2).bytes : 0});
     return p;
 }
 

@@ -38,3 +38,17 @@ def test_new_lengths_meet_no_input(name, changed):
 def test_addresses_are_those_of_whole_pieces(name, changed):
     """Rows are moved 16 bytes at a time and output 8."""
     assert call(name, **changed) == kv.KV_ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("heads", [1, 2, 3, 4, 5, 6, 7, 10, 12, 14, 18, 20, 22, 24, 36, 40, 52, 100, 300, 1030])
+@pytest.mark.parametrize("d", [64, 128])
+def test_workspaces_of_any_number_of_heads_serve_smaller_calls(heads, d):
+    """The variants cut the work into numbers of shares that round differently: a larger bound never asks for less."""
+    v = kv.kv_view_create(4 * heads, heads, d, 16, kv.KV_LAYOUT_DP, 1, 0)
+    bounds = [(b, n) for b in (1, 3, 64, 65, 200) for n in (64, 1000, 8192, 131072)]
+    tree = {(b, n, q): kv.paged_tree_attn_workspace_bytes(v, b, b * q, n, q) for b, n in bounds for q in (1, 8, 9, 16, 17, 32, 33, 64) if q <= n}
+    weights = {x: kv.paged_decode_attn_weights_workspace_bytes(v, *x) for x in bounds}
+    evict = {x: kv.kv_evict_workspace_bytes(v, *x) for x in bounds}
+    for sizes in (tree, weights, evict):
+        for x, need in sizes.items():
+            assert all(given >= need for y, given in sizes.items() if all(j >= i for i, j in zip(x, y))), x
