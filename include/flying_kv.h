@@ -439,7 +439,7 @@ int paged_decode_attn_weights(const void* q, void* out, const void* kv_pool, int
  * No block may belong to two sequences of the call, unless nothing in it moves (a prompt that several share is
  * copied first).  A row whose block lies outside the pool is not moved.
  * Errors: KV_ERR_INVALID_ARG (null pointers, negative sizes, strides too small), KV_ERR_UNSUPPORTED (max_ctx_len
- * above 2^24, kv_pool not 16-byte aligned), KV_ERR_WORKSPACE, KV_ERR_HIP.
+ * above 2^24, or max_ctx_len * head_dim near 2^34 and above, kv_pool not 16-byte aligned), KV_ERR_WORKSPACE, KV_ERR_HIP.
  */
 size_t kv_evict_workspace_bytes(const kv_view* view, int batch, int max_ctx_len);
 int kv_evict(void* kv_pool, int64_t n_pool_blocks, const kv_view* view, const int32_t* block_table,

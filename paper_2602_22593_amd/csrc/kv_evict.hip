@@ -516,7 +516,7 @@ __global__ __launch_bounds__(kThreads) void evict_move_kernel(evict_args a)
     const int32_t* table = a.table + (int64_t)s * a.table_stride;
     const int row_pieces = v.head_dim / 8, per_move = 2 * row_pieces;   // 16-byte pieces of K and V
     constexpr int kUnroll = 2;   // (four in half as many workgroups: 24 us in place of 22 for 60 MB)
-    const int total = count * per_move;   // (a list is shorter than 2^24)
+    const int total = count * per_move;   // (the host keeps it below 2^31 by more than a step)
     for (int x0 = (int)blockIdx.x * kThreads * kUnroll + tid; x0 < total; x0 += (int)gridDim.x * kThreads * kUnroll) {
         kv_u32x4 val[kUnroll];
         int64_t to[kUnroll];
@@ -621,7 +621,9 @@ extern "C" int kv_evict(void* kv_pool, int64_t n_pool_blocks, const kv_view* vie
     if (stride < max_ctx_len || out_stride < 0 || ((weights_out == weights || token_pos_out == token_pos) && out_stride != stride) ||
         block_table_stride < ((int64_t)max_ctx_len + view->block_tokens - 1) / view->block_tokens)
         return KV_ERR_INVALID_ARG;
-    if (!kv_aligned(kv_pool, 16) || max_ctx_len > (1 << 24) || batch > 65535 || view->n_kv_local > 65535) return KV_ERR_UNSUPPORTED;
+    // (a list holds half of the tokens; evict_move_kernel counts 16-byte pieces of K and V, and goes past the end by a step of all its workgroups, 2^21)
+    const int64_t most_pieces = ((int64_t)max_ctx_len / 2 + 1) * (view->geom.head_dim / 4);
+    if (!kv_aligned(kv_pool, 16) || most_pieces > 0x7f000000 || max_ctx_len > (1 << 24) || batch > 65535 || view->n_kv_local > 65535) return KV_ERR_UNSUPPORTED;
     if (max_ctx_len > 0) {
         if (!workspace || ((uintptr_t)workspace & 255u)) return KV_ERR_INVALID_ARG;
         if (workspace_bytes < kv_evict_workspace_bytes(view, batch, max_ctx_len)) return KV_ERR_WORKSPACE;

@@ -52,3 +52,9 @@ def test_workspaces_of_any_number_of_heads_serve_smaller_calls(heads, d):
     for sizes in (tree, weights, evict):
         for x, need in sizes.items():
             assert all(given >= need for y, given in sizes.items() if all(j >= i for i, j in zip(x, y))), x
+
+
+@pytest.mark.parametrize("d,status", [(1024, kv.KV_ERR_UNSUPPORTED), (4096, kv.KV_ERR_UNSUPPORTED), (512, kv.KV_ERR_WORKSPACE)])
+def test_evictions_that_32_bits_count(d, status):
+    """A head's rows that move are numbered by their 16-byte pieces in 32 bits; what passes that is refused."""
+    assert call("kv_evict", view=view(8, 8, d), max_ctx=1 << 24, w_stride=1 << 24, out_stride=1 << 24, stride=1 << 20, ws_bytes=64) == status
