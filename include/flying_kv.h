@@ -384,7 +384,8 @@ int paged_tree_attn(const void* q, void* out, const void* kv_pool, int64_t n_poo
  * kv_accept -- keep the accepted ones of the drafted tokens (after paged_tree_attn and the caller's
  * verification): the K and V rows of drafted token accepted[s][i], i < n_accepted[s], are moved to
  * token ctx_lens[s] - q_len[s] + i of the sequence, for all heads of the view, so that the accepted
- * tokens follow the cache in order.  What lies behind them is left as it is.
+ * tokens follow the cache in order.  What lies behind them is left as it is, and so are arrays with a value per token:
+ * where token_pos or weights are kept for the sequences (kv_evict goes by them), kv_accept_tracked moves their entries too.
  *   accepted       device, int32 [batch][accepted_stride]: numbers of drafted tokens, each row strictly
  *                  ascending, in [0, q_len[s]).  An entry below its own index (in an ascending row there is
  *                  none) or not below q_len[s] moves nothing
@@ -398,6 +399,17 @@ int kv_accept(void* kv_pool, int64_t n_pool_blocks, const kv_view* view, const i
               int64_t block_table_stride, const int32_t* ctx_lens, const int32_t* q_offsets,
               const int32_t* accepted, int64_t accepted_stride, const int32_t* n_accepted, int batch,
               int32_t* new_lens, void* hip_stream);
+/*
+ * kv_accept_tracked -- kv_accept, and for every row that moves the entries of its token in
+ *   token_pos      device, int32 [batch][n_kv_local][token_pos_stride], or null
+ *   weights        device, fp32 [batch][n_kv_local][weights_stride], or null
+ * Entries from the stride on are none and move nothing.  Errors as kv_accept, KV_ERR_INVALID_ARG for negative strides.
+ */
+int kv_accept_tracked(void* kv_pool, int64_t n_pool_blocks, const kv_view* view, const int32_t* block_table,
+                      int64_t block_table_stride, const int32_t* ctx_lens, const int32_t* q_offsets,
+                      const int32_t* accepted, int64_t accepted_stride, const int32_t* n_accepted, int batch,
+                      int32_t* new_lens, int32_t* token_pos, int64_t token_pos_stride, float* weights,
+                      int64_t weights_stride, void* hip_stream);
 
 /*
  * paged_decode_attn_weights -- paged_decode_attn that also adds up, per KV head, how much attention

@@ -81,6 +81,7 @@ def lib() -> C.CDLL:
     L.paged_tree_attn.argtypes = [vp, vp, vp, i64, vp, i64, vp, vp, vp, i64, C.c_int, i64, C.c_int, C.c_int, vp, C.c_float,
                                   vp, C.c_size_t, vp]
     L.kv_accept.argtypes = [vp, i64, vp, vp, i64, vp, vp, vp, i64, vp, C.c_int, vp, vp]
+    L.kv_accept_tracked.argtypes = [vp, i64, vp, vp, i64, vp, vp, vp, i64, vp, C.c_int, vp, vp, i64, vp, i64, vp]
     L.paged_decode_attn_weights_workspace_bytes.argtypes = [vp, C.c_int, C.c_int]
     L.paged_decode_attn_weights_workspace_bytes.restype = C.c_size_t
     L.paged_decode_attn_weights.argtypes = [vp, vp, vp, i64, vp, i64, vp, C.c_int, C.c_int, vp, C.c_float, vp, i64, vp,
@@ -210,7 +211,7 @@ def _calls():
         m.setup(tuple(C.cast(f, C.c_void_p).value for f in functions),
                 (torch.Tensor, torch.nn.Parameter, kv_weight_view), (_BF16, torch.int32, torch.uint8),
                 (torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream), _workspaces)
-        operators = (L.kv_rope_append, L.kv_accept, L.paged_tree_attn, L.paged_decode_attn_weights)
+        operators = (L.kv_rope_append, L.kv_accept_tracked, L.paged_tree_attn, L.paged_decode_attn_weights)
         m.setup_operators(tuple(C.cast(f, C.c_void_p).value for f in operators), (torch.float32, _WORDS))
         _calls_module = m
     return _calls_module
@@ -502,6 +503,11 @@ def _per_token(t: torch.Tensor, view: KVView, batch: int, dtype, name: str) -> i
     return _dev(t, (dtype,), name)
 
 
+def _kept_per_token(t: Optional[torch.Tensor], view: KVView, batch: int, dtype, name: str):
+    """Address and tokens of such an array, or of none."""
+    return (None, 0) if t is None else (_per_token(t, view, batch, dtype, name), int(t.shape[2]))
+
+
 def _token_rows(t: torch.Tensor, total: int, heads: int, d: int, name: str):
     """Rows [total][heads][d] whose tokens may lie apart: address and elements between tokens."""
     if not t.is_cuda:
@@ -553,8 +559,7 @@ def kv_rope_append(kv_pool: torch.Tensor, view: KVView, q: torch.Tensor, k: torc
             _shaped(out, (total, view.n_q_local, d), _BF16, "out"), pos_ptr, total, n_axes, freq_ptr, 2 * half, axes, pairs,
             _table(block_table, batch), block_table.stride(0), _ints(ctx_lens, batch, "ctx_lens"),
             None if q_offsets is None else _ints(q_offsets, batch + 1, "q_offsets"), batch, total,
-            None if token_pos is None else _per_token(token_pos, view, batch, torch.int32, "token_pos"),
-            0 if token_pos is None else int(token_pos.shape[2]))
+            *_kept_per_token(token_pos, view, batch, torch.int32, "token_pos"))
     _check(_launch(device, stream, lambda st: lib().kv_rope_append(*args, st)), "kv_rope_append")
     return out
 
@@ -598,18 +603,19 @@ def paged_tree_attn(q: torch.Tensor, kv_pool: torch.Tensor, block_table: torch.T
 
 
 def kv_accept(kv_pool: torch.Tensor, view: KVView, block_table: torch.Tensor, ctx_lens: torch.Tensor, q_offsets: torch.Tensor,
-              accepted: torch.Tensor, n_accepted: torch.Tensor, new_lens: Optional[torch.Tensor] = None,
-              stream=None) -> torch.Tensor:
+              accepted: torch.Tensor, n_accepted: torch.Tensor, new_lens: Optional[torch.Tensor] = None, stream=None, *,
+              token_pos: Optional[torch.Tensor] = None, weights: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Move the K and V rows of the accepted drafted tokens (int32 [batch][n], ascending numbers in the draft) behind the cache,
-    in order; returns the new lengths."""
+    in order; returns the new lengths.  ``token_pos`` (int32) and ``weights`` (fp32, both [batch][n_kv_local][tokens]), where they
+    are kept, move along."""
     if new_lens is not None:
         rc = (_calls_module or _calls()).accept(kv_pool, view, block_table, ctx_lens, q_offsets, accepted, n_accepted, new_lens,
-                                                stream)
+                                                stream, token_pos, weights)
         if rc is not None:
             _check(rc, "kv_accept")
             return new_lens
     batch = int(ctx_lens.shape[0])
-    device = _one_device(kv_pool, block_table, ctx_lens, q_offsets, accepted, n_accepted, new_lens)
+    device = _one_device(kv_pool, block_table, ctx_lens, q_offsets, accepted, n_accepted, new_lens, token_pos, weights)
     if accepted.dim() != 2 or accepted.shape[0] != batch:
         raise ValueError(f"accepted has shape {tuple(accepted.shape)}, expected [{batch}, n]")
     if new_lens is None:
@@ -617,8 +623,9 @@ def kv_accept(kv_pool: torch.Tensor, view: KVView, block_table: torch.Tensor, ct
     args = (_dev(kv_pool, _BF16, "kv_pool"), _blocks_of(kv_pool, view), view.handle, _table(block_table, batch),
             block_table.stride(0), _ints(ctx_lens, batch, "ctx_lens"), _ints(q_offsets, batch + 1, "q_offsets"),
             _dev(accepted, (torch.int32,), "accepted"), int(accepted.shape[1]), _ints(n_accepted, batch, "n_accepted"), batch,
-            _ints(new_lens, batch, "new_lens"))
-    _check(_launch(device, stream, lambda st: lib().kv_accept(*args, st)), "kv_accept")
+            _ints(new_lens, batch, "new_lens"), *_kept_per_token(token_pos, view, batch, torch.int32, "token_pos"),
+            *_kept_per_token(weights, view, batch, torch.float32, "weights"))
+    _check(_launch(device, stream, lambda st: lib().kv_accept_tracked(*args, st)), "kv_accept")
     return new_lens
 
 

@@ -31,7 +31,7 @@ typedef int (*rope_fn)(void*, int64_t, const kv_view*, const void*, int64_t, con
                        const int32_t*, int64_t, int, const float*, int, const int32_t*, int, const int32_t*, int64_t,
                        const int32_t*, const int32_t*, int, int64_t, int32_t*, int64_t, void*);
 typedef int (*accept_fn)(void*, int64_t, const kv_view*, const int32_t*, int64_t, const int32_t*, const int32_t*, const int32_t*,
-                         int64_t, const int32_t*, int, int32_t*, void*);
+                         int64_t, const int32_t*, int, int32_t*, int32_t*, int64_t, float*, int64_t, void*);
 typedef int (*tree_fn)(const void*, void*, const void*, int64_t, const int32_t*, int64_t, const int32_t*, const int32_t*,
                        const uint64_t*, int64_t, int, int64_t, int, int, const kv_view*, float, void*, size_t, void*);
 typedef int (*weights_fn)(const void*, void*, const void*, int64_t, const int32_t*, int64_t, const int32_t*, int, int,
@@ -405,13 +405,25 @@ static int cache_of(PyObject* pool, PyObject* view, PyObject* table, PyObject* c
            ask_int(pool, n_get_device, NULL, &on) && on == c->device && pool_blocks(pool, c->bb, 1, &c->blocks);
 }
 
+/* binding._kept_per_token: [batch][n_kv_local][tokens], or none */
+static int kept_per_token(PyObject* t, PyObject* dtype, const cache_args* c, void** out, int64_t* tokens)
+{
+    int64_t size[3] = {c->batch, c->hkv, -1};
+    *out = NULL;
+    *tokens = 0;
+    if (t == Py_None) return 1;
+    if (!shaped(t, dtype, c->device, 3, size, out)) return 0;
+    *tokens = size[2];
+    return 1;
+}
+
 /* rope(kv_pool, view, q, k, v, positions, inv_freq, block_table, ctx_lens, q_offsets, axes, pairs, out, token_pos, stream) */
 static PyObject* call_rope(PyObject* self, PyObject* const* a, Py_ssize_t nargs)
 {
     ARGS(15)
     enum { kMost = 128 };
-    int64_t q[3], q_row, k_row, v_row, pos[2] = {-1, -1}, half = -1, off, out[3], per[3] = {0, 0, 0}, pairs, stream;
-    void *pq, *pk, *pv, *pout, *ppos, *pfreq, *poff = NULL, *pper = NULL;
+    int64_t q[3], q_row, k_row, v_row, pos[2] = {-1, -1}, half = -1, off, out[3], per, pairs, stream;
+    void *pq, *pk, *pv, *pout, *ppos, *pfreq, *poff = NULL, *pper;
     int32_t axes[kMost];
     cache_args c;
     int rc = 0, n_axes = 1;
@@ -445,28 +457,23 @@ static PyObject* call_rope(PyObject* self, PyObject* const* a, Py_ssize_t nargs)
         off = c.batch + 1;
         ok = shaped(a[9], int32_type, c.device, 1, &off, &poff);
     }
-    if (ok && a[13] != Py_None) {
-        per[0] = c.batch;
-        per[1] = c.hkv;
-        per[2] = -1;
-        ok = shaped(a[13], int32_type, c.device, 3, per, &pper);
-    }
+    ok = ok && kept_per_token(a[13], int32_type, &c, &pper, &per);
     if (ok) {
         Py_BEGIN_ALLOW_THREADS
         rc = f_rope(c.pool, c.blocks, c.view, pq, q_row, pk, k_row, pv, v_row, pout, ppos, q[0], n_axes, pfreq, (int)(2 * half),
-                    a[10] == Py_None ? NULL : axes, (int)pairs, c.table, c.row, c.ctx, poff, (int)c.batch, q[0], pper, per[2],
+                    a[10] == Py_None ? NULL : axes, (int)pairs, c.table, c.row, c.ctx, poff, (int)c.batch, q[0], pper, per,
                     (void*)(uintptr_t)stream);
         Py_END_ALLOW_THREADS
     }
     return answer(ok, rc);
 }
 
-/* accept(kv_pool, view, block_table, ctx_lens, q_offsets, accepted, n_accepted, new_lens, stream) */
+/* accept(kv_pool, view, block_table, ctx_lens, q_offsets, accepted, n_accepted, new_lens, stream, token_pos, weights) */
 static PyObject* call_accept(PyObject* self, PyObject* const* a, Py_ssize_t nargs)
 {
-    ARGS(9)
-    int64_t off, acc[2], n, stream;
-    void *poff, *pacc, *pn, *pnew;
+    ARGS(11)
+    int64_t off, acc[2], n, pos_n, w_n, stream;
+    void *poff, *pacc, *pn, *pnew, *ppos, *pw;
     cache_args c;
     int rc = 0, ok = cache_of(a[0], a[1], a[2], a[3], &c);
     if (ok) {
@@ -475,11 +482,12 @@ static PyObject* call_accept(PyObject* self, PyObject* const* a, Py_ssize_t narg
         acc[1] = -1;
         ok = shaped(a[4], int32_type, c.device, 1, &off, &poff) && shaped(a[5], int32_type, c.device, 2, acc, &pacc) &&
              shaped(a[6], int32_type, c.device, 1, &n, &pn) && shaped(a[7], int32_type, c.device, 1, &n, &pnew) &&
+             kept_per_token(a[9], int32_type, &c, &ppos, &pos_n) && kept_per_token(a[10], float_type, &c, &pw, &w_n) &&
              stream_handle(a[8], NULL, &stream);
     }
     if (ok) {
         Py_BEGIN_ALLOW_THREADS
-        rc = f_accept(c.pool, c.blocks, c.view, c.table, c.row, c.ctx, poff, pacc, acc[1], pn, (int)c.batch, pnew,
+        rc = f_accept(c.pool, c.blocks, c.view, c.table, c.row, c.ctx, poff, pacc, acc[1], pn, (int)c.batch, pnew, ppos, pos_n, pw, w_n,
                       (void*)(uintptr_t)stream);
         Py_END_ALLOW_THREADS
     }

@@ -19,7 +19,8 @@ __device__ __forceinline__ int64_t row_at(const kv_view_dev& v, const int32_t* t
 // ---- kv_accept ---------------------------------------------------------------------------------------
 // Row first + accepted[i] goes to first + i.  The accepted nodes ascend, so a row's new place is never that of a later one's
 // old row: a lane that owns one 16-byte column of the sequence's rows and goes through them in order needs no other's
-// progress, and may request several before it stores them.  Latency is all there is to it: lengths, nodes, table, rows.
+// progress, and may request several before it stores them.  Latency is all there is to it: lengths, nodes, table, rows.  The values
+// per token of a head (its position, its weight) are columns of 4 bytes.
 
 struct accept_args {
     uint16_t* pool;
@@ -29,6 +30,9 @@ struct accept_args {
     const int32_t *ctx_lens, *q_off, *accepted, *n_accepted;
     int64_t accepted_stride;
     int32_t* new_lens;
+    uint32_t* per_token[2];      // [batch][n_kv_local][per_token_stride], the first n_per_token of them
+    int64_t per_token_stride[2];
+    int32_t n_per_token;
     kv_view_dev v;
 };
 constexpr int kMostAccepted = 256;   // rows whose places are worked out at a time
@@ -37,6 +41,7 @@ constexpr int kRowsAhead = 8;
 __global__ __launch_bounds__(kThreads) void kv_accept_kernel(accept_args a)
 {
     __shared__ int64_t s_from[kMostAccepted], s_to[kMostAccepted];
+    __shared__ int s_node[kMostAccepted];
     const kv_view_dev& v = a.v;
     const int s = blockIdx.x, tid = threadIdx.x;
     const int q0 = a.q_off[s], q_len = a.q_off[s + 1] - q0, n = a.ctx_lens[s], first = n - q_len;
@@ -49,6 +54,11 @@ __global__ __launch_bounds__(kThreads) void kv_accept_kernel(accept_args a)
     const bool mine = column < 2 * row_pieces;
     const int plane = column >= row_pieces;
     const int64_t at = plane * v.plane_elems + (int64_t)(column - plane * row_pieces) * 8;
+    // or a column of values per token
+    const int value = column - 2 * row_pieces, which = value >= v.n_kv_local, head = value - which * v.n_kv_local;
+    const bool has_value = !mine && which < a.n_per_token && head < v.n_kv_local;
+    const int64_t value_stride = a.per_token_stride[which];
+    uint32_t* const values = has_value ? a.per_token[which] + ((int64_t)s * v.n_kv_local + head) * value_stride : nullptr;
     for (int i0 = 0; i0 < count; i0 += kMostAccepted) {
         const int m = min(count - i0, kMostAccepted);
         __syncthreads();
@@ -61,8 +71,21 @@ __global__ __launch_bounds__(kThreads) void kv_accept_kernel(accept_args a)
             }
             s_from[tid] = to < 0 ? -1 : from;
             s_to[tid] = to;
+            s_node[tid] = node;
         }
         __syncthreads();
+        if (has_value) {
+            for (int r = 0; r < m; r += kRowsAhead) {
+                uint32_t x[kRowsAhead];
+                auto moves = [&](int u) { return r + u < m && s_from[r + u] >= 0 && first + s_node[r + u] < value_stride; };
+#pragma unroll
+                for (int u = 0; u < kRowsAhead; ++u)
+                    if (moves(u)) x[u] = values[first + s_node[r + u]];
+#pragma unroll
+                for (int u = 0; u < kRowsAhead; ++u)
+                    if (moves(u)) values[first + i0 + r + u] = x[u];   // (its place lies before the old one)
+            }
+        }
         if (!mine) continue;
         for (int r = 0; r < m; r += kRowsAhead) {
             kv_u32x4 x[kRowsAhead];
@@ -572,7 +595,18 @@ extern "C" int kv_accept(void* kv_pool, int64_t n_pool_blocks, const kv_view* vi
                          int64_t block_table_stride, const int32_t* ctx_lens, const int32_t* q_offsets, const int32_t* accepted,
                          int64_t accepted_stride, const int32_t* n_accepted, int batch, int32_t* new_lens, void* hip_stream)
 {
-    if (!kv_view_ok(view) || n_pool_blocks < 0 || block_table_stride < 0 || accepted_stride < 0 || batch < 0) return KV_ERR_INVALID_ARG;
+    return kv_accept_tracked(kv_pool, n_pool_blocks, view, block_table, block_table_stride, ctx_lens, q_offsets, accepted, accepted_stride,
+                             n_accepted, batch, new_lens, nullptr, 0, nullptr, 0, hip_stream);
+}
+
+extern "C" int kv_accept_tracked(void* kv_pool, int64_t n_pool_blocks, const kv_view* view, const int32_t* block_table,
+                                 int64_t block_table_stride, const int32_t* ctx_lens, const int32_t* q_offsets, const int32_t* accepted,
+                                 int64_t accepted_stride, const int32_t* n_accepted, int batch, int32_t* new_lens, int32_t* token_pos,
+                                 int64_t token_pos_stride, float* weights, int64_t weights_stride, void* hip_stream)
+{
+    if (!kv_view_ok(view) || n_pool_blocks < 0 || block_table_stride < 0 || accepted_stride < 0 || batch < 0 || token_pos_stride < 0 ||
+        weights_stride < 0)
+        return KV_ERR_INVALID_ARG;
     if (batch == 0) return KV_OK;
     if (!kv_pool || !block_table || !ctx_lens || !q_offsets || !accepted || !n_accepted) return KV_ERR_INVALID_ARG;
     // (a sequence's workgroups all read what one of them would overwrite)
@@ -592,7 +626,15 @@ extern "C" int kv_accept(void* kv_pool, int64_t n_pool_blocks, const kv_view* vi
     a.n_accepted = n_accepted;
     a.new_lens = new_lens;
     a.v = kv_view_to_dev(view);
-    const int64_t columns = 2 * (int64_t)view->n_kv_local * view->geom.head_dim / 8, parts = (columns + kThreads - 1) / kThreads;
+    if (token_pos) {
+        a.per_token[a.n_per_token] = (uint32_t*)token_pos;
+        a.per_token_stride[a.n_per_token++] = token_pos_stride;
+    }
+    if (weights) {
+        a.per_token[a.n_per_token] = (uint32_t*)weights;
+        a.per_token_stride[a.n_per_token++] = weights_stride;
+    }
+    const int64_t columns = (int64_t)view->n_kv_local * (view->geom.head_dim / 4 + a.n_per_token), parts = (columns + kThreads - 1) / kThreads;
     if (parts > 65535) return KV_ERR_UNSUPPORTED;
     hipLaunchKernelGGL(kv_accept_kernel, dim3((unsigned)batch, (unsigned)parts), dim3(kThreads), 0, (hipStream_t)hip_stream, a);
     return kv_record_hip_error(hipGetLastError(), "kv_accept launch");

@@ -105,3 +105,45 @@ def test_a_decode_row_meets_every_value(low, heads, bound, d, bad):
     assert (np.abs(got - want) <= tol)[:, :, keep].all() and (np.abs(got[1] - want[1]) <= tol[1]).all()
     assert not np.isfinite(got[0][:, ::3]).any()
     assert (np.abs(host(weights).astype(np.float64) - sums) <= sums_tol).all()
+
+
+def accepted_entries(c, nodes, counts, values):
+    """Values per token [batch][heads][tokens] after acceptance."""
+    out = values.copy()
+    for s, k in enumerate(counts):
+        first = int(c.ctx[s] - c.q_lens[s])
+        for i in range(int(k)):
+            if first + nodes[s][i] < values.shape[2]:
+                out[s, :, first + i] = values[s, :, first + nodes[s][i]]
+    return out
+
+
+@pytest.mark.parametrize("through_c", [True, False])
+@pytest.mark.parametrize("geom,triple,ctx,q_lens,counts", [
+    ((8, 2, 64, 16), (DP, 1, 0), [17, 1, 300, 64], [3, 1, 8, 5], [2, 1, 0, 5]),
+    ((32, 8, 128, 16), (DP, 1, 0), [700, 256, 40], [64, 256, 40], [7, 200, 39]),
+    ((32, 8, 128, 16), (ref.TP, 4, 3), [90, 0, 33], [33, 0, 17], [12, 0, 1]),
+    ((32, 8, 128, 16), (DP, 2, 1), [300], [300], [270]),
+    ((6, 2, 96, 5), (ref.TP, 2, 1), [23, 9], [11, 9], [4, 6]),
+    ((300, 300, 64, 16), (DP, 1, 0), [40], [20], [9]),              # values per token of many workgroups
+])
+def test_acceptance_moves_what_is_kept_per_token(geom, triple, ctx, q_lens, counts, through_c):
+    c = ref.case(geom, triple, ctx, q_lens, index=83)
+    rng, hl = np.random.default_rng(39), c.info["n_kv_local"]
+    nodes = np.full((len(ctx), max(counts) + 2), -1, np.int32)
+    for s, k in enumerate(counts):
+        nodes[s, :k] = np.sort(rng.permutation(int(c.q_lens[s]))[:k])
+    pos = rng.integers(0, 1 << 30, (len(ctx), hl, max(ctx) + 3)).astype(np.int32)
+    w = rng.random((len(ctx), hl, max(max(ctx) - 6, 1))).astype(np.float32)       # (some places have no entry)
+    want, lens = ref.accepted_pool(c, c.pool, nodes, counts)
+    args = (view_of(c), dev(c.table), dev(c.ctx), dev(c.q_off.astype(np.int32)), dev(nodes), dev(np.asarray(counts, np.int32)))
+    for token_pos, weights in ((pos, w), (pos, None), (None, w)):
+        pool, kept = dev(c.pool), [None if x is None else dev(x) for x in (token_pos, weights)]
+        new = torch.zeros(len(ctx), dtype=torch.int32, device=DEV) if through_c else None
+        got = kv.kv_accept(pool, *args, new_lens=new, token_pos=kept[0], weights=kept[1])
+        assert np.array_equal(host(pool).reshape(want.shape), want) and np.array_equal(host(got), lens)
+        for x, y in zip(kept, (token_pos, weights)):
+            if x is not None:
+                assert np.array_equal(host(x), accepted_entries(c, nodes, counts, y))
+    with pytest.raises(ValueError, match="token_pos"):
+        kv.kv_accept(dev(c.pool), *args, new_lens=torch.zeros(len(ctx), dtype=torch.int32, device=DEV), token_pos=dev(pos).long())

@@ -58,3 +58,18 @@ def test_workspaces_of_any_number_of_heads_serve_smaller_calls(heads, d):
 def test_evictions_that_32_bits_count(d, status):
     """A head's rows that move are numbered by their 16-byte pieces in 32 bits; what passes that is refused."""
     assert call("kv_evict", view=view(8, 8, d), max_ctx=1 << 24, w_stride=1 << 24, out_stride=1 << 24, stride=1 << 20, ws_bytes=64) == status
+
+
+@pytest.mark.parametrize("changed,status", [
+    *[({x: -1}, INVALID) for x in ("n_pool_blocks", "stride", "acc_stride", "batch", "pos_stride", "w_stride")],
+    *[({x: None}, INVALID) for x in ("kv_pool", "view", "block_table", "ctx", "q_off", "accepted", "n_accepted")],
+    (dict(n_accepted=at(512)), INVALID),
+    (dict(batch=0, kv_pool=None), kv.KV_OK),
+])
+def test_accept_tracked_refusals(changed, status):
+    v = view()
+    args = dict(kv_pool=FAKE, n_pool_blocks=10, view=v.handle, block_table=FAKE, stride=64, ctx=FAKE, q_off=FAKE, accepted=FAKE, acc_stride=4,
+                n_accepted=FAKE, batch=2, new_lens=at(512), token_pos=FAKE, pos_stride=100, weights=FAKE, w_stride=100, st=None)
+    assert set(changed) <= set(args)
+    args.update(changed)
+    assert kv.lib().kv_accept_tracked(*args.values()) == status
