@@ -353,6 +353,19 @@ int kv_rope_append(void* kv_pool, int64_t n_pool_blocks, const kv_view* view, co
                    int rotary_dim, const int32_t* axis_of_pair, int pairs, const int32_t* block_table,
                    int64_t block_table_stride, const int32_t* ctx_lens, const int32_t* q_offsets, int batch,
                    int64_t total, int32_t* token_pos, int64_t token_pos_stride, void* hip_stream);
+/*
+ * kv_rope_append_tracked -- kv_rope_append, and for every token written
+ *   weights        device, fp32 [batch][n_kv_local][weights_stride], or null: 0 at its place (nothing has attended to it;
+ *                  places from weights_stride on are left out), for paged_decode_attn_weights
+ * Errors as kv_rope_append, KV_ERR_INVALID_ARG for a negative weights_stride.
+ */
+int kv_rope_append_tracked(void* kv_pool, int64_t n_pool_blocks, const kv_view* view, const void* q, int64_t q_stride,
+                           const void* k, int64_t k_stride, const void* v, int64_t v_stride, void* q_out,
+                           const int32_t* positions, int64_t position_stride, int n_axes, const float* inv_freq,
+                           int rotary_dim, const int32_t* axis_of_pair, int pairs, const int32_t* block_table,
+                           int64_t block_table_stride, const int32_t* ctx_lens, const int32_t* q_offsets, int batch,
+                           int64_t total, int32_t* token_pos, int64_t token_pos_stride, float* weights,
+                           int64_t weights_stride, void* hip_stream);
 
 /*
  * paged_tree_attn -- attention for speculative decoding with a tree of drafted tokens.  The last
@@ -416,8 +429,10 @@ int kv_accept_tracked(void* kv_pool, int64_t n_pool_blocks, const kv_view* view,
  * weight every cached token gets (what kv_evict goes by):
  *     w[t] = sum over the G query heads of KV head h of softmax_t(scale * q . K[t])
  *     weights[s][h][t] += w[t] for t < ctx_lens[s] - 1;   weights[s][h][ctx_lens[s] - 1] = w[t]
- * The newest token's entry is set, not added to, so that a place in the cache may be used again without
- * clearing anything; entries from ctx_lens[s] on are not touched.
+ * The newest token's entry is set, not added to: where tokens are appended one by one with a call after each, a
+ * place in the cache may be used again without clearing anything.  Of tokens that came several at a time (a prompt,
+ * accepted drafts) the entries have to be 0 before the first call after: kv_rope_append_tracked sets them as it
+ * writes the tokens.  Entries from ctx_lens[s] on are not touched.
  *   weights        device, fp32 [batch][n_kv_local][weights_stride], weights_stride >= max_ctx_len
  *   workspace      at least paged_decode_attn_weights_workspace_bytes(...) bytes (4 bytes per query head
  *                  and token of the bound, and some MB), 256-byte aligned; contents need not be initialised

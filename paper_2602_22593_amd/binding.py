@@ -76,6 +76,7 @@ def lib() -> C.CDLL:
     L.kv_append.argtypes = [vp, i64, vp, vp, vp, vp, i64, vp, C.c_int, vp]
     L.kv_rope_append.argtypes = [vp, i64, vp, vp, i64, vp, i64, vp, i64, vp, vp, i64, C.c_int, vp, C.c_int, vp, C.c_int, vp,
                                  i64, vp, vp, C.c_int, i64, vp, i64, vp]
+    L.kv_rope_append_tracked.argtypes = L.kv_rope_append.argtypes[:-1] + [vp, i64, vp]
     L.paged_tree_attn_workspace_bytes.argtypes = [vp, C.c_int, i64, C.c_int, C.c_int]
     L.paged_tree_attn_workspace_bytes.restype = C.c_size_t
     L.paged_tree_attn.argtypes = [vp, vp, vp, i64, vp, i64, vp, vp, vp, i64, C.c_int, i64, C.c_int, C.c_int, vp, C.c_float,
@@ -211,7 +212,7 @@ def _calls():
         m.setup(tuple(C.cast(f, C.c_void_p).value for f in functions),
                 (torch.Tensor, torch.nn.Parameter, kv_weight_view), (_BF16, torch.int32, torch.uint8),
                 (torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream), _workspaces)
-        operators = (L.kv_rope_append, L.kv_accept_tracked, L.paged_tree_attn, L.paged_decode_attn_weights)
+        operators = (L.kv_rope_append_tracked, L.kv_accept_tracked, L.paged_tree_attn, L.paged_decode_attn_weights)
         m.setup_operators(tuple(C.cast(f, C.c_void_p).value for f in operators), (torch.float32, _WORDS))
         _calls_module = m
     return _calls_module
@@ -524,22 +525,24 @@ def _token_rows(t: torch.Tensor, total: int, heads: int, d: int, name: str):
 def kv_rope_append(kv_pool: torch.Tensor, view: KVView, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
                    positions: torch.Tensor, inv_freq: torch.Tensor, block_table: torch.Tensor, ctx_lens: torch.Tensor,
                    q_offsets: Optional[torch.Tensor] = None, axes=None, pairs: int = KV_ROPE_HALVES,
-                   out: Optional[torch.Tensor] = None, token_pos: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+                   out: Optional[torch.Tensor] = None, token_pos: Optional[torch.Tensor] = None, stream=None, *,
+                   weights: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Rotate the new tokens' q and k by their positions; q is returned, k and v go into the pool through ``view``.
 
     q [total][n_q_local][d], k and v [total][n_kv_local][d] (tokens may lie apart: the parts of a fused QKV row serve);
     positions int32 [total] or [axes][total]; inv_freq fp32, one per pair; ``axes`` the axis of each pair (a sequence of
     ints on the host).  ``q_offsets`` int32 [batch + 1], or None for one token per sequence; the new tokens are the last of
-    ctx_lens.  ``token_pos`` int32 [batch][n_kv_local][tokens] gets the positions on axis 0 of what is written.
+    ctx_lens.  ``token_pos`` int32 [batch][n_kv_local][tokens] gets the positions on axis 0 of what is written,
+    ``weights`` (fp32, same shape) zeros: what paged_decode_attn_weights adds to and kv_evict goes by.
     """
     if out is not None:
         rc = (_calls_module or _calls()).rope(kv_pool, view, q, k, v, positions, inv_freq, block_table, ctx_lens, q_offsets, axes,
-                                              pairs, out, token_pos, stream)
+                                              pairs, out, token_pos, stream, weights)
         if rc is not None:
             _check(rc, "kv_rope_append")
             return out
     batch, total, d = int(ctx_lens.shape[0]), int(q.shape[0]), view.head_dim
-    device = _one_device(q, k, v, kv_pool, positions, inv_freq, block_table, ctx_lens, q_offsets, out, token_pos)
+    device = _one_device(q, k, v, kv_pool, positions, inv_freq, block_table, ctx_lens, q_offsets, out, token_pos, weights)
     q_ptr, q_stride = _token_rows(q, total, view.n_q_local, d, "q")
     k_ptr, k_stride = _token_rows(k, total, view.n_kv_local, d, "k")
     v_ptr, v_stride = _token_rows(v, total, view.n_kv_local, d, "v")
@@ -559,8 +562,8 @@ def kv_rope_append(kv_pool: torch.Tensor, view: KVView, q: torch.Tensor, k: torc
             _shaped(out, (total, view.n_q_local, d), _BF16, "out"), pos_ptr, total, n_axes, freq_ptr, 2 * half, axes, pairs,
             _table(block_table, batch), block_table.stride(0), _ints(ctx_lens, batch, "ctx_lens"),
             None if q_offsets is None else _ints(q_offsets, batch + 1, "q_offsets"), batch, total,
-            *_kept_per_token(token_pos, view, batch, torch.int32, "token_pos"))
-    _check(_launch(device, stream, lambda st: lib().kv_rope_append(*args, st)), "kv_rope_append")
+            *_kept_per_token(token_pos, view, batch, torch.int32, "token_pos"), *_kept_per_token(weights, view, batch, torch.float32, "weights"))
+    _check(_launch(device, stream, lambda st: lib().kv_rope_append_tracked(*args, st)), "kv_rope_append")
     return out
 
 
@@ -637,7 +640,7 @@ def paged_decode_attn_weights(q: torch.Tensor, kv_pool: torch.Tensor, block_tabl
                               view: KVView, max_ctx_len: int, weights: torch.Tensor, out: Optional[torch.Tensor] = None,
                               scale: float = 0.0, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """paged_decode_attn that also adds the attention weight of every cached token, summed over the query heads of its KV head,
-    to ``weights`` (fp32 [batch][n_kv_local][tokens]; the newest token's entry is set)."""
+    to ``weights`` (fp32 [batch][n_kv_local][tokens]; the newest token's entry is set, those of others that are new have to be 0)."""
     if out is not None and workspace is not None:
         rc = (_calls_module or _calls()).weights(q, kv_pool, block_table, ctx_lens, view, max_ctx_len, weights, out, scale, workspace,
                                                  stream)

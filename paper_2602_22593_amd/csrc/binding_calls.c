@@ -29,7 +29,7 @@ typedef int (*repack_fn)(void*, int64_t, const kv_view*, const kv_view*, const i
 
 typedef int (*rope_fn)(void*, int64_t, const kv_view*, const void*, int64_t, const void*, int64_t, const void*, int64_t, void*,
                        const int32_t*, int64_t, int, const float*, int, const int32_t*, int, const int32_t*, int64_t,
-                       const int32_t*, const int32_t*, int, int64_t, int32_t*, int64_t, void*);
+                       const int32_t*, const int32_t*, int, int64_t, int32_t*, int64_t, float*, int64_t, void*);
 typedef int (*accept_fn)(void*, int64_t, const kv_view*, const int32_t*, int64_t, const int32_t*, const int32_t*, const int32_t*,
                          int64_t, const int32_t*, int, int32_t*, int32_t*, int64_t, float*, int64_t, void*);
 typedef int (*tree_fn)(const void*, void*, const void*, int64_t, const int32_t*, int64_t, const int32_t*, const int32_t*,
@@ -417,13 +417,13 @@ static int kept_per_token(PyObject* t, PyObject* dtype, const cache_args* c, voi
     return 1;
 }
 
-/* rope(kv_pool, view, q, k, v, positions, inv_freq, block_table, ctx_lens, q_offsets, axes, pairs, out, token_pos, stream) */
+/* rope(kv_pool, view, q, k, v, positions, inv_freq, block_table, ctx_lens, q_offsets, axes, pairs, out, token_pos, stream, weights) */
 static PyObject* call_rope(PyObject* self, PyObject* const* a, Py_ssize_t nargs)
 {
-    ARGS(15)
+    ARGS(16)
     enum { kMost = 128 };
-    int64_t q[3], q_row, k_row, v_row, pos[2] = {-1, -1}, half = -1, off, out[3], per, pairs, stream;
-    void *pq, *pk, *pv, *pout, *ppos, *pfreq, *poff = NULL, *pper;
+    int64_t q[3], q_row, k_row, v_row, pos[2] = {-1, -1}, half = -1, off, out[3], per, w_n, pairs, stream;
+    void *pq, *pk, *pv, *pout, *ppos, *pfreq, *poff = NULL, *pper, *pw;
     int32_t axes[kMost];
     cache_args c;
     int rc = 0, n_axes = 1;
@@ -457,12 +457,12 @@ static PyObject* call_rope(PyObject* self, PyObject* const* a, Py_ssize_t nargs)
         off = c.batch + 1;
         ok = shaped(a[9], int32_type, c.device, 1, &off, &poff);
     }
-    ok = ok && kept_per_token(a[13], int32_type, &c, &pper, &per);
+    ok = ok && kept_per_token(a[13], int32_type, &c, &pper, &per) && kept_per_token(a[15], float_type, &c, &pw, &w_n);
     if (ok) {
         Py_BEGIN_ALLOW_THREADS
         rc = f_rope(c.pool, c.blocks, c.view, pq, q_row, pk, k_row, pv, v_row, pout, ppos, q[0], n_axes, pfreq, (int)(2 * half),
                     a[10] == Py_None ? NULL : axes, (int)pairs, c.table, c.row, c.ctx, poff, (int)c.batch, q[0], pper, per,
-                    (void*)(uintptr_t)stream);
+                    pw, w_n, (void*)(uintptr_t)stream);
         Py_END_ALLOW_THREADS
     }
     return answer(ok, rc);

@@ -37,6 +37,8 @@ struct rope_args {
     const int32_t *ctx_lens, *q_off;
     int32_t* token_pos;                     // [batch][n_kv_local][token_pos_stride] or null
     int64_t token_pos_stride;
+    float* weights;                         // [batch][n_kv_local][weights_stride] or null
+    int64_t weights_stride;
     int64_t total;
     kv_view_dev v;
     int32_t batch, pairs, adjacent, tokens;
@@ -89,6 +91,8 @@ __global__ __launch_bounds__(kThreads) void kv_rope_append_kernel(rope_args a)
                 if (place >= 0 && a.token_pos && t < a.token_pos_stride)
                     for (int h = lane; h < v.n_kv_local; h += 64)
                         a.token_pos[((int64_t)s * v.n_kv_local + h) * a.token_pos_stride + t] = a.positions[i];
+                if (place >= 0 && a.weights && t < a.weights_stride)
+                    for (int h = lane; h < v.n_kv_local; h += 64) a.weights[((int64_t)s * v.n_kv_local + h) * a.weights_stride + t] = 0.f;
             }
         }
         if (lane == 0) s_place[x] = place;
@@ -156,8 +160,21 @@ extern "C" int kv_rope_append(void* kv_pool, int64_t n_pool_blocks, const kv_vie
                               int64_t block_table_stride, const int32_t* ctx_lens, const int32_t* q_offsets, int batch,
                               int64_t total, int32_t* token_pos, int64_t token_pos_stride, void* hip_stream)
 {
+    return kv_rope_append_tracked(kv_pool, n_pool_blocks, view, q, q_stride, k, k_stride, v, v_stride, q_out, positions, position_stride, n_axes,
+                                  inv_freq, rotary_dim, axis_of_pair, pairs, block_table, block_table_stride, ctx_lens, q_offsets, batch, total,
+                                  token_pos, token_pos_stride, nullptr, 0, hip_stream);
+}
+
+extern "C" int kv_rope_append_tracked(void* kv_pool, int64_t n_pool_blocks, const kv_view* view, const void* q, int64_t q_stride,
+                                      const void* k, int64_t k_stride, const void* v, int64_t v_stride, void* q_out,
+                                      const int32_t* positions, int64_t position_stride, int n_axes, const float* inv_freq,
+                                      int rotary_dim, const int32_t* axis_of_pair, int pairs, const int32_t* block_table,
+                                      int64_t block_table_stride, const int32_t* ctx_lens, const int32_t* q_offsets, int batch,
+                                      int64_t total, int32_t* token_pos, int64_t token_pos_stride, float* weights,
+                                      int64_t weights_stride, void* hip_stream)
+{
     if (!kv_view_ok(view) || n_pool_blocks < 0 || block_table_stride < 0 || batch < 0 || total < 0 || rotary_dim < 0 ||
-        position_stride < 0 || token_pos_stride < 0 || (pairs != KV_ROPE_HALVES && pairs != KV_ROPE_ADJACENT) || n_axes < 1)
+        position_stride < 0 || token_pos_stride < 0 || weights_stride < 0 || (pairs != KV_ROPE_HALVES && pairs != KV_ROPE_ADJACENT) || n_axes < 1)
         return KV_ERR_INVALID_ARG;
     const int d = view->geom.head_dim, half = rotary_dim / 2;
     if (rotary_dim > d || position_stride < total || (!q_offsets && total != batch)) return KV_ERR_INVALID_ARG;
@@ -191,6 +208,8 @@ extern "C" int kv_rope_append(void* kv_pool, int64_t n_pool_blocks, const kv_vie
     a.q_off = q_offsets;
     a.token_pos = token_pos;
     a.token_pos_stride = token_pos_stride;
+    a.weights = weights;
+    a.weights_stride = weights_stride;
     a.total = total;
     a.v = kv_view_to_dev(view);
     a.batch = batch;

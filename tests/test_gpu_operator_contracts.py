@@ -10,6 +10,7 @@ from paper_2602_22593_amd import binding as kv
 from paper_2602_22593_amd import workloads as wl
 
 from helpers import bf16_bits_to_f64
+from test_gpu_operator_runs import read_back
 from test_gpu_operators import DEV, dev, host, view_of, within
 
 pytestmark = pytest.mark.gpu
@@ -147,3 +148,90 @@ def test_acceptance_moves_what_is_kept_per_token(geom, triple, ctx, q_lens, coun
                 assert np.array_equal(host(x), accepted_entries(c, nodes, counts, y))
     with pytest.raises(ValueError, match="token_pos"):
         kv.kv_accept(dev(c.pool), *args, new_lens=torch.zeros(len(ctx), dtype=torch.int32, device=DEV), token_pos=dev(pos).long())
+
+
+def longest_path(seen):
+    """Nodes of the deepest path of a tree: bool [nodes][nodes], a row for each."""
+    return max((np.flatnonzero(row[:len(seen)]) for row in seen), key=len)
+
+
+@pytest.mark.parametrize("through_c", [True, False])
+@pytest.mark.parametrize("geom,triple", [((32, 8, 128, 16), (ref.TP, 2, 1)), ((8, 2, 64, 16), (DP, 1, 0))])
+def test_drafts_on_a_budget(geom, triple, through_c):
+    """Prompts, then steps that draft, verify, accept several tokens, decode one with sums of weights, and go back to the budget in place.
+    Arrays per token start as they come: whatever was there, and whatever evicted tokens left, counts for nothing."""
+    start, steps, q_lens = np.array([70, 41, 9], np.int32), 7, np.array([9, 14, 5], np.int32)
+    budget, sinks, recent = np.array([60, 45, 30]), 2, 12
+    c = ref.case(geom, triple, start + steps * (q_lens + 1), q_lens, index=84)
+    hl, ql, d = c.info["n_kv_local"], c.info["n_q_local"], geom[2]
+    view, most, rng, g = view_of(c), int(c.ctx.max()), np.random.default_rng(40), wl.generator(85, wl.SUB_MISC)
+    pool, table, freq = dev(c.pool), dev(c.table), dev((1e4 ** (-np.arange(d // 2) / (d // 2))).astype(np.float32))
+    weights = torch.full((3, hl, most), 1e6, device=DEV)
+    token_pos = torch.full((3, hl, most), 1 << 29, dtype=torch.int32, device=DEV)
+    model = host(weights)                       # of weights: verified values, zeros where tokens were written
+
+    def append(lens, counts, positions):
+        total = int(counts.sum())
+        x = dev(wl.randn_bf16((total, ql + 2 * hl, d), g))
+        out = torch.zeros((total, ql, d), dtype=torch.bfloat16, device=DEV) if through_c else None
+        off = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+        for s in range(3):
+            model[s, :, lens[s] - counts[s]:lens[s]] = 0
+        return kv.kv_rope_append(pool, view, x[:, :ql], x[:, ql:ql + hl], x[:, ql + hl:], dev(positions.astype(np.int32)), freq, table,
+                                 dev(lens.astype(np.int32)), dev(off), out=out, token_pos=token_pos, weights=weights)
+
+    append(start, start, np.concatenate([np.arange(k) for k in start]))
+    lens, next_pos, evictions = start.astype(np.int64), start.astype(np.int64), 0
+    for step in range(steps):
+        seen, words = ref.tree_masks(q_lens, rng)
+        trees = [seen[a:a + k, :k] for a, k in zip(c.q_off, q_lens)]
+        q = append(lens + q_lens, q_lens, np.concatenate([next_pos[s] + trees[s].sum(axis=1) - 1 for s in range(3)]))
+        c.ctx, c.q = (lens + q_lens).astype(np.int32), host(q)
+        read_back(c, pool)
+        n, off = dev(c.ctx), dev(c.q_off.astype(np.int32))
+        within(host(kv.paged_tree_attn(q, pool, table, n, off, dev(words), view, most, int(q_lens.max()))), *ref.tree_attention(c, seen), f"step {step}")
+        paths = [longest_path(x) for x in trees]
+        counts = np.array([len(x) for x in paths], np.int32)
+        nodes = np.zeros((3, counts.max()), np.int32)
+        for s, x in enumerate(paths):
+            nodes[s, :len(x)] = x
+        before = host(pool).reshape(c.pool.shape)
+        new = kv.kv_accept(pool, view, table, n, off, dev(nodes), dev(counts), token_pos=token_pos, weights=weights,
+                           new_lens=torch.zeros(3, dtype=torch.int32, device=DEV) if through_c else None)
+        want_pool, want_lens = ref.accepted_pool(c, before, nodes, counts)
+        assert np.array_equal(host(pool).reshape(before.shape), want_pool) and np.array_equal(host(new), want_lens)
+        lens, next_pos = want_lens + 1, next_pos + counts + 1
+        q = append(lens, np.ones(3, np.int32), next_pos - 1)
+        c.ctx, c.q = lens.astype(np.int32), host(q)
+        read_back(c, pool)
+        kv.paged_decode_attn_weights(q, pool, table, dev(c.ctx), view, most, weights)
+        _, _, sums, sums_tol = ref.decode_weights(c, model)
+        model, pos = host(weights), host(token_pos)
+        for s in range(3):
+            here = slice(0, int(lens[s]))
+            assert (np.abs(model[s, :, here].astype(np.float64) - sums[s, :, here]) <= sums_tol[s, :, here]).all(), (step, s)
+            for h in range(hl):           # every token is there once, the recent ones and the first ones without a gap
+                there = set(pos[s, h, here].tolist())
+                assert len(there) == lens[s] and set(range(max(next_pos[s] - recent, 0), next_pos[s])) | set(range(sinks)) <= there
+                assert max(there) == next_pos[s] - 1
+        if (lens > budget).any():
+            keep = np.minimum(lens, budget).astype(np.int32)
+            kv.kv_evict(pool, view, table, dev(c.ctx), dev(keep), weights, token_pos, dev(next_pos.astype(np.int32)), most, sinks=sinks, recent=recent)
+            _, w2, p2, _ = ref.evicted(c, host(pool).reshape(c.pool.shape), keep, model, pos, next_pos, sinks, recent)
+            assert np.array_equal(host(weights), w2) and np.array_equal(host(token_pos), p2)
+            model, lens, evictions = host(weights), keep.astype(np.int64), evictions + 1
+    assert evictions >= 4
+
+
+def test_append_clears_the_weights_of_what_it_writes():
+    """Entries of other tokens stay, and those of tokens without a place in the pool or in the array."""
+    c = ref.case((8, 2, 64, 16), (DP, 1, 0), [20, 20, 20, 40], [1, 1, 1, 30], index=86)
+    ctx, table = c.ctx.copy(), c.table.copy()
+    ctx[0], table[1, 1], table[2, 1] = 0, -1, len(c.pool)
+    qkv = dev(wl.randn_bf16((33, 12, 64), wl.generator(87, wl.SUB_MISC)))
+    weights = torch.full((4, 2, 25), 3.0, device=DEV)
+    kv.kv_rope_append(dev(c.pool), view_of(c), qkv[:, :8], qkv[:, 8:10], qkv[:, 10:], dev(np.arange(33, dtype=np.int32)),
+                      dev(np.ones(32, np.float32)), dev(table), dev(ctx), dev(c.q_off.astype(np.int32)), weights=weights)
+    want = np.full((4, 2, 25), 3.0, np.float32)
+    want[3, :, 10:] = 0
+    assert np.array_equal(host(weights), want)

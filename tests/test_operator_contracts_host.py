@@ -73,3 +73,18 @@ def test_accept_tracked_refusals(changed, status):
     assert set(changed) <= set(args)
     args.update(changed)
     assert kv.lib().kv_accept_tracked(*args.values()) == status
+
+
+@pytest.mark.parametrize("changed,status", [
+    *[({x: -1}, INVALID) for x in ("n_pool_blocks", "stride", "batch", "total", "pos_stride", "w_stride")],
+    *[({x: None}, INVALID) for x in ("kv_pool", "view", "q", "ctx")],
+    (dict(batch=0, total=0, q=None), kv.KV_OK),
+])
+def test_rope_append_tracked_refusals(changed, status):
+    v = view()
+    args = dict(kv_pool=FAKE, n_pool_blocks=10, view=v.handle, q=FAKE, q_stride=6144, k=FAKE, k_stride=6144, v=FAKE, v_stride=6144, q_out=at(512),
+                positions=FAKE, position_stride=9, n_axes=1, inv_freq=FAKE, rotary_dim=128, axes=None, pairs=0, table=FAKE, stride=64, ctx=FAKE,
+                q_off=FAKE, batch=2, total=9, token_pos=FAKE, pos_stride=100, weights=FAKE, w_stride=100, st=None)
+    assert set(changed) <= set(args)
+    args.update(changed)
+    assert kv.lib().kv_rope_append_tracked(*args.values()) == status
