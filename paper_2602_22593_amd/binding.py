@@ -181,6 +181,7 @@ def _dev_rows(t: torch.Tensor, dtypes, name: str) -> int:
 _BF16 = (torch.bfloat16, torch.int16, torch.uint16)
 _WORDS = (torch.int64, torch.uint64)
 _workspaces = {}
+_captured_workspaces = {}
 _calls_module = None
 
 
@@ -211,7 +212,7 @@ def _calls():
                      L.kv_linear_view_workspace_bytes, L.kv_append, L.kv_repack)
         m.setup(tuple(C.cast(f, C.c_void_p).value for f in functions),
                 (torch.Tensor, torch.nn.Parameter, kv_weight_view), (_BF16, torch.int32, torch.uint8),
-                (torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream), _workspaces)
+                (torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, torch._C._cuda_isCurrentStreamCapturing), _workspaces)
         operators = (L.kv_rope_append_tracked, L.kv_accept_tracked, L.paged_tree_attn, L.paged_decode_attn_weights)
         m.setup_operators(tuple(C.cast(f, C.c_void_p).value for f in operators), (torch.float32, _WORDS))
         _calls_module = m
@@ -226,7 +227,10 @@ def _workspace(device, nbytes: int, stream=None, kind: str = "scratch") -> torch
     """Scratch for a call that was given none: one buffer per (device, stream, kind), grown on demand.
     Calls on one stream are ordered and may share it; calls on different streams get their own.
     Decode calls (kind "decode") keep a buffer to themselves: its leading arrival words must stay
-    zero between calls, and the other entry points write their scratch from the first byte on."""
+    zero between calls, and the other entry points write their scratch from the first byte on.
+    A buffer that a graph was captured with is kept for good, also when a larger one takes its place: replays
+    write to it.  Graphs captured on one stream share its buffer: replay them one after the other, or give them
+    workspaces of their own."""
     if device.type != "cuda":
         raise ValueError(f"Expected a cuda device, but got: {device}")
     handle = torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
@@ -237,6 +241,8 @@ def _workspace(device, nbytes: int, stream=None, kind: str = "scratch") -> torch
         with torch.cuda.stream(torch.cuda.current_stream(device) if stream is None else stream):
             ws = torch.zeros(max(nbytes, 1 << 20), dtype=torch.uint8, device=device)
         _workspaces[key] = ws
+    if torch._C._cuda_isCurrentStreamCapturing():
+        _captured_workspaces[ws.data_ptr()] = ws
     return ws
 
 

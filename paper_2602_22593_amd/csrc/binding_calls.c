@@ -53,7 +53,7 @@ static weights_fn f_weights;
 static PyObject *tensor_type, *parameter_type, *weight_view_type;   /* exact types only */
 static PyObject *bf16_types, *int32_type, *uint8_type;              /* dtypes: a tuple, and two */
 static PyObject *float_type, *word_types;                           /* float32; the two of 64-bit masks */
-static PyObject *get_device, *raw_stream, *workspaces;              /* of torch._C; the binding's dict */
+static PyObject *get_device, *raw_stream, *is_capturing, *workspaces;   /* of torch._C; the binding's dict */
 static PyObject *n_is_cuda, *n_dtype, *n_is_contiguous, *n_data_ptr, *n_shape, *n_stride, *n_numel, *n_element_size,
     *n_get_device, *n_cuda_stream, *n_handle, *n_value, *n_block_bytes, *n_n_q_local, *n_n_kv_local, *n_head_dim, *n_scratch,
     *n_zero, *n_one, *n_two;
@@ -188,14 +188,18 @@ static int stream_handle(PyObject* stream, PyObject* device, int64_t* out)
     return to_int64(h, out);
 }
 
-/* The workspace: as given, or the binding's own of that device and stream where it is large enough.  A new reference. */
+/* The workspace: as given, or the binding's own of that device and stream where it is large enough and no graph is being
+ * captured (the Python code keeps what a graph saw).  A new reference. */
 static int workspace(PyObject* ws, PyObject* on, PyObject* stream, size_t need, PyObject** keep, void** out, size_t* bytes)
 {
     int64_t n;
     *keep = NULL;
     if (ws == Py_None) {
-        PyObject *device = ask(on, n_get_device, NULL), *h = NULL, *key = NULL;
+        PyObject *capturing = PyObject_CallNoArgs(is_capturing), *device, *h = NULL, *key = NULL;
         int64_t handle;
+        Py_XDECREF(capturing);
+        if (capturing != Py_False) return 0;
+        device = ask(on, n_get_device, NULL);
         if (device && stream_handle(stream, device, &handle)) h = PyLong_FromLongLong(handle);
         if (h) key = PyTuple_Pack(3, device, h, n_scratch);
         ws = key ? PyDict_GetItemWithError(workspaces, key) : NULL;
@@ -572,9 +576,9 @@ static PyObject* setup_operators(PyObject* self, PyObject* args)
 static PyObject* setup(PyObject* self, PyObject* args)
 {
     unsigned long long f[7];
-    PyObject *t0, *t1, *t2, *bf, *i32, *u8, *gd, *rs, *ws;
-    if (!PyArg_ParseTuple(args, "(KKKKKKK)(OOO)(OOO)(OO)O!", f, f + 1, f + 2, f + 3, f + 4, f + 5, f + 6, &t0, &t1, &t2, &bf, &i32,
-                          &u8, &gd, &rs, &PyDict_Type, &ws))
+    PyObject *t0, *t1, *t2, *bf, *i32, *u8, *gd, *rs, *ic, *ws;
+    if (!PyArg_ParseTuple(args, "(KKKKKKK)(OOO)(OOO)(OOO)O!", f, f + 1, f + 2, f + 3, f + 4, f + 5, f + 6, &t0, &t1, &t2, &bf, &i32,
+                          &u8, &gd, &rs, &ic, &PyDict_Type, &ws))
         return NULL;
     f_decode = (decode_fn)(uintptr_t)f[0];
     f_prefill = (prefill_fn)(uintptr_t)f[1];
@@ -584,9 +588,9 @@ static PyObject* setup(PyObject* self, PyObject* args)
     f_append = (append_fn)(uintptr_t)f[5];
     f_repack = (repack_fn)(uintptr_t)f[6];
     PyObject** const to[] = {&tensor_type, &parameter_type, &weight_view_type, &bf16_types, &int32_type, &uint8_type,
-                             &get_device,  &raw_stream,     &workspaces};
-    PyObject* const from[] = {t0, t1, t2, bf, i32, u8, gd, rs, ws};
-    for (int i = 0; i < 9; ++i) {
+                             &get_device,  &raw_stream,     &is_capturing,     &workspaces};
+    PyObject* const from[] = {t0, t1, t2, bf, i32, u8, gd, rs, ic, ws};
+    for (int i = 0; i < 10; ++i) {
         Py_INCREF(from[i]);
         Py_XSETREF(*to[i], from[i]);
     }

@@ -235,3 +235,44 @@ def test_append_clears_the_weights_of_what_it_writes():
     want = np.full((4, 2, 25), 3.0, np.float32)
     want[3, :, 10:] = 0
     assert np.array_equal(host(weights), want)
+
+
+@pytest.mark.parametrize("call", ["tree", "weights", "prefill"])
+def test_workspace_of_a_graph_outlives_a_larger_one(call):
+    """A call without a workspace is captured on a stream; then an eager call there needs more.  The graph still writes to its own."""
+    c = ref.case((8, 2, 128, 16), (DP, 1, 0), [2000, 700], [9, 30], index=88)
+    view, words = view_of(c), dev(ref.tree_masks(c.q_lens, np.random.default_rng(41))[1])
+    q, pool, table, n, off = dev(c.q), dev(c.pool), dev(wide_table(c, WIDE)), dev(c.ctx), dev(c.q_off.astype(np.int32))
+    weights, out = torch.zeros((2, 2, WIDE), device=DEV), torch.zeros_like(q)
+
+    def run(bound, out):
+        if call == "tree":
+            return kv.paged_tree_attn(q, pool, table, n, off, words, view, bound, 30, out=out)
+        if call == "prefill":
+            return kv.paged_prefill_attn(q, pool, table, n, off, view, bound, 30, out=out)
+        return kv.paged_decode_attn_weights(q[:2], pool, table, n, view, bound, weights, out=out[:2])
+
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    key = (0, side.cuda_stream, "scratch")
+    kv._workspaces.pop(key, None)
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        kv._workspace(q.device, 1 << 21)                # what an eager call before left, of an ordinary size
+        run(2000, out)
+        want = host(out)
+        with torch.cuda.graph(graph, stream=side):
+            run(2000, out)
+        mine = kv._workspaces[key]
+        address, size = mine.data_ptr(), mine.numel()
+        del mine
+        kv._workspace(q.device, size + (1 << 20))       # a larger call comes
+        assert kv._workspaces[key].data_ptr() != address
+        others = [torch.full((size,), 0x5a, dtype=torch.uint8, device=DEV) for _ in range(4)]
+        assert all(not x.data_ptr() <= address < x.data_ptr() + size for x in others)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        out.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert np.array_equal(host(out), want) and all(bool((x == 0x5a).all()) for x in others)
