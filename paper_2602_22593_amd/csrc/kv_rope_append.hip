@@ -37,12 +37,12 @@ struct rope_args {
     const int32_t *ctx_lens, *q_off;
     int32_t* token_pos;                     // [batch][n_kv_local][token_pos_stride] or null
     int64_t token_pos_stride;
-    float* weights;                         // [batch][n_kv_local][weights_stride] or null
-    int64_t weights_stride;
     int64_t total;
     kv_view_dev v;
     int32_t batch, pairs, adjacent, tokens;
     uint32_t axis[kMostPairs / 16];         // two bits a pair
+    float* weights;                         // [batch][n_kv_local][weights_stride], where the kernel has them
+    int64_t weights_stride;
 };
 
 // The sequence whose rows hold row i, or -1: the last one that starts at or before it, 64 probes at a time (all lanes alike).
@@ -61,6 +61,9 @@ __device__ __forceinline__ int row_sequence(const rope_args& a, int64_t i, int l
     return a.q_off[s] <= i && i < a.q_off[s + 1] ? s : -1;
 }
 
+// WEIGHTS: also clears the weights of the tokens written (a kernel of its own: the chain before the rows grows by it, 80.3 us for the prompts
+// above become 82.0).
+template <bool WEIGHTS>
 __global__ __launch_bounds__(kThreads) void kv_rope_append_kernel(rope_args a)
 {
     __shared__ float2 s_turn[kMostTokens][kMostPairs];
@@ -91,7 +94,7 @@ __global__ __launch_bounds__(kThreads) void kv_rope_append_kernel(rope_args a)
                 if (place >= 0 && a.token_pos && t < a.token_pos_stride)
                     for (int h = lane; h < v.n_kv_local; h += 64)
                         a.token_pos[((int64_t)s * v.n_kv_local + h) * a.token_pos_stride + t] = a.positions[i];
-                if (place >= 0 && a.weights && t < a.weights_stride)
+                if (WEIGHTS && place >= 0 && t < a.weights_stride)
                     for (int h = lane; h < v.n_kv_local; h += 64) a.weights[((int64_t)s * v.n_kv_local + h) * a.weights_stride + t] = 0.f;
             }
         }
@@ -220,6 +223,7 @@ extern "C" int kv_rope_append_tracked(void* kv_pool, int64_t n_pool_blocks, cons
     a.tokens = (int32_t)(tokens < 1 ? 1 : tokens > kMostTokens ? kMostTokens : tokens);
     const int64_t grid = (total + a.tokens - 1) / a.tokens;
     if (grid > 0x7fffffff) return KV_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL(kv_rope_append_kernel, dim3((unsigned)grid), dim3(kThreads), 0, (hipStream_t)hip_stream, a);
+    if (weights) hipLaunchKernelGGL(kv_rope_append_kernel<true>, dim3((unsigned)grid), dim3(kThreads), 0, (hipStream_t)hip_stream, a);
+    else hipLaunchKernelGGL(kv_rope_append_kernel<false>, dim3((unsigned)grid), dim3(kThreads), 0, (hipStream_t)hip_stream, a);
     return kv_record_hip_error(hipGetLastError(), "kv_rope_append launch");
 }
