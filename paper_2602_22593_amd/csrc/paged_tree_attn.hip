@@ -27,9 +27,11 @@
 // Per tile, lane l = (c = l % 32, half = l / 32):
 //   S^T[token][c] = K[token][:] . q[c][:]     A operand = K rows from LDS, B operand = q
 //   O^T[e][c]     = sum_t V[t][e] P[c][t]     A operand = V^T by the transposing LDS read
-// Weights enter the second product in bf16, the type of the values that the matrix units multiply them with: off by 2^-8 of themselves
-// at most, each on its own, against one rounding of the output (measured against 64 bits, 2-norms: 2.3e-3 with, 1.7e-3 with weights of
-// 32 bits, of which 1.7e-3 is the output's own rounding).  All sums are fp32.
+// Weights of drafted rows enter the second product in bf16, the type of the values that the matrix units multiply them with: off by 2^-8 of
+// themselves at most, each on its own, against one rounding of the output (measured against 64 bits, 2-norms: 2.3e-3 with, 1.7e-3 with
+// weights of 32 bits, of which 1.7e-3 is the output's own rounding).  What the rounding leaves out as a second operand would take four drafts of
+// up to 256 102 us in place of 81, 32 of up to 64 107 in place of 92.  With sums of weights, which are handed out in 32 bits, it is added (64
+// sequences of 512 to 4096 144 us in place of 141.5): the output then is that of these weights, 2^-16 off.  All sums are fp32.
 // Register 4 a + i of S^T holds token 8 a + 4 half + i; contraction index 8 half + 4 a' + i of step c' of the second product
 // stands for token 16 c' + 8 a' + 4 half + i, so weights stay in their lane.
 #include <algorithm>
@@ -485,7 +487,7 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
             return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
         };
         f32x16 sc, ex;    // scores of a tile, then exponents: score scale log2(e) - reference
-        uint32_t pw[8];   // weights
+        uint32_t pw[8], pf[SUMS ? 8 : 1];   // weights, and what their rounding leaves out
         auto zero = [&]() {
             f32x16 x;
 #pragma unroll
@@ -495,10 +497,18 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
         auto weights = [&](int u) {   // two of the sixteen
             const float e0 = fast_exp2(ex[2 * u]), e1 = fast_exp2(ex[2 * u + 1]);
             pw[u] = pack_bf16x2(e0, e1);
-            if constexpr (SUMS) l += e0 + e1;   // the weights handed out are not rounded
-            else l = add_pair(pw[u], l);        // the same rounding above and below the fraction
+            if constexpr (SUMS) {   // no rounding above or below the fraction
+                pf[u] = pack_bf16x2(e0 - bf16_lo(pw[u]), e1 - bf16_hi(pw[u]));
+                l += e0 + e1;
+            } else {   // the same rounding above and below
+                l = add_pair(pw[u], l);
+            }
         };
         auto weight_operand = [&](int c) { return as_bf16x8(kv_u32x4{pw[4 * c], pw[4 * c + 1], pw[4 * c + 2], pw[4 * c + 3]}); };
+        auto rest_operand = [&](int c) {
+            if constexpr (SUMS) return as_bf16x8(kv_u32x4{pf[4 * c], pf[4 * c + 1], pf[4 * c + 2], pf[4 * c + 3]});
+            else return bf16x8{};
+        };
         // Scores of as many tiles as make 32 rows leave together, through LDS, whole lines at a time.  (The loads of later tiles are
         // counted in order with the stores, whose way out is long: storing every tile's takes 64 sequences of 512 to 4096
         // 131 us in place of 129, at heads of 64 83 in place of 81.)  Returns whether it stored four times,
@@ -571,25 +581,32 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
             for (int u = 0; u < 2 * NJ; ++u) va[u] = v_operand(sv, u);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int u = 0; u < 2 * NJ; ++u)
+            for (int u = 0; u < 2 * NJ; ++u) {
                 o[u % NJ] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[u], weight_operand(u / NJ), o[u % NJ], 0, 0, 0);
+                if constexpr (SUMS) o[u % NJ] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[u], rest_operand(u / NJ), o[u % NJ], 0, 0, 0);
+            }
         };
-        // The tokens of a tile from first_edge on that this lane's row sees
+        // The tokens of a tile (with a mask: from first_edge on) that this lane's row sees
         auto seen_of = [&](int tile) -> uint32_t {
             if constexpr (SUMS) return n - kKeys * tile >= 32 ? ~0u : (1u << (n - kKeys * tile)) - 1u;
             else return s_seen[tile - first_edge][srow];
         };
         // Sums of values where a token that a row does not see may hold an infinity or NaN, which its weight of 0 would turn into NaN:
-        // token by token, without those.  (One that the row sees counts whatever its weight: 0 times infinity is NaN then.)
-        auto add_values_one_by_one = [&](const kv_u32x4* sv, const uint32_t* pw, uint32_t seen) {
+        // token by token, without those.  (One that the row sees counts whatever its weight: 0 times infinity is NaN then.)  And where
+        // weights have two parts: an infinity is multiplied with their sum, not with each.
+        auto add_values_one_by_one = [&](const kv_u32x4* sv, uint32_t seen) {
 #pragma unroll 1
             for (int t = 0; t < 32; ++t) {
                 const int u = 2 * (t >> 3) + ((t & 3) >> 1);
-                uint32_t two = pw[0];
+                auto of_token = [&](const uint32_t* pairs) {
+                    uint32_t two = pairs[0];
 #pragma unroll
-                for (int x = 1; x < 8; ++x) two = u == x ? pw[x] : two;
-                two = (uint32_t)__shfl((int)two, col + 32 * ((t >> 2) & 1));
-                const float wt = (t & 1) ? bf16_hi(two) : bf16_lo(two);
+                    for (int x = 1; x < 8; ++x) two = u == x ? pairs[x] : two;
+                    two = (uint32_t)__shfl((int)two, col + 32 * ((t >> 2) & 1));
+                    return (t & 1) ? bf16_hi(two) : bf16_lo(two);
+                };
+                float wt = of_token(pw);
+                if constexpr (SUMS) wt += of_token(pf);
                 const char* row = reinterpret_cast<const char*>(sv + kg * kPieces) + t * kStride + head_place(hw, t) * kRow;
                 const int g = D == 128 ? 4 * (t & 3) : 4 * ((t >> 1) & 1);
 #pragma unroll
@@ -621,7 +638,7 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
             exponents();
 #pragma unroll
             for (int u = 0; u < 8; ++u) weights(u);
-            if (decltype(careful)::value && tile >= first_edge) add_values_one_by_one(sv, pw, seen_of(tile));
+            if (decltype(careful)::value && (SUMS || tile >= first_edge)) add_values_one_by_one(sv, seen_of(tile));
             else values(sv);
         };
         // The chain of a tile is cut across tiles: the weights of tile i are made beside the score products of tile i + 1, its
@@ -652,10 +669,11 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
                     for (int u = kk * 8 / NK; u < (kk + 1) * 8 / NK; ++u) {
                         weights(u);
                         asm volatile("" : "+v"(pw[u]), "+v"(l));   // (else moved to where they are used)
+                        if constexpr (SUMS) asm volatile("" : "+v"(pf[u]));
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 }
-                const bf16x8 pb[2] = {weight_operand(0), weight_operand(1)};
+                const bf16x8 pb[2] = {weight_operand(0), weight_operand(1)}, pr[2] = {rest_operand(0), rest_operand(1)};
                 const int tile = kt0 + i + 1;
                 hide(tile);
                 stored = keep_scores(i + 1);
@@ -664,6 +682,7 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
 #pragma unroll
                 for (int u = 0; u < 2 * NJ; ++u) {
                     o[u % NJ] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[u], pb[u / NJ], o[u % NJ], 0, 0, 0);
+                    if constexpr (SUMS) o[u % NJ] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[u], pr[u / NJ], o[u % NJ], 0, 0, 0);
                     if (u + kAhead < 2 * NJ) va[u + kAhead] = v_operand(v_now, u + kAhead);
                     // (the first two give the last score product time to finish)
 #pragma unroll
@@ -722,9 +741,9 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
             if constexpr (KW > 1) staged(std::integral_constant<int, 0>());
         }
         if (KW > 1 && i < mine && !idle) whole_step(std::false_type(), i, k_buf(i), v_buf(i));   // one that only some key groups have
-        // A value that is no number in a tile where rows do not see every token may have reached rows that do not see it: once more then,
-        // tile by tile, with care.
-        if (t0 + count > first_edge) {
+        // A value that is no number in a tile where rows do not see every token may have reached rows that do not see it, and one anywhere
+        // has met the parts of weights apart: once more then, tile by tile, with care.
+        if (SUMS || t0 + count > first_edge) {
             float probe = 0.f;
 #pragma unroll
             for (int j = 0; j < NJ; ++j)

@@ -276,3 +276,45 @@ def test_workspace_of_a_graph_outlives_a_larger_one(call):
         graph.replay()
         torch.cuda.synchronize()
         assert np.array_equal(host(out), want) and all(bool((x == 0x5a).all()) for x in others)
+
+
+@pytest.mark.parametrize("geom,ctx,bound", [
+    ((8, 2, 64, 16), [17, 1, 300, 64], 300),
+    ((10, 2, 128, 48), [777, 97], 777),
+    ((32, 8, 128, 16), [700, 33, 2100], WIDE),
+    ((48, 4, 64, 16), [513, 1100], WIDE),
+    ((64, 2, 128, 16), [1100, 31], 1100),
+])
+def test_decode_with_sums_rounds_its_output_alone(geom, ctx, bound):
+    """The weights that are handed out in 32 bits are those that the values are added up with: each enters the product in two parts of
+    bf16, whose second is off by 2^-8 of the first's 2^-8.  So out is off by 2^-16 sum p |v|, and 2^-15 of it and of itself for sums, the
+    quotient and exponentials in fp32 (as elsewhere), before its one rounding."""
+    c = decode_case(geom, ctx, index=89)
+    weights = torch.zeros((len(ctx), geom[1], bound), device=DEV)
+    got = bf16_bits_to_f64(host(kv.paged_decode_attn_weights(dev(c.q), dev(c.pool), dev(wide_table(c, bound)), dev(c.ctx), view_of(c), bound, weights)))
+    G, q = geom[0] // geom[1], bf16_bits_to_f64(c.q)
+    for s, n in enumerate(ctx):
+        K, V = ref.heads_of(c, s)
+        for i in range(geom[0]):
+            want, _, p = ref.attend(q[s, i][None], K[:, i // G], V[:, i // G], np.ones((1, n), bool), geom[2] ** -0.5)
+            off = (2.0 ** -15 + 2.0 ** -16) * (p @ np.abs(V[:, i // G]) + np.abs(want))
+            assert (np.abs(got[s, i] - want[0]) <= ref.HALF_BF16 * (np.abs(want[0]) + off[0]) + off[0]).all(), (s, i)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("heads,bound", [(2, 1000), (4, WIDE)])
+@pytest.mark.parametrize("token", [3, 500, 999])
+def test_infinite_values_in_decode_with_sums(token, heads, bound, d):
+    """An infinity among the values is one in the output, with its sign, wherever it lies: no part of a weight turns it into NaN."""
+    c = decode_case((4 * heads, heads, d, 16), [1000, 33, 1], index=90)
+    set_token(c, 0, token, value=INF)
+    set_token(c, 1, 32, value=INF | 0x8000)
+    set_token(c, 2, 0, value=INF)                                   # of weight 1
+    prior = np.zeros((3, heads, bound), np.float32)
+    want, tol, sums, sums_tol = ref.decode_weights(c, prior)
+    weights = dev(prior)
+    out = kv.paged_decode_attn_weights(dev(c.q), dev(c.pool), dev(wide_table(c, bound)), dev(c.ctx), view_of(c), bound, weights)
+    got, keep = bf16_bits_to_f64(host(out)), np.arange(d) % 3 != 0
+    assert (np.abs(got - want) <= tol)[:, :, keep].all()
+    assert (got[[0, 2]][:, :, ::3] == np.inf).all() and (got[1][:, ::3] == -np.inf).all()
+    assert (np.abs(host(weights).astype(np.float64) - sums) <= sums_tol).all()
