@@ -403,8 +403,8 @@ int paged_tree_attn(const void* q, void* out, const void* kv_pool, int64_t n_poo
  *                  ascending, in [0, q_len[s]).  An entry below its own index (in an ascending row there is
  *                  none) or not below q_len[s] moves nothing
  *   n_accepted     device, int32 [batch], at most accepted_stride and q_len[s] (more counts as that)
- *   new_lens       device, int32 [batch], written: ctx_lens[s] - q_len[s] + n_accepted[s]; may be null,
- *                  must not overlap ctx_lens, q_offsets, accepted or n_accepted
+ *   new_lens       device, int32 [batch], written: ctx_lens[s] - q_len[s] + n_accepted[s], not below 0 (a batch filled up
+ *                  with sequences of no tokens, for which nothing moves); may be null, must not overlap ctx_lens, q_offsets, accepted or n_accepted
  * No block may belong to two sequences of the call, unless nothing in it moves.
  * Errors: KV_ERR_INVALID_ARG, KV_ERR_UNSUPPORTED (kv_pool not 16-byte aligned), KV_ERR_HIP.
  */

@@ -46,7 +46,7 @@ __global__ __launch_bounds__(kThreads) void kv_accept_kernel(accept_args a)
     const int s = blockIdx.x, tid = threadIdx.x;
     const int q0 = a.q_off[s], q_len = a.q_off[s + 1] - q0, n = a.ctx_lens[s], first = n - q_len;
     const int count = (int)min((int64_t)min(max(a.n_accepted[s], 0), max(q_len, 0)), a.accepted_stride);
-    if (a.new_lens && blockIdx.y == 0 && tid == 0) a.new_lens[s] = first + count;
+    if (a.new_lens && blockIdx.y == 0 && tid == 0) a.new_lens[s] = max(first + count, 0);
     if (first < 0) return;
     const int32_t* table = a.table + (int64_t)s * a.table_stride;
     const int row_pieces = v.n_kv_local * v.head_dim / 8;

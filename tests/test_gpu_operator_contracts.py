@@ -318,3 +318,51 @@ def test_infinite_values_in_decode_with_sums(token, heads, bound, d):
     assert (np.abs(got - want) <= tol)[:, :, keep].all()
     assert (got[[0, 2]][:, :, ::3] == np.inf).all() and (got[1][:, ::3] == -np.inf).all()
     assert (np.abs(host(weights).astype(np.float64) - sums) <= sums_tol).all()
+
+
+def test_padded_batch():
+    """A batch filled up with sequences of no tokens goes through every operator: their rows are zeros, nothing of theirs is written, and
+    their lengths stay 0."""
+    ctx, q_lens = [40, 0, 23, 0], [6, 1, 3, 4]
+    c = ref.case((8, 2, 64, 16), (DP, 1, 0), ctx, np.minimum(ctx, q_lens), index=91)
+    off = np.concatenate([[0], np.cumsum(q_lens)]).astype(np.int32)
+    view, pool, table, n = view_of(c), dev(c.pool), dev(c.table), dev(c.ctx)
+    qkv = dev(wl.randn_bf16((14, 12, 64), wl.generator(92, wl.SUB_MISC)))
+    token_pos, weights = torch.full((4, 2, 48), -7, dtype=torch.int32, device=DEV), torch.full((4, 2, 48), 5.0, device=DEV)
+    q = kv.kv_rope_append(pool, view, qkv[:, :8], qkv[:, 8:10], qkv[:, 10:], dev(np.arange(14, dtype=np.int32)), dev(np.ones(32, np.float32)),
+                          table, n, dev(off), token_pos=token_pos, weights=weights)
+    words = dev(np.concatenate([ref.tree_masks([k], np.random.default_rng(42))[1] for k in q_lens]))
+    out = kv.paged_tree_attn(q, pool, table, n, dev(off), words, view, 48, 6)
+    assert not out[6].any() and not out[10:].any() and out[:6].any() and out[7:10].any()
+    for count in (0, 1):
+        new = kv.kv_accept(pool, view, table, n, dev(off), dev(np.zeros((4, 2), np.int32)), dev(np.array([2, count, 1, count], np.int32)),
+                           token_pos=token_pos, weights=weights)
+        assert host(new).tolist() == [36, 0, 21, 0]
+    got = kv.paged_decode_attn_weights(q[:4].contiguous(), pool, table, new, view, 48, weights)
+    assert not got[1].any() and not got[3].any() and got[0].any()
+    state = host(pool)
+    new2 = kv.kv_evict(pool, view, table, new, dev(np.full(4, 30, np.int32)), weights, token_pos, n, 48, sinks=1, recent=5)
+    assert host(new2).tolist() == [30, 0, 21, 0]
+    for x, untouched in ((host(weights), 5.0), (host(token_pos), -7)):
+        assert (x[[1, 3]] == untouched).all()
+    moved = np.flatnonzero((host(pool) != state).reshape(len(state), -1).any(axis=1))
+    assert len(moved) and set(moved) <= set(c.table[0][:3].tolist())
+
+
+@pytest.mark.parametrize("batch", [3, 100])
+def test_a_batch_of_nothing(batch):
+    """Bounds of 0 and 1 where no sequence has a token."""
+    view = kv.kv_view_create(8, 2, 64, 16, DP, 1, 0)
+    pool = torch.full((4, 2 * 16 * 2 * 64), float("nan"), dtype=torch.bfloat16, device=DEV)
+    n, table = torch.zeros(batch, dtype=torch.int32, device=DEV), torch.full((batch, 1), -1, dtype=torch.int32, device=DEV)
+    q = torch.ones((batch, 8, 64), dtype=torch.bfloat16, device=DEV)
+    for bound in (0, 1):
+        weights = torch.full((batch, 2, 3), 5.0, device=DEV)
+        out = torch.ones_like(q)
+        assert not kv.paged_decode_attn_weights(q, pool, table, n, view, bound, weights, out=out).any() and (weights == 5.0).all()
+        pos = torch.zeros((batch, 2, 3), dtype=torch.int32, device=DEV)
+        assert not kv.kv_evict(pool, view, table, n, n, weights, pos, n, bound).any() and (weights == 5.0).all()
+    off = torch.arange(batch + 1, dtype=torch.int32, device=DEV)
+    out = torch.ones_like(q)
+    assert not kv.paged_tree_attn(q, pool, table, n, off, torch.full((batch, 1), -1, dtype=torch.int64, device=DEV), view, 1, 1, out=out).any()
+    assert pool.isnan().all()
