@@ -15,8 +15,9 @@
 // What bounds it: reading K and V, 4 D bytes a token and KV head, as long as the rows are few: 32 rows x 32 keys take
 // 2 D / 16 + 2 D / 16 products of 32 x 32 x 16, 512 cycles at D = 128, and bring 16 KiB, for which HBM takes 1440 cycles of one
 // compute unit's share.  RW wavefronts share a tile, each with 32 rows: K and V pass through LDS once per workgroup.  Four of them
-// (RW = 4) are the general form, two workgroups of which fill a compute unit, also where rows leave some without work: what they share
-// is three tiles on their way ahead of the one in hand.  Large batches of up to 64 rows take the wavefronts for other heads (HW = 4
+// (RW = 4) are the general form, two workgroups of which fill a compute unit, also where rows leave some without work: a piece asks for its
+// first four tiles at once.  Every later step asks for one tile more and ends with a barrier, at which the compiler waits for all loads into
+// LDS, so that one tile is under way beside the one in hand.  Large batches of up to 64 rows take the wavefronts for other heads (HW = 4
 // or 2), which reads rows of several heads in one piece; large ones of many rows have eight to a tile (RW = 8).  With sums of weights
 // there are 32 rows, and where heads are not side by side the wavefronts take different tiles (KW = 4) and each stores its scores.
 //
@@ -31,7 +32,8 @@
 // themselves at most, each on its own, against one rounding of the output (measured against 64 bits, 2-norms: 2.3e-3 with, 1.7e-3 with
 // weights of 32 bits, of which 1.7e-3 is the output's own rounding).  What the rounding leaves out as a second operand would take four drafts of
 // up to 256 102 us in place of 81, 32 of up to 64 107 in place of 92.  With sums of weights, which are handed out in 32 bits, it is added (64
-// sequences of 512 to 4096 144 us in place of 141.5): the output then is that of these weights, 2^-16 off.  All sums are fp32.
+// sequences of 512 to 4096 141.6 us in place of 139.9, four of up to 300 12.9 in place of 12.7): the output then is that of these weights,
+// 2^-16 off.  All sums are fp32.
 // Register 4 a + i of S^T holds token 8 a + 4 half + i; contraction index 8 half + 4 a' + i of step c' of the second product
 // stands for token 16 c' + 8 a' + 4 half + i, so weights stay in their lane.
 #include <algorithm>
@@ -438,14 +440,15 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
         auto stage_v = [&](kv_u32x4* dst, auto sure) {
             if (!kSplitPlanes || rw >= NK) stage(at_v, v_lane, plane_bytes, dst, sure);
         };
-        // this wavefront's loads have landed, and then those of the wavefronts that share its tiles
-        auto staged = [&](auto under_way) {   // but for the last so many
+        // This wavefront's loads have landed, and then those of the wavefronts that share its tiles; but for the last so many.  (In front of a
+        // barrier the count holds where the compiler can follow what is under way: in straight code, at the start of a piece under RW = 4.)
+        auto staged = [&](auto under_way) {
             constexpr int kLeft = decltype(under_way)::value;
             __builtin_amdgcn_s_waitcnt(0x0f70 | (kLeft & 15) | (kLeft >> 4) << 14);   // vmcnt
             if constexpr (kShared) __syncthreads();
             else asm volatile("" ::: "memory");
         };
-        // Of a ring of several tiles the first steps need K of two and V of one; the others land meanwhile
+        // Of several tiles the first scores need K of two and V of one; the others land beside them
         constexpr int kRing = (NB - 2) * (kSplitPlanes ? 1 : 2) * NP;
         auto start = [&](auto sure) {
 #pragma unroll
@@ -643,10 +646,9 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
         };
         // The chain of a tile is cut across tiles: the weights of tile i are made beside the score products of tile i + 1, its
         // output products run beside the exponents of tile i + 1.  The order is pinned: a product, the vector
-        // instructions that fit under it, the operand read of the second product after it.  The loads of the
-        // NB - 1 tiles after it are under way meanwhile.
+        // instructions that fit under it, the operand read of the second product after it.  The loads of one tile, the
+        // NB - 1st after it, are under way meanwhile.
         constexpr int kAhead = 2;
-        constexpr bool kStoresLast = SUMS;
         auto step = [&](auto phase, int i) {
             constexpr int B = decltype(phase)::value;   // i % NB
             kv_u32x4* const k_next = k_buf(B + 1);
@@ -694,9 +696,8 @@ __global__ __launch_bounds__(RW == 8 ? 512 : 256, 2) void tree_kernel(tree_args 
                 }
                 move_reference(top);
             }
-            // K of tile i + 2 and V of tile i + 1 are needed next: what the last NB - 2 steps asked for may still be under way
-            if (NB > 2 && i + NB < mine) staged(std::integral_constant<int, kRing>());
-            else if (stored && kStoresLast) staged(std::integral_constant<int, 4>());   // (scores on their way out)
+            // (a wavefront that shares no tile has no barrier, and its four stores of scores may go on)
+            if (!kShared && stored) staged(std::integral_constant<int, 4>());
             else staged(std::integral_constant<int, 0>());
         };
         const int common = count / KW;   // tiles that every key group has
