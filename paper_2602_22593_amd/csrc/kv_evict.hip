@@ -30,18 +30,20 @@ struct accept_args {
     const int32_t *ctx_lens, *q_off, *accepted, *n_accepted;
     int64_t accepted_stride;
     int32_t* new_lens;
+    kv_view_dev v;
     uint32_t* per_token[2];      // [batch][n_kv_local][per_token_stride], the first n_per_token of them
     int64_t per_token_stride[2];
     int32_t n_per_token;
-    kv_view_dev v;
 };
 constexpr int kMostAccepted = 256;   // rows whose places are worked out at a time
 constexpr int kRowsAhead = 8;
 
+// VALUES: with columns of values per token (128 sequences 4.6 us without, 4.9 where one kernel serves both)
+template <bool VALUES>
 __global__ __launch_bounds__(kThreads) void kv_accept_kernel(accept_args a)
 {
     __shared__ int64_t s_from[kMostAccepted], s_to[kMostAccepted];
-    __shared__ int s_node[kMostAccepted];
+    __shared__ int s_node[VALUES ? kMostAccepted : 1];
     const kv_view_dev& v = a.v;
     const int s = blockIdx.x, tid = threadIdx.x;
     const int q0 = a.q_off[s], q_len = a.q_off[s + 1] - q0, n = a.ctx_lens[s], first = n - q_len;
@@ -56,8 +58,8 @@ __global__ __launch_bounds__(kThreads) void kv_accept_kernel(accept_args a)
     const int64_t at = plane * v.plane_elems + (int64_t)(column - plane * row_pieces) * 8;
     // or a column of values per token
     const int value = column - 2 * row_pieces, which = value >= v.n_kv_local, head = value - which * v.n_kv_local;
-    const bool has_value = !mine && which < a.n_per_token && head < v.n_kv_local;
-    const int64_t value_stride = a.per_token_stride[which];
+    const bool has_value = VALUES && !mine && which < a.n_per_token && head < v.n_kv_local;
+    const int64_t value_stride = has_value ? a.per_token_stride[which] : 0;
     uint32_t* const values = has_value ? a.per_token[which] + ((int64_t)s * v.n_kv_local + head) * value_stride : nullptr;
     for (int i0 = 0; i0 < count; i0 += kMostAccepted) {
         const int m = min(count - i0, kMostAccepted);
@@ -71,7 +73,7 @@ __global__ __launch_bounds__(kThreads) void kv_accept_kernel(accept_args a)
             }
             s_from[tid] = to < 0 ? -1 : from;
             s_to[tid] = to;
-            s_node[tid] = node;
+            if constexpr (VALUES) s_node[tid] = node;
         }
         __syncthreads();
         if (has_value) {
@@ -636,7 +638,9 @@ extern "C" int kv_accept_tracked(void* kv_pool, int64_t n_pool_blocks, const kv_
     }
     const int64_t columns = (int64_t)view->n_kv_local * (view->geom.head_dim / 4 + a.n_per_token), parts = (columns + kThreads - 1) / kThreads;
     if (parts > 65535) return KV_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL(kv_accept_kernel, dim3((unsigned)batch, (unsigned)parts), dim3(kThreads), 0, (hipStream_t)hip_stream, a);
+    const dim3 grid((unsigned)batch, (unsigned)parts);
+    if (a.n_per_token) hipLaunchKernelGGL(kv_accept_kernel<true>, grid, dim3(kThreads), 0, (hipStream_t)hip_stream, a);
+    else hipLaunchKernelGGL(kv_accept_kernel<false>, grid, dim3(kThreads), 0, (hipStream_t)hip_stream, a);
     return kv_record_hip_error(hipGetLastError(), "kv_accept launch");
 }
 
