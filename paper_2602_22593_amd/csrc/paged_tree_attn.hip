@@ -1115,7 +1115,8 @@ tree_plan plan_with(const kv_view* view, int batch, int max_ctx_len, int64_t row
     // 100 to 500 20.6 / 17.8 / 18.1)
     p.least = rw == 1 ? 8 : 4;
     const int64_t most = blocks * batch * ((tiles + p.least - 1) / p.least);
-    const int fill = kCus * (rw == 2 || rw == 4 ? 2 : 1) * hw;   // heads that the chip holds workgroups for
+    // heads that the chip holds workgroups for (four heads of 64 without sums would fit twice; the shares are made for one)
+    const int fill = kCus * (rw == 2 || rw == 4 ? 2 : 1) * hw;
     p.teams = (int32_t)std::max<int64_t>(std::min<int64_t>(most, fill / view->n_kv_local), 1);
     const size_t records = (size_t)2 * p.teams * view->n_kv_local * rb;
     p.part_o = records * view->geom.head_dim * 4;
