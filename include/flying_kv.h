@@ -455,7 +455,7 @@ int paged_decode_attn_weights(const void* q, void* out, const void* kv_pool, int
  * attention; token_pos says which is which).  K and V rows, weights and token_pos move alike.
  *   keep_lens      device, int32 [batch] (negative counts as 0)
  *   weights        device, fp32 [batch][n_kv_local][stride], stride >= max_ctx_len
- *   token_pos      device, int32, same shape: positions of the tokens (kv_rope_append writes them)
+ *   token_pos      device, int32, same shape: positions of the tokens (kv_rope_append writes them, kv_accept_tracked moves them)
  *   next_pos       device, int32 [batch]: the position that the next token takes
  *   weights_out, token_pos_out  device, [batch][n_kv_local][out_stride]: the arrays as they are afterwards, entries
  *                  below min(k, out_stride) written; may be weights and token_pos themselves (only what moves is
