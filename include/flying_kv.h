@@ -477,6 +477,77 @@ int kv_evict(void* kv_pool, int64_t n_pool_blocks, const kv_view* view, const in
              void* hip_stream);
 
 /*
+ * A cache held in 8 bits.  Its pool holds codes of one byte where a bf16 pool holds elements: blocks
+ *     uint8 [2 (K, V)] [Bv] [Hrow] [head_dim],   half of view->block_bytes each,
+ * read through the same views, tables and lengths, and beside it lie
+ *     scales   device, fp32 [n_pool_blocks][2 (K, V)][Bv / base_block_size][Hrow]
+ * one scale for every base_block_size tokens of a KV head (a group); n_kv_heads scales a plane under every view, so
+ * a block's scales never change in number either.  A value is its code times its group's scale.  Formats:
+ *   KV_Q8_E4M3  8-bit floats of four exponent and three mantissa bits, no infinities, largest 448
+ *   KV_Q8_INT8  integers in [-127, 127]
+ * Any finite scales are read; those that kv_rope_append_q8 writes are powers of two, so that its values are exact in bf16.
+ * A scale that is not finite makes every number of its group NaN: a row of attention that sees one of its tokens is
+ * NaN, and no other.  (The codes 0x7f and 0xff of e4m3 are NaN too; the library writes none.  Where a cache of
+ * other origin has them, rows of a paged_prefill_attn_q8 call before such a token may be NaN as well.)
+ * All four operators want base_block_size a multiple of 16 (KV_ERR_UNSUPPORTED), and pools, queries and outputs aligned
+ * to 16 bytes, scales to 4.
+ */
+enum { KV_Q8_E4M3 = 0, KV_Q8_INT8 = 1 };
+
+/*
+ * kv_rope_append_q8 -- kv_rope_append into a cache held in 8 bits: rotary positions for the new tokens' queries and keys,
+ * queries to an array (bf16), keys and values to codes in the pool, rounded once from fp32 to the nearest code (ties to
+ * even).  A group's scale becomes the smallest power of two, at least 2^-120, under which all its new tokens fit into the
+ * format, and no smaller than it was where the group holds older tokens (those before the call's first); where it
+ * grows the older tokens' codes are rounded again.  (e4m3: exact but for what falls below its normal range.  int8:
+ * off by half a step each time; the steps at least double, so by one step in all.)  A new token with an infinity or a NaN
+ * makes its group's scale NaN, which it stays until the group is written from its first token on.
+ *   q, q_out       as kv_rope_append, or both null: keys and values only
+ *   positions, inv_freq   may be null where rotary_dim is 0: nothing is rotated
+ * A group that is written belongs to one sequence of the call, and to no other sequence at all where it holds older
+ * tokens (they may be rounded again).
+ * Other arguments and errors as kv_rope_append, KV_ERR_INVALID_ARG for an unknown format or only one of q and q_out,
+ * KV_ERR_UNSUPPORTED for head_dim other than 64 and 128 or base_block_size above 128.
+ */
+int kv_rope_append_q8(void* kv_pool, float* scales, int format, int64_t n_pool_blocks, const kv_view* view, const void* q,
+                      int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride, void* q_out,
+                      const int32_t* positions, int64_t position_stride, int n_axes, const float* inv_freq, int rotary_dim,
+                      const int32_t* axis_of_pair, int pairs, const int32_t* block_table, int64_t block_table_stride,
+                      const int32_t* ctx_lens, const int32_t* q_offsets, int batch, int64_t total, void* hip_stream);
+
+/*
+ * paged_decode_attn_q8 -- paged_decode_attn over a cache held in 8 bits.  Queries and weights enter the products in bf16, codes exactly.
+ *   workspace      at least paged_decode_attn_q8_workspace_bytes(...) bytes (may be 0: then null is accepted), 256-byte
+ *                  aligned; contents need not be initialised; one for larger bounds serves smaller calls
+ * Other arguments as paged_decode_attn.  Errors: KV_ERR_INVALID_ARG (null pointers, negative sizes, an unknown format,
+ * block_table_stride too small), KV_ERR_UNSUPPORTED (head_dim not 64 or 128, group size above 16), KV_ERR_WORKSPACE, KV_ERR_HIP.
+ */
+size_t paged_decode_attn_q8_workspace_bytes(const kv_view* view, int batch, int max_ctx_len);
+int paged_decode_attn_q8(const void* q, void* out, const void* kv_pool, const float* scales, int format, int64_t n_pool_blocks,
+                         const int32_t* block_table, int64_t block_table_stride, const int32_t* ctx_lens, int batch, int max_ctx_len,
+                         const kv_view* view, float scale, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * paged_prefill_attn_q8 -- paged_prefill_attn over a cache held in 8 bits (the new tokens' codes are in the pool).  Values enter the
+ * products in bf16: exactly where scales are powers of two, rounded to it otherwise.
+ * Workspace, other arguments and errors as paged_prefill_attn, KV_ERR_INVALID_ARG for an unknown format.
+ */
+size_t paged_prefill_attn_q8_workspace_bytes(const kv_view* view, int batch, int64_t total_q, int max_ctx_len, int max_q_len);
+int paged_prefill_attn_q8(const void* q, void* out, const void* kv_pool, const float* scales, int format, int64_t n_pool_blocks,
+                          const int32_t* block_table, int64_t block_table_stride, const int32_t* ctx_lens, const int32_t* q_offsets,
+                          int batch, int64_t total_q, int max_ctx_len, int max_q_len, const kv_view* view, float scale, void* workspace,
+                          size_t workspace_bytes, void* hip_stream);
+
+/*
+ * kv_repack_q8 -- kv_repack for a cache held in 8 bits: codes of the tokens and scales of their groups move as they are, in
+ * either format (a group is the same in every layout: nothing is rounded).  Of a group that is not full its scale moves whole.
+ * Arguments, preconditions and errors as kv_repack, KV_ERR_UNSUPPORTED for head_dim not a multiple of 16.
+ */
+int kv_repack_q8(void* kv_pool, float* scales, int64_t n_pool_blocks, const kv_view* src_view, const kv_view* dst_view,
+                 const int32_t* src_block_table, int64_t src_stride, const int32_t* dst_block_table, int64_t dst_stride,
+                 const int32_t* n_tokens, int n_seqs, int max_tokens, void* hip_stream);
+
+/*
  * kv_validate_tables -- debugging aid, NOT for the hot path: copies the tables to the host
  * (synchronises the stream) and checks that every block id a valid token needs lies in
  * [0, n_pool_blocks) (KV_ERR_RANGE) and that no block is used twice within the table

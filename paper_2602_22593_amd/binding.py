@@ -91,6 +91,16 @@ def lib() -> C.CDLL:
     L.kv_evict_workspace_bytes.restype = C.c_size_t
     L.kv_evict.argtypes = [vp, i64, vp, vp, i64, vp, vp, C.c_int, C.c_int, vp, vp, i64, vp, C.c_int, C.c_int, vp, vp, i64, vp,
                            vp, C.c_size_t, vp]
+    L.kv_rope_append_q8.argtypes = [vp, vp, C.c_int, i64, vp, vp, i64, vp, i64, vp, i64, vp, vp, i64, C.c_int, vp, C.c_int, vp, C.c_int,
+                                    vp, i64, vp, vp, C.c_int, i64, vp]
+    L.paged_decode_attn_q8_workspace_bytes.argtypes = [vp, C.c_int, C.c_int]
+    L.paged_decode_attn_q8_workspace_bytes.restype = C.c_size_t
+    L.paged_decode_attn_q8.argtypes = [vp, vp, vp, vp, C.c_int, i64, vp, i64, vp, C.c_int, C.c_int, vp, C.c_float, vp, C.c_size_t, vp]
+    L.paged_prefill_attn_q8_workspace_bytes.argtypes = [vp, C.c_int, i64, C.c_int, C.c_int]
+    L.paged_prefill_attn_q8_workspace_bytes.restype = C.c_size_t
+    L.paged_prefill_attn_q8.argtypes = [vp, vp, vp, vp, C.c_int, i64, vp, i64, vp, vp, C.c_int, i64, C.c_int, C.c_int, vp, C.c_float, vp,
+                                        C.c_size_t, vp]
+    L.kv_repack_q8.argtypes = [vp, vp, i64, vp, vp, vp, i64, vp, i64, vp, C.c_int, C.c_int, vp]
     L.kv_validate_tables.argtypes = [vp, i64, vp, i64, vp, C.c_int, vp, vp, i64, vp]
     L.kv_set_option.argtypes = [C.c_char_p, i64]
     L.kv_get_option.argtypes = [C.c_char_p]
@@ -701,6 +711,122 @@ def kv_evict(kv_pool: torch.Tensor, view: KVView, block_table: torch.Tensor, ctx
             _ints(new_lens, batch, "new_lens"), _dev(workspace, (torch.uint8,), "workspace"), workspace.numel())
     _check(_launch(device, stream, lambda st: lib().kv_evict(*args, st)), "kv_evict")
     return new_lens
+
+
+KV_Q8_E4M3, KV_Q8_INT8 = 0, 1
+_Q8_FORMATS = {torch.float8_e4m3fn: KV_Q8_E4M3, torch.int8: KV_Q8_INT8}
+
+
+def _q8_cache(kv_pool: torch.Tensor, scales: torch.Tensor, view: KVView):
+    """Address, scales' address, format and blocks of an 8-bit cache: codes (e4m3 or int8, by their dtype), blocks of half the view's
+    bytes; fp32 scales [blocks][2][KV heads]."""
+    pool_ptr = _dev(kv_pool, tuple(_Q8_FORMATS), "kv_pool")
+    per_block = view.block_bytes // 2
+    if kv_pool.numel() % per_block:
+        raise ValueError("kv_pool size is not a whole number of blocks")
+    n = kv_pool.numel() // per_block
+    if scales.numel() != n * 2 * view.geometry.n_kv_heads:
+        raise ValueError(f"scales has {scales.numel()} entries, expected [{n}, 2, {view.geometry.n_kv_heads}]")
+    return pool_ptr, _dev(scales, (torch.float32,), "scales"), _Q8_FORMATS[kv_pool.dtype], n
+
+
+def kv_rope_append_q8(kv_pool: torch.Tensor, scales: torch.Tensor, view: KVView, q: Optional[torch.Tensor], k: torch.Tensor,
+                      v: torch.Tensor, positions: Optional[torch.Tensor], inv_freq: Optional[torch.Tensor], block_table: torch.Tensor,
+                      ctx_lens: torch.Tensor, q_offsets: Optional[torch.Tensor] = None, axes=None, pairs: int = KV_ROPE_HALVES,
+                      out: Optional[torch.Tensor] = None, stream=None) -> Optional[torch.Tensor]:
+    """kv_rope_append into a cache held in 8 bits: ``kv_pool`` e4m3 (torch.float8_e4m3fn) or int8 codes, ``scales`` fp32
+    [blocks][2][KV heads], one for every B_base tokens of a head.
+
+    ``q`` may be None (keys and values only; None is returned), ``positions`` and ``inv_freq`` where nothing is rotated.
+    Other arguments as kv_rope_append.  Older tokens of a group that the new ones fall into are rounded again where its scale grows.
+    """
+    batch, total, d = int(ctx_lens.shape[0]), int(k.shape[0]), view.head_dim
+    device = _one_device(kv_pool, scales, q, k, v, positions, inv_freq, block_table, ctx_lens, q_offsets, out)
+    if q is None and out is not None:
+        raise ValueError("out without q")
+    if inv_freq is not None and positions is None:
+        raise ValueError("inv_freq without positions")
+    q_ptr, q_stride = (None, 0) if q is None else _token_rows(q, total, view.n_q_local, d, "q")
+    k_ptr, k_stride = _token_rows(k, total, view.n_kv_local, d, "k")
+    v_ptr, v_stride = _token_rows(v, total, view.n_kv_local, d, "v")
+    if out is None and q is not None:
+        out = torch.empty((total, view.n_q_local, d), dtype=q.dtype, device=device)
+    half = 0 if inv_freq is None else int(inv_freq.numel())
+    n_axes = 1 if positions is None or positions.dim() == 1 else int(positions.shape[0])
+    pos_ptr = None if positions is None else _shaped(positions, (total,) if positions.dim() == 1 else (n_axes, total), (torch.int32,), "positions")
+    freq_ptr = None if inv_freq is None else _shaped(inv_freq, (half,), (torch.float32,), "inv_freq")
+    if axes is not None:
+        if len(axes) != half:
+            raise ValueError(f"axes has {len(axes)} entries, expected {half}")
+        axes = (C.c_int32 * half)(*axes)
+    elif n_axes != 1:
+        raise ValueError("positions with several axes need axes")
+    pool_ptr, scales_ptr, fmt, blocks = _q8_cache(kv_pool, scales, view)
+    args = (pool_ptr, scales_ptr, fmt, blocks, view.handle, q_ptr, q_stride, k_ptr, k_stride, v_ptr, v_stride,
+            None if q is None else _shaped(out, (total, view.n_q_local, d), _BF16, "out"), pos_ptr, total, n_axes, freq_ptr, 2 * half, axes,
+            pairs, _table(block_table, batch), block_table.stride(0), _ints(ctx_lens, batch, "ctx_lens"),
+            None if q_offsets is None else _ints(q_offsets, batch + 1, "q_offsets"), batch, total)
+    _check(_launch(device, stream, lambda st: lib().kv_rope_append_q8(*args, st)), "kv_rope_append_q8")
+    return out
+
+
+def paged_decode_attn_q8_workspace_bytes(view: KVView, batch: int, max_ctx_len: int) -> int:
+    return int(lib().paged_decode_attn_q8_workspace_bytes(view.handle, batch, max_ctx_len))
+
+
+def paged_decode_attn_q8(q: torch.Tensor, kv_pool: torch.Tensor, scales: torch.Tensor, block_table: torch.Tensor, ctx_lens: torch.Tensor,
+                         view: KVView, max_ctx_len: int, out: Optional[torch.Tensor] = None, scale: float = 0.0,
+                         workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """paged_decode_attn over a cache held in 8 bits (``kv_pool`` and ``scales`` as kv_rope_append_q8 takes them)."""
+    batch = int(ctx_lens.shape[0])
+    device = _one_device(q, kv_pool, scales, block_table, ctx_lens, out, workspace)
+    shape = (batch, view.n_q_local, view.head_dim)
+    q_ptr = _shaped(q, shape, _BF16, "q")
+    if out is None:
+        out = torch.empty_like(q)
+    if workspace is None:
+        workspace = _workspace(device, paged_decode_attn_q8_workspace_bytes(view, batch, max_ctx_len), stream)
+    pool_ptr, scales_ptr, fmt, blocks = _q8_cache(kv_pool, scales, view)
+    args = (q_ptr, _shaped(out, shape, _BF16, "out"), pool_ptr, scales_ptr, fmt, blocks, _table(block_table, batch), block_table.stride(0),
+            _ints(ctx_lens, batch, "ctx_lens"), batch, int(max_ctx_len), view.handle, float(scale),
+            _dev(workspace, (torch.uint8,), "workspace"), workspace.numel())
+    _check(_launch(device, stream, lambda st: lib().paged_decode_attn_q8(*args, st)), "paged_decode_attn_q8")
+    return out
+
+
+def paged_prefill_attn_q8_workspace_bytes(view: KVView, batch: int, total_q: int, max_ctx_len: int, max_q_len: int) -> int:
+    return int(lib().paged_prefill_attn_q8_workspace_bytes(view.handle, batch, total_q, max_ctx_len, max_q_len))
+
+
+def paged_prefill_attn_q8(q: torch.Tensor, kv_pool: torch.Tensor, scales: torch.Tensor, block_table: torch.Tensor, ctx_lens: torch.Tensor,
+                          q_offsets: torch.Tensor, view: KVView, max_ctx_len: int, max_q_len: int, out: Optional[torch.Tensor] = None,
+                          scale: float = 0.0, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """paged_prefill_attn over a cache held in 8 bits (``kv_pool`` and ``scales`` as kv_rope_append_q8 takes them)."""
+    batch, total = int(ctx_lens.shape[0]), int(q.shape[0])
+    device = _one_device(q, kv_pool, scales, block_table, ctx_lens, q_offsets, out, workspace)
+    shape = (total, view.n_q_local, view.head_dim)
+    q_ptr = _shaped(q, shape, _BF16, "q")
+    if out is None:
+        out = torch.empty_like(q)
+    if workspace is None:
+        workspace = _workspace(device, paged_prefill_attn_q8_workspace_bytes(view, batch, total, max_ctx_len, max_q_len), stream)
+    pool_ptr, scales_ptr, fmt, blocks = _q8_cache(kv_pool, scales, view)
+    args = (q_ptr, _shaped(out, shape, _BF16, "out"), pool_ptr, scales_ptr, fmt, blocks, _table(block_table, batch), block_table.stride(0),
+            _ints(ctx_lens, batch, "ctx_lens"), _ints(q_offsets, batch + 1, "q_offsets"), batch, total, int(max_ctx_len), int(max_q_len),
+            view.handle, float(scale), _dev(workspace, (torch.uint8,), "workspace"), workspace.numel())
+    _check(_launch(device, stream, lambda st: lib().paged_prefill_attn_q8(*args, st)), "paged_prefill_attn_q8")
+    return out
+
+
+def kv_repack_q8(kv_pool: torch.Tensor, scales: torch.Tensor, src_view: KVView, dst_view: KVView, src_block_table: torch.Tensor,
+                 dst_block_table: torch.Tensor, n_tokens: torch.Tensor, max_tokens: int, stream=None) -> None:
+    """kv_repack for a cache held in 8 bits: codes and scales of the heads common to both views move as they are."""
+    n_seqs = int(n_tokens.shape[0])
+    device = _one_device(kv_pool, scales, src_block_table, dst_block_table, n_tokens)
+    pool_ptr, scales_ptr, _, blocks = _q8_cache(kv_pool, scales, src_view)
+    args = (pool_ptr, scales_ptr, blocks, src_view.handle, dst_view.handle, _table(src_block_table, n_seqs), src_block_table.stride(0),
+            _table(dst_block_table, n_seqs), dst_block_table.stride(0), _ints(n_tokens, n_seqs, "n_tokens"), n_seqs, int(max_tokens))
+    _check(_launch(device, stream, lambda st: lib().kv_repack_q8(*args, st)), "kv_repack_q8")
 
 
 def kv_validate_tables(view: KVView, n_pool_blocks: int, block_table: torch.Tensor,

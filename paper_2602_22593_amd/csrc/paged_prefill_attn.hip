@@ -26,9 +26,9 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "decode_common.h"
+#include "kv_q8.h"
 
-using namespace kvdec;
+using namespace kvq8;
 
 namespace {
 
@@ -39,6 +39,7 @@ constexpr int kMostCut = 1024;          // sequences up to which a workgroup rea
 // How the workgroups of a launch that cuts no key ranges find their query tiles, see the host code below
 constexpr int kSlots = 0, kDense = 1, kLongestFirst = 2;
 constexpr float kUnset = 1e30f;       // exponent addend of a column that has no reference maximum yet
+constexpr int kBf16 = -1;             // what the cache holds: rows, or codes of one of the 8-bit formats
 
 struct prefill_args {
     const uint16_t* q;      // [total_q][n_q_local][128]
@@ -63,6 +64,9 @@ struct prefill_args {
     int4* tiles;            // [slots] (first record, pieces, first token in q, tokens), for the merge kernel
     float* part_o;          // [record = a piece's token][n_q_local][128] un-normalised sums
     float* part_ml;         // [record][n_q_local][2]  (reference maximum in exponent units, sum of weights)
+    // of an 8-bit cache (the pool then holds codes, its elements are bytes)
+    const float* scales;
+    q8_view x;
 };
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
@@ -424,7 +428,7 @@ __device__ __forceinline__ int piece_slot(const int2* s_slot, int slots, int idx
 // of up to 190 registers launches of many tiles are slower (tp2 chunks above 221, 64 of 30 to 600 135).  Eight
 // wavefronts that share the staged tiles (half the loads) wait for each other: 16 prompts 810, 4 of 8192 1969.
 // CUT: the items are the pieces of plan_pieces() instead of whole query tiles.
-template <bool CUT>
+template <bool CUT, int FMT>
 __global__ __launch_bounds__(kThreads, 3) void prefill_kernel(prefill_args a)
 {
     // [row][piece]: K pieces swizzled (piece c of row t at c ^ (t % 16)); V pieces at c ^ (4 * (t % 4)), which puts
@@ -542,18 +546,21 @@ __global__ __launch_bounds__(kThreads, 3) void prefill_kernel(prefill_args a)
     // which piece of its row a lane fetches is the LDS swizzle applied on the global side.
     // A wavefront fills eight rows of a tile, all of one group of 16 (wave / 2), which lies in one block: per tile it works
     // out one address, from a block id asked for a tile before.
-    const int dma_r = lane >> 4, dma_c = lane & 15;
-    const int row8 = 8 * (wave & 1) + dma_r;                  // and + 4: rows within the group
-    const int token_stride_bytes = v.token_stride * 2;
-    const int64_t plane_bytes = v.plane_elems * 2;
+    // Of codes one load of 16 bytes a lane is a wavefront's eight rows.
+    constexpr bool kCodes = FMT != kBf16;
+    constexpr int kElem = kCodes ? 1 : 2;
+    const int dma_r = kCodes ? lane >> 3 : lane >> 4, dma_c = kCodes ? lane & 7 : lane & 15;
+    const int row8 = 8 * (wave & 1) + dma_r;                  // and + 4 (rows of bf16): rows within the group
+    const int token_stride_bytes = v.token_stride * kElem;
+    const int64_t plane_bytes = v.plane_elems * kElem;
     const int groups_per_block = v.block_tokens >> 4;
     const int last_group = (n - 1) >> 4;
     // Within the loop block ids come by vector loads: a scalar load under way shares the counter of the LDS reads and
     // returns out of order, so that every product would wait for all reads issued instead of its own.
     const int32_t* const ids = a.table + (int64_t)s * a.table_stride;
     const __amdgpu_buffer_rsrc_t id_row = __builtin_amdgcn_make_buffer_rsrc(const_cast<int32_t*>(ids), 0, 0x7ffffff0, 0x00020000);
-    const char* pool_head = reinterpret_cast<const char*>(a.pool + v.head_off + hl * D);
-    const int64_t block_bytes = (int64_t)v.block_elems * 2;
+    const char* pool_head = reinterpret_cast<const char*>(a.pool) + (int64_t)(v.head_off + hl * D) * kElem;
+    const int64_t block_bytes = (int64_t)v.block_elems * kElem;
     const uint32_t group_bytes = 16u * (uint32_t)token_stride_bytes;
     uint32_t k_lane[2], v_lane[2];
 #pragma unroll
@@ -562,11 +569,13 @@ __global__ __launch_bounds__(kThreads, 3) void prefill_kernel(prefill_args a)
         k_lane[i] = (uint32_t)(row * token_stride_bytes) + (uint32_t)((dma_c ^ row) << 4);
         v_lane[i] = (uint32_t)(row * token_stride_bytes) + (uint32_t)((dma_c ^ (4 * (row & 3))) << 4);
     }
+    const uint32_t code_lane = (uint32_t)(row8 * token_stride_bytes) + (uint32_t)(dma_c << 4);
     typedef __attribute__((address_space(3))) void* lds_ptr;
     // where a tile's rows of this wavefront lie, and the number of their group
     struct tile_rows {
         const char* rows;
         int group;
+        int64_t scale;   // place of the group's K scale
     };
     // the group to be fetched next: its number, place in its block, and the block's id.  Past the end it is the last one
     // (what is fetched then is masked, or of a tile past the last)
@@ -578,7 +587,8 @@ __global__ __launch_bounds__(kThreads, 3) void prefill_kernel(prefill_args a)
         return blk;
     };
     auto rows_of = [&](int id) -> tile_rows {
-        return {pool_head + (uint64_t)(uint32_t)id * (uint64_t)block_bytes + (uint64_t)(uint32_t)g_in * group_bytes, g_at};
+        return {pool_head + (uint64_t)(uint32_t)id * (uint64_t)block_bytes + (uint64_t)(uint32_t)g_in * group_bytes, g_at,
+                kCodes ? q8_scale_at(a.x, (uint32_t)id, 16 * g_in, hl) : 0};
     };
     auto request_id = [&](uint32_t blk) { return (int)__builtin_amdgcn_raw_buffer_load_b32(id_row, 0, 4 * blk, 0); };
     auto next_rows = [&]() {
@@ -605,9 +615,52 @@ __global__ __launch_bounds__(kThreads, 3) void prefill_kernel(prefill_args a)
             }
         }
     };
+    // Codes come through registers: a lane fetches 16 of a row, a tile ahead, and writes them to LDS as bf16 where staged rows of bf16 would
+    // lie.  The scale is taken in on the way: exactly where it is a power of two, as the library writes them, rounded to bf16 otherwise.
+    struct fetched {
+        kv_u32x4 codes;
+        float scale, other;   // other: V's, with K
+    };
+    auto fetch = [&](const tile_rows& x, int plane) -> fetched {
+        const __amdgpu_buffer_rsrc_t rows =
+            __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(x.rows + (plane ? plane_bytes : 0)), 0, 0x7ffffff0, 0x00020000);
+        uint32_t at = code_lane;
+        if (x.group >= last_group) at -= (uint32_t)(max(row8 - (n - 1 - 16 * x.group), 0) * token_stride_bytes);
+        fetched f;
+        f.codes = __builtin_bit_cast(kv_u32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, at, 0, 0));
+        f.scale = a.scales[x.scale + (plane ? a.x.block_scales / 2 : 0)];
+        f.other = plane ? 0.f : a.scales[x.scale + a.x.block_scales / 2];
+        return f;
+    };
+    auto put = [&](const fetched& f, int plane, kv_u32x4* dst) {
+        float scale = f.scale;
+        // A scale of V that is no number: K's stands for it, so that rows that do not see the group (whose weights are 0) keep theirs.
+        const float of_v = plane ? f.scale : f.other;
+        const bool no_number = !(fabsf(of_v) < INFINITY);
+        if (no_number) scale = plane ? 0.f : __builtin_nanf("");
+        kv_u32x4 x[2];
+        const uint32_t bits = (uint32_t)uniform((int)__float_as_uint(scale));
+        if (FMT == kE4M3 && (bits & 0x807fffffu) == 0u && bits - 1u < 0x7f7fffffu) {
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                x[w >> 1][2 * (w & 1)] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(f.codes[w], scale, false));
+                x[w >> 1][2 * (w & 1) + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(f.codes[w], scale, true));
+            }
+        } else {
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const f32x2 lo = two_f32<FMT == kInt8 ? kInt8 : kE4M3, false>(f.codes[w]), hi = two_f32<FMT == kInt8 ? kInt8 : kE4M3, true>(f.codes[w]);
+                x[w >> 1][2 * (w & 1)] = pack_bf16x2(lo[0] * scale, lo[1] * scale);
+                x[w >> 1][2 * (w & 1) + 1] = pack_bf16x2(hi[0] * scale, hi[1] * scale);
+            }
+        }
+        const int row = 16 * (wave >> 1) + row8, turn = plane ? 4 * (row & 3) : row & 15;
+        dst[row * 16 + ((2 * dma_c) ^ turn)] = x[0];
+        dst[row * 16 + ((2 * dma_c + 1) ^ turn)] = x[1];
+    };
     // all of this wavefront's loads have landed in LDS; then every wavefront's
     auto staged = [&]() {
-        __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
+        if constexpr (!kCodes) __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
         __syncthreads();
     };
 
@@ -626,13 +679,25 @@ __global__ __launch_bounds__(kThreads, 3) void prefill_kernel(prefill_args a)
     const int in0 = g_in, at0 = g_at;
     const int id1 = first_ids[next_block()];
     tile_rows rows2 = rows_of(id1);
-    tile_rows rows1 = {pool_head + (uint64_t)(uint32_t)id0 * (uint64_t)block_bytes + (uint64_t)(uint32_t)in0 * group_bytes, at0};
+    tile_rows rows1 = {pool_head + (uint64_t)(uint32_t)id0 * (uint64_t)block_bytes + (uint64_t)(uint32_t)in0 * group_bytes, at0,
+                       kCodes ? q8_scale_at(a.x, (uint32_t)id0, 16 * in0, hl) : 0};
     g_id = request_id(next_block());
-    if (t_begin < n_tiles) {
-        stage_rows(rows1, k_lane, 0, s_k0);
-        stage_rows(rows1, v_lane, plane_bytes, s_v0);
+    fetched next_k, next_v;   // codes of tiles t + 2 and t + 1, to be put before tile t
+    if constexpr (kCodes) {
+        const fetched k0 = fetch(rows1, 0), v0 = fetch(rows1, 1), k1 = fetch(rows2, 0);   // (past the end: the last group again)
+        next_v = fetch(rows2, 1);
+        rows2 = next_rows();
+        next_k = fetch(rows2, 0);
+        put(k0, 0, s_k0);
+        put(v0, 1, s_v0);
+        put(k1, 0, s_k1);
+    } else {
+        if (t_begin < n_tiles) {
+            stage_rows(rows1, k_lane, 0, s_k0);
+            stage_rows(rows1, v_lane, plane_bytes, s_v0);
+        }
+        if (t_begin + 1 < n_tiles) stage_rows(rows2, k_lane, 0, s_k1);
     }
-    if (t_begin + 1 < n_tiles) stage_rows(rows2, k_lane, 0, s_k1);
     // ---- this lane's query row (B operand) ------------------------------------------------------
     // element offset of the row of the column in q and out, or -1 if the column is
     // padding (recomputed at the end rather than kept in registers through the loop)
@@ -753,10 +818,19 @@ __global__ __launch_bounds__(kThreads, 3) void prefill_kernel(prefill_args a)
     // Tile t: its weights from the exponents beside the scores of tile t + 1, its output products beside the
     // exponents of tile t + 1.  K of tile t + 2 and V of tile t + 1 land meanwhile.
     auto stage_ahead = [&](int t, kv_u32x4* dk, kv_u32x4* dv) {
+        if constexpr (kCodes) {
+            if (t + 1 < n_tiles) put(next_v, 1, dv);
+            if (t + 2 < n_tiles) put(next_k, 0, dk);
+        }
         rows1 = rows2;
         rows2 = next_rows();
-        if (t + 1 < n_tiles) stage_rows(rows1, v_lane, plane_bytes, dv);
-        if (t + 2 < n_tiles) stage_rows(rows2, k_lane, 0, dk);
+        if constexpr (kCodes) {   // a tile further on
+            next_v = fetch(rows1, 1);
+            next_k = fetch(rows2, 0);
+        } else {
+            if (t + 1 < n_tiles) stage_rows(rows1, v_lane, plane_bytes, dv);
+            if (t + 2 < n_tiles) stage_rows(rows2, k_lane, 0, dk);
+        }
     };
     auto step = [&](int t, kv_u32x4* k_now, kv_u32x4* k_next, kv_u32x4* v_now, kv_u32x4* v_next) {
         stage_ahead(t, k_now, v_next);
@@ -834,7 +908,7 @@ __global__ __launch_bounds__(kThreads, 3) void prefill_kernel(prefill_args a)
                 for (int u = 0; u < 4; ++u)
                     *reinterpret_cast<f32x4*>(dst + 32 * j + 8 * u) = f32x4{o[j][4 * u], o[j][4 * u + 1], o[j][4 * u + 2], o[j][4 * u + 3]};
             if (half == 0) {
-                a.part_ml[rec * 2 + 0] = lt > 0.f ? -neg_mc : kNegInf;   // (no valid key: left out)
+                a.part_ml[rec * 2 + 0] = lt > 0.f ? -neg_mc : kCodes && lt != lt ? 0.f : kNegInf;   // (no valid key: left out)
                 a.part_ml[rec * 2 + 1] = lt;
             }
         } else if (orow >= 0) {
@@ -868,6 +942,8 @@ __global__ __launch_bounds__(kThreads, 3) void prefill_kernel(prefill_args a)
 // is the last again (two prompts of 1500 to 2500, 2 KV heads of 4 query heads, 58.9 us per call with eight, 56.9 so;
 // 33 tokens on 300 to 8000 in eight sequences, 1 KV head, most with more pieces than eight, 28.0 either way, 29.0 with
 // four for all).
+// KEEP_NAN: of an 8-bit cache, where a scale that is no number has to show in the rows that see its group.
+template <bool KEEP_NAN>
 __global__ __launch_bounds__(kThreads) void prefill_merge_kernel(prefill_args a)
 {
     const int4 tile = a.tiles[blockIdx.x];
@@ -894,7 +970,7 @@ __global__ __launch_bounds__(kThreads) void prefill_merge_kernel(prefill_args a)
             float mn = mm;
 #pragma unroll
             for (int u = 0; u < kBatch; ++u) {
-                if (z0 + u >= pieces || !(ml[u].y > 0.f)) ml[u] = make_float2(kNegInf, 0.f);
+                if (z0 + u >= pieces || (KEEP_NAN ? ml[u].y <= 0.f : !(ml[u].y > 0.f))) ml[u] = make_float2(kNegInf, 0.f);
                 mn = fmaxf(mn, ml[u].x);
             }
             if (mn == kNegInf) continue;
@@ -995,11 +1071,13 @@ extern "C" size_t paged_prefill_attn_workspace_bytes(const kv_view* view, int ba
     return prefill_workspace(view, batch, total_q, max_ctx_len, max_q_len).ask;
 }
 
-extern "C" int paged_prefill_attn(const void* q, void* out, const void* kv_pool, int64_t n_pool_blocks,
-                                  const int32_t* block_table, int64_t block_table_stride,
-                                  const int32_t* ctx_lens, const int32_t* q_offsets, int batch,
-                                  int64_t total_q, int max_ctx_len, int max_q_len, const kv_view* view,
-                                  float scale, void* workspace, size_t workspace_bytes, void* hip_stream)
+namespace {
+
+// Both entry points: format kBf16, or one of the 8-bit ones (scales are theirs).
+int prefill_call(const void* q, void* out, const void* kv_pool, const float* scales, int format, int64_t n_pool_blocks,
+                 const int32_t* block_table, int64_t block_table_stride, const int32_t* ctx_lens, const int32_t* q_offsets, int batch,
+                 int64_t total_q, int max_ctx_len, int max_q_len, const kv_view* view, float scale, void* workspace, size_t workspace_bytes,
+                 void* hip_stream)
 {
     if (!kv_view_ok(view) || batch < 0 || total_q < 0 || max_ctx_len < 0 || max_q_len < 0 ||
         n_pool_blocks < 0 || block_table_stride < 0 || max_q_len > max_ctx_len)
@@ -1012,7 +1090,12 @@ extern "C" int paged_prefill_attn(const void* q, void* out, const void* kv_pool,
     if (view->geom.head_dim != D || view->block_tokens % 16 != 0 || G > 16)
         return KV_ERR_UNSUPPORTED;
     if (batch > 65535 || view->n_kv_local > 65535) return KV_ERR_UNSUPPORTED;
+    if (format != kBf16 && (view->geom.base_block_size % 16 != 0 || !kv_aligned(kv_pool, 16) || !kv_aligned(q, 16) || !kv_aligned(out, 16) ||
+                            !kv_aligned(scales, 4)))
+        return KV_ERR_UNSUPPORTED;
     prefill_args a;
+    a.scales = scales;
+    a.x = q8_view_of(view);
     a.q = (const uint16_t*)q;
     a.out = (uint16_t*)out;
     a.pool = (const uint16_t*)kv_pool;
@@ -1086,12 +1169,42 @@ extern "C" int paged_prefill_attn(const void* q, void* out, const void* kv_pool,
     if (n_wgs > 0x7fffffff) return KV_ERR_UNSUPPORTED;
     const dim3 grid((unsigned)n_wgs);
     int slot = kv_prof_begin(KV_PROF_PREFILL, st);
+    auto* f = format == kE4M3 ? (cut ? prefill_kernel<true, kE4M3> : prefill_kernel<false, kE4M3>)
+              : format == kInt8 ? (cut ? prefill_kernel<true, kInt8> : prefill_kernel<false, kInt8>)
+                                : (cut ? prefill_kernel<true, kBf16> : prefill_kernel<false, kBf16>);
+    hipLaunchKernelGGL(f, grid, dim3(kThreads), 0, st, a);
     if (cut) {
-        hipLaunchKernelGGL((prefill_kernel<true>), grid, dim3(kThreads), 0, st, a);
-        hipLaunchKernelGGL(prefill_merge_kernel, dim3((unsigned)slots, (unsigned)Hl, kTileRows / (kThreads / 32)), dim3(kThreads), 0, st, a);
-    } else {
-        hipLaunchKernelGGL((prefill_kernel<false>), grid, dim3(kThreads), 0, st, a);
+        auto* merge = format == kBf16 ? prefill_merge_kernel<false> : prefill_merge_kernel<true>;
+        hipLaunchKernelGGL(merge, dim3((unsigned)slots, (unsigned)Hl, kTileRows / (kThreads / 32)), dim3(kThreads), 0, st, a);
     }
     kv_prof_end(KV_PROF_PREFILL, slot, st);
-    return kv_record_hip_error(hipGetLastError(), "paged_prefill_attn launch");
+    return kv_record_hip_error(hipGetLastError(), format == kBf16 ? "paged_prefill_attn launch" : "paged_prefill_attn_q8 launch");
+}
+
+}  // namespace
+
+extern "C" int paged_prefill_attn(const void* q, void* out, const void* kv_pool, int64_t n_pool_blocks,
+                                  const int32_t* block_table, int64_t block_table_stride,
+                                  const int32_t* ctx_lens, const int32_t* q_offsets, int batch,
+                                  int64_t total_q, int max_ctx_len, int max_q_len, const kv_view* view,
+                                  float scale, void* workspace, size_t workspace_bytes, void* hip_stream)
+{
+    return prefill_call(q, out, kv_pool, nullptr, kBf16, n_pool_blocks, block_table, block_table_stride, ctx_lens, q_offsets, batch, total_q,
+                        max_ctx_len, max_q_len, view, scale, workspace, workspace_bytes, hip_stream);
+}
+
+extern "C" size_t paged_prefill_attn_q8_workspace_bytes(const kv_view* view, int batch, int64_t total_q, int max_ctx_len, int max_q_len)
+{
+    return paged_prefill_attn_workspace_bytes(view, batch, total_q, max_ctx_len, max_q_len);
+}
+
+extern "C" int paged_prefill_attn_q8(const void* q, void* out, const void* kv_pool, const float* scales, int format, int64_t n_pool_blocks,
+                                     const int32_t* block_table, int64_t block_table_stride, const int32_t* ctx_lens,
+                                     const int32_t* q_offsets, int batch, int64_t total_q, int max_ctx_len, int max_q_len,
+                                     const kv_view* view, float scale, void* workspace, size_t workspace_bytes, void* hip_stream)
+{
+    if (!q8_format_ok(format)) return KV_ERR_INVALID_ARG;
+    if (!scales && batch > 0 && max_q_len > 0 && total_q > 0) return KV_ERR_INVALID_ARG;
+    return prefill_call(q, out, kv_pool, scales, format, n_pool_blocks, block_table, block_table_stride, ctx_lens, q_offsets, batch, total_q,
+                        max_ctx_len, max_q_len, view, scale, workspace, workspace_bytes, hip_stream);
 }

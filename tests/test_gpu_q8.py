@@ -1,0 +1,482 @@
+"""GPU parity of the operators on a cache held in 8 bits with their plain 64-bit forms: formats, sizes, layouts, masks and scales where
+they can go wrong.  Codes and scales are poisoned wherever no valid token lies, and compared whole."""
+import numpy as np
+import pytest
+import torch
+
+import operator_refs as ref
+import q8_refs as q8
+from operator_refs import DP, TP, place
+from paper_2602_22593_amd import binding as kv
+from q8_refs import E4M3, INT8
+
+from helpers import bf16_bits_to_f64
+from test_gpu_operators import DEV, G8B, G70B, TINY, dev, host, view_of, within
+
+pytestmark = pytest.mark.gpu
+TYPES = {E4M3: torch.float8_e4m3fn, INT8: torch.int8}
+FORMATS = [E4M3, INT8]
+
+
+def pool_of(x):
+    return torch.from_numpy(x.codes.reshape(len(x.codes), -1)).to(DEV).view(TYPES[x.fmt]), dev(x.scales.reshape(len(x.scales), -1))
+
+
+def codes_back(pool, x):
+    return pool.view(torch.uint8).cpu().numpy().reshape(x.codes.shape)
+
+
+def same(got, want):
+    return np.array_equal(got.view(np.uint32), want.view(np.uint32))
+
+
+def decode(x, pool=None, scales=None, **more):
+    c = x.c
+    if pool is None:
+        pool, scales = pool_of(x)
+    return kv.paged_decode_attn_q8(dev(c.q), pool, scales, dev(c.table), dev(c.ctx), view_of(c), max(int(c.ctx.max()), 1), **more)
+
+
+def prefill(x, pool=None, scales=None, **more):
+    c = x.c
+    if pool is None:
+        pool, scales = pool_of(x)
+    return kv.paged_prefill_attn_q8(dev(c.q), pool, scales, dev(c.table), dev(c.ctx), dev(c.q_off.astype(np.int32)), view_of(c),
+                                    int(c.ctx.max()), int(c.q_lens.max()), **more)
+
+
+# ---- kv_rope_append_q8 -------------------------------------------------------------------------------
+
+def check_append(x, qkv, turned, tol, q_lens, pool, scales, rotated):
+    """Codes and scales after an append of these rows: values and what is not rotated exactly, keys within half a step and their bound."""
+    c, fmt = x.c, x.fmt
+    hl, ql = c.info["n_kv_local"], c.info["n_q_local"]
+    v = bf16_bits_to_f64(qkv)[:, ql + hl:]
+    rows = np.stack([turned[:, ql:], v], axis=1)
+    numbers, want_scales = q8.appended(x, rows, q_lens)
+    got, got_scales = q8.values(codes_back(pool, x), fmt), host(scales).reshape(x.scales.shape)
+    assert same(got_scales, want_scales), "scales"
+    h0 = c.info["row_head0"]
+    if rotated:
+        at = 0
+        for s in range(len(c.ctx)):
+            n, k = int(c.ctx[s]), int(q_lens[s])
+            t = np.arange(n - k, n)
+            (b, slot), (_, g) = place(c, s, t), x.group_of(s, t)
+            scale = want_scales[b, 0, g, h0:h0 + hl].astype(np.float64)[..., None]
+            y = rows[at:at + k, 0] / scale
+            # the bound of one rounding to bf16 is left out: keys are rounded once, to 8 bits
+            off = np.abs(got[b, 0, slot, h0:h0 + hl] - y) - q8.half_step(np.abs(y) * 1.0001, fmt)
+            # (elements that are not rotated have no bound there: they are exact in fp32)
+            fp32 = np.maximum(tol[at:at + k, ql:] - ref.HALF_BF16 * np.abs(rows[at:at + k, 0]), 0) / scale
+            assert (off <= fp32 + 1e-12).all(), f"keys of {s}: {(off - fp32).max()}"
+            numbers[b, 0, slot, h0:h0 + hl] = got[b, 0, slot, h0:h0 + hl]
+            at += k
+    assert np.array_equal(got, numbers, equal_nan=True), "values, or codes that are nobody's"
+
+
+def rope_inputs(c, axes, rot, index=81):
+    total = int(c.q_off[-1])
+    hl, ql, d = c.info["n_kv_local"], c.info["n_q_local"], c.w.head_dim
+    rng = np.random.default_rng(index)
+    positions = rng.integers(0, 5000, (axes, total)).astype(np.int32)
+    half = rot // 2
+    freq = (1e4 ** (-np.arange(half) / max(half, 1))).astype(np.float32)
+    return q8.normal_rows(total, ql, hl, d, index), positions, freq, [int(a) for a in rng.integers(0, axes, half)]
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("geom,triple,ctx,q_lens,axes,adjacent,rot", [
+    (TINY, (DP, 1, 0), [17, 1, 300, 64, 16], [1, 1, 1, 1, 1], 1, False, 64),
+    (G8B, (DP, 1, 0), [33, 47, 48, 1, 2, 1000], [1] * 6, 2, True, 128),
+    (G70B, (TP, 8, 5), [130] * 300, [1] * 300, 1, False, 64),
+    ((6, 2, 128, 32), (TP, 2, 1), [40, 63, 64, 65], [1] * 4, 1, False, 16),
+])
+def test_append_one_token(fmt, geom, triple, ctx, q_lens, axes, adjacent, rot):
+    x = q8.case(geom, triple, ctx, q_lens, fmt)
+    qkv, positions, freq, axis_of = rope_inputs(x.c, axes, rot)
+    hl, ql = x.c.info["n_kv_local"], x.c.info["n_q_local"]
+    want, tol = ref.rotated(bf16_bits_to_f64(qkv)[:, :ql + hl], positions, freq, axis_of, adjacent)
+    pool, scales = pool_of(x)
+    parts = dev(qkv)
+    out = kv.kv_rope_append_q8(pool, scales, view_of(x.c), parts[:, :ql], parts[:, ql:ql + hl], parts[:, ql + hl:], dev(positions), dev(freq),
+                               dev(x.c.table), dev(x.c.ctx), axes=axis_of, pairs=kv.KV_ROPE_ADJACENT if adjacent else kv.KV_ROPE_HALVES)
+    within(host(out), want[:, :ql], tol[:, :ql], "q")
+    check_append(x, qkv, want, tol, q_lens, pool, scales, True)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("geom,triple,ctx,q_lens,axes,adjacent,rot", [
+    (TINY, (TP, 2, 1), [40, 33, 5, 0, 64], [3, 33, 1, 0, 0], 2, True, 32),
+    (TINY, (DP, 1, 0), [16, 17, 31, 32, 33, 48], [16, 2, 15, 17, 1, 20], 1, False, 64),
+    (G8B, (DP, 1, 0), [300, 1, 77], [129, 1, 40], 3, False, 128),
+    (G8B, (TP, 4, 2), [2100], [2100], 4, True, 128),
+    (G8B, (DP, 4, 3), [50, 61], [20, 7], 3, False, 64),
+    (G70B, (TP, 8, 5), [16] * 70 + [1200], [2] * 70 + [1100], 1, False, 16),
+    ((6, 2, 128, 32), (TP, 2, 1), [200, 31, 64], [190, 30, 33], 2, False, 48),
+    ((4, 2, 64, 128), (DP, 1, 0), [300, 128, 129], [290, 1, 128], 1, False, 64),
+    ((12, 6, 64, 48), (DP, 3, 1), [100, 47], [60, 40], 1, True, 64),
+    (G8B, (DP, 1, 0), [5, 3], [2, 3], 1, False, 0),
+])
+def test_append_several_tokens(fmt, geom, triple, ctx, q_lens, axes, adjacent, rot):
+    x = q8.case(geom, triple, ctx, q_lens, fmt)
+    qkv, positions, freq, axis_of = rope_inputs(x.c, axes, rot)
+    hl, ql, total = x.c.info["n_kv_local"], x.c.info["n_q_local"], int(x.c.q_off[-1])
+    want, tol = ref.rotated(bf16_bits_to_f64(qkv)[:, :ql + hl], positions, freq, axis_of, adjacent)
+    # two rows more than the sequences have: they stay as they are
+    parts = dev(np.concatenate([qkv, qkv[:1], qkv[:1]]))
+    pos = np.concatenate([positions, positions[:, :1], positions[:, :1]], axis=1)
+    out = torch.full((total + 2, ql, geom[2]), 7.0, dtype=torch.bfloat16, device=DEV)
+    pool, scales = pool_of(x)
+    kv.kv_rope_append_q8(pool, scales, view_of(x.c), parts[:, :ql], parts[:, ql:ql + hl], parts[:, ql + hl:], dev(pos), dev(freq),
+                         dev(x.c.table), dev(x.c.ctx), dev(x.c.q_off.astype(np.int32)), axes=axis_of,
+                         pairs=kv.KV_ROPE_ADJACENT if adjacent else kv.KV_ROPE_HALVES, out=out)
+    got = host(out)
+    assert (out[total:] == 7.0).all()
+    within(got[:total], want[:, :ql], tol[:, :ql], "q")
+    check_append(x, qkv, want, tol, q_lens, pool, scales, rot > 0)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_append_without_queries_grows_scales_step_by_step(fmt):
+    """Tokens of ever larger numbers one by one: older ones are rounded again each time their group's scale grows."""
+    x = q8.case(G8B, (DP, 1, 0), [40, 37], [1, 1], fmt, size=2.0 ** -6)
+    hl, d = 8, 128
+    pool, scales = pool_of(x)
+    table, view = dev(x.c.table), view_of(x.c)
+    for step in range(4):
+        rows = q8.normal_rows(2, 0, hl, d, 90 + step)
+        kf = (bf16_bits_to_f64(rows) * 4.0 ** (step - 2)).astype(np.float32)
+        parts = torch.from_numpy(kf).to(DEV).bfloat16()
+        x.c.ctx = (np.array([40, 37]) + step).astype(np.int32)
+        assert kv.kv_rope_append_q8(pool, scales, view, None, parts[:, :hl], parts[:, hl:], None, None, table, dev(x.c.ctx)) is None
+        exact = np.stack([kf[:, :hl], kf[:, hl:]], axis=1).astype(np.float64)
+        numbers, want_scales = q8.appended(x, exact, [1, 1])
+        assert same(host(scales).reshape(x.scales.shape), want_scales), step
+        got = codes_back(pool, x)
+        assert np.array_equal(q8.values(got, fmt), numbers, equal_nan=True), step
+        x.codes, x.scales = got, want_scales
+
+
+@pytest.mark.parametrize("one", [True, False])
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_numbers_that_are_not_finite_make_their_group_nan(fmt, one):
+    """An infinity in a key, a NaN in a value: the scale of that head and plane is NaN and stays so, the others are as ever."""
+    x = q8.case(TINY, (DP, 1, 0), [20, 20], [1, 1], fmt)
+    rows = bf16_bits_to_f64(q8.normal_rows(2, 0, 2, 64, 95))
+    rows[0, 1, 5], rows[1, 2, 63] = np.inf, np.nan
+    parts = torch.from_numpy(rows.astype(np.float32)).to(DEV).bfloat16()
+    pool, scales = pool_of(x)
+    off = None if one else dev(np.array([0, 1, 2], np.int32))
+    for again in range(2):
+        kv.kv_rope_append_q8(pool, scales, view_of(x.c), None, parts[:, :2], parts[:, 2:], None, None, dev(x.c.table), dev(x.c.ctx), off)
+        parts = torch.nan_to_num(parts, nan=1.0, posinf=1.0)
+        got = host(scales).reshape(x.scales.shape)
+        for s, p, h in [(s, p, h) for s in (0, 1) for p in (0, 1) for h in (0, 1)]:
+            b, g = x.group_of(s, 19)
+            assert np.isnan(got[b, p, g, h]) == ((s, p, h) in ((0, 0, 1), (1, 1, 0))), (again, s, p, h)
+    x.codes, x.scales = codes_back(pool, x), got
+    out = bf16_bits_to_f64(host(decode(x, pool, scales)))
+    want, tol = q8.attention(x, causal=False)
+    nan = np.zeros((2, 8), bool)
+    nan[0, 4:], nan[1, :4] = True, True
+    assert (np.isnan(out).all(axis=2) == nan).all() and (np.isnan(out).any(axis=2) == nan).all()
+    assert (np.abs(out - want) <= tol)[~nan].all()
+
+
+@pytest.mark.parametrize("one", [True, False])
+def test_append_skips_places_that_are_none(one):
+    """A padded sequence (length 0), a block of -1, one past the pool and one past the table: queries turn, nothing is written."""
+    x = q8.case(TINY, (DP, 1, 0), [20, 20, 20, 20], [1, 1, 1, 1], E4M3)
+    qkv, positions, freq, axis_of = rope_inputs(x.c, 1, 64)
+    ctx, table = x.c.ctx.copy(), x.c.table.copy()
+    ctx[0], table[1, 1], table[2, 1], ctx[3] = 0, -1, len(x.codes), 16 * table.shape[1] + 1
+    pool, scales = pool_of(x)
+    out = kv.kv_rope_append_q8(pool, scales, view_of(x.c), dev(qkv[:, :8]), dev(qkv[:, 8:10]), dev(qkv[:, 10:]), dev(positions), dev(freq),
+                               dev(table), dev(ctx), None if one else dev(np.arange(5, dtype=np.int32)), axes=axis_of)
+    want, tol = ref.rotated(bf16_bits_to_f64(qkv)[:, :8], positions, freq, axis_of, False)
+    within(host(out), want, tol)
+    assert np.array_equal(codes_back(pool, x), x.codes) and same(host(scales).reshape(x.scales.shape), x.scales)
+
+
+def test_append_of_zeros_and_of_the_smallest_and_largest_numbers():
+    x = q8.case(TINY, (DP, 1, 0), [1, 1, 1, 1], [1] * 4, INT8)
+    rows = np.zeros((4, 4, 64), np.float32)
+    rows[1], rows[2], rows[3, :, 0] = 2.0 ** -126, 3.3e38, -1.0
+    rows[2] = torch.from_numpy(rows[2]).bfloat16().float().numpy()
+    parts = torch.from_numpy(rows).to(DEV).bfloat16()
+    pool, scales = pool_of(x)
+    kv.kv_rope_append_q8(pool, scales, view_of(x.c), None, parts[:, :2], parts[:, 2:], None, None, dev(x.c.table), dev(x.c.ctx))
+    numbers, want = q8.appended(x, np.stack([rows[:, :2], rows[:, 2:]], axis=1).astype(np.float64), [1] * 4)
+    assert same(host(scales).reshape(x.scales.shape), want)
+    assert np.array_equal(q8.values(codes_back(pool, x), INT8), numbers, equal_nan=True)
+
+
+# ---- paged_decode_attn_q8 ----------------------------------------------------------------------------
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("geom,triple,ctx", [
+    (TINY, (DP, 1, 0), [17, 64, 150, 300]),                        # a workgroup a pair
+    (TINY, (TP, 2, 1), [1, 2, 15, 16, 17, 31, 32, 33, 127, 128, 129, 0, 512]),
+    (TINY, (DP, 1, 0), [513, 0, 0, 5, 1900, 0]),                   # pairs are cut
+    (G8B, (DP, 1, 0), [700, 33, 2049, 1, 64, 0, 1300]),
+    (G8B, (TP, 4, 3), [700, 33, 2049, 1, 64, 0, 1300]),
+    (G8B, (DP, 4, 1), [1000, 31]),                                 # a rank's heads in place
+    (G70B, (TP, 8, 2), [3000, 0, 640, 1] + [40] * 30),
+    (G70B, (DP, 1, 0), [600, 1]),
+    ((48, 3, 128, 32), (DP, 1, 0), [600, 95, 97]),                 # sixteen query heads on one, blocks of 32
+    ((5, 1, 64, 16), (DP, 1, 0), [9000, 20]),
+    ((6, 6, 128, 48), (TP, 3, 2), [700, 290]),                     # one on one, groups that are no power of two
+])
+def test_decode(fmt, geom, triple, ctx):
+    x = q8.case(geom, triple, ctx, [1 if n else 0 for n in ctx], fmt)
+    x.c.q = q_for(x, len(ctx))
+    within(host(decode(x)), *q8.attention(x, causal=False))
+
+
+def q_for(x, n):
+    from paper_2602_22593_amd import workloads as wl
+    return wl.randn_bf16((n, x.c.info["n_q_local"], x.c.w.head_dim), wl.generator(82, wl.SUB_QUERY))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("ctx", [[300, 17], [2000, 600, 33]])
+def test_decode_with_any_scales(fmt, ctx):
+    x = q8.case(G8B, (TP, 2, 1), ctx, [1] * len(ctx), fmt, powers=False)
+    x.c.q = q_for(x, len(ctx))
+    within(host(decode(x, scale=0.2)), *q8.attention(x, causal=False, scale=0.2))
+
+
+def test_decode_of_many_sequences():
+    """More sequences than a workgroup has threads, some without tokens, some long."""
+    rng = np.random.default_rng(11)
+    ctx = rng.integers(0, 40, 700)
+    ctx[rng.integers(0, 700, 200)] = 0
+    ctx[[0, 350, 699]] = [600, 1500, 900]
+    x = q8.case((8, 2, 64, 16), (TP, 2, 0), ctx, np.minimum(ctx, 1), E4M3)
+    x.c.q = q_for(x, 700)
+    within(host(decode(x)), *q8.attention(x, causal=False))
+
+
+def test_decode_with_large_scores_and_a_reference_that_moves():
+    """Scores up to some hundreds, largest at the end: weights of all that came before vanish."""
+    x = q8.case(G8B, (TP, 8, 0), [1500, 77], [1, 1], INT8, size=16.0)
+    x.c.q = q_for(x, 2)
+    out = bf16_bits_to_f64(host(decode(x)))
+    want, tol = q8.attention(x, causal=False)
+    # a score of s is off by 2^-21 s at most (sums of 128 products in fp32, and its exponent): weights by twice that for s up to 2000
+    assert np.isfinite(out).all() and (np.abs(out - want) <= tol + 2 * 2000 * 2.0 ** -21 * np.abs(want).max()).all()
+
+
+def test_decode_into_given_buffers_and_on_another_stream():
+    x = q8.case(G8B, (DP, 1, 0), [1000, 5, 333], [1] * 3, E4M3)
+    x.c.q = q_for(x, 3)
+    pool, scales = pool_of(x)
+    view, want = view_of(x.c), q8.attention(x, causal=False)
+    need = kv.paged_decode_attn_q8_workspace_bytes(view, 3, 1000)
+    guard = torch.full((need + 256,), 77, dtype=torch.uint8, device=DEV)
+    out = torch.empty((3, 32, 128), dtype=torch.bfloat16, device=DEV)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    assert decode(x, pool, scales, out=out, workspace=guard[:need], stream=stream) is out
+    stream.synchronize()
+    within(host(out), *want)
+    assert (guard[need:] == 77).all()
+    torch.cuda.current_stream().wait_stream(stream)
+
+
+# ---- paged_prefill_attn_q8 ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("geom,triple,ctx,q_lens", [
+    (G8B, (DP, 1, 0), [40, 31, 32, 33, 1], [8, 31, 2, 33, 1]),
+    (G8B, (TP, 4, 1), [300, 64, 17, 0, 130], [300, 1, 17, 0, 65]),
+    (G8B, (DP, 4, 2), [400, 333], [31, 200]),
+    (G70B, (TP, 8, 3), [1200, 16, 130, 2], [16, 16, 7, 2]),                  # keys cut
+    (G8B, (TP, 2, 1), [2000, 700], [40, 3]),
+    (G8B, (TP, 4, 0), [700] * 9, [200] * 9),                                 # several tiles, none cut
+    ((10, 2, 128, 32), (DP, 1, 0), [77, 500, 200], [13, 33, 200]),           # odd groups
+    ((32, 2, 128, 48), (DP, 1, 0), [97, 50], [49, 50]),
+])
+def test_prefill(fmt, geom, triple, ctx, q_lens):
+    x = q8.case(geom, triple, ctx, q_lens, fmt)
+    within(host(prefill(x)), *q8.attention(x, causal=True))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_prefill_with_any_scales(fmt):
+    x = q8.case(G8B, (TP, 4, 1), [300, 70], [100, 70], fmt, powers=False)
+    within(host(prefill(x, scale=0.1)), *q8.attention(x, causal=True, scale=0.1, rounded=True))
+
+
+@pytest.mark.parametrize("cut", [False, True])
+@pytest.mark.parametrize("plane", [0, 1])
+def test_prefill_rows_see_nan_scales_of_their_groups_only(plane, cut):
+    """A NaN scale in the middle: rows before that group keep their results, in both lanes and in pieces of cut ranges."""
+    ctx, q_lens = ([1500, 200], [60, 200]) if cut else ([200, 100], [200, 100])
+    x = q8.case(G8B, (TP, 8, 0), ctx, q_lens, E4M3)
+    want, tol = q8.attention(x, causal=True)
+    at = ctx[0] - 40
+    b, g = x.group_of(0, at)
+    x.scales[b, plane, g, x.c.info["row_head0"]] = np.nan
+    out = bf16_bits_to_f64(host(prefill(x)))
+    first = ctx[0] - q_lens[0]
+    hit = np.zeros(len(out), bool)
+    hit[:q_lens[0]] = first + np.arange(q_lens[0]) >= at // 16 * 16
+    assert np.isnan(out[hit]).all() and (np.abs(out - want) <= tol)[~hit].all()
+
+
+# ---- kv_repack_q8 ------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("geom,src,dst,ctx", [
+    (G8B, (DP, 1, 0), (TP, 4, 2), [300, 1, 17, 0, 64]),
+    (G8B, (TP, 4, 2), (DP, 1, 0), [300, 1, 17, 0, 64]),
+    (G8B, (TP, 2, 1), (TP, 8, 5), [129, 500]),
+    (TINY, (DP, 1, 0), (TP, 2, 0), [33, 2000]),
+    ((12, 6, 64, 32), (DP, 3, 1), (TP, 2, 0), [40, 100]),
+    (G8B, (DP, 1, 0), (TP, 4, 2), [9000]),
+])
+def test_repack(fmt, geom, src, dst, ctx):
+    a = q8.case(geom, src, ctx, [0] * len(ctx), fmt)
+    z = ref.case(geom, dst, ctx, [0] * len(ctx))
+    # both tables in one pool: the destination's blocks behind the source's
+    n = len(a.codes)
+    table = np.where(z.table >= 0, z.table + n, -1).astype(np.int32)
+    grown = n + len(z.pool)
+    codes = np.concatenate([a.codes.reshape(n, -1), np.full((grown - n, a.codes[0].size), 0x55, np.uint8)])
+    scales = np.concatenate([a.scales.reshape(n, -1), np.full((grown - n, a.scales[0].size), 0.25, np.float32)])
+    z.table = table
+    want_codes, want_scales = q8.repacked(a, z, codes, scales)
+    pool, sc = torch.from_numpy(codes).to(DEV).view(TYPES[fmt]), dev(scales)
+    kv.kv_repack_q8(pool, sc, view_of(a.c), view_of(z), dev(a.c.table), dev(table), dev(a.c.ctx), int(max(ctx)))
+    assert np.array_equal(pool.view(torch.uint8).cpu().numpy(), want_codes.reshape(codes.shape))
+    assert same(host(sc), want_scales.reshape(scales.shape))
+
+
+# ---- together ----------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_prompt_decode_steps_and_a_change_of_layout(fmt):
+    """As an engine runs them: prompts written and attended to, decode steps, the cache taken over by one rank of four and decoded there.
+    Every stage is checked against the plain forms fed with what the stage before left."""
+    lens = [37, 150, 16]
+    x = q8.case(G8B, (DP, 1, 0), [n + 3 for n in lens], lens, fmt)
+    x.codes[:], x.scales[:] = q8.POISON[fmt], np.nan
+    c, hl, ql, d = x.c, 8, 32, 128
+    view, table = view_of(c), dev(c.table)
+    pool, scales = pool_of(x)
+    freq = (1e4 ** (-np.arange(64) / 64)).astype(np.float32)
+    c.ctx, off = np.array(lens, np.int32), np.concatenate([[0], np.cumsum(lens)])
+    qkv = q8.normal_rows(sum(lens), ql, hl, d, 100)
+    positions = np.concatenate([np.arange(n) for n in lens]).astype(np.int32)
+    parts = dev(qkv)
+    q = kv.kv_rope_append_q8(pool, scales, view, parts[:, :ql], parts[:, ql:ql + hl], parts[:, ql + hl:], dev(positions), dev(freq), table,
+                             dev(c.ctx), dev(off.astype(np.int32)))
+    want, tol = ref.rotated(bf16_bits_to_f64(qkv)[:, :ql + hl], positions[None], freq, [0] * 64, False)
+    within(host(q), want[:, :ql], tol[:, :ql])
+    check_append(x, qkv, want, tol, lens, pool, scales, True)
+    x.codes, x.scales = codes_back(pool, x), host(scales).reshape(x.scales.shape)
+    c.q, c.q_off, c.q_lens = host(q), off, np.array(lens)
+    within(host(prefill(x, pool, scales)), *q8.attention(x, causal=True))
+    for step in range(3):
+        c.ctx = c.ctx + 1
+        c.q_off, c.q_lens = np.arange(4), np.ones(3, int)
+        qkv, positions = q8.normal_rows(3, ql, hl, d, 101 + step), c.ctx - 1
+        parts = dev(qkv)
+        q = kv.kv_rope_append_q8(pool, scales, view, parts[:, :ql], parts[:, ql:ql + hl], parts[:, ql + hl:], dev(positions), dev(freq),
+                                 table, dev(c.ctx))
+        want, tol = ref.rotated(bf16_bits_to_f64(qkv)[:, :ql + hl], positions[None], freq, [0] * 64, False)
+        check_append(x, qkv, want, tol, [1, 1, 1], pool, scales, True)
+        x.codes, x.scales, c.q = codes_back(pool, x), host(scales).reshape(x.scales.shape), host(q)
+        within(host(decode(x, pool, scales)), *q8.attention(x, causal=False))
+    # rank 1 of 4 takes the cache over
+    z = q8.case(G8B, (TP, 4, 1), c.ctx, [1, 1, 1], fmt)
+    n = len(x.codes)
+    both = torch.cat([pool.view(torch.uint8), torch.full((len(z.codes), pool.shape[1]), q8.POISON[fmt], dtype=torch.uint8, device=DEV)])
+    both_scales = torch.cat([scales, torch.full((len(z.codes), scales.shape[1]), float("nan"), device=DEV)])
+    there = dev(np.where(z.c.table >= 0, z.c.table + n, -1).astype(np.int32))
+    kv.kv_repack_q8(both.view(TYPES[fmt]), both_scales, view, view_of(z.c), table, there, dev(c.ctx), int(c.ctx.max()))
+    got = kv.paged_decode_attn_q8(dev(np.ascontiguousarray(c.q[:, 8:16])), both.view(TYPES[fmt]), both_scales, there, dev(c.ctx), view_of(z.c),
+                                  int(c.ctx.max()))
+    want, tol = q8.attention(x, causal=False)
+    within(host(got), want[:, 8:16], tol[:, 8:16])
+
+
+def test_a_decode_step_replayed_from_a_graph():
+    """One captured step, append and attention, replayed with other rows and lengths in the captured buffers; eager work in between."""
+    x = q8.case(G8B, (TP, 2, 1), [600, 47, 130, 0], [1, 1, 1, 0], INT8)
+    c, hl, ql, d = x.c, 4, 16, 128
+    view, table, n = view_of(c), dev(c.table), dev(c.ctx)
+    pool, scales = pool_of(x)
+    freq = dev((1e4 ** (-np.arange(64) / 64)).astype(np.float32))
+    rows, positions = torch.zeros((4, ql + 2 * hl, d), dtype=torch.bfloat16, device=DEV), torch.zeros(4, dtype=torch.int32, device=DEV)
+    q, out = (torch.zeros((4, ql, d), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    ws = torch.empty(kv.paged_decode_attn_q8_workspace_bytes(view, 4, 600), dtype=torch.uint8, device=DEV)
+
+    def step():
+        kv.kv_rope_append_q8(pool, scales, view, rows[:, :ql], rows[:, ql:ql + hl], rows[:, ql + hl:], positions, freq, table, n, out=q)
+        kv.paged_decode_attn_q8(q, pool, scales, table, n, view, 600, out=out, workspace=ws)
+    kept = pool.clone(), scales.clone()
+    step()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step()
+    pool.copy_(kept[0])
+    scales.copy_(kept[1])
+    for rep in range(3):
+        # (the last of the tokens that are there is written anew, in the first replay; then lengths within what the case has)
+        qkv = q8.normal_rows(4, ql, hl, d, 110 + rep)
+        c.ctx = np.array([600 - rep, 47 - 13 * rep, 130 - rep, 0], np.int32)
+        rows.copy_(dev(qkv))
+        n.copy_(dev(c.ctx))
+        positions.copy_(n - 1)
+        out.zero_()
+        ws.fill_(255 - rep)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        want, tol = ref.rotated(bf16_bits_to_f64(qkv)[:3, :ql + hl], (c.ctx - 1)[None, :3], freq.cpu().numpy(), [0] * 64, False)
+        check_append(x, qkv[:3], want, tol, [1, 1, 1, 0], pool, scales, True)
+        x.codes, x.scales, c.q = codes_back(pool, x), host(scales).reshape(x.scales.shape), host(q)
+        within(host(out), *q8.attention(x, causal=False), f"replay {rep}")
+
+
+def test_offsets_past_32_bits():
+    """A pool of codes past 4 GiB with the caches' blocks spread over all of it: written, attended to and moved."""
+    ctx = [400, 77]
+    x = q8.case(G8B, (DP, 1, 0), ctx, [400, 77], INT8)
+    n_blocks = (5 << 30) // (32 << 10)
+    used = int((x.c.table >= 0).sum())
+    spread = np.linspace(0, n_blocks // 2 - 1, used).astype(np.int64)
+    table = x.c.table.copy()
+    small = table[table >= 0].copy()
+    table[table >= 0] = spread[::-1]
+    pool = torch.empty((n_blocks, 32 << 10), dtype=torch.int8, device=DEV)
+    scales = torch.empty((n_blocks, 16), device=DEV)
+    at = torch.from_numpy(spread[::-1].copy()).to(DEV)
+    pool[at] = torch.from_numpy(x.codes[small].reshape(used, -1)).to(DEV).view(torch.int8)
+    scales[at] = torch.from_numpy(x.scales[small].reshape(used, -1)).to(DEV)
+    c = x.c
+    view, n, off = view_of(c), dev(c.ctx), dev(c.q_off.astype(np.int32))
+    want, tol = q8.attention(x, causal=True)
+    out = kv.paged_prefill_attn_q8(dev(c.q), pool, scales, dev(table), n, off, view, 400, 400)
+    within(host(out), want, tol)
+    last = [399, 476]
+    out = kv.paged_decode_attn_q8(dev(np.ascontiguousarray(c.q[last])), pool, scales, dev(table), n, view, 400)
+    within(host(out), want[last], tol[last])
+    # to blocks of the upper half under another layout
+    dst = kv.kv_view_create(*G8B, TP, 2, 1)
+    there = np.full((2, 13), -1, np.int32)
+    there[0, :13], there[1, :3] = n_blocks - 1 - 1000 * np.arange(13), n_blocks - 20000 - 1000 * np.arange(3)
+    kv.kv_repack_q8(pool, scales, view, dst, dev(table), dev(there), n, 400)
+    out = kv.paged_decode_attn_q8(dev(np.ascontiguousarray(c.q[last][:, 16:])), pool, scales, dev(there), n, dst, 400)
+    within(host(out), want[last][:, 16:], tol[last][:, 16:])
+    # the last tokens written again, rotated by nothing
+    rows = q8.normal_rows(2, 0, 8, 128, 120)
+    parts = dev(rows)
+    kv.kv_rope_append_q8(pool, scales, view, None, parts[:, :8], parts[:, 8:], None, None, dev(table), n)
+    numbers, want_scales = q8.appended(x, np.stack([bf16_bits_to_f64(rows)[:, :8], bf16_bits_to_f64(rows)[:, 8:]], axis=1), [1, 1])
+    got = pool[at].view(torch.uint8).cpu().numpy().reshape((used,) + x.codes.shape[1:])
+    assert np.array_equal(q8.values(got, INT8), numbers[small]) and same(scales[at].cpu().numpy().reshape(x.scales[small].shape), want_scales[small])
