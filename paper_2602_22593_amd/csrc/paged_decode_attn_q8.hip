@@ -37,6 +37,8 @@ struct decode_args {
     int32_t group, batch;
     int32_t head_sets;     // n_kv_local / HPW
     int32_t whole;         // a workgroup takes a whole pair (sequence, set of heads)
+    int32_t unit_shift, start_units;   // of the axis that is cut
+    uint32_t inverse;      // 2^32 / workgroups
     float* part_o;         // [2 * workgroups][HPW * G][D] sums of a cut pair's piece
     float* part_ml;        // [2 * workgroups][HPW * G][2] (reference in exponent units, sum of weights)
     int2* ends;            // [batch * head_sets] workgroups that hold a pair's first and last piece
@@ -48,38 +50,84 @@ __device__ __forceinline__ float uniform(float x) { return __builtin_bit_cast(fl
 typedef const __attribute__((address_space(4))) int32_t* const_ints;
 typedef const __attribute__((address_space(4))) float* const_floats;
 
-// Steps of the pairs lie on one axis, sequence by sequence, in each its sets of heads in turn.  Thread i of the workgroup sums the steps of
-// sequences [i k, (i + 1) k), k = batch / 256 rounded up; s_incl are the inclusive sums over the threads.
-struct axis_sums {
-    long long total;
-    int per;   // k
-};
-template <int STEP>
-__device__ __forceinline__ int steps_of(int n) { return n > 0 ? (n + STEP - 1) / STEP : 0; }
+// The pairs lie on one axis, sequence by sequence, in each its sets of heads in turn: a pair's start counts start_units, each of its steps
+// 2^unit_shift.  Workgroup i takes the steps between two positions on it, which all workgroups work out alike.  (A start costs about what a step does:
+// lengths of the pieces are then as unequal as whole steps make them and no more.)
+__device__ __forceinline__ int steps_of(int n, int step) { return n > 0 ? (int)(((unsigned)n + step - 1) / (unsigned)step) : 0; }
 
-template <int STEP>
-__device__ __forceinline__ axis_sums sum_axis(const decode_args& a, long long* s_incl)
+template <int CTRL>
+__device__ __forceinline__ int dpp_shr(int x) { return __builtin_amdgcn_update_dpp(0, x, CTRL, 0xf, 0xf, true); }
+// Inclusive sum over the 64 lanes.
+__device__ __forceinline__ int inclusive_sum(int x, int lane)
 {
-    const int tid = threadIdx.x, per = (a.batch + kThreads - 1) / kThreads;
-    long long mine = 0;
-    for (int i = 0; i < per; ++i) {
-        const int s = tid * per + i;
-        if (s < a.batch) mine += steps_of<STEP>(a.ctx_lens[s]);
-    }
-    // inclusive sum over the wavefront, then over the workgroup
+    x += dpp_shr<0x111>(x);
+    x += dpp_shr<0x112>(x);
+    x += dpp_shr<0x114>(x);
+    x += dpp_shr<0x118>(x);
+    const int t0 = __builtin_amdgcn_readlane(x, 15), t1 = t0 + __builtin_amdgcn_readlane(x, 31), t2 = t1 + __builtin_amdgcn_readlane(x, 47);
+    const int row = lane >> 4;
+    return x + (row == 0 ? 0 : row == 1 ? t0 : row == 2 ? t1 : t2);
+}
+struct axis_place {
+    int s, set, step;
+};
+// Steps of sequences s0 + 4 lane .. + 3 of a run of 256, their sum over the lanes so far, and that of those with any.
+struct axis_run {
+    int steps[4], sum, some, sum_incl, some_incl;
+};
+__device__ __forceinline__ axis_run run_of(const decode_args& a, int s0, int lane, int step)
+{
+    axis_run r;
+    r.sum = r.some = 0;
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const long long y = __shfl_up(mine, d);
-        if ((tid & 63) >= d) mine += y;
+    for (int i = 0; i < 4; ++i) {
+        const int s = s0 + 4 * lane + i;
+        r.steps[i] = s < a.batch ? steps_of(a.ctx_lens[s], step) : 0;
+        r.sum += r.steps[i];
+        r.some += r.steps[i] > 0;
     }
-    s_incl[tid] = mine;
-    __syncthreads();
-    long long before = 0;
-    for (int w = 0; w < (tid >> 6); ++w) before += s_incl[64 * w + 63];
-    __syncthreads();
-    s_incl[tid] = mine + before;
-    __syncthreads();
-    return {s_incl[kThreads - 1], per};
+    r.sum_incl = inclusive_sum(r.sum, lane);
+    r.some_incl = inclusive_sum(r.some, lane);
+    return r;
+}
+// The step that starts at or behind position x of a run (x less than what the run counts).
+__device__ __forceinline__ axis_place place_in(const decode_args& a, const axis_run& r, int s0, int x, int start_units, int lane)
+{
+    const int hs = a.head_sets;
+    const int mine = hs * ((r.sum << a.unit_shift) + start_units * r.some);
+    const int incl = hs * ((r.sum_incl << a.unit_shift) + start_units * r.some_incl);
+    const int at = __builtin_ctzll(__builtin_amdgcn_ballot_w64(incl > x));
+    x -= __builtin_amdgcn_readlane(incl - mine, at);
+    int i = 0, n = __builtin_amdgcn_readlane(r.steps[0], at), per_pair = n > 0 ? (n << a.unit_shift) + start_units : 0;
+#pragma unroll
+    for (int k = 1; k < 4; ++k) {
+        const int next = __builtin_amdgcn_readlane(r.steps[k], at);
+        if (i == k - 1 && x >= hs * per_pair) {
+            x -= hs * per_pair;
+            i = k;
+            n = next;
+            per_pair = n > 0 ? (n << a.unit_shift) + start_units : 0;
+        }
+    }
+    int set = 0;
+    if (hs > 1) {   // x / per_pair, less than hs
+        set = uniform((int)((float)x * __builtin_amdgcn_rcpf((float)per_pair)));
+        set += (set + 1) * per_pair <= x ? 1 : 0;
+        set -= set * per_pair > x ? 1 : 0;
+    }
+    const int in = x - set * per_pair - start_units;
+    return {s0 + 4 * at + i, set, in <= 0 ? 0 : (in + (1 << a.unit_shift) - 1) >> a.unit_shift};
+}
+__device__ __forceinline__ axis_place place_at(const decode_args& a, axis_run r, int x, int start_units, int lane, int step)
+{
+    for (int s0 = 0;;) {
+        const int all = a.head_sets * ((__builtin_amdgcn_readlane(r.sum_incl, 63) << a.unit_shift) + start_units * __builtin_amdgcn_readlane(r.some_incl, 63));
+        if (x < all) return place_in(a, r, s0, x, start_units, lane);
+        x -= all;
+        s0 += 256;
+        if (s0 >= a.batch) return {a.batch, 0, 0};
+        r = run_of(a, s0, lane, step);
+    }
 }
 
 // V^T operands of one dword (dims 4 w .. 4 w + 3) of eight tokens: operand b of dim 4 w + b holds the eight tokens' values.
@@ -109,7 +157,6 @@ __global__ __launch_bounds__(kThreads) void decode_q8_kernel(decode_args a)
     constexpr int kSubs = kWaves / HPW;     // wavefronts that share a head
     constexpr int kStep = kTile * kSubs;    // tokens of a step
     constexpr int kPad = D + 4;
-    __shared__ long long s_incl[kThreads];
     __shared__ float s_o[kWaves][16][kPad];
     __shared__ float s_ml[kWaves][16][2];
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), m = lane & 15, g = lane >> 4;
@@ -121,46 +168,54 @@ __global__ __launch_bounds__(kThreads) void decode_q8_kernel(decode_args a)
             for (int i = tid; i < v.n_q_local * D / 8; i += kThreads)
                 reinterpret_cast<kv_u32x4*>(a.out + (int64_t)s * v.n_q_local * D)[i] = kv_u32x4{0u, 0u, 0u, 0u};
 
-    int s, set, step;             // where the workgroup's steps start
-    long long left;               // and how many they are
+    axis_place at, to;   // where the workgroup's steps start, and where they end
     if (a.whole) {
-        s = (int)blockIdx.x / a.head_sets;
-        set = (int)blockIdx.x - s * a.head_sets;
-        step = 0;
-        left = steps_of<kStep>(a.ctx_lens[s]);
+        at.s = (int)blockIdx.x / a.head_sets;
+        at.set = (int)blockIdx.x - at.s * a.head_sets;
+        at.step = 0;
+        to = {at.s, at.set, steps_of(a.ctx_lens[at.s], kStep)};
     } else {
-        const axis_sums sums = sum_axis<kStep>(a, s_incl);
-        // (no workgroup without a step among those that have some: the pieces of a pair lie in consecutive ones)
-        const long long total = sums.total * a.head_sets, W = min((long long)gridDim.x, total);
-        if (blockIdx.x >= W) return;
-        const long long from = total * blockIdx.x / W, to = total * (blockIdx.x + 1) / W;
-        left = to - from;
-        // the thread in whose sequences it lies, then the sequence
-        int at = 0;
-#pragma unroll
-        for (int w = 0; w < kThreads / 64; ++w)
-            at += __builtin_popcountll(__builtin_amdgcn_ballot_w64(s_incl[64 * w + lane] * a.head_sets <= from));
-        long long in = from - (at > 0 ? s_incl[at - 1] : 0) * a.head_sets;
-        s = uniform(at * sums.per);
-        for (;; ++s) {
-            const long long n = (long long)steps_of<kStep>(a.ctx_lens[s]) * a.head_sets;
-            if (in < n) break;
-            in -= n;
+        // every wavefront for itself, four lengths a lane: no barrier stands between the lengths and the first tiles
+        const axis_run first = run_of(a, 0, lane, kStep);
+        int all = __builtin_amdgcn_readlane(first.sum_incl, 63), some = __builtin_amdgcn_readlane(first.some_incl, 63);
+        for (int s0 = 256; s0 < a.batch; s0 += 256) {
+            const axis_run r = run_of(a, s0, lane, kStep);
+            all += __builtin_amdgcn_readlane(r.sum_incl, 63);
+            some += __builtin_amdgcn_readlane(r.some_incl, 63);
         }
-        const int steps = steps_of<kStep>(a.ctx_lens[s]);
-        set = uniform((int)(in / steps));
-        step = uniform((int)(in - (long long)set * steps));
+        all *= a.head_sets;
+        some *= a.head_sets;
+        // (no workgroup without a step among those that have some: the pieces of a pair lie in consecutive ones)
+        const int W = min((int)gridDim.x, all), i = (int)blockIdx.x;
+        if (i >= W) return;
+        const int least = (1 << a.unit_shift) + a.start_units;
+        const int start_units = (all << a.unit_shift) + a.start_units * some >= 3 * least * W ? a.start_units : 0;
+        const int total = (all << a.unit_shift) + start_units * some;
+        auto cut = [&](int k) -> int {
+            return k == W ? total : W == all ? k << a.unit_shift : (int)(((uint64_t)(uint32_t)total * ((uint32_t)k * a.inverse)) >> 32);
+        };
+        const int from = cut(i), until = cut(i + 1);
+        if (a.batch <= 256) {
+            at = place_in(a, first, 0, from, start_units, lane);
+            to = place_in(a, first, 0, until == total ? 0 : until, start_units, lane);
+            if (until == total) to = {a.batch, 0, 0};
+        } else {
+            at = place_at(a, first, from, start_units, lane, kStep);
+            to = place_at(a, first, until, start_units, lane, kStep);
+        }
     }
 
     const int hw = HPW == 1 ? 0 : wave % HPW, sub = HPW == 1 ? wave : wave / HPW;
     const uint32_t row_bytes = (uint32_t)v.token_stride;
-    while (left > 0) {
-        const int n = uniform(a.ctx_lens[s]), steps = steps_of<kStep>(n);
-        if (steps == 0) {   // (of a sequence without tokens)
-            ++s;
+    for (; at.s < a.batch; at.step = 0, ++at.set, at.s += at.set == a.head_sets, at.set = at.set == a.head_sets ? 0 : at.set) {
+        const int s = at.s, set = at.set, step = at.step;
+        const int n = uniform(a.ctx_lens[s]), steps = steps_of(n, kStep);
+        const bool last_pair = s == to.s && set == to.set;
+        const int end = last_pair ? to.step : steps;
+        if (step >= end) {   // (a sequence without tokens, a start at a pair's end, an end at its start)
+            if (last_pair) break;
             continue;
         }
-        const int end = (int)min((long long)steps, step + left);
         const int h = set * HPW + hw;   // this wavefront's local KV head
         const const_ints ids = (const_ints)(a.table + (int64_t)s * a.table_stride);
         const int last16 = (n - 1) & ~15;
@@ -330,21 +385,17 @@ __global__ __launch_bounds__(kThreads) void decode_q8_kernel(decode_args a)
             if (starts) a.ends[pair].x = blockIdx.x;
             if (ends) a.ends[pair].y = blockIdx.x;
         }
+        if (last_pair) break;
         __syncthreads();
-        left -= end - step;
-        step = 0;
-        if (++set == a.head_sets) {
-            set = 0;
-            ++s;
-        }
     }
 }
 
 // Row r of a cut pair: the sum of its pieces.  D / 4 lanes a slice of the list, the slices then over LDS.
-template <int D>
-__global__ __launch_bounds__(kThreads) void merge_q8_kernel(decode_args a, int rows)
+// THREADS: 1024, and four pieces a slice requested at a time, where pairs are cut into many.
+template <int D, int THREADS>
+__global__ __launch_bounds__(THREADS) void merge_q8_kernel(decode_args a, int rows)
 {
-    constexpr int kSlices = kThreads / (D / 4);
+    constexpr int kSlices = THREADS / (D / 4), kBatch = THREADS > 256 ? 4 : 1;
     __shared__ f32x4 s_o[kSlices][D / 4];
     __shared__ float2 s_ml[kSlices];
     const int pair = blockIdx.x, row = blockIdx.y, s = pair / a.head_sets, set = pair - s * a.head_sets;
@@ -354,13 +405,31 @@ __global__ __launch_bounds__(kThreads) void merge_q8_kernel(decode_args a, int r
     const int slice = threadIdx.x / (D / 4), d4 = threadIdx.x % (D / 4);
     float top = kLowest, sum = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int w = first + slice; w <= last; w += kSlices) {
-        const int64_t rec = (2 * (int64_t)w + (w == first ? 1 : 0)) * rows + row;
-        const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + rec * 2);
-        const f32x4 o = *reinterpret_cast<const f32x4*>(a.part_o + rec * D + 4 * d4);
-        const float to = fmaxf(top, ml.x), f = fast_exp2(top - to), e = fast_exp2(ml.x - to);
-        acc = acc * f + o * e;
-        sum = sum * f + ml.y * e;
+    for (int w0 = first + slice; w0 <= last; w0 += kBatch * kSlices) {
+        float2 ml[kBatch];
+        f32x4 o[kBatch];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {   // (past the end: the last one again, not used)
+            const int w = min(w0 + u * kSlices, last);
+            const int64_t rec = (2 * (int64_t)w + (w == first ? 1 : 0)) * rows + row;
+            ml[u] = *reinterpret_cast<const float2*>(a.part_ml + rec * 2);
+            o[u] = *reinterpret_cast<const f32x4*>(a.part_o + rec * D + 4 * d4);
+        }
+        float to = top;
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            if (w0 + u * kSlices > last) ml[u] = make_float2(kLowest, 0.f);
+            to = fmaxf(to, ml[u].x);
+        }
+        const float keep = fast_exp2(top - to);
+        acc *= keep;
+        sum *= keep;
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            const float e = w0 + u * kSlices > last ? 0.f : fast_exp2(ml[u].x - to);
+            acc += o[u] * e;
+            sum += ml[u].y * e;
+        }
         top = to;
     }
     s_o[slice][d4] = acc;
@@ -381,6 +450,7 @@ __global__ __launch_bounds__(kThreads) void merge_q8_kernel(decode_args a, int r
 }
 
 constexpr int kMostWorkgroups = 512;   // two for each of 256 compute units
+constexpr int kUnitShift = 3, kStartUnits = 8;   // a start counts as much as a step
 
 // How a call is cut: the same for the workspace and the launch.
 struct decode_plan {
@@ -411,8 +481,12 @@ void launch(const decode_plan& p, const decode_args& a, hipStream_t st)
 {
     auto* f = p.hpw == 4 ? decode_q8_kernel<D, FMT, 4> : p.hpw == 2 ? decode_q8_kernel<D, FMT, 2> : decode_q8_kernel<D, FMT, 1>;
     hipLaunchKernelGGL(f, dim3((unsigned)p.workgroups), dim3(kThreads), 0, st, a);
-    if (!p.whole)
-        hipLaunchKernelGGL(merge_q8_kernel<D>, dim3((unsigned)(a.batch * p.head_sets), (unsigned)(p.hpw * a.group)), dim3(kThreads), 0, st, a, p.hpw * a.group);
+    if (!p.whole) {
+        const int pairs = a.batch * p.head_sets, rows = p.hpw * a.group;
+        const bool many = p.workgroups >= 16 * pairs;   // pieces a pair
+        hipLaunchKernelGGL((many ? merge_q8_kernel<D, 1024> : merge_q8_kernel<D, 256>), dim3((unsigned)pairs, (unsigned)rows),
+                           dim3(many ? 1024 : 256), 0, st, a, rows);
+    }
 }
 
 }  // namespace
@@ -457,6 +531,11 @@ extern "C" int paged_decode_attn_q8(const void* q, void* out, const void* kv_poo
     a.batch = batch;
     a.head_sets = p.head_sets;
     a.whole = p.whole;
+    // (32 bits hold the axis: bounds that would pass them are cut by whole steps)
+    const bool fine = (double)batch * p.head_sets * (max_ctx_len / (kTile * kWaves / p.hpw) + 2.0) < (double)(1 << 26);
+    a.unit_shift = fine ? kUnitShift : 0;
+    a.start_units = fine ? kStartUnits : 0;
+    a.inverse = (uint32_t)((1ull << 32) / (unsigned)p.workgroups);
     a.part_o = (float*)workspace;
     a.part_ml = (float*)((char*)workspace + p.o_bytes);
     a.ends = (int2*)((char*)workspace + p.o_bytes + p.ml_bytes);
