@@ -11,7 +11,9 @@
 //                               lane loads of a token is a run of bytes, and product j takes dim d / 16 m + j from every lane
 // The scores come out with tokens 4 g .. 4 g + 3 of each half in lane (row, g): the B operand of the second product as it is.  Codes
 // become bf16 exactly (e4m3 by the conversion instruction, int8 over fp32), K's scale goes to the score, V's to the weight.
-// Softmax by a running reference that lags up to 2^8 behind the maximum; the denominator sums the weights as they are rounded to bf16.
+// Softmax by a running reference that lags up to 2^8 behind the maximum.  The weights go to the products as two bf16, the rounded value and
+// what the rounding left: that costs 1 % of the time (the reads bound it), and the error against 64 bits is that of the output's own
+// rounding, where single bf16 weights made it 1.2 to 1.4 times that.
 #include "kv_q8.h"
 
 #include <algorithm>
@@ -20,7 +22,6 @@ using namespace kvq8;
 
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kTile = 32;
 
 struct decode_args {
@@ -45,8 +46,8 @@ struct decode_args {
 };
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ __forceinline__ float uniform(float x) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x))); }
 
+typedef const __attribute__((address_space(1))) uint8_t* global_bytes;
 typedef const __attribute__((address_space(4))) int32_t* const_ints;
 typedef const __attribute__((address_space(4))) float* const_floats;
 
@@ -79,10 +80,12 @@ __device__ __forceinline__ axis_run run_of(const decode_args& a, int s0, int lan
 {
     axis_run r;
     r.sum = r.some = 0;
+    int n[4];   // (loads without branches: all at once)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) n[i] = a.ctx_lens[min(s0 + 4 * lane + i, a.batch - 1)];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int s = s0 + 4 * lane + i;
-        r.steps[i] = s < a.batch ? steps_of(a.ctx_lens[s], step) : 0;
+        r.steps[i] = s0 + 4 * lane + i < a.batch ? steps_of(n[i], step) : 0;
         r.sum += r.steps[i];
         r.some += r.steps[i] > 0;
     }
@@ -147,10 +150,14 @@ __device__ __forceinline__ void dims_of(const uint32_t (&t)[8], bf16x8 (&to)[4])
     for (int b = 0; b < 4; ++b) to[b] = as_bf16x8(d[b]);
 }
 
-// HPW: heads that the wavefronts of a workgroup take side by side; the others follow each other in the tokens.
+// HPW: heads that the wavefronts of a workgroup take side by side; the others follow each other in the tokens.  8 heads have 8 wavefronts: a
+// workgroup then reads whole token rows of 1 KiB as one stream (8 heads, 64 sequences around 2048 tokens: 56 us, 59 us as 4 heads and 4).
+// Two tiles at a time, or two heads a wavefront, with one wavefront a SIMD: 58 us there, the same or up to 2 % better elsewhere.
+constexpr int waves_of(int hpw) { return hpw == 8 ? 8 : 4; }   // of a workgroup
 template <int D, int FMT, int HPW>
-__global__ __launch_bounds__(kThreads) void decode_q8_kernel(decode_args a)
+__global__ __launch_bounds__(64 * waves_of(HPW), 2) void decode_q8_kernel(decode_args a)
 {
+    constexpr int kWaves = waves_of(HPW), kThreads = 64 * kWaves;
     constexpr int kLoads = D / 64;          // of 16 bytes of a K row
     constexpr int kWords = D / 64;          // dwords of a V row in a lane
     constexpr int kDims = D / 16;           // dims of a lane's V
@@ -205,7 +212,7 @@ __global__ __launch_bounds__(kThreads) void decode_q8_kernel(decode_args a)
         }
     }
 
-    const int hw = HPW == 1 ? 0 : wave % HPW, sub = HPW == 1 ? wave : wave / HPW;
+    const int hw = wave % HPW, sub = wave / HPW;
     const uint32_t row_bytes = (uint32_t)v.token_stride;
     for (; at.s < a.batch; at.step = 0, ++at.set, at.s += at.set == a.head_sets, at.set = at.set == a.head_sets ? 0 : at.set) {
         const int s = at.s, set = at.set, step = at.step;
@@ -236,6 +243,7 @@ __global__ __launch_bounds__(kThreads) void decode_q8_kernel(decode_args a)
         for (int j = 0; j < kDims; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
         float ref = kLowest, l = 0.f;
 
+        const int t_first = step * kStep + sub * kTile, t_end = min(end * kStep, n);
         struct tile {
             kv_u32x4 k[2][kLoads];
             uint32_t v[8][kWords];
@@ -304,13 +312,13 @@ __global__ __launch_bounds__(kThreads) void decode_q8_kernel(decode_args a)
                 for (int j = 0; j < kDims; ++j) o[j] *= alpha;
                 ref = to;
             }
-            kv_u32x4 pb;
+            kv_u32x4 pb, pr;   // weights in bf16, and what that rounding left
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float w0 = fast_exp2(u[2 * i] - ref), w1 = fast_exp2(u[2 * i + 1] - ref), sv = x.sv[i >> 1];
-                const uint32_t w = pack_bf16x2(w0, w1);
-                l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), __builtin_bit_cast(bf16x2, 0x3f803f80u), l, false);
+                l += w0 + w1;
                 pb[i] = pack_bf16x2(w0 * sv, w1 * sv);
+                pr[i] = pack_bf16x2(w0 * sv - __uint_as_float(pb[i] << 16), w1 * sv - __uint_as_float(pb[i] & 0xffff0000u));
             }
 #pragma unroll
             for (int w = 0; w < kWords; ++w) {
@@ -320,21 +328,24 @@ __global__ __launch_bounds__(kThreads) void decode_q8_kernel(decode_args a)
                 bf16x8 va[4];
                 dims_of<FMT>(t, va);
 #pragma unroll
-                for (int b = 0; b < 4; ++b)
+                for (int b = 0; b < 4; ++b) {
+                    o[4 * w + b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[b], as_bf16x8(pr), o[4 * w + b], 0, 0, 0);
                     o[4 * w + b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va[b], as_bf16x8(pb), o[4 * w + b], 0, 0, 0);
+                }
             }
         };
         {
-            int t = step * kStep + sub * kTile;
-            const int t_end = min(end * kStep, n);
+            int t = t_first;
             tile x, y;
             if (t < t_end) request(t, x);
             while (t < t_end) {
                 if (t + kStep < t_end) request(t + kStep, y);
+                __builtin_amdgcn_sched_barrier(0);   // (all of the next tile is asked for before anything waits for this one)
                 take(t, x);
                 t += kStep;
                 if (t >= t_end) break;
                 if (t + kStep < t_end) request(t + kStep, x);
+                __builtin_amdgcn_sched_barrier(0);
                 take(t, y);
                 t += kStep;
             }
@@ -449,7 +460,7 @@ __global__ __launch_bounds__(THREADS) void merge_q8_kernel(decode_args a, int ro
         kv_u32x2{pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)};
 }
 
-constexpr int kMostWorkgroups = 512;   // two for each of 256 compute units
+constexpr int kMostWaves = 2048;   // two for each SIMD of 256 compute units
 constexpr int kUnitShift = 3, kStartUnits = 8;   // a start counts as much as a step
 
 // How a call is cut: the same for the workspace and the launch.
@@ -458,17 +469,18 @@ struct decode_plan {
     bool whole;
     size_t o_bytes, ml_bytes, bytes;
 };
+int step_tokens(int hpw) { return kTile * waves_of(hpw) / hpw; }
 decode_plan plan_of(const kv_view* view, int batch, int max_ctx_len)
 {
     decode_plan p;
     const int hl = view->n_kv_local;
-    p.hpw = hl % 4 == 0 ? 4 : hl % 2 == 0 ? 2 : 1;
+    p.hpw = hl % 8 == 0 ? 8 : hl % 4 == 0 ? 4 : hl % 2 == 0 ? 2 : 1;
     p.whole = max_ctx_len <= 512;
     if (p.whole) p.hpw = 1;
     p.head_sets = hl / p.hpw;
-    const int step = kTile * kWaves / p.hpw;
+    const int step = step_tokens(p.hpw);
     const int64_t pairs = (int64_t)batch * p.head_sets, steps = pairs * (((int64_t)max_ctx_len + step - 1) / step);
-    p.workgroups = (int)(p.whole ? pairs : std::min<int64_t>(steps, kMostWorkgroups));
+    p.workgroups = (int)(p.whole ? pairs : std::min<int64_t>(steps, kMostWaves / waves_of(p.hpw)));
     const int rows = p.hpw * view->group;
     p.o_bytes = p.whole ? 0 : (size_t)2 * p.workgroups * rows * view->geom.head_dim * 4;
     p.ml_bytes = p.whole ? 0 : (size_t)2 * p.workgroups * rows * 8;
@@ -479,8 +491,11 @@ decode_plan plan_of(const kv_view* view, int batch, int max_ctx_len)
 template <int D, int FMT>
 void launch(const decode_plan& p, const decode_args& a, hipStream_t st)
 {
-    auto* f = p.hpw == 4 ? decode_q8_kernel<D, FMT, 4> : p.hpw == 2 ? decode_q8_kernel<D, FMT, 2> : decode_q8_kernel<D, FMT, 1>;
-    hipLaunchKernelGGL(f, dim3((unsigned)p.workgroups), dim3(kThreads), 0, st, a);
+    auto* f = p.hpw == 8   ? decode_q8_kernel<D, FMT, 8>
+              : p.hpw == 4 ? decode_q8_kernel<D, FMT, 4>
+              : p.hpw == 2 ? decode_q8_kernel<D, FMT, 2>
+                           : decode_q8_kernel<D, FMT, 1>;
+    hipLaunchKernelGGL(f, dim3((unsigned)p.workgroups), dim3(64 * waves_of(p.hpw)), 0, st, a);
     if (!p.whole) {
         const int pairs = a.batch * p.head_sets, rows = p.hpw * a.group;
         const bool many = p.workgroups >= 16 * pairs;   // pieces a pair
@@ -532,7 +547,7 @@ extern "C" int paged_decode_attn_q8(const void* q, void* out, const void* kv_poo
     a.head_sets = p.head_sets;
     a.whole = p.whole;
     // (32 bits hold the axis: bounds that would pass them are cut by whole steps)
-    const bool fine = (double)batch * p.head_sets * (max_ctx_len / (kTile * kWaves / p.hpw) + 2.0) < (double)(1 << 26);
+    const bool fine = (double)batch * p.head_sets * (max_ctx_len / step_tokens(p.hpw) + 2.0) < (double)(1 << 26);
     a.unit_shift = fine ? kUnitShift : 0;
     a.start_units = fine ? kStartUnits : 0;
     a.inverse = (uint32_t)((1ull << 32) / (unsigned)p.workgroups);
