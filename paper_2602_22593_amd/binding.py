@@ -202,6 +202,7 @@ class _InPython:
         return None
 
     decode = prefill = linear = append = repack = rope = accept = tree = weights = _none
+    rope_q8 = decode_q8 = prefill_q8 = repack_q8 = _none
 
 
 def _calls():
@@ -225,6 +226,8 @@ def _calls():
                 (torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, torch._C._cuda_isCurrentStreamCapturing), _workspaces)
         operators = (L.kv_rope_append_tracked, L.kv_accept_tracked, L.paged_tree_attn, L.paged_decode_attn_weights)
         m.setup_operators(tuple(C.cast(f, C.c_void_p).value for f in operators), (torch.float32, _WORDS))
+        q8 = (L.kv_rope_append_q8, L.paged_decode_attn_q8, L.paged_prefill_attn_q8, L.kv_repack_q8)
+        m.setup_q8(tuple(C.cast(f, C.c_void_p).value for f in q8), _Q8_FORMATS)
         _calls_module = m
     return _calls_module
 
@@ -740,6 +743,14 @@ def kv_rope_append_q8(kv_pool: torch.Tensor, scales: torch.Tensor, view: KVView,
     ``q`` may be None (keys and values only; None is returned), ``positions`` and ``inv_freq`` where nothing is rotated.
     Other arguments as kv_rope_append.  Older tokens of a group that the new ones fall into are rounded again where its scale grows.
     """
+    if out is None and q is not None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if q is not None or out is None:
+        rc = (_calls_module or _calls()).rope_q8(kv_pool, scales, view, q, k, v, positions, inv_freq, block_table, ctx_lens, q_offsets,
+                                                 axes, pairs, out, stream)
+        if rc is not None:
+            _check(rc, "kv_rope_append_q8")
+            return out
     batch, total, d = int(ctx_lens.shape[0]), int(k.shape[0]), view.head_dim
     device = _one_device(kv_pool, scales, q, k, v, positions, inv_freq, block_table, ctx_lens, q_offsets, out)
     if q is None and out is not None:
@@ -749,8 +760,6 @@ def kv_rope_append_q8(kv_pool: torch.Tensor, scales: torch.Tensor, view: KVView,
     q_ptr, q_stride = (None, 0) if q is None else _token_rows(q, total, view.n_q_local, d, "q")
     k_ptr, k_stride = _token_rows(k, total, view.n_kv_local, d, "k")
     v_ptr, v_stride = _token_rows(v, total, view.n_kv_local, d, "v")
-    if out is None and q is not None:
-        out = torch.empty((total, view.n_q_local, d), dtype=q.dtype, device=device)
     half = 0 if inv_freq is None else int(inv_freq.numel())
     n_axes = 1 if positions is None or positions.dim() == 1 else int(positions.shape[0])
     pos_ptr = None if positions is None else _shaped(positions, (total,) if positions.dim() == 1 else (n_axes, total), (torch.int32,), "positions")
@@ -778,6 +787,11 @@ def paged_decode_attn_q8(q: torch.Tensor, kv_pool: torch.Tensor, scales: torch.T
                          view: KVView, max_ctx_len: int, out: Optional[torch.Tensor] = None, scale: float = 0.0,
                          workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """paged_decode_attn over a cache held in 8 bits (``kv_pool`` and ``scales`` as kv_rope_append_q8 takes them)."""
+    if out is not None and workspace is not None:
+        rc = (_calls_module or _calls()).decode_q8(q, kv_pool, scales, block_table, ctx_lens, view, max_ctx_len, out, scale, workspace, stream)
+        if rc is not None:
+            _check(rc, "paged_decode_attn_q8")
+            return out
     batch = int(ctx_lens.shape[0])
     device = _one_device(q, kv_pool, scales, block_table, ctx_lens, out, workspace)
     shape = (batch, view.n_q_local, view.head_dim)
@@ -802,6 +816,12 @@ def paged_prefill_attn_q8(q: torch.Tensor, kv_pool: torch.Tensor, scales: torch.
                           q_offsets: torch.Tensor, view: KVView, max_ctx_len: int, max_q_len: int, out: Optional[torch.Tensor] = None,
                           scale: float = 0.0, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """paged_prefill_attn over a cache held in 8 bits (``kv_pool`` and ``scales`` as kv_rope_append_q8 takes them)."""
+    if out is not None and workspace is not None:
+        rc = (_calls_module or _calls()).prefill_q8(q, kv_pool, scales, block_table, ctx_lens, q_offsets, view, max_ctx_len, max_q_len, out,
+                                                    scale, workspace, stream)
+        if rc is not None:
+            _check(rc, "paged_prefill_attn_q8")
+            return out
     batch, total = int(ctx_lens.shape[0]), int(q.shape[0])
     device = _one_device(q, kv_pool, scales, block_table, ctx_lens, q_offsets, out, workspace)
     shape = (total, view.n_q_local, view.head_dim)
@@ -821,6 +841,10 @@ def paged_prefill_attn_q8(q: torch.Tensor, kv_pool: torch.Tensor, scales: torch.
 def kv_repack_q8(kv_pool: torch.Tensor, scales: torch.Tensor, src_view: KVView, dst_view: KVView, src_block_table: torch.Tensor,
                  dst_block_table: torch.Tensor, n_tokens: torch.Tensor, max_tokens: int, stream=None) -> None:
     """kv_repack for a cache held in 8 bits: codes and scales of the heads common to both views move as they are."""
+    rc = (_calls_module or _calls()).repack_q8(kv_pool, scales, src_view, dst_view, src_block_table, dst_block_table, n_tokens, max_tokens,
+                                               stream)
+    if rc is not None:
+        return _check(rc, "kv_repack_q8")
     n_seqs = int(n_tokens.shape[0])
     device = _one_device(kv_pool, scales, src_block_table, dst_block_table, n_tokens)
     pool_ptr, scales_ptr, _, blocks = _q8_cache(kv_pool, scales, src_view)

@@ -36,6 +36,15 @@ typedef int (*tree_fn)(const void*, void*, const void*, int64_t, const int32_t*,
                        const uint64_t*, int64_t, int, int64_t, int, int, const kv_view*, float, void*, size_t, void*);
 typedef int (*weights_fn)(const void*, void*, const void*, int64_t, const int32_t*, int64_t, const int32_t*, int, int,
                           const kv_view*, float, float*, int64_t, void*, size_t, void*);
+typedef int (*rope_q8_fn)(void*, float*, int, int64_t, const kv_view*, const void*, int64_t, const void*, int64_t, const void*,
+                          int64_t, void*, const int32_t*, int64_t, int, const float*, int, const int32_t*, int, const int32_t*,
+                          int64_t, const int32_t*, const int32_t*, int, int64_t, void*);
+typedef int (*decode_q8_fn)(const void*, void*, const void*, const float*, int, int64_t, const int32_t*, int64_t, const int32_t*,
+                            int, int, const kv_view*, float, void*, size_t, void*);
+typedef int (*prefill_q8_fn)(const void*, void*, const void*, const float*, int, int64_t, const int32_t*, int64_t, const int32_t*,
+                             const int32_t*, int, int64_t, int, int, const kv_view*, float, void*, size_t, void*);
+typedef int (*repack_q8_fn)(void*, float*, int64_t, const kv_view*, const kv_view*, const int32_t*, int64_t, const int32_t*,
+                            int64_t, const int32_t*, int, int, void*);
 
 static decode_fn f_decode;
 static prefill_fn f_prefill;
@@ -50,13 +59,19 @@ static accept_fn f_accept;
 static tree_fn f_tree;
 static weights_fn f_weights;
 
+static rope_q8_fn f_rope_q8;
+static decode_q8_fn f_decode_q8;
+static prefill_q8_fn f_prefill_q8;
+static repack_q8_fn f_repack_q8;
+
 static PyObject *tensor_type, *parameter_type, *weight_view_type;   /* exact types only */
 static PyObject *bf16_types, *int32_type, *uint8_type;              /* dtypes: a tuple, and two */
 static PyObject *float_type, *word_types;                           /* float32; the two of 64-bit masks */
+static PyObject* q8_formats;                                        /* dtype of an 8-bit cache -> its format */
 static PyObject *get_device, *raw_stream, *is_capturing, *workspaces;   /* of torch._C; the binding's dict */
 static PyObject *n_is_cuda, *n_dtype, *n_is_contiguous, *n_data_ptr, *n_shape, *n_stride, *n_numel, *n_element_size,
     *n_get_device, *n_cuda_stream, *n_handle, *n_value, *n_block_bytes, *n_n_q_local, *n_n_kv_local, *n_head_dim, *n_scratch,
-    *n_zero, *n_one, *n_two;
+    *n_geometry, *n_n_kv_heads, *n_zero, *n_one, *n_two;
 
 /* All helpers return 1, or 0 where the Python code is to answer (an exception may be set then: `answer` clears it). */
 
@@ -396,17 +411,51 @@ typedef struct {
     void *pool, *table, *ctx;
     const kv_view* view;
 } cache_args;
-static int cache_of(PyObject* pool, PyObject* view, PyObject* table, PyObject* ctx, cache_args* c)
+static int places_of(PyObject* view, PyObject* table, PyObject* ctx, cache_args* c)   /* all but the pool */
 {
-    int64_t on, tab[2];
+    int64_t tab[2];
     c->batch = -1;
     if (!current(&c->device) || !shaped(ctx, int32_type, c->device, 1, &c->batch, &c->ctx) || c->batch > INT32_MAX) return 0;
     tab[0] = c->batch;
     tab[1] = -1;
     return shaped(table, int32_type, c->device, 2, tab, &c->table) && ask_int(table, n_stride, n_zero, &c->row) &&
            int_attr(view, n_n_q_local, &c->hq) && int_attr(view, n_n_kv_local, &c->hkv) && int_attr(view, n_head_dim, &c->d) &&
-           int_attr(view, n_block_bytes, &c->bb) && view_handle(view, &c->view) && dev(pool, bf16_types, &c->pool) &&
-           ask_int(pool, n_get_device, NULL, &on) && on == c->device && pool_blocks(pool, c->bb, 1, &c->blocks);
+           int_attr(view, n_block_bytes, &c->bb) && view_handle(view, &c->view);
+}
+static int cache_of(PyObject* pool, PyObject* view, PyObject* table, PyObject* ctx, cache_args* c)
+{
+    int64_t on;
+    return places_of(view, table, ctx, c) && dev(pool, bf16_types, &c->pool) && ask_int(pool, n_get_device, NULL, &on) &&
+           on == c->device && pool_blocks(pool, c->bb, 1, &c->blocks);
+}
+
+/* binding._q8_cache on top of that: codes, their format, scales */
+typedef struct {
+    cache_args c;
+    int format;
+    void* scales;
+} q8_args;
+static int q8_of(PyObject* pool, PyObject* scales, PyObject* view, PyObject* table, PyObject* ctx, q8_args* x)
+{
+    cache_args* c = &x->c;
+    int64_t on, n, heads, format;
+    if (!places_of(view, table, ctx, c) || !is_tensor(pool)) return 0;
+    PyObject* dtype = PyObject_GetAttr(pool, n_dtype);
+    PyObject* f = dtype ? PyDict_GetItemWithError(q8_formats, dtype) : NULL;
+    Py_XDECREF(dtype);
+    if (!f || !int_arg(f, &format)) return 0;
+    x->format = (int)format;
+    PyObject* cont = ask(pool, n_is_contiguous, NULL);
+    const int dense = cont == Py_True;
+    Py_XDECREF(cont);
+    if (!dense || !ask_int(pool, n_get_device, NULL, &on) || on != c->device || on < 0 || !address(pool, &c->pool) ||
+        !pool_blocks(pool, c->bb / 2, 1, &c->blocks))
+        return 0;
+    PyObject* g = PyObject_GetAttr(view, n_geometry);
+    const int ok = g && int_attr(g, n_n_kv_heads, &heads);
+    Py_XDECREF(g);
+    return ok && dev(scales, float_type, &x->scales) && ask_int(scales, n_get_device, NULL, &on) && on == c->device &&
+           ask_int(scales, n_numel, NULL, &n) && n == c->blocks * 2 * heads;
 }
 
 /* binding._kept_per_token: [batch][n_kv_local][tokens], or none */
@@ -421,41 +470,50 @@ static int kept_per_token(PyObject* t, PyObject* dtype, const cache_args* c, voi
     return 1;
 }
 
+/* Positions, [tokens] or [axes][tokens], and which axis a pair of dims takes. */
+enum { kMostPairs = 128 };
+static int positions_of(PyObject* t, int64_t device, int64_t tokens, void** out, int* n_axes)
+{
+    int64_t pos[2] = {tokens, -1};
+    *n_axes = 1;
+    if (shaped(t, int32_type, device, 1, pos, out)) return 1;
+    PyErr_Clear();
+    pos[0] = -1;
+    pos[1] = tokens;
+    if (!shaped(t, int32_type, device, 2, pos, out) || pos[0] < 1 || pos[0] > 4) return 0;
+    *n_axes = (int)pos[0];
+    return 1;
+}
+static int axes_of(PyObject* list, int n_axes, int64_t half, int32_t axes[kMostPairs])
+{
+    if (list == Py_None) return n_axes == 1;
+    int ok = (PyList_CheckExact(list) || PyTuple_CheckExact(list)) && PySequence_Fast_GET_SIZE(list) == half;
+    for (int64_t i = 0; ok && i < half; ++i) {
+        int64_t x;
+        ok = int_arg(PySequence_Fast_GET_ITEM(list, i), &x);
+        axes[i] = (int32_t)x;
+    }
+    return ok;
+}
+
 /* rope(kv_pool, view, q, k, v, positions, inv_freq, block_table, ctx_lens, q_offsets, axes, pairs, out, token_pos, stream, weights) */
 static PyObject* call_rope(PyObject* self, PyObject* const* a, Py_ssize_t nargs)
 {
     ARGS(16)
-    enum { kMost = 128 };
-    int64_t q[3], q_row, k_row, v_row, pos[2] = {-1, -1}, half = -1, off, out[3], per, w_n, pairs, stream;
+    int64_t q[3], q_row, k_row, v_row, half = -1, off, out[3], per, w_n, pairs, stream;
     void *pq, *pk, *pv, *pout, *ppos, *pfreq, *poff = NULL, *pper, *pw;
-    int32_t axes[kMost];
+    int32_t axes[kMostPairs];
     cache_args c;
     int rc = 0, n_axes = 1;
     int ok = cache_of(a[0], a[1], a[7], a[8], &c) && sizes(a[2], 3, q) && token_rows(a[2], c.device, q[0], c.hq, c.d, &pq, &q_row) &&
              token_rows(a[3], c.device, q[0], c.hkv, c.d, &pk, &k_row) && token_rows(a[4], c.device, q[0], c.hkv, c.d, &pv, &v_row);
     if (ok) {
-        out[0] = pos[0] = q[0];
+        out[0] = q[0];
         out[1] = c.hq;
         out[2] = c.d;
-        if (!shaped(a[5], int32_type, c.device, 1, pos, &ppos)) {
-            PyErr_Clear();
-            pos[0] = -1;
-            pos[1] = q[0];
-            ok = shaped(a[5], int32_type, c.device, 2, pos, &ppos) && pos[0] >= 1 && pos[0] <= 4;
-            n_axes = (int)pos[0];
-        }
-        ok = ok && shaped(a[6], float_type, c.device, 1, &half, &pfreq) && half <= kMost && shaped(a[12], bf16_types, c.device, 3, out, &pout) &&
-             int_arg(a[11], &pairs) && stream_handle(a[14], NULL, &stream);
-    }
-    if (ok && a[10] != Py_None) {
-        ok = (PyList_CheckExact(a[10]) || PyTuple_CheckExact(a[10])) && PySequence_Fast_GET_SIZE(a[10]) == half;
-        for (int64_t i = 0; ok && i < half; ++i) {
-            int64_t x;
-            ok = int_arg(PySequence_Fast_GET_ITEM(a[10], i), &x);
-            axes[i] = (int32_t)x;
-        }
-    } else if (n_axes != 1) {
-        ok = 0;
+        ok = positions_of(a[5], c.device, q[0], &ppos, &n_axes) && shaped(a[6], float_type, c.device, 1, &half, &pfreq) &&
+             half <= kMostPairs && shaped(a[12], bf16_types, c.device, 3, out, &pout) && int_arg(a[11], &pairs) &&
+             stream_handle(a[14], NULL, &stream) && axes_of(a[10], n_axes, half, axes);
     }
     if (ok && a[9] != Py_None) {
         off = c.batch + 1;
@@ -555,6 +613,139 @@ static PyObject* call_weights(PyObject* self, PyObject* const* a, Py_ssize_t nar
     return answer(ok, rc);
 }
 
+/* rope_q8(kv_pool, scales, view, q, k, v, positions, inv_freq, block_table, ctx_lens, q_offsets, axes, pairs, out, stream) */
+static PyObject* call_rope_q8(PyObject* self, PyObject* const* a, Py_ssize_t nargs)
+{
+    ARGS(15)
+    int64_t k[3], q_row = 0, k_row, v_row, half = 0, off, out[3], pairs, stream;
+    void *pq = NULL, *pk, *pv, *pout = NULL, *ppos = NULL, *pfreq = NULL, *poff = NULL;
+    int32_t axes[kMostPairs];
+    q8_args x;
+    const cache_args* c = &x.c;
+    int rc = 0, n_axes = 1;
+    int ok = q8_of(a[0], a[1], a[2], a[8], a[9], &x) && sizes(a[4], 3, k) && token_rows(a[4], c->device, k[0], c->hkv, c->d, &pk, &k_row) &&
+             token_rows(a[5], c->device, k[0], c->hkv, c->d, &pv, &v_row) && (a[3] == Py_None) == (a[13] == Py_None) &&
+             (a[7] == Py_None || a[6] != Py_None);
+    if (ok && a[3] != Py_None) {
+        out[0] = k[0];
+        out[1] = c->hq;
+        out[2] = c->d;
+        ok = token_rows(a[3], c->device, k[0], c->hq, c->d, &pq, &q_row) && shaped(a[13], bf16_types, c->device, 3, out, &pout);
+    }
+    if (ok && a[6] != Py_None) ok = positions_of(a[6], c->device, k[0], &ppos, &n_axes);
+    if (ok && a[7] != Py_None) {
+        half = -1;
+        ok = shaped(a[7], float_type, c->device, 1, &half, &pfreq) && half <= kMostPairs;
+    }
+    ok = ok && axes_of(a[11], n_axes, half, axes) && int_arg(a[12], &pairs) && stream_handle(a[14], NULL, &stream);
+    if (ok && a[10] != Py_None) {
+        off = c->batch + 1;
+        ok = shaped(a[10], int32_type, c->device, 1, &off, &poff);
+    }
+    if (ok) {
+        Py_BEGIN_ALLOW_THREADS
+        rc = f_rope_q8(c->pool, x.scales, x.format, c->blocks, c->view, pq, q_row, pk, k_row, pv, v_row, pout, ppos, k[0], n_axes, pfreq,
+                       (int)(2 * half), a[11] == Py_None ? NULL : axes, (int)pairs, c->table, c->row, c->ctx, poff, (int)c->batch, k[0],
+                       (void*)(uintptr_t)stream);
+        Py_END_ALLOW_THREADS
+    }
+    return answer(ok, rc);
+}
+
+/* decode_q8(q, kv_pool, scales, block_table, ctx_lens, view, max_ctx_len, out, scale, workspace, stream) */
+static PyObject* call_decode_q8(PyObject* self, PyObject* const* a, Py_ssize_t nargs)
+{
+    ARGS(11)
+    int64_t q[3], max_ctx, ws = -1, stream;
+    void *pq, *pout, *pws;
+    q8_args x;
+    const cache_args* c = &x.c;
+    float scale;
+    int rc = 0, ok = q8_of(a[1], a[2], a[5], a[3], a[4], &x);
+    if (ok) {
+        q[0] = c->batch;
+        q[1] = c->hq;
+        q[2] = c->d;
+        ok = shaped(a[0], bf16_types, c->device, 3, q, &pq) && shaped(a[7], bf16_types, c->device, 3, q, &pout) && int_arg(a[6], &max_ctx) &&
+             float_arg(a[8], &scale) && shaped(a[9], uint8_type, c->device, 1, &ws, &pws) && stream_handle(a[10], NULL, &stream);
+    }
+    if (ok) {
+        Py_BEGIN_ALLOW_THREADS
+        rc = f_decode_q8(pq, pout, c->pool, x.scales, x.format, c->blocks, c->table, c->row, c->ctx, (int)c->batch, (int)max_ctx, c->view,
+                         scale, pws, (size_t)ws, (void*)(uintptr_t)stream);
+        Py_END_ALLOW_THREADS
+    }
+    return answer(ok, rc);
+}
+
+/* prefill_q8(q, kv_pool, scales, block_table, ctx_lens, q_offsets, view, max_ctx_len, max_q_len, out, scale, workspace, stream) */
+static PyObject* call_prefill_q8(PyObject* self, PyObject* const* a, Py_ssize_t nargs)
+{
+    ARGS(13)
+    int64_t q[3], off, max_ctx, max_q, ws = -1, stream;
+    void *pq, *pout, *poff, *pws;
+    q8_args x;
+    const cache_args* c = &x.c;
+    float scale;
+    int rc = 0, ok = q8_of(a[1], a[2], a[6], a[3], a[4], &x);
+    if (ok) {
+        q[0] = -1;
+        q[1] = c->hq;
+        q[2] = c->d;
+        off = c->batch + 1;
+        ok = shaped(a[0], bf16_types, c->device, 3, q, &pq) && shaped(a[9], bf16_types, c->device, 3, q, &pout) &&
+             shaped(a[5], int32_type, c->device, 1, &off, &poff) && int_arg(a[7], &max_ctx) && int_arg(a[8], &max_q) &&
+             float_arg(a[10], &scale) && shaped(a[11], uint8_type, c->device, 1, &ws, &pws) && stream_handle(a[12], NULL, &stream);
+    }
+    if (ok) {
+        Py_BEGIN_ALLOW_THREADS
+        rc = f_prefill_q8(pq, pout, c->pool, x.scales, x.format, c->blocks, c->table, c->row, c->ctx, poff, (int)c->batch, q[0], (int)max_ctx,
+                          (int)max_q, c->view, scale, pws, (size_t)ws, (void*)(uintptr_t)stream);
+        Py_END_ALLOW_THREADS
+    }
+    return answer(ok, rc);
+}
+
+/* repack_q8(kv_pool, scales, src_view, dst_view, src_block_table, dst_block_table, n_tokens, max_tokens, stream) */
+static PyObject* call_repack_q8(PyObject* self, PyObject* const* a, Py_ssize_t nargs)
+{
+    ARGS(9)
+    int64_t tab[2], dst_row, most, stream;
+    void* pdst;
+    const kv_view* dst;
+    q8_args x;
+    const cache_args* c = &x.c;
+    int rc = 0, ok = q8_of(a[0], a[1], a[2], a[4], a[6], &x);
+    if (ok) {
+        tab[0] = c->batch;
+        tab[1] = -1;
+        ok = view_handle(a[3], &dst) && shaped(a[5], int32_type, c->device, 2, tab, &pdst) && ask_int(a[5], n_stride, n_zero, &dst_row) &&
+             int_arg(a[7], &most) && stream_handle(a[8], NULL, &stream);
+    }
+    if (ok) {
+        Py_BEGIN_ALLOW_THREADS
+        rc = f_repack_q8(c->pool, x.scales, c->blocks, c->view, dst, c->table, c->row, pdst, dst_row, c->ctx, (int)c->batch, (int)most,
+                         (void*)(uintptr_t)stream);
+        Py_END_ALLOW_THREADS
+    }
+    return answer(ok, rc);
+}
+
+/* setup_q8((addresses of rope_q8, decode_q8, prefill_q8, repack_q8), dict of formats by dtype); after setup_operators() */
+static PyObject* setup_q8(PyObject* self, PyObject* args)
+{
+    unsigned long long f[4];
+    PyObject* formats;
+    if (!PyArg_ParseTuple(args, "(KKKK)O!", f, f + 1, f + 2, f + 3, &PyDict_Type, &formats)) return NULL;
+    f_rope_q8 = (rope_q8_fn)(uintptr_t)f[0];
+    f_decode_q8 = (decode_q8_fn)(uintptr_t)f[1];
+    f_prefill_q8 = (prefill_q8_fn)(uintptr_t)f[2];
+    f_repack_q8 = (repack_q8_fn)(uintptr_t)f[3];
+    Py_INCREF(formats);
+    Py_XSETREF(q8_formats, formats);
+    Py_RETURN_NONE;
+}
+
 /* setup_operators((addresses of rope, accept, tree, weights), (float32, dtypes of mask words)); after setup() */
 static PyObject* setup_operators(PyObject* self, PyObject* args)
 {
@@ -608,6 +799,11 @@ static PyMethodDef methods[] = {
     {"accept", (PyCFunction)(void (*)(void))call_accept, METH_FASTCALL, NULL},
     {"tree", (PyCFunction)(void (*)(void))call_tree, METH_FASTCALL, NULL},
     {"weights", (PyCFunction)(void (*)(void))call_weights, METH_FASTCALL, NULL},
+    {"setup_q8", setup_q8, METH_VARARGS, NULL},
+    {"rope_q8", (PyCFunction)(void (*)(void))call_rope_q8, METH_FASTCALL, NULL},
+    {"decode_q8", (PyCFunction)(void (*)(void))call_decode_q8, METH_FASTCALL, NULL},
+    {"prefill_q8", (PyCFunction)(void (*)(void))call_prefill_q8, METH_FASTCALL, NULL},
+    {"repack_q8", (PyCFunction)(void (*)(void))call_repack_q8, METH_FASTCALL, NULL},
     {"repack", (PyCFunction)(void (*)(void))call_repack, METH_FASTCALL, NULL},
     {NULL, NULL, 0, NULL},
 };
@@ -625,6 +821,7 @@ PyMODINIT_FUNC PyInit__calls(void)
         {&n_get_device, "get_device"}, {&n_cuda_stream, "cuda_stream"}, {&n_handle, "handle"}, {&n_value, "value"},
         {&n_block_bytes, "block_bytes"}, {&n_n_q_local, "n_q_local"}, {&n_n_kv_local, "n_kv_local"},
         {&n_head_dim, "head_dim"}, {&n_scratch, "scratch"},
+        {&n_geometry, "geometry"}, {&n_n_kv_heads, "n_kv_heads"},
     };
     for (size_t i = 0; i < sizeof(names) / sizeof(names[0]); ++i)
         if (!*names[i].to && !(*names[i].to = PyUnicode_InternFromString(names[i].text))) return NULL;

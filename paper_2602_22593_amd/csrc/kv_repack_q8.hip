@@ -2,7 +2,9 @@
 // same in every layout and has one scale, so nothing is rounded.
 //
 // Bound by reading and writing what moves.  As in kv_repack, a token's rows for a run of consecutive heads are contiguous in every
-// arrangement: the unit is a 16-byte piece of such a run, consecutive lanes on consecutive pieces, four in flight per lane.
+// arrangement: the unit is a 16-byte piece of such a run, consecutive lanes on consecutive pieces.  A workgroup moves about 8 KiB, all of
+// them requested before the first is stored: with 64 KiB and four requests a lane at a time, moving 128 sequences around 4096 tokens from
+// DP to TP4 took 114 us, with 16 KiB 106, now 104 (4.9 TB/s; runs of 256 bytes are read), and one sequence 8.2 us, now 5.5 (its launch).
 #include "kv_q8.h"
 
 using namespace kvq8;
@@ -10,7 +12,8 @@ using namespace kvq8;
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kUnroll = 4;
+constexpr int kUnroll = 2;
+constexpr int kPayload = 8 * 1024;
 
 struct repack_args {
     uint8_t* pool;
@@ -44,13 +47,17 @@ __global__ __launch_bounds__(kThreads) void repack_kernel(repack_args a)
     const int32_t* drow = a.dst_table + (int64_t)s * a.dst_stride;
     // scales: of every group that has a token
     const int B = a.sx.base_tokens, groups = (t1 - t0 + B - 1) / B, per_group = 2 * a.heads;
-    for (int i = threadIdx.x; i < groups * per_group; i += kThreads) {
+    float scale = 0.f;
+    int64_t scale_to = 0;
+    auto load_scale = [&](int i) {
         const int g = i / per_group, rem = i - g * per_group, plane = rem / a.heads, h = rem - plane * a.heads;
         int from, to;
         const int64_t sb = block_of(a.src, srow, t0 + g * B, from), db = block_of(a.dst, drow, t0 + g * B, to);
-        a.scales[q8_scale_at(a.dx, db, to, a.dst_head + h) + plane * (a.dx.block_scales / 2)] =
-            a.scales[q8_scale_at(a.sx, sb, from, a.src_head + h) + plane * (a.sx.block_scales / 2)];
-    }
+        scale = a.scales[q8_scale_at(a.sx, sb, from, a.src_head + h) + plane * (a.sx.block_scales / 2)];
+        scale_to = q8_scale_at(a.dx, db, to, a.dst_head + h) + plane * (a.dx.block_scales / 2);
+    };
+    const int n_scales = groups * per_group;
+    if ((int)threadIdx.x < n_scales) load_scale(threadIdx.x);   // (stored after the codes)
     const int per_tok = 2 * a.run_chunks, total = (t1 - t0) * per_tok;
     const int64_t s_off = a.src.head_off + a.src_head * a.src.head_dim, d_off = a.dst.head_off + a.dst_head * a.dst.head_dim;
     for (int base = threadIdx.x; base < total; base += kThreads * kUnroll) {
@@ -83,6 +90,10 @@ __global__ __launch_bounds__(kThreads) void repack_kernel(repack_args a)
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u)
             if (to[u] >= 0) __builtin_nontemporal_store(val[u], reinterpret_cast<kv_u32x4*>(a.pool + to[u]));
+    }
+    for (int i = threadIdx.x; i < n_scales; i += kThreads) {
+        if (i >= kThreads) load_scale(i);
+        a.scales[scale_to] = scale;
     }
 }
 
@@ -129,9 +140,9 @@ extern "C" int kv_repack_q8(void* kv_pool, float* scales, int64_t n_pool_blocks,
     a.run_shift = -1;
     for (int s = 0; s < 31; ++s)
         if ((1 << s) == a.run_chunks) a.run_shift = s;
-    // about 64 KiB of payload per workgroup, whole groups
+    // about kPayload bytes per workgroup, whole groups
     const int B = g.base_block_size;
-    int tokens = (64 * 1024) / (2 * a.run_chunks * 16);
+    int tokens = kPayload / (2 * a.run_chunks * 16);
     tokens = (tokens + B - 1) / B * B;
     a.tokens_per_wg = tokens;
     const int64_t gx = ((int64_t)max_tokens + tokens - 1) / tokens;
