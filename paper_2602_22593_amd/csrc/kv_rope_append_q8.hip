@@ -41,16 +41,20 @@ struct append_args {
     uint32_t axis[kMostPairs / 16];            // two bits a pair
 };
 
-// Cosine and sine of pair f of row i.  An angle may be many thousand turns: its fraction of a turn is taken in 64 bits, where a position
-// of 31 bits and a frequency of 24 leave an error of 2^-22 turns at most; from there 32 bits do.
+// Cosine and sine of pair f of row i, in 64 bits and rounded once: a key's code depends on which side of a boundary its value falls, and
+// sines that are two steps of fp32 off put half as many codes again on the wrong one.  The angle as a fraction r of a turn from the nearest quarter,
+// |r| <= 1/8, then the Taylor series: the first terms left out are (pi / 4)^13 / 13! = 7e-12 and (pi / 4)^14 / 14! = 4e-13.
 __device__ __forceinline__ float2 turn_of(const append_args& a, int64_t i, int f)
 {
     const int axis = (a.axis[f >> 4] >> (2 * (f & 15))) & 3;
     const double turns = (double)a.positions[axis * a.position_stride + i] * (double)a.inv_freq[f] * 0.15915494309189533577;
-    const float part = (float)(turns - rint(turns));
-    float sn, cs;
-    sincospif(2.f * part, &sn, &cs);
-    return make_float2(cs, sn);
+    const double quarters = rint(4. * (turns - rint(turns)));
+    const double x = (turns - rint(turns) - 0.25 * quarters) * 6.28318530717958647693, y = x * x;
+    const double sn = x + x * y * (-1. / 6 + y * (1. / 120 + y * (-1. / 5040 + y * (1. / 362880 - y * (1. / 39916800)))));
+    const double cs = 1. + y * (-0.5 + y * (1. / 24 + y * (-1. / 720 + y * (1. / 40320 + y * (-1. / 3628800 + y * (1. / 479001600))))));
+    const int k = (int)quarters;
+    const float c = (float)((k & 1) ? sn : cs), s = (float)((k & 1) ? cs : sn);
+    return make_float2(((k + 1) & 2) ? -c : c, (k & 2) ? -s : s);
 }
 
 // A lane's sixteen elements of a row are two pieces of eight, the two halves of eight pairs where the row is rotated by halves, so that
@@ -77,6 +81,7 @@ __device__ __forceinline__ void load_row(const uint16_t* row, const pieces& p, c
     if (!p.turns) return;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
+#pragma clang fp contract(off)
         const int i = adjacent ? 2 * e : e, j = adjacent ? 2 * e + 1 : 8 + e;
         const float2 t = turn[e];
         const float u = x[i], w = x[j];

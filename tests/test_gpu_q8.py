@@ -258,6 +258,50 @@ def test_decode_of_many_sequences():
     within(host(decode(x)), *q8.attention(x, causal=False))
 
 
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("geom,triple,ctx,powers", [
+    (G8B, (DP, 1, 0), [900, 1, 0, 517] + [30] * 296, True),          # eight heads side by side, more sequences than lanes list at once
+    (G8B, (DP, 1, 0), [5000, 2600], False),                          # long pieces
+    ((32, 16, 64, 16), (DP, 1, 0), [1800, 40, 513], False),          # two sets of eight heads
+    ((16, 4, 64, 16), (DP, 1, 0), [2500, 31], True),                 # four
+    ((7, 1, 128, 16), (DP, 1, 0), [40000], True),                    # one pair in hundreds of pieces
+    ((7, 1, 64, 16), (DP, 1, 0), [33000, 3], False),
+])
+def test_decode_of_long_and_of_many(fmt, geom, triple, ctx, powers):
+    x = q8.case(geom, triple, ctx, [1 if n else 0 for n in ctx], fmt, powers=powers)
+    x.c.q = q_for(x, len(ctx))
+    within(host(decode(x)), *q8.attention(x, causal=False))
+
+
+@pytest.mark.parametrize("plane", [0, 1])
+@pytest.mark.parametrize("ctx", [[300, 40], [3000, 40]])
+def test_decode_with_a_scale_that_is_no_number(ctx, plane):
+    """Query heads of that KV head and sequence become NaN, all others keep their results."""
+    x = q8.case(G8B, (DP, 1, 0), ctx, [1, 1], E4M3)
+    x.c.q = q_for(x, 2)
+    want, tol = q8.attention(x, causal=False)
+    b, g = x.group_of(0, 100)
+    x.scales[b, plane, g, 5] = np.nan
+    out = bf16_bits_to_f64(host(decode(x)))
+    hit = np.zeros(out.shape, bool)
+    hit[0, 20:24] = True
+    assert np.isnan(out[hit]).all() and (np.abs(out - want) <= tol)[~hit].all()
+
+
+def test_decode_with_a_larger_bound_than_any_length():
+    """The bound decides how a call is cut: short sequences under a bound of many, and a workspace for more of them."""
+    x = q8.case(G8B, (TP, 2, 0), [40, 0, 7, 333], [1, 0, 1, 1], INT8)
+    c = x.c
+    c.q = q_for(x, 4)
+    c.table = np.concatenate([c.table, np.full((4, 600), -1, np.int32)], axis=1)
+    pool, scales = pool_of(x)
+    view, want = view_of(c), q8.attention(x, causal=False)
+    ws = torch.full((kv.paged_decode_attn_q8_workspace_bytes(view, 64, 9000),), 255, dtype=torch.uint8, device=DEV)
+    for bound in (333, 513, 1000, 9000):
+        got = kv.paged_decode_attn_q8(dev(c.q), pool, scales, dev(c.table), dev(c.ctx), view, bound, workspace=ws)
+        within(host(got), *want, f"bound {bound}")
+
+
 def test_decode_with_large_scores_and_a_reference_that_moves():
     """Scores up to some hundreds, largest at the end: weights of all that came before vanish."""
     x = q8.case(G8B, (TP, 8, 0), [1500, 77], [1, 1], INT8, size=16.0)
@@ -307,6 +351,18 @@ def test_prefill(fmt, geom, triple, ctx, q_lens):
 def test_prefill_with_any_scales(fmt):
     x = q8.case(G8B, (TP, 4, 1), [300, 70], [100, 70], fmt, powers=False)
     within(host(prefill(x, scale=0.1)), *q8.attention(x, causal=True, scale=0.1, rounded=True))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("powers", [False, True])
+@pytest.mark.parametrize("triple,ctx,q_lens", [
+    ((TP, 4, 1), [2300, 2200] + [512] * 11, [512] * 13),      # not cut, one after the other over 70 tiles
+    ((TP, 4, 1), [6000] + [512] * 7, [512] * 8),              # cut into long pieces
+    ((TP, 8, 1), [12000, 40], [3, 1]),                        # and into many
+])
+def test_prefill_of_many_tiles(fmt, powers, triple, ctx, q_lens):
+    x = q8.case(G8B, triple, ctx, q_lens, fmt, powers=powers)
+    within(host(prefill(x)), *q8.attention(x, causal=True, rounded=not powers))
 
 
 @pytest.mark.parametrize("cut", [False, True])
@@ -441,6 +497,62 @@ def test_a_decode_step_replayed_from_a_graph():
         check_append(x, qkv[:3], want, tol, [1, 1, 1, 0], pool, scales, True)
         x.codes, x.scales, c.q = codes_back(pool, x), host(scales).reshape(x.scales.shape), host(q)
         within(host(out), *q8.attention(x, causal=False), f"replay {rep}")
+
+
+def test_two_graphs_that_share_a_workspace():
+    """Decode of one batch and prefill of another captured with one workspace, replayed in turn: nothing is left in it from one to the other."""
+    a, b = q8.case(G8B, (TP, 2, 1), [1500, 47, 130], [1] * 3, INT8), q8.case(G8B, (TP, 8, 3), [1300, 16, 130], [16, 16, 7], E4M3, index=83)
+    a.c.q = q_for(a, 3)
+    pools = pool_of(a), pool_of(b)
+    va, vb = view_of(a.c), view_of(b.c)
+    args = [[dev(x) for x in (c.q, c.table, c.ctx, c.q_off.astype(np.int32))] for c in (a.c, b.c)]
+    outs = [torch.zeros_like(x[0]) for x in args]
+    ws = torch.empty(max(kv.paged_decode_attn_q8_workspace_bytes(va, 3, 1500),
+                         kv.paged_prefill_attn_q8_workspace_bytes(vb, 3, 39, 1300, 16)), dtype=torch.uint8, device=DEV)
+    assert ws.numel() > 0
+
+    def first():
+        q, table, n, _ = args[0]
+        kv.paged_decode_attn_q8(q, *pools[0], table, n, va, 1500, out=outs[0], workspace=ws)
+
+    def second():
+        q, table, n, off = args[1]
+        kv.paged_prefill_attn_q8(q, *pools[1], table, n, off, vb, 1300, 16, out=outs[1], workspace=ws)
+    graphs = []
+    for call in (first, second):
+        call()
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            call()
+    want = q8.attention(a, causal=False), q8.attention(b, causal=True)
+    for which in (0, 1, 1, 0, 1, 0, 0):
+        outs[which].fill_(float("nan"))
+        graphs[which].replay()
+        (second if which == 0 else first)()
+        torch.cuda.synchronize()
+        for k in (0, 1):
+            within(host(outs[k]), *want[k])
+
+
+def test_two_calls_at_once():
+    """Decode of two batches on two streams that nothing orders, each with a workspace of the binding's own."""
+    xs = [q8.case(G8B, (DP, 1, 0), [1500, 47, 600], [1] * 3, fmt, index=84 + i) for i, fmt in enumerate(FORMATS)]
+    streams, pools, outs, args = [torch.cuda.Stream() for _ in xs], [pool_of(x) for x in xs], [], []
+    for x in xs:
+        x.c.q = q_for(x, 3)
+        args.append([dev(t) for t in (x.c.q, x.c.table, x.c.ctx)] + [view_of(x.c)])
+        outs.append([torch.zeros((3, 32, 128), dtype=torch.bfloat16, device=DEV) for _ in range(8)])
+    torch.cuda.synchronize()
+    for i in range(8):
+        for k in (0, 1):
+            q, table, n, view = args[k]
+            kv.paged_decode_attn_q8(q, *pools[k], table, n, view, 1500, out=outs[k][i], stream=streams[k])
+    torch.cuda.synchronize()
+    for k, x in enumerate(xs):
+        want = q8.attention(x, causal=False)
+        for out in outs[k]:
+            within(host(out), *want)
 
 
 def test_offsets_past_32_bits():
