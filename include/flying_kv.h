@@ -15,7 +15,7 @@
  *     debugging aid, is the one exception to the first two).
  *   - "device" pointers are HIP device memory owned by the caller; "host" pointers are
  *     ordinary host memory.  The library owns only kv_view objects (host).
- *   - bf16 everywhere in memory; all accumulation is fp32 on the device.
+ *   - bf16 everywhere in memory, but for a cache held in 8 bits (its own section below); all accumulation is fp32 on the device.
  *   - Physical layout of the pool: n_pool_blocks blocks of block_bytes each.  A block read
  *     under a view with capacity Bv (tokens) and Hrow KV heads per token row is the array
  *         bf16 [2 (0 = K, 1 = V)] [Bv] [Hrow] [head_dim]
@@ -485,7 +485,7 @@ int kv_evict(void* kv_pool, int64_t n_pool_blocks, const kv_view* view, const in
  * a block's scales never change in number either.  A value is its code times its group's scale.  Formats:
  *   KV_Q8_E4M3  8-bit floats of four exponent and three mantissa bits, no infinities, largest 448
  *   KV_Q8_INT8  integers in [-127, 127]
- * Any finite scales are read; those that kv_rope_append_q8 writes are powers of two, so that its values are exact in bf16.
+ * Scales of any magnitude up to 2^80 are read; those that kv_rope_append_q8 writes are powers of two, so that its values are exact in bf16.
  * A scale that is not finite makes every number of its group NaN: a row of attention that sees one of its tokens is
  * NaN, and no other.  (The codes 0x7f and 0xff of e4m3 are NaN too; the library writes none.  Where a cache of
  * other origin has them, rows of a paged_prefill_attn_q8 call before such a token may be NaN as well.)

@@ -42,7 +42,7 @@ __device__ __forceinline__ int64_t q8_scale_at(const q8_view& x, int64_t block, 
     return block * x.block_scales + group * x.row_heads + x.row_head0 + h;
 }
 
-// Codes 2 w, 2 w + 1 of a dword as two bf16, times 2^(exponent of scale) (e4m3) or as they are (int8: |code| < 2^7 is exact).
+// Two codes of a dword (HI: the upper two) as two bf16: exact in either format (e4m3 has four significant bits, int8 eight).
 template <int FMT, bool HI>
 __device__ __forceinline__ uint32_t two_bf16(uint32_t codes)
 {

@@ -2,7 +2,9 @@
 //
 //   out = sum_t softmax_t(c q . sK[t] k_t) sV[t] v_t,  k_t and v_t the codes of token t, sK and sV the scales of its group
 //
-// Bound by reading codes and scales: 2 d + 8 / B_base bytes a token and head.
+// Bound by reading codes and scales: 2 d + 8 / B_base bytes a token and head.  Measured: 64 sequences around 2048 tokens, 8 heads, 56 us
+// (306 MB read at 5.8 TB/s, 6.3 between 64 and 192 sequences, and 4.6 us of second launch; the same cache in bf16 97); 256 around 1024,
+// one head, 44 (70); 8 long and short ones, 2 heads, 33 (53).  Without its arithmetic the kernel takes 2 to 8 % less.
 //
 // A wavefront takes 32 tokens of a KV head at a time (a tile), its G <= 16 query rows as the 16 columns of the products, and needs nothing
 // of LDS or of other wavefronts until it is through.  Lane l = (m = l % 16, g = l / 16), products of 16 x 16 x 32 in bf16:
@@ -462,6 +464,12 @@ __global__ __launch_bounds__(THREADS) void merge_q8_kernel(decode_args a, int ro
 
 constexpr int kMostWaves = 2048;   // two for each SIMD of 256 compute units
 constexpr int kUnitShift = 3, kStartUnits = 8;   // a start counts as much as a step
+// Up to which bound of the lengths a workgroup takes a whole pair: cutting costs a second launch, 4 us and more, and pieces to write and read;
+// not cutting leaves a workgroup 1 us for each 128 tokens, and from 256 pairs on compute units with two.  (Lengths from 0.3 of the bound to it, us
+// whole and cut: 24 pairs, 500: 8.0, 8.7; 700: 9.9, 8.9; 192 pairs, 1000: 16.2, 18.6; 256 pairs, 1300: 17.3, 19.9; 384 pairs, 500: 14.6, 16.4;
+// 700: 19.6, 19.2; 1024 pairs, 500: 27.4, 27.9; 1440 pairs, 300: 25.9, 27.5; 500: 36.5, 34.3.)
+int whole_bound(int64_t pairs) { return pairs >= 96 && pairs <= 256 ? 1024 : pairs <= 1024 ? 512 : 256; }
+constexpr int kLeastCut = 256;   // no pair is cut up to this bound
 
 // How a call is cut: the same for the workspace and the launch.
 struct decode_plan {
@@ -475,16 +483,22 @@ decode_plan plan_of(const kv_view* view, int batch, int max_ctx_len)
     decode_plan p;
     const int hl = view->n_kv_local;
     p.hpw = hl % 8 == 0 ? 8 : hl % 4 == 0 ? 4 : hl % 2 == 0 ? 2 : 1;
-    p.whole = max_ctx_len <= 512;
-    if (p.whole) p.hpw = 1;
+    // (the room asked for does not depend on it: what serves large calls is to serve all smaller ones)
+    p.whole = max_ctx_len <= whole_bound((int64_t)batch * hl);
+    const bool never_cut = max_ctx_len <= kLeastCut;
     p.head_sets = hl / p.hpw;
     const int step = step_tokens(p.hpw);
     const int64_t pairs = (int64_t)batch * p.head_sets, steps = pairs * (((int64_t)max_ctx_len + step - 1) / step);
-    p.workgroups = (int)(p.whole ? pairs : std::min<int64_t>(steps, kMostWaves / waves_of(p.hpw)));
+    p.workgroups = (int)std::min<int64_t>(steps, kMostWaves / waves_of(p.hpw));
     const int rows = p.hpw * view->group;
-    p.o_bytes = p.whole ? 0 : (size_t)2 * p.workgroups * rows * view->geom.head_dim * 4;
-    p.ml_bytes = p.whole ? 0 : (size_t)2 * p.workgroups * rows * 8;
-    p.bytes = p.whole ? 0 : p.o_bytes + p.ml_bytes + (size_t)pairs * sizeof(int2);
+    p.o_bytes = never_cut ? 0 : (size_t)2 * p.workgroups * rows * view->geom.head_dim * 4;
+    p.ml_bytes = never_cut ? 0 : (size_t)2 * p.workgroups * rows * 8;
+    p.bytes = never_cut ? 0 : p.o_bytes + p.ml_bytes + (size_t)pairs * sizeof(int2);
+    if (p.whole) {
+        p.hpw = 1;
+        p.head_sets = hl;
+        p.workgroups = batch * hl;
+    }
     return p;
 }
 
@@ -498,7 +512,8 @@ void launch(const decode_plan& p, const decode_args& a, hipStream_t st)
     hipLaunchKernelGGL(f, dim3((unsigned)p.workgroups), dim3(64 * waves_of(p.hpw)), 0, st, a);
     if (!p.whole) {
         const int pairs = a.batch * p.head_sets, rows = p.hpw * a.group;
-        const bool many = p.workgroups >= 16 * pairs;   // pieces a pair
+        // pieces a pair: one of 20000 tokens and 8 heads in 256 pieces 19.8 us, 27.4 with 256 threads; 16 of 1000 to 3000 in 16 each 25.5, 23.4
+        const bool many = p.workgroups > 32 * pairs;
         hipLaunchKernelGGL((many ? merge_q8_kernel<D, 1024> : merge_q8_kernel<D, 256>), dim3((unsigned)pairs, (unsigned)rows),
                            dim3(many ? 1024 : 256), 0, st, a, rows);
     }

@@ -262,6 +262,8 @@ def test_decode_of_many_sequences():
 @pytest.mark.parametrize("geom,triple,ctx,powers", [
     (G8B, (DP, 1, 0), [900, 1, 0, 517] + [30] * 296, True),          # eight heads side by side, more sequences than lanes list at once
     (G8B, (DP, 1, 0), [5000, 2600], False),                          # long pieces
+    (G8B, (DP, 1, 0), [500, 1, 0] + [37] * 177, True),               # short, and cut since they are many
+    (G8B, (DP, 1, 0), [1000, 0, 513, 129] + [50] * 20, True),        # long, and not cut since they fill the chip once
     ((32, 16, 64, 16), (DP, 1, 0), [1800, 40, 513], False),          # two sets of eight heads
     ((16, 4, 64, 16), (DP, 1, 0), [2500, 31], True),                 # four
     ((7, 1, 128, 16), (DP, 1, 0), [40000], True),                    # one pair in hundreds of pieces
