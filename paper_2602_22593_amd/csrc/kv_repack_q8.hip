@@ -113,7 +113,7 @@ extern "C" int kv_repack_q8(void* kv_pool, float* scales, int64_t n_pool_blocks,
     const int64_t need_src = ((int64_t)max_tokens + src_view->block_tokens - 1) / src_view->block_tokens;
     const int64_t need_dst = ((int64_t)max_tokens + dst_view->block_tokens - 1) / dst_view->block_tokens;
     if (src_stride < need_src || dst_stride < need_dst) return KV_ERR_INVALID_ARG;
-    if (g.head_dim % 16 != 0 || !kv_aligned(kv_pool, 16) || !kv_aligned(scales, 4)) return KV_ERR_UNSUPPORTED;
+    if (g.head_dim % 16 != 0 || g.base_block_size % 16 != 0 || !kv_aligned(kv_pool, 16) || !kv_aligned(scales, 4)) return KV_ERR_UNSUPPORTED;
 
     // heads exposed by both views
     const int lo = src_view->kv_head0 > dst_view->kv_head0 ? src_view->kv_head0 : dst_view->kv_head0;

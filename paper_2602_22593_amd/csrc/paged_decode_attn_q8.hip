@@ -39,7 +39,7 @@ struct decode_args {
     float scale_log2e;
     int32_t group, batch;
     int32_t head_sets;     // n_kv_local / HPW
-    int32_t whole;         // a workgroup takes a whole pair (sequence, set of heads)
+    int32_t last_block;    // of a row of the table, by the bound of the lengths
     int32_t unit_shift, start_units;   // of the axis that is cut
     uint32_t inverse;      // 2^32 / workgroups
     float* part_o;         // [2 * workgroups][HPW * G][D] sums of a cut pair's piece
@@ -155,8 +155,10 @@ __device__ __forceinline__ void dims_of(const uint32_t (&t)[8], bf16x8 (&to)[4])
 // HPW: heads that the wavefronts of a workgroup take side by side; the others follow each other in the tokens.  8 heads have 8 wavefronts: a
 // workgroup then reads whole token rows of 1 KiB as one stream (8 heads, 64 sequences around 2048 tokens: 56 us, 59 us as 4 heads and 4).
 // Two tiles at a time, or two heads a wavefront, with one wavefront a SIMD: 58 us there, the same or up to 2 % better elsewhere.
+// WHOLE: a workgroup takes a pair (sequence, head).  Trips to memory are what counts then: the length, the blocks of the wavefront's first 32 tiles
+// and q are asked for together, scales beside the first tile.
 constexpr int waves_of(int hpw) { return hpw == 8 ? 8 : 4; }   // of a workgroup
-template <int D, int FMT, int HPW>
+template <int D, int FMT, int HPW, bool WHOLE>
 __global__ __launch_bounds__(64 * waves_of(HPW), 2) void decode_q8_kernel(decode_args a)
 {
     constexpr int kWaves = waves_of(HPW), kThreads = 64 * kWaves;
@@ -171,18 +173,24 @@ __global__ __launch_bounds__(64 * waves_of(HPW), 2) void decode_q8_kernel(decode
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), m = lane & 15, g = lane >> 4;
     const kv_view_dev& v = a.v;
     const int G = a.group;
-    // rows of sequences without tokens are zeros
-    for (int s = blockIdx.x; s < a.batch; s += gridDim.x)
-        if (a.ctx_lens[s] <= 0)
-            for (int i = tid; i < v.n_q_local * D / 8; i += kThreads)
-                reinterpret_cast<kv_u32x4*>(a.out + (int64_t)s * v.n_q_local * D)[i] = kv_u32x4{0u, 0u, 0u, 0u};
-
+    const int hw = wave % HPW, sub = wave / HPW;
     axis_place at, to;   // where the workgroup's steps start, and where they end
-    if (a.whole) {
+    int whole_id = 0, whole_t = 0, whole_slot = 0;   // a lane's 16 tokens of those that the wavefront takes first, their block and place in it
+    if constexpr (WHOLE) {
         at.s = (int)blockIdx.x / a.head_sets;
         at.set = (int)blockIdx.x - at.s * a.head_sets;
         at.step = 0;
-        to = {at.s, at.set, steps_of(a.ctx_lens[at.s], kStep)};
+        whole_t = (lane >> 1) * kStep + sub * kTile + 16 * (lane & 1);
+        int b;
+        kv_split_token(v, whole_t, b, whole_slot);
+        if (a.last_block >= 0) whole_id = a.table[(int64_t)at.s * a.table_stride + min(b, a.last_block)];
+        const int n = a.ctx_lens[at.s];
+        if (n <= 0) {   // zeros
+            for (int i = tid; i < G * D / 8; i += kThreads)
+                reinterpret_cast<kv_u32x4*>(a.out + ((int64_t)at.s * v.n_q_local + at.set * G) * D)[i] = kv_u32x4{0u, 0u, 0u, 0u};
+            return;
+        }
+        to = {at.s, at.set, steps_of(n, kStep)};
     } else {
         // every wavefront for itself, four lengths a lane: no barrier stands between the lengths and the first tiles
         const axis_run first = run_of(a, 0, lane, kStep);
@@ -214,7 +222,6 @@ __global__ __launch_bounds__(64 * waves_of(HPW), 2) void decode_q8_kernel(decode
         }
     }
 
-    const int hw = wave % HPW, sub = wave / HPW;
     const uint32_t row_bytes = (uint32_t)v.token_stride;
     for (; at.s < a.batch; at.step = 0, ++at.set, at.s += at.set == a.head_sets, at.set = at.set == a.head_sets ? 0 : at.set) {
         const int s = at.s, set = at.set, step = at.step;
@@ -246,6 +253,12 @@ __global__ __launch_bounds__(64 * waves_of(HPW), 2) void decode_q8_kernel(decode
         float ref = kLowest, l = 0.f;
 
         const int t_first = step * kStep + sub * kTile, t_end = min(end * kStep, n);
+        // WHOLE: where the groups lie, and (asked for beside the first tile) their scales
+        uint64_t whole_at = 0;
+        float whole_k = 0.f, whole_v = 0.f;
+        auto group_of = [&](int t) -> int { return t / kStep * 2 + (t >> 4 & 1); };   // the lane that has it
+        if constexpr (WHOLE)
+            whole_at = reinterpret_cast<uint64_t>(a.pool) + (uint64_t)(whole_id * v.block_elems + (int64_t)whole_slot * row_bytes + v.head_off + h * D);
         struct tile {
             kv_u32x4 k[2][kLoads];
             uint32_t v[8][kWords];
@@ -256,33 +269,53 @@ __global__ __launch_bounds__(64 * waves_of(HPW), 2) void decode_q8_kernel(decode
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const int t = min(t0 + 16 * half, last16);
-                int b, slot;
-                kv_split_token(v, t, b, slot);
-                const int64_t id = ids[b];
-                const uint8_t* base = a.pool + id * v.block_elems + (int64_t)slot * row_bytes + v.head_off + h * D;
+                global_bytes base;
+                int64_t id = 0;
+                int slot = 0;
+                if constexpr (WHOLE) {
+                    const int i = group_of(t);
+                    base = (global_bytes)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((uint32_t)whole_at, i) |
+                                          (uint64_t)(uint32_t)__builtin_amdgcn_readlane((uint32_t)(whole_at >> 32), i) << 32);
+                } else {
+                    int b;
+                    kv_split_token(v, t, b, slot);
+                    id = ids[b];
+                    base = (global_bytes)(reinterpret_cast<uint64_t>(a.pool) +
+                                          (uint64_t)(id * v.block_elems + (int64_t)slot * row_bytes + v.head_off + h * D));
+                }
                 const int most = n - 1 - t;   // the last row that there is
                 const uint32_t kr = (uint32_t)min(m, most) * row_bytes + 16 * g;
 #pragma unroll
                 for (int i = 0; i < kLoads; ++i)
-                    x.k[half][i] = __builtin_nontemporal_load(reinterpret_cast<const kv_u32x4*>(base + kr + 64 * i));
-                const uint8_t* vb = base + v.plane_elems;
+                    x.k[half][i] = __builtin_nontemporal_load((const __attribute__((address_space(1))) kv_u32x4*)(base + kr + 64 * i));
+                const global_bytes vb = base + v.plane_elems;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const uint32_t vr = (uint32_t)min(4 * g + e, most) * row_bytes + kDims * m;
                     if constexpr (kWords == 2) {
-                        const kv_u32x2 y = __builtin_nontemporal_load(reinterpret_cast<const kv_u32x2*>(vb + vr));
+                        const kv_u32x2 y = __builtin_nontemporal_load((const __attribute__((address_space(1))) kv_u32x2*)(vb + vr));
                         x.v[4 * half + e][0] = y[0];
                         x.v[4 * half + e][1] = y[1];
                     } else {
-                        x.v[4 * half + e][0] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(vb + vr));
+                        x.v[4 * half + e][0] = __builtin_nontemporal_load((const __attribute__((address_space(1))) uint32_t*)(vb + vr));
                     }
                 }
-                const const_floats sc = (const_floats)(a.scales + q8_scale_at(a.x, id, slot, h));
-                x.sk[half] = sc[0];
-                x.sv[half] = sc[a.x.block_scales / 2];
+                if constexpr (!WHOLE) {
+                    const const_floats sc = (const_floats)(a.scales + q8_scale_at(a.x, id, slot, h));
+                    x.sk[half] = sc[0];
+                    x.sv[half] = sc[a.x.block_scales / 2];
+                }
             }
         };
-        auto take = [&](int t0, const tile& x) {
+        auto take = [&](int t0, tile& x) {
+            if constexpr (WHOLE) {
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const int i = group_of(min(t0 + 16 * half, last16));
+                    x.sk[half] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(whole_k), i));
+                    x.sv[half] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(whole_v), i));
+                }
+            }
             float u[8];   // scores in units of the exponent
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
@@ -340,6 +373,13 @@ __global__ __launch_bounds__(64 * waves_of(HPW), 2) void decode_q8_kernel(decode
             int t = t_first;
             tile x, y;
             if (t < t_end) request(t, x);
+            if constexpr (WHOLE) {
+                if (whole_t <= last16) {
+                    const float* sc = a.scales + q8_scale_at(a.x, whole_id, whole_slot, h);
+                    whole_k = sc[0];
+                    whole_v = sc[a.x.block_scales / 2];
+                }
+            }
             while (t < t_end) {
                 if (t + kStep < t_end) request(t + kStep, y);
                 __builtin_amdgcn_sched_barrier(0);   // (all of the next tile is asked for before anything waits for this one)
@@ -385,7 +425,7 @@ __global__ __launch_bounds__(64 * waves_of(HPW), 2) void decode_q8_kernel(decode
                 sum += s_ml[w * HPW + hh][r][1] * f;
                 acc += *reinterpret_cast<const f32x4*>(&s_o[w * HPW + hh][r][4 * d4]) * f;
             }
-            if (starts && ends) {
+            if (WHOLE || (starts && ends)) {
                 const float inv = 1.f / sum;
                 *reinterpret_cast<kv_u32x2*>(a.out + ((int64_t)s * v.n_q_local + set * rows + row) * D + 4 * d4) =
                     kv_u32x2{pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)};
@@ -394,16 +434,16 @@ __global__ __launch_bounds__(64 * waves_of(HPW), 2) void decode_q8_kernel(decode
                 if (d4 == 0) *reinterpret_cast<float2*>(a.part_ml + (slot * rows + row) * 2) = make_float2(top, sum);
             }
         }
-        if (!a.whole && tid == 0) {
+        if (!WHOLE && tid == 0) {
             if (starts) a.ends[pair].x = blockIdx.x;
             if (ends) a.ends[pair].y = blockIdx.x;
         }
-        if (last_pair) break;
+        if (WHOLE || last_pair) break;
         __syncthreads();
     }
 }
 
-// Row r of a cut pair: the sum of its pieces.  D / 4 lanes a slice of the list, the slices then over LDS.
+// Row r of a cut pair: the sum of its pieces; zeros where the sequence has no tokens.  D / 4 lanes a slice of the list, the slices then over LDS.
 // THREADS: 1024, and four pieces a slice requested at a time, where pairs are cut into many.
 template <int D, int THREADS>
 __global__ __launch_bounds__(THREADS) void merge_q8_kernel(decode_args a, int rows)
@@ -412,10 +452,14 @@ __global__ __launch_bounds__(THREADS) void merge_q8_kernel(decode_args a, int ro
     __shared__ f32x4 s_o[kSlices][D / 4];
     __shared__ float2 s_ml[kSlices];
     const int pair = blockIdx.x, row = blockIdx.y, s = pair / a.head_sets, set = pair - s * a.head_sets;
-    if (a.ctx_lens[s] <= 0) return;
-    const int first = a.ends[pair].x, last = a.ends[pair].y;
-    if (first == last) return;
     const int slice = threadIdx.x / (D / 4), d4 = threadIdx.x % (D / 4);
+    kv_u32x2* const out = reinterpret_cast<kv_u32x2*>(a.out + ((int64_t)s * a.v.n_q_local + set * rows + row) * D + 4 * d4);
+    const int n = a.ctx_lens[s], first = a.ends[pair].x, last = a.ends[pair].y;   // (one trip for all)
+    if (n <= 0) {
+        if (slice == 0) *out = kv_u32x2{0u, 0u};
+        return;
+    }
+    if (first == last) return;
     float top = kLowest, sum = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     for (int w0 = first + slice; w0 <= last; w0 += kBatch * kSlices) {
@@ -449,17 +493,18 @@ __global__ __launch_bounds__(THREADS) void merge_q8_kernel(decode_args a, int ro
     if (d4 == 0) s_ml[slice] = make_float2(top, sum);
     __syncthreads();
     if (slice != 0) return;
+#pragma unroll 8
     for (int i = 0; i < kSlices; ++i) top = fmaxf(top, s_ml[i].x);
     sum = 0.f;
     acc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
     for (int i = 0; i < kSlices; ++i) {
         const float f = fast_exp2(s_ml[i].x - top);
         sum += s_ml[i].y * f;
         acc += s_o[i][d4] * f;
     }
     const float inv = 1.f / sum;
-    *reinterpret_cast<kv_u32x2*>(a.out + ((int64_t)s * a.v.n_q_local + set * rows + row) * D + 4 * d4) =
-        kv_u32x2{pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)};
+    *out = kv_u32x2{pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)};
 }
 
 constexpr int kMostWaves = 2048;   // two for each SIMD of 256 compute units
@@ -505,10 +550,11 @@ decode_plan plan_of(const kv_view* view, int batch, int max_ctx_len)
 template <int D, int FMT>
 void launch(const decode_plan& p, const decode_args& a, hipStream_t st)
 {
-    auto* f = p.hpw == 8   ? decode_q8_kernel<D, FMT, 8>
-              : p.hpw == 4 ? decode_q8_kernel<D, FMT, 4>
-              : p.hpw == 2 ? decode_q8_kernel<D, FMT, 2>
-                           : decode_q8_kernel<D, FMT, 1>;
+    auto* f = p.whole      ? decode_q8_kernel<D, FMT, 1, true>
+              : p.hpw == 8 ? decode_q8_kernel<D, FMT, 8, false>
+              : p.hpw == 4 ? decode_q8_kernel<D, FMT, 4, false>
+              : p.hpw == 2 ? decode_q8_kernel<D, FMT, 2, false>
+                           : decode_q8_kernel<D, FMT, 1, false>;
     hipLaunchKernelGGL(f, dim3((unsigned)p.workgroups), dim3(64 * waves_of(p.hpw)), 0, st, a);
     if (!p.whole) {
         const int pairs = a.batch * p.head_sets, rows = p.hpw * a.group;
@@ -560,7 +606,7 @@ extern "C" int paged_decode_attn_q8(const void* q, void* out, const void* kv_poo
     a.group = G;
     a.batch = batch;
     a.head_sets = p.head_sets;
-    a.whole = p.whole;
+    a.last_block = max_ctx_len > 0 ? (max_ctx_len - 1) / view->block_tokens : -1;
     // (32 bits hold the axis: bounds that would pass them are cut by whole steps)
     const bool fine = (double)batch * p.head_sets * (max_ctx_len / step_tokens(p.hpw) + 2.0) < (double)(1 << 26);
     a.unit_shift = fine ? kUnitShift : 0;

@@ -106,6 +106,7 @@ def call(name, **changed):
     ("kv_repack_q8", dict(dst_view=view(hkv=4, hq=32)), INVALID),
     ("kv_repack_q8", dict(view=view(d=72), dst_view=view(d=72, layout=kv.KV_LAYOUT_TP, p=2)), UNSUPPORTED),
     ("kv_repack_q8", dict(kv_pool=C.c_void_p(264)), UNSUPPORTED),
+    ("kv_repack_q8", dict(view=view(bs=24), dst_view=view(bs=24, layout=kv.KV_LAYOUT_TP, p=2), stride=4096, dst_stride=4096), UNSUPPORTED),
     ("kv_repack_q8", dict(view=view(layout=kv.KV_LAYOUT_TP, p=2, r=1)), OK),   # no head in common
     ("kv_repack_q8", dict(batch=0, kv_pool=None), OK),
 ])
