@@ -389,6 +389,8 @@ __global__ __launch_bounds__(kThreads, kPerCu) void prefill_q8_kernel(prefill_ar
 #pragma unroll
         for (int kk = 0; kk < kAhead; ++kk) ka[kk] = k_operand(i, kk);
         __builtin_amdgcn_sched_barrier(0);
+        // (the scores and the weights go before the output products of the SIMD's other wavefront: 1 % less time, int8 3 %)
+        __builtin_amdgcn_s_setprio(1);
         sc = zero();
 #pragma unroll
         for (int kk = 0; kk < 8; ++kk) {
@@ -400,6 +402,7 @@ __global__ __launch_bounds__(kThreads, kPerCu) void prefill_q8_kernel(prefill_ar
             put_two(kf, kk, write_k, k_to(i));
             __builtin_amdgcn_sched_barrier(0);
         }
+        __builtin_amdgcn_s_setprio(0);
         mask(t + 1);
         const bf16x8 pb[2] = {weight_operand(0), weight_operand(1)};
         float tmax = kNegInf;
