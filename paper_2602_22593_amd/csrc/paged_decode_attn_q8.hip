@@ -185,7 +185,7 @@ __global__ __launch_bounds__(64 * waves_of(HPW), 2) void decode_q8_kernel(decode
         kv_split_token(v, whole_t, b, whole_slot);
         if (a.last_block >= 0) whole_id = a.table[(int64_t)at.s * a.table_stride + min(b, a.last_block)];
         const int n = a.ctx_lens[at.s];
-        if (n <= 0) {   // zeros
+        if (n <= 0 || a.last_block < 0) {   // zeros
             for (int i = tid; i < G * D / 8; i += kThreads)
                 reinterpret_cast<kv_u32x4*>(a.out + ((int64_t)at.s * v.n_q_local + at.set * G) * D)[i] = kv_u32x4{0u, 0u, 0u, 0u};
             return;

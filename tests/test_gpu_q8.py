@@ -160,6 +160,26 @@ def test_append_without_queries_grows_scales_step_by_step(fmt):
 
 @pytest.mark.parametrize("one", [True, False])
 @pytest.mark.parametrize("fmt", FORMATS)
+def test_append_of_rotated_keys_without_queries(fmt, one):
+    """The cache is written as it is beside queries, bit for bit."""
+    q_lens = [1, 1, 1, 1] if one else [3, 33, 1, 0]
+    x = q8.case(G8B, (TP, 2, 1), [40, 33, 5, 64], q_lens, fmt)
+    c = x.c
+    hl, ql = c.info["n_kv_local"], c.info["n_q_local"]
+    parts = dev(q8.normal_rows(sum(q_lens), ql, hl, 128, 130))
+    positions, freq = dev(np.arange(sum(q_lens), dtype=np.int32) * 77), dev((1e4 ** (-np.arange(64) / 64)).astype(np.float32))
+    off = None if one else dev(np.concatenate([[0], np.cumsum(q_lens)]).astype(np.int32))
+    got = []
+    for q in (parts[:, :ql], None):
+        pool, scales = pool_of(x)
+        out = kv.kv_rope_append_q8(pool, scales, view_of(c), q, parts[:, ql:ql + hl], parts[:, ql + hl:], positions, freq, dev(c.table), dev(c.ctx), off)
+        assert (out is None) == (q is None)
+        got.append((codes_back(pool, x), host(scales)))
+    assert np.array_equal(got[0][0], got[1][0]) and same(got[0][1], got[1][1])
+
+
+@pytest.mark.parametrize("one", [True, False])
+@pytest.mark.parametrize("fmt", FORMATS)
 def test_numbers_that_are_not_finite_make_their_group_nan(fmt, one):
     """An infinity in a key, a NaN in a value: the scale of that head and plane is NaN and stays so, the others are as ever."""
     x = q8.case(TINY, (DP, 1, 0), [20, 20], [1, 1], fmt)
@@ -302,6 +322,18 @@ def test_decode_with_a_larger_bound_than_any_length():
     for bound in (333, 513, 1000, 9000):
         got = kv.paged_decode_attn_q8(dev(c.q), pool, scales, dev(c.table), dev(c.ctx), view, bound, workspace=ws)
         within(host(got), *want, f"bound {bound}")
+
+
+def test_decode_of_empty_caches():
+    """No sequence has a token, under a bound of none, of few, and of many (cut): zeros."""
+    x = q8.case(G8B, (TP, 2, 0), [0, 0, 0], [0, 0, 0], E4M3)
+    q = torch.full((3, 16, 128), float("nan"), dtype=torch.bfloat16, device=DEV)
+    pool, scales = torch.zeros((4, 2 * 16 * 8 * 128), dtype=torch.uint8, device=DEV).view(torch.float8_e4m3fn), torch.ones((4, 16), device=DEV)
+    n = torch.zeros(3, dtype=torch.int32, device=DEV)
+    for bound in (0, 40, 5000):
+        table = torch.full((3, max(bound // 32 + 1, 1)), -1, dtype=torch.int32, device=DEV)
+        out = kv.paged_decode_attn_q8(q, pool, scales, table, n, view_of(x.c), bound)
+        assert (out == 0).all(), bound
 
 
 def test_decode_with_large_scores_and_a_reference_that_moves():
