@@ -516,7 +516,8 @@ int kv_rope_append_q8(void* kv_pool, float* scales, int format, int64_t n_pool_b
                       const int32_t* ctx_lens, const int32_t* q_offsets, int batch, int64_t total, void* hip_stream);
 
 /*
- * paged_decode_attn_q8 -- paged_decode_attn over a cache held in 8 bits.  Queries and weights enter the products in bf16, codes exactly.
+ * paged_decode_attn_q8 -- paged_decode_attn over a cache held in 8 bits.  Queries enter the products in bf16, weights as the
+ * sum of two bf16, codes exactly.
  *   workspace      at least paged_decode_attn_q8_workspace_bytes(...) bytes (may be 0: then null is accepted), 256-byte
  *                  aligned; contents need not be initialised; one for larger bounds serves smaller calls
  * Other arguments as paged_decode_attn.  Errors: KV_ERR_INVALID_ARG (null pointers, negative sizes, an unknown format,

@@ -141,12 +141,14 @@ class KVView:
         self.token_stride_elems, self.row_heads, self.row_head0 = ts.value, rh.value, r0.value
         self.head_dim = geometry.head_dim
         self.group = geometry.n_q_heads // geometry.n_kv_heads
+        # what csrc/binding_calls.c asks of a view, in one attribute
+        self._numbers = (handle, self.n_q_local, self.n_kv_local, self.head_dim, self.block_bytes, geometry.n_kv_heads)
 
     def __del__(self):
         try:
             if self.handle:
                 lib().kv_view_destroy(self.handle)
-                self.handle = None
+                self.handle = self._numbers = None
         except Exception:
             pass
 

@@ -71,7 +71,7 @@ static PyObject* q8_formats;                                        /* dtype of 
 static PyObject *get_device, *raw_stream, *is_capturing, *workspaces;   /* of torch._C; the binding's dict */
 static PyObject *n_is_cuda, *n_dtype, *n_is_contiguous, *n_data_ptr, *n_shape, *n_stride, *n_numel, *n_element_size,
     *n_get_device, *n_cuda_stream, *n_handle, *n_value, *n_block_bytes, *n_n_q_local, *n_n_kv_local, *n_head_dim, *n_scratch,
-    *n_geometry, *n_n_kv_heads, *n_zero, *n_one, *n_two;
+    *n_numbers, *n_zero, *n_one, *n_two;
 
 /* All helpers return 1, or 0 where the Python code is to answer (an exception may be set then: `answer` clears it). */
 
@@ -407,10 +407,26 @@ static int token_rows(PyObject* t, int64_t device, int64_t tokens, int64_t heads
 
 /* What all of the calls below ask of the pool, its view and its table. */
 typedef struct {
-    int64_t device, batch, blocks, row, hq, hkv, d, bb;
+    int64_t device, batch, blocks, row, hq, hkv, d, bb, heads;   /* heads: KV heads of all ranks */
     void *pool, *table, *ctx;
     const kv_view* view;
 } cache_args;
+/* The view's handle and numbers, which it keeps in a tuple for this (one attribute in place of seven: 0.15 us). */
+static int view_of(PyObject* view, cache_args* c)
+{
+    int64_t handle = 0;
+    int64_t* const to[] = {&handle, &c->hq, &c->hkv, &c->d, &c->bb, &c->heads};
+    PyObject* t = PyObject_GetAttr(view, n_numbers);
+    int ok = t && PyTuple_CheckExact(t) && PyTuple_GET_SIZE(t) == 6;
+    for (int i = 0; ok && i < 6; ++i) {
+        PyObject* x = PyTuple_GET_ITEM(t, i);
+        Py_INCREF(x);
+        ok = to_int64(x, to[i]);
+    }
+    Py_XDECREF(t);
+    c->view = (const kv_view*)(uintptr_t)handle;
+    return ok && handle != 0;
+}
 static int places_of(PyObject* view, PyObject* table, PyObject* ctx, cache_args* c)   /* all but the pool */
 {
     int64_t tab[2];
@@ -418,9 +434,7 @@ static int places_of(PyObject* view, PyObject* table, PyObject* ctx, cache_args*
     if (!current(&c->device) || !shaped(ctx, int32_type, c->device, 1, &c->batch, &c->ctx) || c->batch > INT32_MAX) return 0;
     tab[0] = c->batch;
     tab[1] = -1;
-    return shaped(table, int32_type, c->device, 2, tab, &c->table) && ask_int(table, n_stride, n_zero, &c->row) &&
-           int_attr(view, n_n_q_local, &c->hq) && int_attr(view, n_n_kv_local, &c->hkv) && int_attr(view, n_head_dim, &c->d) &&
-           int_attr(view, n_block_bytes, &c->bb) && view_handle(view, &c->view);
+    return shaped(table, int32_type, c->device, 2, tab, &c->table) && ask_int(table, n_stride, n_zero, &c->row) && view_of(view, c);
 }
 static int cache_of(PyObject* pool, PyObject* view, PyObject* table, PyObject* ctx, cache_args* c)
 {
@@ -438,7 +452,7 @@ typedef struct {
 static int q8_of(PyObject* pool, PyObject* scales, PyObject* view, PyObject* table, PyObject* ctx, q8_args* x)
 {
     cache_args* c = &x->c;
-    int64_t on, n, heads, format;
+    int64_t on, n, format;
     if (!places_of(view, table, ctx, c) || !is_tensor(pool)) return 0;
     PyObject* dtype = PyObject_GetAttr(pool, n_dtype);
     PyObject* f = dtype ? PyDict_GetItemWithError(q8_formats, dtype) : NULL;
@@ -449,13 +463,16 @@ static int q8_of(PyObject* pool, PyObject* scales, PyObject* view, PyObject* tab
     const int dense = cont == Py_True;
     Py_XDECREF(cont);
     if (!dense || !ask_int(pool, n_get_device, NULL, &on) || on != c->device || on < 0 || !address(pool, &c->pool) ||
-        !pool_blocks(pool, c->bb / 2, 1, &c->blocks))
+        !ask_int(pool, n_numel, NULL, &n) || c->bb <= 0 || n % (c->bb / 2))   /* (codes of one byte) */
         return 0;
-    PyObject* g = PyObject_GetAttr(view, n_geometry);
-    const int ok = g && int_attr(g, n_n_kv_heads, &heads);
-    Py_XDECREF(g);
-    return ok && dev(scales, float_type, &x->scales) && ask_int(scales, n_get_device, NULL, &on) && on == c->device &&
-           ask_int(scales, n_numel, NULL, &n) && n == c->blocks * 2 * heads;
+    c->blocks = n / (c->bb / 2);
+    if (!is_tensor(scales) || !dtype_is(scales, float_type) || !ask_int(scales, n_get_device, NULL, &on) || on != c->device ||
+        !ask_int(scales, n_numel, NULL, &n) || n != c->blocks * 2 * c->heads)
+        return 0;
+    cont = ask(scales, n_is_contiguous, NULL);
+    const int dense_too = cont == Py_True;
+    Py_XDECREF(cont);
+    return dense_too && address(scales, &x->scales);
 }
 
 /* binding._kept_per_token: [batch][n_kv_local][tokens], or none */
@@ -821,7 +838,7 @@ PyMODINIT_FUNC PyInit__calls(void)
         {&n_get_device, "get_device"}, {&n_cuda_stream, "cuda_stream"}, {&n_handle, "handle"}, {&n_value, "value"},
         {&n_block_bytes, "block_bytes"}, {&n_n_q_local, "n_q_local"}, {&n_n_kv_local, "n_kv_local"},
         {&n_head_dim, "head_dim"}, {&n_scratch, "scratch"},
-        {&n_geometry, "geometry"}, {&n_n_kv_heads, "n_kv_heads"},
+        {&n_numbers, "_numbers"},
     };
     for (size_t i = 0; i < sizeof(names) / sizeof(names[0]); ++i)
         if (!*names[i].to && !(*names[i].to = PyUnicode_InternFromString(names[i].text))) return NULL;
