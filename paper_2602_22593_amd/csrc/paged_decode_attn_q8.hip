@@ -443,16 +443,17 @@ __global__ __launch_bounds__(64 * waves_of(HPW), 2) void decode_q8_kernel(decode
     }
 }
 
-// Row r of a cut pair: the sum of its pieces; zeros where the sequence has no tokens.  D / 4 lanes a slice of the list, the slices then over LDS.
-// THREADS: 1024, and four pieces a slice requested at a time, where pairs are cut into many.
-template <int D, int THREADS>
-__global__ __launch_bounds__(THREADS) void merge_q8_kernel(decode_args a, int rows)
+// A row of a cut pair: the sum of its pieces; zeros where the sequence has no tokens.  D / 4 lanes a slice of the list of pieces, BATCH pieces of each
+// requested at a time, the slices then over LDS.  WAVES: of a row.
+template <int D, int WAVES, int BATCH>
+__global__ __launch_bounds__(64 * WAVES) void merge_q8_kernel(decode_args a, int rows)
 {
-    constexpr int kSlices = THREADS / (D / 4), kBatch = THREADS > 256 ? 4 : 1;
-    __shared__ f32x4 s_o[kSlices][D / 4];
-    __shared__ float2 s_ml[kSlices];
+    constexpr int kLanes = D / 4, kSlices = 64 / kLanes * WAVES, kBatch = BATCH;
+    __shared__ f32x4 s_o[WAVES][kLanes];
+    __shared__ float2 s_ml[WAVES];
+    const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
     const int pair = blockIdx.x, row = blockIdx.y, s = pair / a.head_sets, set = pair - s * a.head_sets;
-    const int slice = threadIdx.x / (D / 4), d4 = threadIdx.x % (D / 4);
+    const int slice = threadIdx.x / kLanes, d4 = lane % kLanes;
     kv_u32x2* const out = reinterpret_cast<kv_u32x2*>(a.out + ((int64_t)s * a.v.n_q_local + set * rows + row) * D + 4 * d4);
     const int n = a.ctx_lens[s], first = a.ends[pair].x, last = a.ends[pair].y;   // (one trip for all)
     if (n <= 0) {
@@ -462,6 +463,11 @@ __global__ __launch_bounds__(THREADS) void merge_q8_kernel(decode_args a, int ro
     if (first == last) return;
     float top = kLowest, sum = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    auto add = [&](float m, float l, const f32x4& o, float to) {
+        const float f = fast_exp2(m - to);
+        sum += l * f;
+        acc += o * f;
+    };
     for (int w0 = first + slice; w0 <= last; w0 += kBatch * kSlices) {
         float2 ml[kBatch];
         f32x4 o[kBatch];
@@ -482,29 +488,33 @@ __global__ __launch_bounds__(THREADS) void merge_q8_kernel(decode_args a, int ro
         acc *= keep;
         sum *= keep;
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-            const float e = w0 + u * kSlices > last ? 0.f : fast_exp2(ml[u].x - to);
-            acc += o[u] * e;
-            sum += ml[u].y * e;
-        }
+        for (int u = 0; u < kBatch; ++u)
+            if (w0 + u * kSlices <= last) add(ml[u].x, ml[u].y, o[u], to);
         top = to;
     }
-    s_o[slice][d4] = acc;
-    if (d4 == 0) s_ml[slice] = make_float2(top, sum);
+    // the wavefront's slices, then the wavefronts
+#pragma unroll
+    for (int d = kLanes; d < 64; d *= 2) {
+        const float m = __shfl_xor(top, d), l = __shfl_xor(sum, d), to = fmaxf(top, m);
+        const f32x4 o = {__shfl_xor(acc[0], d), __shfl_xor(acc[1], d), __shfl_xor(acc[2], d), __shfl_xor(acc[3], d)};
+        const float keep = fast_exp2(top - to);
+        acc *= keep;
+        sum *= keep;
+        add(m, l, o, to);
+        top = to;
+    }
+    if (lane < kLanes) s_o[wave][d4] = acc;
+    if (lane == 0) s_ml[wave] = make_float2(top, sum);
     __syncthreads();
-    if (slice != 0) return;
-#pragma unroll 8
-    for (int i = 0; i < kSlices; ++i) top = fmaxf(top, s_ml[i].x);
+    if (wave != 0) return;
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) top = fmaxf(top, s_ml[i].x);
     sum = 0.f;
     acc = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-    for (int i = 0; i < kSlices; ++i) {
-        const float f = fast_exp2(s_ml[i].x - top);
-        sum += s_ml[i].y * f;
-        acc += s_o[i][d4] * f;
-    }
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) add(s_ml[i].x, s_ml[i].y, s_o[i][d4], top);
     const float inv = 1.f / sum;
-    *out = kv_u32x2{pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)};
+    if (lane < kLanes) *out = kv_u32x2{pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)};
 }
 
 constexpr int kMostWaves = 2048;   // two for each SIMD of 256 compute units
@@ -558,10 +568,11 @@ void launch(const decode_plan& p, const decode_args& a, hipStream_t st)
     hipLaunchKernelGGL(f, dim3((unsigned)p.workgroups), dim3(64 * waves_of(p.hpw)), 0, st, a);
     if (!p.whole) {
         const int pairs = a.batch * p.head_sets, rows = p.hpw * a.group;
-        // pieces a pair: one of 20000 tokens and 8 heads in 256 pieces 19.8 us, 27.4 with 256 threads; 16 of 1000 to 3000 in 16 each 25.5, 23.4
-        const bool many = p.workgroups > 32 * pairs;
-        hipLaunchKernelGGL((many ? merge_q8_kernel<D, 1024> : merge_q8_kernel<D, 256>), dim3((unsigned)pairs, (unsigned)rows),
-                           dim3(many ? 1024 : 256), 0, st, a, rows);
+        // By the pieces of a pair, where all are alike.  One of 20000 tokens, 8 heads, 256 pieces: 16.5 us, with 4 wavefronts a row 27; 9 of 600 to 4700, one
+        // head, 57 pieces: 9.8, as many with 4, with one piece at a time 10.4; 256 around 1024, 2 pieces: 44.4, with four at a time 45.5.
+        const int pieces = p.workgroups / pairs;
+        auto* f = pieces > 32 ? merge_q8_kernel<D, 16, 4> : pieces > 8 ? merge_q8_kernel<D, 4, 4> : merge_q8_kernel<D, 4, 1>;
+        hipLaunchKernelGGL(f, dim3((unsigned)pairs, (unsigned)rows), dim3(pieces > 32 ? 1024 : 256), 0, st, a, rows);
     }
 }
 
