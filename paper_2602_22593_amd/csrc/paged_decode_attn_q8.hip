@@ -76,18 +76,23 @@ struct axis_place {
 };
 // Steps of sequences s0 + 4 lane .. + 3 of a run of 256, their sum over the lanes so far, and that of those with any.
 struct axis_run {
-    int steps[4], sum, some, sum_incl, some_incl;
+    int n[4], steps[4], sum, some, sum_incl, some_incl;
 };
+// The length of sequence s of a run that starts at s0.
+__device__ __forceinline__ int length_in(const axis_run& r, int s, int s0)
+{
+    const int i = (s - s0) & 3;
+    return __builtin_amdgcn_readlane(i == 0 ? r.n[0] : i == 1 ? r.n[1] : i == 2 ? r.n[2] : r.n[3], (s - s0) >> 2);
+}
 __device__ __forceinline__ axis_run run_of(const decode_args& a, int s0, int lane, int step)
 {
     axis_run r;
     r.sum = r.some = 0;
-    int n[4];   // (loads without branches: all at once)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) n[i] = a.ctx_lens[min(s0 + 4 * lane + i, a.batch - 1)];
+    for (int i = 0; i < 4; ++i) r.n[i] = a.ctx_lens[min(s0 + 4 * lane + i, a.batch - 1)];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        r.steps[i] = s0 + 4 * lane + i < a.batch ? steps_of(n[i], step) : 0;
+        r.steps[i] = s0 + 4 * lane + i < a.batch ? steps_of(r.n[i], step) : 0;   // (loads without branches: all at once)
         r.sum += r.steps[i];
         r.some += r.steps[i] > 0;
     }
@@ -175,6 +180,7 @@ __global__ __launch_bounds__(64 * waves_of(HPW), 2) void decode_q8_kernel(decode
     const int G = a.group;
     const int hw = wave % HPW, sub = wave / HPW;
     axis_place at, to;   // where the workgroup's steps start, and where they end
+    int known = -1;      // length of the first sequence
     int whole_id = 0, whole_t = 0, whole_slot = 0;   // a lane's 16 tokens of those that the wavefront takes first, their block and place in it
     if constexpr (WHOLE) {
         at.s = (int)blockIdx.x / a.head_sets;
@@ -183,8 +189,10 @@ __global__ __launch_bounds__(64 * waves_of(HPW), 2) void decode_q8_kernel(decode
         whole_t = (lane >> 1) * kStep + sub * kTile + 16 * (lane & 1);
         int b;
         kv_split_token(v, whole_t, b, whole_slot);
-        if (a.last_block >= 0) whole_id = a.table[(int64_t)at.s * a.table_stride + min(b, a.last_block)];
+        // (no branch around the load: it would be waited for before the length is asked for)
+        whole_id = *(a.last_block >= 0 ? a.table + (int64_t)at.s * a.table_stride + min(b, a.last_block) : a.ctx_lens);
         const int n = a.ctx_lens[at.s];
+        known = n;
         if (n <= 0 || a.last_block < 0) {   // zeros
             for (int i = tid; i < G * D / 8; i += kThreads)
                 reinterpret_cast<kv_u32x4*>(a.out + ((int64_t)at.s * v.n_q_local + at.set * G) * D)[i] = kv_u32x4{0u, 0u, 0u, 0u};
@@ -216,6 +224,7 @@ __global__ __launch_bounds__(64 * waves_of(HPW), 2) void decode_q8_kernel(decode
             at = place_in(a, first, 0, from, start_units, lane);
             to = place_in(a, first, 0, until == total ? 0 : until, start_units, lane);
             if (until == total) to = {a.batch, 0, 0};
+            known = length_in(first, at.s, 0);
         } else {
             at = place_at(a, first, from, start_units, lane, kStep);
             to = place_at(a, first, until, start_units, lane, kStep);
@@ -225,7 +234,8 @@ __global__ __launch_bounds__(64 * waves_of(HPW), 2) void decode_q8_kernel(decode
     const uint32_t row_bytes = (uint32_t)v.token_stride;
     for (; at.s < a.batch; at.step = 0, ++at.set, at.s += at.set == a.head_sets, at.set = at.set == a.head_sets ? 0 : at.set) {
         const int s = at.s, set = at.set, step = at.step;
-        const int n = uniform(a.ctx_lens[s]), steps = steps_of(n, kStep);
+        const int n = known >= 0 ? known : uniform(a.ctx_lens[s]), steps = steps_of(n, kStep);
+        known = -1;
         const bool last_pair = s == to.s && set == to.set;
         const int end = last_pair ? to.step : steps;
         if (step >= end) {   // (a sequence without tokens, a start at a pair's end, an end at its start)
@@ -265,42 +275,57 @@ __global__ __launch_bounds__(64 * waves_of(HPW), 2) void decode_q8_kernel(decode
             float sk[2], sv[2];
         };
         // Tokens past the end are replaced by the last one of its 16 (finite, masked later).
+        // WHOLE: no branch is in the way where there is no tile at t0, and nothing is read: the descriptor is of no bytes.  (Loads behind a branch are
+        // waited for as if they were not there, and with them the tile before.  Where pairs are cut that costs nothing, 2048 wavefronts have
+        // enough under way, and ordinary loads behind a branch are 2 % faster than these.)
         auto request = [&](int t0, tile& x) {
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-                const int t = min(t0 + 16 * half, last16);
-                global_bytes base;
-                int64_t id = 0;
-                int slot = 0;
-                if constexpr (WHOLE) {
-                    const int i = group_of(t);
-                    base = (global_bytes)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((uint32_t)whole_at, i) |
-                                          (uint64_t)(uint32_t)__builtin_amdgcn_readlane((uint32_t)(whole_at >> 32), i) << 32);
-                } else {
-                    int b;
-                    kv_split_token(v, t, b, slot);
-                    id = ids[b];
-                    base = (global_bytes)(reinterpret_cast<uint64_t>(a.pool) +
-                                          (uint64_t)(id * v.block_elems + (int64_t)slot * row_bytes + v.head_off + h * D));
-                }
-                const int most = n - 1 - t;   // the last row that there is
+                const int t = min(t0 + 16 * half, last16), most = n - 1 - t;   // the last row that there is
                 const uint32_t kr = (uint32_t)min(m, most) * row_bytes + 16 * g;
+                uint32_t vr[4];
 #pragma unroll
-                for (int i = 0; i < kLoads; ++i)
-                    x.k[half][i] = __builtin_nontemporal_load((const __attribute__((address_space(1))) kv_u32x4*)(base + kr + 64 * i));
-                const global_bytes vb = base + v.plane_elems;
+                for (int e = 0; e < 4; ++e) vr[e] = (uint32_t)min(4 * g + e, most) * row_bytes + kDims * m;
+                if constexpr (WHOLE) {
+                    const int i = group_of(t), bytes = t0 < t_end ? 0x7ffffff0 : 0;
+                    const uint64_t at = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((uint32_t)whole_at, i) |
+                                        (uint64_t)(uint32_t)__builtin_amdgcn_readlane((uint32_t)(whole_at >> 32), i) << 32;
+                    const __amdgpu_buffer_rsrc_t kb = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<char*>(at), 0, bytes, 0x00020000);
+                    const __amdgpu_buffer_rsrc_t vb =
+                        __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<char*>(at + (uint64_t)v.plane_elems), 0, bytes, 0x00020000);
+                    constexpr int kPast = 2;   // (non-temporal)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const uint32_t vr = (uint32_t)min(4 * g + e, most) * row_bytes + kDims * m;
-                    if constexpr (kWords == 2) {
-                        const kv_u32x2 y = __builtin_nontemporal_load((const __attribute__((address_space(1))) kv_u32x2*)(vb + vr));
-                        x.v[4 * half + e][0] = y[0];
-                        x.v[4 * half + e][1] = y[1];
-                    } else {
-                        x.v[4 * half + e][0] = __builtin_nontemporal_load((const __attribute__((address_space(1))) uint32_t*)(vb + vr));
+                    for (int i = 0; i < kLoads; ++i) x.k[half][i] = __builtin_amdgcn_raw_buffer_load_b128(kb, kr + 64 * i, 0, kPast);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if constexpr (kWords == 2) {
+                            const kv_u32x2 y = __builtin_bit_cast(kv_u32x2, __builtin_amdgcn_raw_buffer_load_b64(vb, vr[e], 0, kPast));
+                            x.v[4 * half + e][0] = y[0];
+                            x.v[4 * half + e][1] = y[1];
+                        } else {
+                            x.v[4 * half + e][0] = __builtin_amdgcn_raw_buffer_load_b32(vb, vr[e], 0, kPast);
+                        }
                     }
-                }
-                if constexpr (!WHOLE) {
+                } else {
+                    int b, slot;
+                    kv_split_token(v, t, b, slot);
+                    const int64_t id = ids[b];
+                    const global_bytes kb = (global_bytes)(reinterpret_cast<uint64_t>(a.pool) +
+                                                           (uint64_t)(id * v.block_elems + (int64_t)slot * row_bytes + v.head_off + h * D));
+                    const global_bytes vb = kb + v.plane_elems;
+#pragma unroll
+                    for (int i = 0; i < kLoads; ++i)
+                        x.k[half][i] = __builtin_nontemporal_load((const __attribute__((address_space(1))) kv_u32x4*)(kb + kr + 64 * i));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if constexpr (kWords == 2) {
+                            const kv_u32x2 y = __builtin_nontemporal_load((const __attribute__((address_space(1))) kv_u32x2*)(vb + vr[e]));
+                            x.v[4 * half + e][0] = y[0];
+                            x.v[4 * half + e][1] = y[1];
+                        } else {
+                            x.v[4 * half + e][0] = __builtin_nontemporal_load((const __attribute__((address_space(1))) uint32_t*)(vb + vr[e]));
+                        }
+                    }
                     const const_floats sc = (const_floats)(a.scales + q8_scale_at(a.x, id, slot, h));
                     x.sk[half] = sc[0];
                     x.sv[half] = sc[a.x.block_scales / 2];
@@ -369,27 +394,41 @@ __global__ __launch_bounds__(64 * waves_of(HPW), 2) void decode_q8_kernel(decode
                 }
             }
         };
-        {
+        if (t_first < t_end) {
             int t = t_first;
             tile x, y;
-            if (t < t_end) request(t, x);
+            request(t, x);
             if constexpr (WHOLE) {
-                if (whole_t <= last16) {
-                    const float* sc = a.scales + q8_scale_at(a.x, whole_id, whole_slot, h);
-                    whole_k = sc[0];
-                    whole_v = sc[a.x.block_scales / 2];
+                // scales (a lane without tokens takes any)
+                const float* sc = whole_t <= last16 ? a.scales + q8_scale_at(a.x, whole_id, whole_slot, h) : a.scales;
+                whole_k = sc[0];
+                whole_v = sc[a.x.block_scales / 2];
+                __builtin_amdgcn_sched_barrier(0);   // (in this order: the loop waits for the last of x on the way into it as in it)
+                request(t + kStep, y);
+                asm volatile("" : "+v"(whole_k), "+v"(whole_v));   // (waited for here and not in the loop)
+                // (one way out of the loop: with a second one between the tiles, loads on the way to it are waited for as if they were not there)
+                for (; t + kStep < t_end; t += 2 * kStep) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    take(t, x);
+                    request(t + 2 * kStep, x);
+                    __builtin_amdgcn_sched_barrier(0);
+                    take(t + kStep, y);
+                    request(t + 3 * kStep, y);
                 }
-            }
-            while (t < t_end) {
-                if (t + kStep < t_end) request(t + kStep, y);
-                __builtin_amdgcn_sched_barrier(0);   // (all of the next tile is asked for before anything waits for this one)
-                take(t, x);
-                t += kStep;
-                if (t >= t_end) break;
-                if (t + kStep < t_end) request(t + kStep, x);
-                __builtin_amdgcn_sched_barrier(0);
-                take(t, y);
-                t += kStep;
+                if (t < t_end) take(t, x);
+            } else {
+                for (;;) {
+                    if (t + kStep < t_end) request(t + kStep, y);
+                    __builtin_amdgcn_sched_barrier(0);   // (all of the next tile is asked for before anything waits for this one)
+                    take(t, x);
+                    t += kStep;
+                    if (t >= t_end) break;
+                    if (t + kStep < t_end) request(t + kStep, x);
+                    __builtin_amdgcn_sched_barrier(0);
+                    take(t, y);
+                    t += kStep;
+                    if (t >= t_end) break;
+                }
             }
         }
         l += __shfl_xor(l, 16);
