@@ -3,8 +3,8 @@
 //   out = sum_t softmax_t(c q . sK[t] k_t) sV[t] v_t,  k_t and v_t the codes of token t, sK and sV the scales of its group
 //
 // Bound by reading codes and scales: 2 d + 8 / B_base bytes a token and head.  Measured: 64 sequences around 2048 tokens, 8 heads, 56 us
-// (306 MB read at 5.8 TB/s, 6.3 between 64 and 192 sequences, and 4.6 us of second launch; the same cache in bf16 97); 256 around 1024,
-// one head, 44 (70); 8 long and short ones, 2 heads, 33 (53).  Without its arithmetic the kernel takes 2 to 8 % less.
+// (308 MB read at 5.8 TB/s, 6.3 between 64 and 192 sequences, and 4.6 us of second launch; the same cache in bf16 97); 256 around 1024,
+// one head, 44 (70); 8 long and short ones, 2 heads, 32 (53).  Without its arithmetic the kernel takes 2 to 8 % less.
 //
 // A wavefront takes 32 tokens of a KV head at a time (a tile), its G <= 16 query rows as the 16 columns of the products, and needs nothing
 // of LDS or of other wavefronts until it is through.  Lane l = (m = l % 16, g = l / 16), products of 16 x 16 x 32 in bf16:
@@ -559,7 +559,7 @@ __global__ __launch_bounds__(64 * WAVES) void merge_q8_kernel(decode_args a, int
 constexpr int kMostWaves = 2048;   // two for each SIMD of 256 compute units
 constexpr int kUnitShift = 3, kStartUnits = 8;   // a start counts as much as a step
 // Up to which bound of the lengths a workgroup takes a whole pair: cutting costs a second launch, 4 us and more, and pieces to write and read;
-// not cutting leaves a workgroup 1 us for each 128 tokens, and from 256 pairs on compute units with two.  (Lengths from 0.3 of the bound to it, us
+// not cutting leaves a workgroup 0.9 us for each 128 tokens, and from 256 pairs on compute units with two.  (Lengths from 0.3 of the bound to it, us
 // whole and cut: 24 pairs, 500: 8.0, 8.7; 700: 9.9, 8.9; 192 pairs, 1000: 16.2, 18.6; 256 pairs, 1300: 17.3, 19.9; 384 pairs, 500: 14.6, 16.4;
 // 700: 19.6, 19.2; 1024 pairs, 500: 27.4, 27.9; 1440 pairs, 300: 25.9, 27.5; 500: 36.5, 34.3.)
 int whole_bound(int64_t pairs) { return pairs >= 96 && pairs <= 256 ? 1024 : pairs <= 1024 ? 512 : 256; }
