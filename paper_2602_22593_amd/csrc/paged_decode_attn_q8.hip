@@ -578,8 +578,8 @@ decode_plan plan_of(const kv_view* view, int batch, int max_ctx_len)
     const int hl = view->n_kv_local;
     p.hpw = hl % 8 == 0 ? 8 : hl % 4 == 0 ? 4 : hl % 2 == 0 ? 2 : 1;
     // (the room asked for does not depend on it: what serves large calls is to serve all smaller ones)
-    p.whole = max_ctx_len <= whole_bound((int64_t)batch * hl);
-    const bool never_cut = max_ctx_len <= kLeastCut;
+    const bool never_cut = max_ctx_len <= kLeastCut;   // (and there is no room for pieces)
+    p.whole = never_cut || max_ctx_len <= whole_bound((int64_t)batch * hl);
     p.head_sets = hl / p.hpw;
     const int step = step_tokens(p.hpw);
     const int64_t pairs = (int64_t)batch * p.head_sets, steps = pairs * (((int64_t)max_ctx_len + step - 1) / step);

@@ -141,6 +141,7 @@ def test_workspaces_for_larger_bounds_serve_smaller_calls(geom, p):
              for b in (0, 1, 3, 16, 64, 200, 1000) for n in (0, 32, 256, 512, 513, 1000, 8192, 8193, 131072)}
     for x, need in sizes.items():
         assert all(given >= need for y, given in sizes.items() if all(j >= i for i, j in zip(x, y))), x
+        assert (need == 0) == (x[0] == 0 or x[1] <= 256)   # (no pair is cut up to there, whatever the batch)
 
 
 def test_names_in_the_binding_match_the_header():
