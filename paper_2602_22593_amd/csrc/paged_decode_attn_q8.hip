@@ -559,10 +559,10 @@ __global__ __launch_bounds__(64 * WAVES) void merge_q8_kernel(decode_args a, int
 constexpr int kMostWaves = 2048;   // two for each SIMD of 256 compute units
 constexpr int kUnitShift = 3, kStartUnits = 8;   // a start counts as much as a step
 // Up to which bound of the lengths a workgroup takes a whole pair: cutting costs a second launch, 4 us and more, and pieces to write and read;
-// not cutting leaves a workgroup 0.9 us for each 128 tokens, and from 256 pairs on compute units with two.  (Lengths from 0.3 of the bound to it, us
-// whole and cut: 24 pairs, 500: 8.0, 8.7; 700: 9.9, 8.9; 192 pairs, 1000: 16.2, 18.6; 256 pairs, 1300: 17.3, 19.9; 384 pairs, 500: 14.6, 16.4;
-// 700: 19.6, 19.2; 1024 pairs, 500: 27.4, 27.9; 1440 pairs, 300: 25.9, 27.5; 500: 36.5, 34.3.)
-int whole_bound(int64_t pairs) { return pairs >= 96 && pairs <= 256 ? 1024 : pairs <= 1024 ? 512 : 256; }
+// not cutting leaves a workgroup 0.8 us for each 128 tokens, and from 256 pairs on compute units with two.  (Lengths from 0.3 of the bound to it, us
+// whole and cut: 16 pairs, 700: 7.4, 9.8; 1000: 10.2, 9.9; 96 pairs, 1000: 11.3, 14.3; 192 pairs, 1000: 15.7, 18.9; 1700: 23.7, 21.4; 384 pairs, 500:
+// 14.4, 16.0; 700: 19.2, 19.2; 1000: 25.9, 23.9; 768 pairs, 500: 21.2, 24.5; 700: 27.8, 27.4; 1520 pairs, 300: 25.4, 27.3; 500: 36.6, 34.6.)
+int whole_bound(int64_t pairs) { return pairs >= 96 && pairs <= 256 ? 1024 : pairs <= 512 ? 704 : pairs <= 1024 ? 512 : 256; }
 constexpr int kLeastCut = 256;   // no pair is cut up to this bound
 
 // How a call is cut: the same for the workspace and the launch.

@@ -284,6 +284,8 @@ def test_decode_of_many_sequences():
     (G8B, (DP, 1, 0), [5000, 2600], False),                          # long pieces
     (G8B, (DP, 1, 0), [500, 1, 0] + [37] * 177, True),               # short, and cut since they are many
     (G8B, (DP, 1, 0), [1000, 0, 513, 129] + [50] * 20, True),        # long, and not cut since they fill the chip once
+    (G8B, (DP, 1, 0), [704, 640, 641, 0, 639, 1], True),             # the last bound up to which few are not cut
+    (G8B, (TP, 8, 5), [705, 3], False),
     ((32, 16, 64, 16), (DP, 1, 0), [1800, 40, 513], False),          # two sets of eight heads
     ((16, 4, 64, 16), (DP, 1, 0), [2500, 31], True),                 # four
     ((7, 1, 128, 16), (DP, 1, 0), [40000], True),                    # one pair in hundreds of pieces
