@@ -71,7 +71,7 @@ static PyObject* q8_formats;                                        /* dtype of 
 static PyObject *get_device, *raw_stream, *is_capturing, *workspaces;   /* of torch._C; the binding's dict */
 static PyObject *n_is_cuda, *n_dtype, *n_is_contiguous, *n_data_ptr, *n_shape, *n_stride, *n_numel, *n_element_size,
     *n_get_device, *n_cuda_stream, *n_handle, *n_value, *n_block_bytes, *n_n_q_local, *n_n_kv_local, *n_head_dim, *n_scratch,
-    *n_numbers, *n_zero, *n_one, *n_two;
+    *n_numbers, *n_zero, *n_one;
 
 /* All helpers return 1, or 0 where the Python code is to answer (an exception may be set then: `answer` clears it). */
 
@@ -389,19 +389,24 @@ static int shaped(PyObject* t, PyObject* dtype, int64_t device, int n, int64_t* 
     return yes && address(t, out);
 }
 
-/* binding._token_rows: [tokens][heads][d], tokens may lie apart */
-static int token_rows(PyObject* t, int64_t device, int64_t tokens, int64_t heads, int64_t d, void** out, int64_t* row)
+/* binding._token_rows: [tokens][heads][d], tokens may lie apart; tokens of -1 are found out */
+static int token_rows(PyObject* t, int64_t device, int64_t* tokens, int64_t heads, int64_t d, void** out, int64_t* row)
 {
-    int64_t found[3], s, on;
-    if (!sizes(t, 3, found) || found[0] != tokens || found[1] != heads || found[2] != d ||
+    int64_t found[3], stride[3], on;
+    if (!sizes(t, 3, found) || (*tokens >= 0 && found[0] != *tokens) || found[1] != heads || found[2] != d ||
         !dtype_is(t, bf16_types) || !ask_int(t, n_get_device, NULL, &on) || on != device || on < 0)
         return 0;
-    if (!ask_int(t, n_stride, n_two, &s) || s != 1 || (heads > 1 && !(ask_int(t, n_stride, n_one, &s) && s == d))) return 0;
-    if (tokens > 1) {
-        if (!ask_int(t, n_stride, n_zero, row)) return 0;
-    } else {
-        *row = heads * d;
+    *tokens = found[0];
+    PyObject* all = ask(t, n_stride, NULL);   /* (all three in one call) */
+    int ok = all && PyTuple_Check(all) && PyTuple_GET_SIZE(all) == 3;
+    for (int i = 0; ok && i < 3; ++i) {
+        PyObject* x = PyTuple_GET_ITEM(all, i);
+        Py_INCREF(x);
+        ok = to_int64(x, stride + i);
     }
+    Py_XDECREF(all);
+    if (!ok || stride[2] != 1 || (heads > 1 && stride[1] != d)) return 0;
+    *row = *tokens > 1 ? stride[0] : heads * d;
     return address(t, out);
 }
 
@@ -517,13 +522,13 @@ static int axes_of(PyObject* list, int n_axes, int64_t half, int32_t axes[kMostP
 static PyObject* call_rope(PyObject* self, PyObject* const* a, Py_ssize_t nargs)
 {
     ARGS(16)
-    int64_t q[3], q_row, k_row, v_row, half = -1, off, out[3], per, w_n, pairs, stream;
+    int64_t q[1] = {-1}, q_row, k_row, v_row, half = -1, off, out[3], per, w_n, pairs, stream;
     void *pq, *pk, *pv, *pout, *ppos, *pfreq, *poff = NULL, *pper, *pw;
     int32_t axes[kMostPairs];
     cache_args c;
     int rc = 0, n_axes = 1;
-    int ok = cache_of(a[0], a[1], a[7], a[8], &c) && sizes(a[2], 3, q) && token_rows(a[2], c.device, q[0], c.hq, c.d, &pq, &q_row) &&
-             token_rows(a[3], c.device, q[0], c.hkv, c.d, &pk, &k_row) && token_rows(a[4], c.device, q[0], c.hkv, c.d, &pv, &v_row);
+    int ok = cache_of(a[0], a[1], a[7], a[8], &c) && token_rows(a[2], c.device, q, c.hq, c.d, &pq, &q_row) &&
+             token_rows(a[3], c.device, q, c.hkv, c.d, &pk, &k_row) && token_rows(a[4], c.device, q, c.hkv, c.d, &pv, &v_row);
     if (ok) {
         out[0] = q[0];
         out[1] = c.hq;
@@ -634,20 +639,20 @@ static PyObject* call_weights(PyObject* self, PyObject* const* a, Py_ssize_t nar
 static PyObject* call_rope_q8(PyObject* self, PyObject* const* a, Py_ssize_t nargs)
 {
     ARGS(15)
-    int64_t k[3], q_row = 0, k_row, v_row, half = 0, off, out[3], pairs, stream;
+    int64_t k[1] = {-1}, q_row = 0, k_row, v_row, half = 0, off, out[3], pairs, stream;
     void *pq = NULL, *pk, *pv, *pout = NULL, *ppos = NULL, *pfreq = NULL, *poff = NULL;
     int32_t axes[kMostPairs];
     q8_args x;
     const cache_args* c = &x.c;
     int rc = 0, n_axes = 1;
-    int ok = q8_of(a[0], a[1], a[2], a[8], a[9], &x) && sizes(a[4], 3, k) && token_rows(a[4], c->device, k[0], c->hkv, c->d, &pk, &k_row) &&
-             token_rows(a[5], c->device, k[0], c->hkv, c->d, &pv, &v_row) && (a[3] == Py_None) == (a[13] == Py_None) &&
+    int ok = q8_of(a[0], a[1], a[2], a[8], a[9], &x) && token_rows(a[4], c->device, k, c->hkv, c->d, &pk, &k_row) &&
+             token_rows(a[5], c->device, k, c->hkv, c->d, &pv, &v_row) && (a[3] == Py_None) == (a[13] == Py_None) &&
              (a[7] == Py_None || a[6] != Py_None);
     if (ok && a[3] != Py_None) {
         out[0] = k[0];
         out[1] = c->hq;
         out[2] = c->d;
-        ok = token_rows(a[3], c->device, k[0], c->hq, c->d, &pq, &q_row) && shaped(a[13], bf16_types, c->device, 3, out, &pout);
+        ok = token_rows(a[3], c->device, k, c->hq, c->d, &pq, &q_row) && shaped(a[13], bf16_types, c->device, 3, out, &pout);
     }
     if (ok && a[6] != Py_None) ok = positions_of(a[6], c->device, k[0], &ppos, &n_axes);
     if (ok && a[7] != Py_None) {
@@ -842,6 +847,6 @@ PyMODINIT_FUNC PyInit__calls(void)
     };
     for (size_t i = 0; i < sizeof(names) / sizeof(names[0]); ++i)
         if (!*names[i].to && !(*names[i].to = PyUnicode_InternFromString(names[i].text))) return NULL;
-    if (!(n_zero = PyLong_FromLong(0)) || !(n_one = PyLong_FromLong(1)) || !(n_two = PyLong_FromLong(2))) return NULL;
+    if (!(n_zero = PyLong_FromLong(0)) || !(n_one = PyLong_FromLong(1))) return NULL;
     return PyModule_Create(&module);
 }
