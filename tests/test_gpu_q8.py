@@ -286,6 +286,10 @@ def test_decode_of_many_sequences():
     (G8B, (DP, 1, 0), [1000, 0, 513, 129] + [50] * 20, True),        # long, and not cut since they fill the chip once
     (G8B, (DP, 1, 0), [704, 640, 641, 0, 639, 1], True),             # the last bound up to which few are not cut
     (G8B, (TP, 8, 5), [705, 3], False),
+    ((128, 8, 64, 16), (DP, 1, 0), [1900, 0, 33], True),             # sixteen query heads on each of eight, of four, of two
+    ((64, 4, 128, 32), (DP, 1, 0), [1300, 97], False),
+    ((32, 2, 128, 64), (DP, 1, 0), [2100, 1], True),
+    ((32, 2, 128, 64), (DP, 1, 0), [600, 65, 0, 64], False),
     ((32, 16, 64, 16), (DP, 1, 0), [1800, 40, 513], False),          # two sets of eight heads
     ((16, 4, 64, 16), (DP, 1, 0), [2500, 31], True),                 # four
     ((7, 1, 128, 16), (DP, 1, 0), [40000], True),                    # one pair in hundreds of pieces
