@@ -91,4 +91,10 @@ __device__ __forceinline__ float scale_for(uint32_t top)
     return __uint_as_float((uint32_t)(max(s, kLeastExponent) + 127) << 23);
 }
 
+// K's scale as attention takes it: NaN for an infinity.  (A score times an infinity may be -inf, whose weight is 0: the group would be left out.)
+__device__ __forceinline__ float key_scale(float s)
+{
+    return (__float_as_uint(s) & 0x7fffffffu) == 0x7f800000u ? __uint_as_float(kNaNBits) : s;
+}
+
 }  // namespace kvq8

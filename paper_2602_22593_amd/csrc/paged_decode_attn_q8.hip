@@ -351,7 +351,7 @@ __global__ __launch_bounds__(64 * waves_of(HPW), 2) void decode_q8_kernel(decode
                     const kv_u32x4 ka = {two_bf16<FMT, false>(w0), two_bf16<FMT, true>(w0), two_bf16<FMT, false>(w1), two_bf16<FMT, true>(w1)};
                     sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(ka), qb[i], sc, 0, 0, 0);
                 }
-                const float c = x.sk[half] * a.scale_log2e;
+                const float c = (WHOLE ? x.sk[half] : key_scale(x.sk[half])) * a.scale_log2e;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) u[4 * half + i] = sc[i] * c;
             }
@@ -406,6 +406,7 @@ __global__ __launch_bounds__(64 * waves_of(HPW), 2) void decode_q8_kernel(decode
                 __builtin_amdgcn_sched_barrier(0);   // (in this order: the loop waits for the last of x on the way into it as in it)
                 request(t + kStep, y);
                 asm volatile("" : "+v"(whole_k), "+v"(whole_v));   // (waited for here and not in the loop)
+                whole_k = key_scale(whole_k);
                 // (one way out of the loop: with a second one between the tiles, loads on the way to it are waited for as if they were not there)
                 for (; t + kStep < t_end; t += 2 * kStep) {
                     __builtin_amdgcn_sched_barrier(0);
