@@ -113,8 +113,9 @@ __global__ __launch_bounds__(kThreads, kPerCu) void prefill_q8_kernel(prefill_ar
         g_hi = (uint32_t)(at >> 32) | (g == last_group ? kLast : 0u);
     };
     auto list_places = [&]() __attribute__((always_inline)) {
-        // Where V's scale is no number K's stands for it, so that rows that do not see the group (whose weights are 0) keep theirs.
-        if ((g_v & 0x7f800000u) == 0x7f800000u) {
+        // Where either scale is not finite K's is NaN: not an infinity, which may make all of a token's scores -inf and so leave the group
+        // out; and in V's place, so that rows that do not see the group (whose weights are 0) keep their results.
+        if ((g_k & 0x7f800000u) == 0x7f800000u || (g_v & 0x7f800000u) == 0x7f800000u) {
             g_k = kNaNBits;
             g_v = 0u;
         }

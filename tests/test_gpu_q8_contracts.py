@@ -8,7 +8,7 @@ from q8_refs import E4M3, INT8
 
 from helpers import bf16_bits_to_f64
 from test_gpu_operators import G8B, host
-from test_gpu_q8 import decode, q_for
+from test_gpu_q8 import decode, prefill, q_for
 
 pytestmark = pytest.mark.gpu
 FORMATS = [E4M3, INT8]
@@ -55,4 +55,26 @@ def test_decode_with_an_infinite_scale(fmt, sign, plane, triple, ctx, at):
         want, tol = q8.attention(x, causal=False)
     hit = np.zeros(out.shape, bool)
     hit[0, G * head:] = True
+    assert np.isnan(out[hit]).all() and (np.abs(out - want) <= tol)[~hit].all()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("plane", [0, 1])
+@pytest.mark.parametrize("ctx,q_lens,back", [
+    ([200, 100], [200, 100], 40),       # not cut
+    ([193, 100], [193, 100], 1),        # a last group of one token
+    ([1500, 200], [60, 200], 40),       # cut
+    ([1505, 200], [60, 200], 1),
+])
+def test_prefill_rows_see_infinite_scales_of_their_groups_only(fmt, sign, plane, ctx, q_lens, back):
+    """Rows before the group keep their results, those that see a token of it are NaN."""
+    x = q8.case(G8B, (TP, 8, 0), ctx, q_lens, fmt)
+    x.c.q &= np.uint16(0x7fff)
+    want, tol = q8.attention(x, causal=True)
+    at = ctx[0] - back
+    make_infinite(x, 0, at, plane, 0, sign)
+    out = bf16_bits_to_f64(host(prefill(x)))
+    hit = np.zeros(len(out), bool)
+    hit[:q_lens[0]] = ctx[0] - q_lens[0] + np.arange(q_lens[0]) >= at // 16 * 16
     assert np.isnan(out[hit]).all() and (np.abs(out - want) <= tol)[~hit].all()
