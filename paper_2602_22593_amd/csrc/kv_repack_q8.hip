@@ -140,10 +140,10 @@ extern "C" int kv_repack_q8(void* kv_pool, float* scales, int64_t n_pool_blocks,
     a.run_shift = -1;
     for (int s = 0; s < 31; ++s)
         if ((1 << s) == a.run_chunks) a.run_shift = s;
-    // about kPayload bytes per workgroup, whole groups
+    // about kPayload bytes per workgroup, whole groups: one at least, however long a token's run is
     const int B = g.base_block_size;
     int tokens = kPayload / (2 * a.run_chunks * 16);
-    tokens = (tokens + B - 1) / B * B;
+    tokens = tokens < 1 ? B : (tokens + B - 1) / B * B;
     a.tokens_per_wg = tokens;
     const int64_t gx = ((int64_t)max_tokens + tokens - 1) / tokens;
     if (gx > 0x7fffffff || n_seqs > 65535) return KV_ERR_INVALID_ARG;

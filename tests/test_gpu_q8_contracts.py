@@ -1,4 +1,5 @@
-"""What the header promises of the operators on a cache held in 8 bits, where a call is easily answered wrongly: scales that are infinite."""
+"""What the header promises of the operators on a cache held in 8 bits, where a call is easily answered wrongly: scales that are
+infinite, moves of many heads."""
 import numpy as np
 import pytest
 
@@ -8,7 +9,7 @@ from q8_refs import E4M3, INT8
 
 from helpers import bf16_bits_to_f64
 from test_gpu_operators import G8B, host
-from test_gpu_q8 import decode, prefill, q_for
+from test_gpu_q8 import decode, prefill, q_for, test_repack as check_repack
 
 pytestmark = pytest.mark.gpu
 FORMATS = [E4M3, INT8]
@@ -78,3 +79,19 @@ def test_prefill_rows_see_infinite_scales_of_their_groups_only(fmt, sign, plane,
     hit = np.zeros(len(out), bool)
     hit[:q_lens[0]] = ctx[0] - q_lens[0] + np.arange(q_lens[0]) >= at // 16 * 16
     assert np.isnan(out[hit]).all() and (np.abs(out - want) <= tol)[~hit].all()
+
+
+# ---- kv_repack_q8 ------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("geom,src,dst,ctx", [
+    ((40, 40, 128, 16), (DP, 1, 0), (DP, 1, 0), [33, 5, 0, 100]),      # runs of 5120 elements, no power of two
+    ((80, 80, 128, 16), (DP, 1, 0), (TP, 2, 1), [17, 64]),
+    ((80, 80, 128, 16), (TP, 2, 1), (DP, 1, 0), [17, 64]),
+    ((64, 64, 128, 16), (TP, 2, 0), (DP, 2, 0), [40, 1]),              # 4096: one token's run is the whole payload
+    ((144, 144, 64, 16), (DP, 1, 0), (DP, 1, 0), [50, 16]),            # more scales of a group than a workgroup has threads
+    ((136, 136, 64, 48), (DP, 1, 0), (TP, 4, 3), [100, 47, 0]),
+    ((288, 288, 64, 32), (TP, 2, 0), (DP, 1, 0), [33]),
+])
+def test_repack_of_many_heads(fmt, geom, src, dst, ctx):
+    check_repack(fmt, geom, src, dst, ctx)
