@@ -2,9 +2,11 @@
 // same in every layout and has one scale, so nothing is rounded.
 //
 // Bound by reading and writing what moves.  As in kv_repack, a token's rows for a run of consecutive heads are contiguous in every
-// arrangement: the unit is a 16-byte piece of such a run, consecutive lanes on consecutive pieces.  A workgroup moves about 8 KiB, all of
-// them requested before the first is stored: with 64 KiB and four requests a lane at a time, moving 128 sequences around 4096 tokens from
-// DP to TP4 took 114 us, with 16 KiB 106, now 104 (4.9 TB/s; runs of 256 bytes are read), and one sequence 8.2 us, now 5.5 (its launch).
+// arrangement: the unit is a 16-byte piece of such a run, consecutive lanes on consecutive pieces.  A workgroup moves 8 KiB, or one group of
+// B_base tokens where that is more (from 3 common heads of 128 and B_base = 16 on), two pieces a lane or 8 KiB at a time: they are requested
+// before the first of them is stored.  With 64 KiB and four pieces at a time, moving 128 sequences around 4096 tokens from DP to TP4 (2 common
+// heads: 8 KiB) took 114 us, with 16 KiB 106, now 104 (4.9 TB/s; runs of 256 bytes are read), and one sequence 8.2 us, now 5.6 (its launch).
+// Larger groups lose nothing by their rounds: 4 and 8 common heads, 32 KiB a group, 5.0 TB/s, and B_base = 64, 128 KiB, 5.1.
 #include "kv_q8.h"
 
 using namespace kvq8;
@@ -18,7 +20,6 @@ constexpr int kPayload = 8 * 1024;
 struct repack_args {
     uint8_t* pool;
     float* scales;
-    int64_t n_pool_blocks;
     const int32_t *src_table, *dst_table;
     int64_t src_stride, dst_stride;
     const int32_t* n_tokens;
@@ -123,7 +124,6 @@ extern "C" int kv_repack_q8(void* kv_pool, float* scales, int64_t n_pool_blocks,
     repack_args a = {};
     a.pool = (uint8_t*)kv_pool;
     a.scales = scales;
-    a.n_pool_blocks = n_pool_blocks;
     a.src_table = src_block_table;
     a.dst_table = dst_block_table;
     a.src_stride = src_stride;
