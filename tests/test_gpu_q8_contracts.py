@@ -1,15 +1,19 @@
 """What the header promises of the operators on a cache held in 8 bits, where a call is easily answered wrongly: scales that are
-infinite, moves of many heads."""
+infinite, moves of many heads, the largest groups and batches; results that repeat themselves."""
 import numpy as np
 import pytest
+import torch
 
 import q8_refs as q8
 from operator_refs import DP, TP, place
+from paper_2602_22593_amd import binding as kv
 from q8_refs import E4M3, INT8
 
 from helpers import bf16_bits_to_f64
-from test_gpu_operators import G8B, host
-from test_gpu_q8 import decode, prefill, q_for, test_repack as check_repack
+from test_gpu_operators import DEV, G8B, G70B, dev, host, view_of, within
+from test_gpu_q8 import decode, pool_of, prefill, q_for
+from test_gpu_q8 import test_append_one_token as check_append_one, test_append_several_tokens as check_append_several
+from test_gpu_q8 import test_repack as check_repack
 
 pytestmark = pytest.mark.gpu
 FORMATS = [E4M3, INT8]
@@ -95,3 +99,78 @@ def test_prefill_rows_see_infinite_scales_of_their_groups_only(fmt, sign, plane,
 ])
 def test_repack_of_many_heads(fmt, geom, src, dst, ctx):
     check_repack(fmt, geom, src, dst, ctx)
+
+
+# ---- kv_rope_append_q8 -------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_append_of_the_longest_groups_with_all_dims_turned(fmt):
+    """Sines of 128 tokens and 64 pairs: all of the 64 KiB that a workgroup may have of LDS by default."""
+    check_append_several(fmt, (4, 2, 128, 128), (DP, 1, 0), [300, 128, 129], [290, 1, 128], 1, False, 128)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_append_one_token_of_many_sequences(fmt):
+    """From 512 on a sequence has one workgroup, which takes all of its rows."""
+    check_append_one(fmt, G8B, (DP, 1, 0), [33 + i % 40 for i in range(530)], [1] * 530, 1, False, 128)
+
+
+def test_append_several_tokens_of_thousands_of_sequences():
+    """A group's sequence is found among 4200 in three steps."""
+    check_append_several(E4M3, (2, 1, 64, 16), (DP, 1, 0), [3 + i % 31 for i in range(4200)], [i % 4 for i in range(4200)], 1, False, 64)
+
+
+@pytest.mark.parametrize("one", [True, False])
+def test_append_turns_queries_in_place(one):
+    """The queries' own array as output, tokens that lie together: the bits that another array gets."""
+    q_lens = [1, 1, 1] if one else [5, 40, 0]
+    x = q8.case(G8B, (TP, 2, 1), [40, 90, 7], q_lens, E4M3)
+    total, view = sum(q_lens), view_of(x.c)
+    rows = dev(q8.normal_rows(total, 16, 4, 128, 131))
+    q, k, v = (part.contiguous() for part in (rows[:, :16], rows[:, 16:20], rows[:, 20:]))
+    positions, freq = dev(np.arange(total, dtype=np.int32) * 77), dev((1e4 ** (-np.arange(64) / 64)).astype(np.float32))
+    off = None if one else dev(x.c.q_off.astype(np.int32))
+    got = []
+    for out in (torch.empty_like(q), q):
+        pool, scales = pool_of(x)
+        assert kv.kv_rope_append_q8(pool, scales, view, q, k, v, positions, freq, dev(x.c.table), dev(x.c.ctx), off, out=out) is out
+        got.append(host(out))
+    assert np.array_equal(got[0], got[1])
+
+
+# ---- paged_prefill_attn_q8 ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("triple,ctx,q_lens", [
+    ((DP, 1, 0), [300, 64], [20, 64]),                          # one workgroup a tile
+    ((TP, 8, 3), [1200, 16, 130], [16, 16, 7]),                 # cut
+    ((TP, 4, 0), [700] * 9, [200] * 9),                         # in the order of their lengths
+])
+def test_prefill_leaves_rows_behind_the_last_sequence(fmt, triple, ctx, q_lens):
+    x = q8.case(G8B, triple, ctx, q_lens, fmt)
+    c, pad = x.c, 300
+    pool, scales = pool_of(x)
+    q = torch.cat([dev(c.q), torch.full((pad,) + c.q.shape[1:], float("nan"), dtype=torch.bfloat16, device=DEV)])
+    out = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device=DEV)
+    kv.paged_prefill_attn_q8(q, pool, scales, dev(c.table), dev(c.ctx), dev(c.q_off.astype(np.int32)), view_of(c), max(ctx), max(q_lens), out=out)
+    assert (out[-pad:] == 7.0).all()
+    within(host(out[:-pad]), *q8.attention(x, causal=True))
+
+
+# ---- every call again --------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("geom,triple,ctx,q_lens", [
+    (G8B, (DP, 1, 0), [300, 17, 0, 64], [9, 17, 0, 1]),             # neither is cut
+    (G8B, (TP, 4, 1), [5000, 2600, 33], [40, 3, 33]),               # both are
+    (G70B, (TP, 8, 2), [2500] + [40] * 30, [16] + [5] * 30),
+])
+def test_attention_repeats_itself(fmt, geom, triple, ctx, q_lens):
+    """Nothing depends on the order in which workgroups come to their ends, or on what a workspace held."""
+    x = q8.case(geom, triple, ctx, q_lens, fmt)
+    pool, scales = pool_of(x)
+    several = [prefill(x, pool, scales).view(torch.int16).clone() for _ in range(4)]
+    x.c.q = q_for(x, len(ctx))
+    one = [decode(x, pool, scales).view(torch.int16).clone() for _ in range(4)]
+    for got in (several, one):
+        assert all(torch.equal(g, got[0]) for g in got[1:])
