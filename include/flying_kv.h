@@ -529,8 +529,9 @@ int paged_decode_attn_q8(const void* q, void* out, const void* kv_pool, const fl
                          const kv_view* view, float scale, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /*
- * paged_prefill_attn_q8 -- paged_prefill_attn over a cache held in 8 bits (the new tokens' codes are in the pool).  Values enter the
- * products in bf16: exactly where scales are powers of two, rounded to it otherwise.
+ * paged_prefill_attn_q8 -- paged_prefill_attn over a cache held in 8 bits (the new tokens' codes are in the pool).  Keys and values
+ * enter the products in bf16: exactly where scales are powers of two, rounded to it otherwise.  So do queries and softmax weights, these
+ * rounded to one bf16 as paged_prefill_attn's are.
  * Workspace, other arguments and errors as paged_prefill_attn, KV_ERR_INVALID_ARG for an unknown format.
  */
 size_t paged_prefill_attn_q8_workspace_bytes(const kv_view* view, int batch, int64_t total_q, int max_ctx_len, int max_q_len);

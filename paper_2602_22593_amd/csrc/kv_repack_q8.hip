@@ -5,7 +5,7 @@
 // arrangement: the unit is a 16-byte piece of such a run, consecutive lanes on consecutive pieces.  A workgroup moves 8 KiB, or one group of
 // B_base tokens where that is more (from 3 common heads of 128 and B_base = 16 on), two pieces a lane or 8 KiB at a time: they are requested
 // before the first of them is stored.  With 64 KiB and four pieces at a time, moving 128 sequences around 4096 tokens from DP to TP4 (2 common
-// heads: 8 KiB) took 114 us, with 16 KiB 106, now 104 (4.9 TB/s; runs of 256 bytes are read), and one sequence 8.2 us, now 5.6 (its launch).
+// heads: 8 KiB) took 114 us, with 16 KiB 106, now 104 (4.8 TB/s; runs of 256 bytes are read), and one sequence 8.2 us, now 5.6 (its launch).
 // Larger groups lose nothing by their rounds: 4 and 8 common heads, 32 KiB a group, 5.0 TB/s, and B_base = 64, 128 KiB, 5.1.
 #include "kv_q8.h"
 

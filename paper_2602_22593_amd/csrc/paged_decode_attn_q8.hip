@@ -562,7 +562,8 @@ constexpr int kUnitShift = 3, kStartUnits = 8;   // a start counts as much as a 
 // Up to which bound of the lengths a workgroup takes a whole pair: cutting costs a second launch, 4 us and more, and pieces to write and read;
 // not cutting leaves a workgroup 0.8 us for each 128 tokens, and from 256 pairs on compute units with two.  (Lengths from 0.3 of the bound to it, us
 // whole and cut: 16 pairs, 700: 7.4, 9.8; 1000: 10.2, 9.9; 96 pairs, 1000: 11.3, 14.3; 192 pairs, 1000: 15.7, 18.9; 1700: 23.7, 21.4; 384 pairs, 500:
-// 14.4, 16.0; 700: 19.2, 19.2; 1000: 25.9, 23.9; 768 pairs, 500: 21.2, 24.5; 700: 27.8, 27.4; 1520 pairs, 300: 25.4, 27.3; 500: 36.6, 34.6.)
+// 14.4, 16.0; 700: 19.2, 19.2; 1000: 25.9, 23.9; 768 pairs, 500: 21.2, 24.5; 700: 27.8, 27.4; 1520 pairs, 300: 25.4, 27.3; 500: 36.6, 34.6.
+// Between 256 and about 400 the rule loses up to 7 % for more than 1024 pairs: 1520 pairs at 300.)
 int whole_bound(int64_t pairs) { return pairs >= 96 && pairs <= 256 ? 1024 : pairs <= 512 ? 704 : pairs <= 1024 ? 512 : 256; }
 constexpr int kLeastCut = 256;   // no pair is cut up to this bound
 
@@ -610,6 +611,8 @@ void launch(const decode_plan& p, const decode_args& a, hipStream_t st)
         const int pairs = a.batch * p.head_sets, rows = p.hpw * a.group;
         // By the pieces of a pair, where all are alike.  One of 20000 tokens, 8 heads, 256 pieces: 16.5 us, with 4 wavefronts a row 27; 9 of 600 to 4700, one
         // head, 57 pieces: 9.8, as many with 4, with one piece at a time 10.4; 256 around 1024, 2 pieces: 44.4, with four at a time 45.5.
+        // (One long sequence among many short ones has far more pieces than this average, and its list is walked one piece at a time: 64 of 100 to 1000
+        // tokens, one head, 9.4 us, with 131072 tokens in place of one of them 32.3.)
         const int pieces = p.workgroups / pairs;
         auto* f = pieces > 32 ? merge_q8_kernel<D, 16, 4> : pieces > 8 ? merge_q8_kernel<D, 4, 4> : merge_q8_kernel<D, 4, 1>;
         hipLaunchKernelGGL(f, dim3((unsigned)pairs, (unsigned)rows), dim3(pieces > 32 ? 1024 : 256), 0, st, a, rows);

@@ -5,8 +5,11 @@
 // the scores of t + 1, output products of t beside the exponents of t + 1.  Other is how K and V get into LDS: codes are fetched into
 // registers two tiles ahead, become bf16 beside the products (a quarter of a tile a wavefront, once for all four) and are written where rows of bf16
 // would lie.  Values are code times scale: exact where the scale is a power of two, as the library writes them, rounded to bf16 otherwise.
-// Bound by the products and what runs beside them (matrix pipe 43 % busy, vector unit 51 %, int8 38 and 60): between long prompts 1040 TFLOP/s,
-// int8 920, 1137 from rows of bf16.  8 prompts of 128 to 3000 tokens, 32 heads on 8: 195 us; converted by every wavefront for itself: 254.
+// Bound by the products and what runs beside them (matrix pipe 44 % busy, vector unit 51 %, int8 39 and 62): between long prompts 1040 TFLOP/s,
+// int8 920, 1137 from rows of bf16.  8 prompts of 128 to 3000 tokens, 32 heads on 8: 194 us; converted by every wavefront for itself: 254.
+// Rounding: the softmax weights enter the output products as one bf16, off by 2^-8 at most, as paged_prefill_attn's do; their sum, the
+// denominator, is of the same rounded weights.  The error against 64 bits is 2.0 to 2.3e-3 in the 2-norm, where that of the output's own rounding is
+// 1.65e-3.  A second product with what the rounding left, as decode has it, would make the products half as many again where they are the bound.
 #include "prefill_common.h"
 
 using namespace kvprefill;
@@ -377,6 +380,7 @@ __global__ __launch_bounds__(kThreads, kPerCu) void prefill_q8_kernel(prefill_ar
     auto step = [&](int t, auto i_, fetched& kf, fetched& vf) __attribute__((always_inline)) {
         constexpr int i = i_.value;
         constexpr bool kPowers = FMT == kE4M3;   // e4m3 under other scales than powers of two is converted at the step's end
+        // (and so twice: the prompts above 231 us in place of 194)
         const bool in_time = !kPowers || (kf.exact && vf.exact);
         const kv_u32x4 next = look_up();
         kv_u32x4 x;

@@ -431,7 +431,7 @@ __device__ __forceinline__ bool items_of(const prefill_args& a, int lane0, int2*
             w.item_end = w.item + 1;
             w.item_step = 1;
         } else if (a.xcds_per_head == 0) {
-            // a contiguous eighth of the (head, slot) list per XCD; one w.item per workgroup
+            // a contiguous eighth of the (head, slot) list per XCD; one item per workgroup
             const int base = N >> 3, rem = N & 7;
             const int x = xcd * base + min(xcd, rem) + k;
             w.hl = x / a.slots;
